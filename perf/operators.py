@@ -6,9 +6,10 @@ A case is a dict of plain values; "op" says which operator it is.
 cache   Keys and values of new tokens go into the cache in 8 bits and are read back.
         Each (token, kv-head) vector x of head_dim keys (or values) is one block with
         a power-of-two scale: 2^e is the smallest power of two with max |x| <= 448 2^e
-        over the finite x, at least 2^-117; the codes are x / 2^e rounded to the
-        nearest e4m3 (ties to even), a non-finite x is NaN.  Reading gives code * 2^e,
-        which bf16 holds exactly.  One pass writes and reads one layer.
+        at least 2^-117; the codes are x / 2^e rounded to the nearest e4m3 (ties to
+        even).  Reading gives code * 2^e, which bf16 holds exactly; NaN for all keys and
+        values of a (token, kv-head) where any of them is not finite.  One pass writes
+        and reads one layer.
 attend  Attention of a step's rows over the cached keys and values (the numbers their
         codes stand for).  Row i of request b is its token at position ctx_b + i; it
         sees the keys 0 .. ctx_b + i (a draft tree's row: the context and its own
@@ -230,6 +231,7 @@ def prepare(case, seed):
                 if own:
                     st["pool"].load(b, layer, 0, torch.stack([k.transpose(0, 1), v.transpose(0, 1)]).contiguous())
                 else:
+                    k, v = _whole(k, v)
                     held.append((*_quantise(k), *_quantise(v)))
             if not own:
                 st["cache"].append(held)
@@ -301,6 +303,12 @@ def _quantise(x):
     e = torch.where(top > 0, e, -117)
     codes = torch.where(fine, x * _power(-e), float("nan")).to(torch.float8_e4m3fn)
     return codes, _power(e)
+
+
+def _whole(k, v):
+    """Keys and values with those of a token and kv-head NaN where any of them is not finite."""
+    ok = torch.isfinite(k).all(-1, keepdim=True) & torch.isfinite(v).all(-1, keepdim=True)
+    return torch.where(ok, k, float("nan")), torch.where(ok, v, float("nan"))
 
 
 def _visible(case, parents, c, r, dtype=torch.bool):
@@ -470,7 +478,7 @@ def run(st):
     if op == "cache":
         out = []
         live = torch.arange(case["n"]) < torch.tensor(st["rows"])[:, None]
-        for x in (st["k"], st["v"]):
+        for x in _whole(st["k"], st["v"]):
             codes, scale = _quantise(x)
             out.append(torch.where(live.to(DEV)[:, :, None, None], codes.float() * scale, 0.0).bfloat16())
         return out
@@ -509,7 +517,9 @@ def exact(case, seed):
         st = prepare(case, seed)
         if case["op"] == "cache":
             live = (torch.arange(case["n"]) < torch.tensor(st["rows"])[:, None]).to(DEV)[:, :, None, None]
-            return [torch.where(live, _stored64(x), 0.0) for x in (st["k"], st["v"])]
+            stored = [_stored64(st["k"]), _stored64(st["v"])]
+            bad = stored[0].isnan().any(-1, keepdim=True) | stored[1].isnan().any(-1, keepdim=True)
+            return [torch.where(live, x.masked_fill(bad, math.nan), 0.0) for x in stored]
         if case["op"] == "logits":
             if case["B"] * case["n"] > 256 or case["B"] * case["bias"] > 6000:
                 return None
