@@ -119,6 +119,33 @@ war_status war_kv_pool_create(const war_model_config* cfg, void* kv_pages, int32
                               void* stream, war_kv_pool** out);
 void war_kv_pool_destroy(war_kv_pool* p);
 
+/* A pool that holds keys and values in 8 bits: half the bytes that attention reads and
+ * twice the tokens in a replica's memory, which is what limits its requests
+ * (Background, "Rollout Bottlenecks").  Every call that takes a pool takes either kind.
+ * One token's head_dim keys (or values) of one kv-head are a block: codes c (OCP e4m3)
+ * with a power-of-two scale 2^e, e the smallest integer with max |x| <= 448 * 2^e, at
+ * least -117.  c is x / 2^e rounded to nearest even, and stands for c * 2^e, which
+ * bf16 holds exactly (from 1.9375 * 2^127 on it is infinite).  A block belongs to one
+ * token so that a rejected draft leaves no trace in the tokens before it, and so that
+ * a step, an append, an import and war_kv_write of the same bf16 numbers store the
+ * same bytes.  Where any key or value of a token and kv-head is not finite, all of
+ * them read as NaN, and rows that see the token get NaN; others do not.
+ *   kv_format     WAR_KV_BF16 (as war_kv_pool_create) or WAR_KV_E4M3
+ *   kv_pages      war_kv_pool_bytes(cfg, num_pages, kv_format) bytes, 16-byte aligned.
+ *                 E4M3: page regions as in war_kv_pool_create but of bytes, at byte
+ *                 ((l * num_pages + p) * n_kv_heads + h) * 2 * 16 * head_dim, behind
+ *                 all of them 32 scale bytes (e + 127) for each (l, p, h).  Key slot
+ *                 s, dim d is byte ((t * head_dim/64 + d/64) * 8 + s8) * 64 + d%64 of
+ *                 the key region (t and s8 as above), its scale byte 2 s8 + t; the
+ *                 value is byte ((d/32 * 2 + s/8) * 16 + d%16) * 16 + (d/16)%2 * 8 +
+ *                 s%8 of the value region, its scale byte 16 + s (0: not finite). */
+#define WAR_KV_BF16 0
+#define WAR_KV_E4M3 1
+int64_t war_kv_pool_bytes(const war_model_config* cfg, int32_t num_pages, int32_t kv_format);
+war_status war_kv_pool_create_format(const war_model_config* cfg, void* kv_pages, int32_t num_pages,
+                                     int32_t kv_format, int32_t* block_tables, int32_t max_seqs,
+                                     int32_t max_pages_per_seq, void* stream, war_kv_pool** out);
+
 /* Ensure capacity for n_tokens[i] slots for sequence seq_ids[i] (host arrays,
  * distinct ids).  A trajectory's KV cache grows with its length and stays
  * resident from turn to turn, so KV memory is the pressure point of rollout
@@ -152,6 +179,60 @@ war_status war_kv_free(war_kv_pool* p, int32_t n, const int32_t* seq_ids_host, v
  * sequence's page count (one stream synchronisation). */
 war_status war_kv_load(war_kv_pool* p, int32_t seq_id, int32_t layer, int32_t pos0, int32_t n,
                        const void* src, void* stream);
+
+/* Keys and values of many sequences' tokens into their pages, one layer, and out of
+ * them (caches move between replicas: System Design, "Overview of WAR" and the
+ * cache-aware scheduler).  Unlike war_kv_load nothing waits for the device.
+ *   seq_ids   device int32 [B], distinct
+ *   pos0      device int32 [B]: the first token's position
+ *   n_max     row b * n_max + i of k and v is token pos0[b] + i
+ *   n_lens    device int32 [B] in [0, n_max], or NULL: all n_max.  Rows beyond are not
+ *             read (written: left as they were).
+ *   k, v      device bf16 rows of n_kv_heads * head_dim, keys after RoPE; strides in
+ *             elements, multiples of 8, at least a row; 16-byte aligned
+ * The tokens must lie within the sequence's pages (war_kv_alloc).  A request that does
+ * not (or has a bad id, position or count) is flagged (war_pool_state) and left out. */
+war_status war_kv_write(war_kv_pool* p, int32_t layer, int32_t B, const int32_t* seq_ids, const int32_t* pos0,
+                        int32_t n_max, const int32_t* n_lens, const void* k, int64_t k_stride, const void* v,
+                        int64_t v_stride, void* stream);
+war_status war_kv_read(war_kv_pool* p, int32_t layer, int32_t B, const int32_t* seq_ids, const int32_t* pos0,
+                       int32_t n_max, const int32_t* n_lens, void* k, int64_t k_stride, void* v,
+                       int64_t v_stride, void* stream);
+
+/* Attention of given rows over a pool, as the steps take it: for decoders whose other
+ * layers are the caller's.  An object owns the workspace of one plan; a plan is made
+ * once a step and serves all its layers.
+ *   max_batch, max_rows   the most requests and rows a request: max_batch <= 1024,
+ *                         max_rows <= 65536, their product <= 2^20
+ * The pool must outlive the object.  Only war_attend_create and _destroy allocate and
+ * wait, so update and run may be captured into a graph; an object holds one plan at a
+ * time, so graphs that may run at the same time take an object each. */
+typedef struct war_attend war_attend;
+war_status war_attend_create(war_kv_pool* p, int32_t max_batch, int32_t max_rows, war_attend** out);
+void war_attend_destroy(war_attend* a);
+
+/* The plan of B requests with n_max rows each.
+ *   seq_ids       device int32 [B], distinct
+ *   ctx_lens      device int32 [B]: position of the request's row 0
+ *   n_lens        device int32 [B] in [0, n_max]: live rows; NULL: all n_max
+ *   draft_parents device int32 [B][n_max - 1]: rows are draft trees as in
+ *                 war_verify_step_tree; NULL: row i is the token at ctx + i.  Trees take
+ *                 n_q_heads / n_kv_heads * n_max <= 48 and n_max <= 32.
+ * The keys and values of positions 0 .. ctx + n_lens - 1 (a tree's node i: ctx + i) must
+ * be in the pool when the attention runs.  A bad id, position or count, an id twice, or
+ * rows beyond a sequence's pages are flagged (war_pool_state), and war_attend_run then
+ * writes nothing. */
+war_status war_attend_update(war_attend* a, int32_t B, int32_t n_max, const int32_t* seq_ids,
+                             const int32_t* ctx_lens, const int32_t* n_lens, const int32_t* draft_parents,
+                             void* stream);
+
+/* o = softmax(q k / sqrt(head_dim)) v of the planned rows in one layer; row i of request
+ * b sees the keys 0 .. ctx_b + i (a tree's node the context and its root path).
+ *   q, o   device bf16, row b * n_max + i at that many strides, n_q_heads * head_dim
+ *          elements; strides in elements, multiples of 8; 16-byte aligned.  Rows of o
+ *          beyond n_lens are left as they were. */
+war_status war_attend_run(war_attend* a, int32_t layer, const void* q, int64_t q_stride, void* o,
+                          int64_t o_stride, void* stream);
 
 /* Append a new turn to cached trajectories (System Design, "Overview of WAR";
  * Background, "Rollout Bottlenecks").

@@ -9,6 +9,7 @@ Modules
   bf16      round-to-nearest-even to bfloat16, written from the IEEE-754 format.
   decoder   the GQA decoder forward over a block of new tokens against a
             request's cached keys/values (dense, per request, row by row).
+  e4m3      keys and values cached in 8 bits: scales, rounding, tokens that are not finite.
   accept    greedy argmax (ties -> lowest id) and longest-matching-prefix
             acceptance of draft tokens.
   pages     the paged-KV bookkeeping model: free stack, refcounts, block tables,

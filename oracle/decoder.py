@@ -123,13 +123,16 @@ KVGetter = Callable[[int], Tuple[np.ndarray, np.ndarray]]
 
 def forward_block(cfg, W: Weights, tokens: Sequence[int], pos0: int, kv_get: KVGetter,
                   rounding: bool = True, want_logits: bool = True, precision: str = "fp64",
-                  trace: Optional[Dict[str, np.ndarray]] = None):
+                  trace: Optional[Dict[str, np.ndarray]] = None, kv_store=None):
     """Run tokens (at positions pos0, pos0+1, ...) through the decoder.
 
     ``kv_get(l)`` returns the cached keys and values of layer l for positions
     0..pos0-1 as [Hkv, pos0, D] arrays.  Returns (logits [n, V] or the final
     normalised hidden state when want_logits is False, new_kv) where new_kv[l]
     = (K_new [Hkv, n, D], V_new [Hkv, n, D]) for the block's own tokens.
+
+    ``kv_store``, when given, maps the new keys and values [n, Hkv, D] to what the
+    cache holds of them (a cache in 8 bits); the block's own rows attend to that.
 
     ``trace``, when given, receives every intermediate under a name (layer l's
     as "l{l}.<name>"): h0 (embedding rows), u1 (attention norm output), qkv
@@ -168,6 +171,8 @@ def forward_block(cfg, W: Weights, tokens: Sequence[int], pos0: int, kv_get: KVG
         q = rb(rope(q, pos, cfg.rope_base))
         k = rb(rope(k, pos, cfg.rope_base))
         v = rb(v)
+        if kv_store is not None:
+            k, v = kv_store(k, v)
         rec(p + "q", q)
         rec(p + "k", k)
         rec(p + "v", v)
@@ -198,10 +203,11 @@ def forward_block(cfg, W: Weights, tokens: Sequence[int], pos0: int, kv_get: KVG
 
 
 class RequestKV:
-    """Dense cached keys/values of one request, per layer [Hkv, length, D]."""
+    """Dense cached keys/values of one request, per layer [Hkv, length, D].  ``store``:
+    what the cache holds of new keys and values (forward_block's kv_store)."""
 
-    def __init__(self, cfg, layers: Optional[List[Tuple[np.ndarray, np.ndarray]]] = None):
-        self.cfg = cfg
+    def __init__(self, cfg, layers: Optional[List[Tuple[np.ndarray, np.ndarray]]] = None, store=None):
+        self.cfg, self.store = cfg, store
         if layers is None:
             e = np.zeros((cfg.n_kv_heads, 0, cfg.head_dim))
             layers = [(e, e) for _ in range(cfg.n_layers)]

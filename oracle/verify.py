@@ -41,7 +41,8 @@ from .decoder import RequestKV, Weights, forward_block
 def verify_request(cfg, W: Weights, kv: RequestKV, last_token: int, drafts: Sequence[int],
                    rounding: bool = True, precision: str = "fp64") -> Dict:
     tokens = [int(last_token)] + [int(d) for d in drafts]
-    logits, new_kv = forward_block(cfg, W, tokens, kv.length, kv.get, rounding, precision=precision)
+    logits, new_kv = forward_block(cfg, W, tokens, kv.length, kv.get, rounding, precision=precision,
+                                   kv_store=kv.store)
     g = argmax_lowest(logits)
     a = accept_length(drafts, g)
     return {"logits": logits, "greedy": g, "accept": a, "next": int(g[a]), "new_kv": new_kv}
@@ -62,7 +63,8 @@ def verify_tree_request(cfg, W: Weights, kv: RequestKV, last_token: int, drafts:
     tok = [int(last_token)] + [int(d) for d in drafts]
     rows = []
     for j in range(n + 1):
-        lg, _ = forward_block(cfg, W, [tok[i] for i in tree_path(parents, j)], kv.length, kv.get, rounding)
+        lg, _ = forward_block(cfg, W, [tok[i] for i in tree_path(parents, j)], kv.length, kv.get, rounding,
+                              kv_store=kv.store)
         rows.append(lg[-1])
     logits = np.stack(rows)
     g = argmax_lowest(logits)
@@ -74,7 +76,7 @@ def verify_tree_request(cfg, W: Weights, kv: RequestKV, last_token: int, drafts:
         depth[j] = depth[p] + 1
     cur = max((j for j in range(n + 1) if ok[j]), key=lambda j: (depth[j], -j))
     path = tree_path(parents, cur)[1:]
-    _, new_kv = forward_block(cfg, W, [tok[i] for i in [0] + path], kv.length, kv.get, rounding)
+    _, new_kv = forward_block(cfg, W, [tok[i] for i in [0] + path], kv.length, kv.get, rounding, kv_store=kv.store)
     return {"logits": logits, "greedy": g, "accept": len(path), "path": path, "next": int(g[cur]),
             "new_kv": new_kv}
 
@@ -92,7 +94,7 @@ def commit_request(kv: RequestKV, result: Dict, accept: int | None = None) -> No
 
 def prefill_request(cfg, W: Weights, kv: RequestKV, tokens: Sequence[int],
                     rounding: bool = True) -> Dict:
-    logits, new_kv = forward_block(cfg, W, [int(t) for t in tokens], kv.length, kv.get, rounding)
+    logits, new_kv = forward_block(cfg, W, [int(t) for t in tokens], kv.length, kv.get, rounding, kv_store=kv.store)
     kv.append(new_kv, len(tokens))
     g = argmax_lowest(logits)
     return {"logits": logits, "greedy": g, "next": int(g[-1])}

@@ -124,6 +124,10 @@ __global__ void __launch_bounds__(kBT) k_grow(PoolDev p, int n, const int32_t* s
 // a wave, and a small batch runs a small workgroup (64 threads a request, up to
 // 1024).  Four groups of four siblings with 512 shared pages 77 -> 13 us (of a
 // 1.75 ms step), 64 long requests 26 -> 13, 4 requests 10 -> 7.
+//
+// PLAN: the rows are there already (war_attend_update): nothing is reserved, draft_lens
+// counts rows, and there may be none.
+template <bool PLAN>
 __global__ void __launch_bounds__(kBT) k_verify_setup(PoolDev p, VerifySetupArgs a, StepMeta m) {
   __shared__ int s_fail;
   __shared__ int s_ctx[kBT], s_dl[kBT];
@@ -150,10 +154,10 @@ __global__ void __launch_bounds__(kBT) k_verify_setup(PoolDev p, VerifySetupArgs
   if (t < a.B) {
     s = a.seq_ids[t];
     ctx = a.ctx_lens[t];
-    dl = a.draft_lens ? a.draft_lens[t] : a.k_max;
+    dl = a.draft_lens ? a.draft_lens[t] - (PLAN ? 1 : 0) : a.k_max;
   }
   // token of row t, in case it is live
-  const int row_tok = t >= R ? 0 : t % kp1 == 0 ? a.last_tokens[t / kp1]
+  const int row_tok = PLAN || t >= R ? 0 : t % kp1 == 0 ? a.last_tokens[t / kp1]
                                                 : a.draft_tokens[(int64_t)(t / kp1) * a.k_max + t % kp1 - 1];
   int hsize = 64;  // a power of two, at least 2 B
   while (hsize < 2 * a.B) hsize *= 2;
@@ -167,11 +171,12 @@ __global__ void __launch_bounds__(kBT) k_verify_setup(PoolDev p, VerifySetupArgs
   __syncthreads();
   int need = 0, hb = 0, page0 = 0;
   if (t < a.B) {
-    dl = min(max(dl, 0), a.k_max);
+    if constexpr (!PLAN) dl = min(max(dl, 0), a.k_max);
     // a bad id, a negative length or a request beyond its block-table row
     // fails the whole step (no page moves, no row is active)
     if (s < 0 || s >= p.max_seqs || ctx < 0 ||
-        cdiv_i(ctx + dl + 1, kPage) > p.max_pages) {
+        (PLAN ? dl < -1 || dl > a.k_max || (int64_t)ctx + dl + 1 > (int64_t)p.held[s] * kPage
+              : cdiv_i(ctx + dl + 1, kPage) > p.max_pages)) {
       s = 0;
       ctx = 0;
       atomicOr(&s_bad, 1);
@@ -190,7 +195,7 @@ __global__ void __launch_bounds__(kBT) k_verify_setup(PoolDev p, VerifySetupArgs
       }
       hb = p.held[s];
       page0 = p.table[(int64_t)s * p.max_pages];
-      need = max(0, cdiv_i(ctx + dl + 1, kPage) - hb);
+      if constexpr (!PLAN) need = max(0, cdiv_i(ctx + dl + 1, kPage) - hb);
     }
   }
   int total;
@@ -203,7 +208,7 @@ __global__ void __launch_bounds__(kBT) k_verify_setup(PoolDev p, VerifySetupArgs
   __syncthreads();
   const bool fail = s_fail;
   if (t < a.B) {
-    if (!fail) {
+    if (!PLAN && !fail) {
       pop_pages(p, s, hb, need, off, fc);
       p.held[s] = hb + need;
       p.base[s] = hb;
@@ -226,7 +231,7 @@ __global__ void __launch_bounds__(kBT) k_verify_setup(PoolDev p, VerifySetupArgs
   // nothing has to be merged).
   if (t < kChunks) s_cnt[t] = 0;
   __syncthreads();
-  const int len = (t < a.B && !fail) ? ctx + dl + 1 : 0;
+  const int len = (t < a.B && !fail && (!PLAN || dl >= 0)) ? ctx + dl + 1 : 0;
   int csh = 31 - __clz(a.chunk);  // log2 of the chunk (a power of two)
   if (w * 64 < a.B)
     for (int c = 0; c < kChunks; ++c) {
@@ -252,7 +257,7 @@ __global__ void __launch_bounds__(kBT) k_verify_setup(PoolDev p, VerifySetupArgs
     m.seg_req[t] = t;
     m.seg_rb[t] = 0;
     s_ioff[t] = ioff;
-    s_pg0[t] = (!fail && ctx > 0 && hb > 0) ? page0 : -1 - t;
+    s_pg0[t] = (!fail && ctx > 0 && hb > 0 && (!PLAN || dl >= 0)) ? page0 : -1 - t;
     s_nch[t] = nch;
     s_seq[t] = s;
     s_shr[t] = 0x7fffffff;
@@ -383,9 +388,11 @@ __global__ void __launch_bounds__(kBT) k_verify_setup(PoolDev p, VerifySetupArgs
     m.n_items[1] = n_units;
     m.n_items[2] = 0;
     m.n_items[3] = chunk;
-    if (fail && !s_bad && !s_dup) p.scalars[1] |= ERR_NO_PAGES;
-    if (!fail) p.scalars[0] = fc - total;
-    p.scalars[2] = fail ? 1 : 0;  // the commit of a failed step changes nothing
+    if constexpr (!PLAN) {
+      if (fail && !s_bad && !s_dup) p.scalars[1] |= ERR_NO_PAGES;
+      if (!fail) p.scalars[0] = fc - total;
+      p.scalars[2] = fail ? 1 : 0;  // the commit of a failed step changes nothing
+    }
   }
   __syncthreads();
   // rows: request b's token i sits in row b*(k_max+1)+i
@@ -394,7 +401,7 @@ __global__ void __launch_bounds__(kBT) k_verify_setup(PoolDev p, VerifySetupArgs
     const int dlb = s_dl[b];
     const bool act = i <= dlb;
     int tok = 0;
-    if (act) tok = r == t ? row_tok : i == 0 ? a.last_tokens[b] : a.draft_tokens[(int64_t)b * a.k_max + i - 1];
+    if (!PLAN && act) tok = r == t ? row_tok : i == 0 ? a.last_tokens[b] : a.draft_tokens[(int64_t)b * a.k_max + i - 1];
     if (tok < 0 || tok >= a.vocab) {
       atomicOr(&p.scalars[1], ERR_BAD_TOKEN);
       tok = 0;
@@ -424,6 +431,105 @@ __global__ void __launch_bounds__(kBT) k_verify_setup(PoolDev p, VerifySetupArgs
       m.tmask[r] = msk;
     } else {
       m.pos[r] = slot;
+    }
+  }
+}
+
+// The attention plan of many rows a request, in blocks of TB tokens.  A block's keys are
+// cut into chunks; the work order is a request's chunks, each with all blocks that reach
+// it, so that the units which read a chunk run together and find it in L2.  With first(c)
+// the first block that reaches chunk c, a request has sum_c (blocks - first(c)) items.
+// Few units (less than half the grid's) take shorter chunks, down to 256 keys.
+__global__ void __launch_bounds__(kBT) k_attend_plan_rows(PoolDev p, RowPlanArgs a, StepMeta m) {
+  __shared__ int s_ctx[kBT], s_n[kBT], s_off[kBT], s_seq[kBT];
+  constexpr int kChunks = 5, kMinChunk = 256;
+  __shared__ int s_cnt[kChunks];
+  __shared__ int s_hash[2 * kBT], s_bad, s_dup;
+  const int t = threadIdx.x;
+  if (t < 8) a.unit_ctr[t * kCtrStride] = 0;
+  if (t < kChunks) s_cnt[t] = 0;
+  if (t == 0) s_bad = s_dup = 0;
+  for (int i = t; i < 2 * kBT; i += kBT) s_hash[i] = -1;
+  __syncthreads();
+  int s = 0, ctx = 0, n = 0;
+  if (t < a.B) {
+    s = a.seq_ids[t];
+    ctx = a.ctx_lens[t];
+    n = a.n_lens ? a.n_lens[t] : a.n_max;
+    if (s < 0 || s >= p.max_seqs || ctx < 0 || n < 0 || n > a.n_max ||
+        (int64_t)ctx + n > (int64_t)p.held[s] * kPage) {
+      atomicOr(&s_bad, 1);
+    } else {
+      unsigned h = ((unsigned)s * 2654435761u) >> 21;
+      for (int probe = 0; probe < 2 * kBT; ++probe, h = (h + 1) & (2 * kBT - 1)) {
+        const int prev = atomicCAS(&s_hash[h], -1, s);
+        if (prev == -1) break;
+        if (prev == s) {
+          atomicOr(&s_dup, 1);
+          break;
+        }
+      }
+    }
+  }
+  __syncthreads();
+  const bool fail = s_bad || s_dup;
+  if (t == 0) {
+    if (s_bad) atomicOr(&p.scalars[1], ERR_BAD_TOKEN);
+    if (s_dup) atomicOr(&p.scalars[1], ERR_DUP_SEQ);
+  }
+  if (fail) n = 0;
+  const int len = n > 0 ? ctx + n : 0, blocks = (n + a.TB - 1) / a.TB;
+  auto first = [&](int ctx_, int c, int chunk) {
+    const int64_t before = (int64_t)c * chunk - ctx_;
+    return before < a.TB ? 0 : (int)(before / a.TB);
+  };
+  auto items_of = [&](int chunk) {
+    int k = 0;
+    for (int c = 0; c * chunk < len; ++c) k += blocks - first(ctx, c, chunk);
+    return k;
+  };
+  if (t < a.B && n > 0)
+    for (int i = 1, ch = a.chunk / 2; i < kChunks && ch >= kMinChunk; ++i, ch /= 2)
+      atomicAdd(&s_cnt[i], min(items_of(ch), 1 << 20));
+  __syncthreads();
+  int chunk = a.chunk;
+  for (int i = 1; i < kChunks && chunk / 2 >= kMinChunk && s_cnt[i] <= a.items_fill; ++i) chunk /= 2;
+  int n_items;
+  const int off = block_excl_scan(t < a.B ? items_of(chunk) : 0, &n_items);
+  if (t < a.B) {
+    s_ctx[t] = ctx;
+    s_n[t] = n;
+    s_off[t] = off;
+    s_seq[t] = s;
+    m.req_seq[t] = s;
+    m.req_pos0[t] = ctx;
+    m.req_ntok[t] = n;
+    m.req_row0[t] = t * a.n_max;
+  }
+  if (t == 0) {
+    m.n_items[0] = m.n_items[1] = n_items;
+    m.n_items[2] = 0;
+    m.n_items[3] = chunk;
+  }
+  __syncthreads();
+  for (int i = t; i < a.B * a.blocks; i += kBT) {
+    const int b = i / a.blocks, rb = i % a.blocks;
+    const int nb = (s_n[b] + a.TB - 1) / a.TB;
+    m.seg_req[i] = b;
+    m.seg_rb[i] = rb;
+    m.seg_begin[i] = m.seg_count[i] = 0;
+    if (rb >= nb) continue;
+    const int ntk = min(a.TB, s_n[b] - rb * a.TB), S = s_ctx[b] + rb * a.TB + ntk;
+    int begin = s_off[b];  // items block by block: the chunks of the blocks before this one
+    for (int c = 0; c * chunk < s_ctx[b] + s_n[b]; ++c) begin += max(0, rb - first(s_ctx[b], c, chunk));
+    m.seg_begin[i] = begin;
+    m.seg_count[i] = (S + chunk - 1) / chunk;
+    int slot = s_off[b];  // work order chunk by chunk
+    for (int c = 0; c * chunk < S; ++c) {
+      const int f = first(s_ctx[b], c, chunk);
+      m.udesc[2 * (slot + rb - f)] = make_int4(begin + c, b, c, (rb * a.TB) | (ntk << 16));
+      m.udesc[2 * (slot + rb - f) + 1] = make_int4(0, s_seq[b], s_ctx[b], b * a.n_max);
+      slot += nb - f;
     }
   }
 }
@@ -605,7 +711,13 @@ void launch_grow(const PoolDev& p, int n, const int32_t* seq, const int32_t* a, 
 }
 void launch_verify_setup(const PoolDev& p, const VerifySetupArgs& a, const StepMeta& m,
                          hipStream_t st) {
-  k_verify_setup<<<1, std::min(kBT, 64 * a.B), 0, st>>>(p, a, m);
+  k_verify_setup<false><<<1, std::min(kBT, 64 * a.B), 0, st>>>(p, a, m);
+}
+void launch_attend_plan(const PoolDev& p, const VerifySetupArgs& a, const StepMeta& m, hipStream_t st) {
+  k_verify_setup<true><<<1, std::min(kBT, 64 * a.B), 0, st>>>(p, a, m);
+}
+void launch_attend_plan_rows(const PoolDev& p, const RowPlanArgs& a, const StepMeta& m, hipStream_t st) {
+  k_attend_plan_rows<<<1, kBT, 0, st>>>(p, a, m);
 }
 void launch_commit(const PoolDev& p, int B, const int32_t* seq, int32_t* ctx, const int32_t* acc,
                    uint32_t commit_seq, hipStream_t st) {

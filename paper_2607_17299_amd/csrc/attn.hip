@@ -22,28 +22,49 @@
 // Block bookkeeping (positions, page ids, page bases) is wave-uniform and kept
 // in scalar registers; only the last blocks of a request take the causal /
 // tree / end-of-sequence masks, in a loop of their own.
+// An e4m3 pool (Q8) halves the bytes.  A block's codes are converted to bf16 in
+// registers, which is exact: keys with their token's scale by the conversion itself,
+// values without, their scales multiply the weights (a lane holds the weights of eight
+// tokens of one row), whose sum stays without them.  16 bytes of a lane are two k-steps
+// of a key (k-step j covers dims 64 (j / 2) + 16 g + 8 (j % 2) + 0..7 of lane group g)
+// or its eight keys in two output tiles.
 // The waves' (max, sum, O) are merged through LDS in a fixed order and one
 // partial per item goes to global memory; the combine kernel merges a
 // request's chunks in item order (deterministic).
 #include <type_traits>
 
 #include "attn.h"
+#include "e4m3.h"
 
 namespace {
 
 // K and V^T fragments of one 32-key block (see the file comment for the layout).
-template <int HD>
+template <int HD, bool Q8>
 struct KVFrag {
   uint4 k[2][HD / 32];
   uint4 v[HD / 16];
 };
+template <int HD>
+struct KVFrag<HD, true> {
+  uint4 k[2][HD / 64];
+  uint4 v[HD / 32];
+  uint32_t ks;  // scale bytes of the lane's two keys
+  uint2 vs;     // and of the values of its eight
+};
+
+// The first n (0..8) codes of eight, zero the rest.
+WAR_DEV uint2 keep_first8(uint2 v, int n) {
+  const uint32_t a = n >= 4 ? 0xffffffffu : (1u << (8 * n)) - 1u;
+  const uint32_t b = n >= 8 ? 0xffffffffu : n <= 4 ? 0u : (1u << (8 * (n - 4))) - 1u;
+  return make_uint2(v.x & a, v.y & b);
+}
 
 // DEPTH = blocks in flight per wave beyond the one being computed (0 or 1);
 // QLDS = queries read from LDS instead of registers; WPE = waves per SIMD the
 // register budget allows.  Two waves per SIMD let one wave's MFMA/softmax work
 // overlap the other's memory waits.
 // TREE = the step has tree drafts (rows carry node masks).
-template <int NR, int HD, int DEPTH, bool QLDS, int WPE, bool TREE>
+template <int NR, int HD, int DEPTH, bool QLDS, int WPE, bool TREE, bool Q8>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(WPE, WPE)))
 k_attn(AttnArgs a) {
   constexpr int KSUB = HD / 32;  // MFMA k-steps over the head dim
@@ -68,8 +89,9 @@ k_attn(AttnArgs a) {
   // key_elem; kind 1 = V^T [dim][slot]): lanes ln < 8 read K rows of the
   // block's first page, the others its second; lane groups lg < 2 read V^T of
   // the first page.  K of tile t, k-step j is one 512-byte run per page.
-  const int koff0 = key_elem(kk0 & 15, lg * 8, HD), koff1 = key_elem((kk0 + 4) & 15, lg * 8, HD);
-  const int voff = P * HD + (lg & 1) * 8 + ln * P;
+  const int koff0 = Q8 ? key_elem8(kk0 & 15, lg * 16, HD) : key_elem(kk0 & 15, lg * 8, HD);
+  const int koff1 = Q8 ? key_elem8((kk0 + 4) & 15, lg * 16, HD) : key_elem((kk0 + 4) & 15, lg * 8, HD);
+  const int voff = P * HD + (Q8 ? ((lg & 1) * 16 + ln) * 16 : (lg & 1) * 8 + ln * P);
   const bool k_second = ln >= 8, v_second = lg >= 2;
 
   // The next unit is taken (UnitQueue) when the key loop of the current one
@@ -126,7 +148,12 @@ k_attn(AttnArgs a) {
     const int32_t* trow = a.table + (int64_t)seq * a.max_pages;
     // elements per page across kv-heads and kinds; this kv-head's part of page 0
     const int64_t pstride = (int64_t)a.kv.n_kv_heads * 2 * P * HD;
-    const bf16_t* kvb = a.kv.kv + a.kv.page_elems(a.layer, 0, kvh, 0);
+    using Elem = std::conditional_t<Q8, uint8_t, bf16_t>;
+    const Elem* kvb;
+    if constexpr (Q8) kvb = a.kv.q8 + a.kv.page_elems(a.layer, 0, kvh, 0);
+    else kvb = a.kv.kv + a.kv.page_elems(a.layer, 0, kvh, 0);
+    const uint8_t* scb = nullptr;  // this kv-head's scales of page 0
+    if constexpr (Q8) scb = a.kv.scale + a.kv.scale_bytes(a.layer, 0, kvh);
 
     // Keys and values are read once per step (a unit's 4 waves take disjoint
     // blocks, the 8 kv-head units of a chunk disjoint pieces of each page), so
@@ -135,12 +162,27 @@ k_attn(AttnArgs a) {
     // 16.5 ms per step (6.0 -> 6.4 TB/s); low load and forked siblings
     // unchanged.
     typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
-    auto ntload = [](const bf16_t* p) {
+    auto ntload = [](const Elem* p) {
       return __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(p)));
     };
-    auto load_block = [&](KVFrag<HD>& f, int kb) {
+    auto load_block = [&](KVFrag<HD, Q8>& f, int kb) {
       const int pg0 = trow[kb / P];
       const int pg1 = (kb + 16 < S) ? trow[kb / P + 1] : pg0;
+      if constexpr (Q8) {
+        const uint8_t* kp = kvb + (int64_t)(k_second ? pg1 : pg0) * pstride;
+        const uint8_t* vp = kvb + (int64_t)(v_second ? pg1 : pg0) * pstride + voff;
+        const int64_t sstride = (int64_t)a.kv.n_kv_heads * 32;
+        f.ks = *reinterpret_cast<const uint16_t*>(scb + (int64_t)(k_second ? pg1 : pg0) * sstride + key_scale8(kk0 & 15));
+        f.vs = *reinterpret_cast<const uint2*>(scb + (int64_t)(v_second ? pg1 : pg0) * sstride + val_scale8((lg & 1) * 8));
+#pragma unroll
+        for (int j = 0; j < KSUB / 2; ++j) {
+          f.k[0][j] = ntload(kp + koff0 + j * 512);
+          f.k[1][j] = ntload(kp + koff1 + j * 512);
+        }
+#pragma unroll
+        for (int dt = 0; dt < NDT / 2; ++dt) f.v[dt] = ntload(vp + dt * 512);
+        return;
+      } else {
       const bf16_t* kp = kvb + (int64_t)(k_second ? pg1 : pg0) * pstride;
 #pragma unroll
       for (int j = 0; j < KSUB; ++j) {
@@ -150,6 +192,7 @@ k_attn(AttnArgs a) {
       const bf16_t* vp = kvb + (int64_t)(v_second ? pg1 : pg0) * pstride + voff;
 #pragma unroll
       for (int dt = 0; dt < NDT; ++dt) f.v[dt] = ntload(vp + dt * 16 * P);
+      }
     };
 
     // The first block is requested before the queries are staged, and each
@@ -157,7 +200,7 @@ k_attn(AttnArgs a) {
     // row tiles, which lack the registers for a block held across those points
     // and load each block right before computing it.
     constexpr bool kEarlyLoad = NR < 3;
-    KVFrag<HD> f0;
+    KVFrag<HD, Q8> f0;
     if (kEarlyLoad && nb > 0) load_block(f0, wk0);
 
     // row r -> (query row, query head) and its partial row; false if r is not live
@@ -179,7 +222,9 @@ k_attn(AttnArgs a) {
       return true;
     };
 
-    // queries (B operand of S^T): lane (n = ln, g = lg) of row tile rt
+    // queries (B operand of S^T): lane (n = ln, g = lg) of row tile rt, first of the
+    // eight dims of k-step j
+    auto qdim = [lg](int j) { return Q8 ? (j >> 1) * 64 + lg * 16 + (j & 1) * 8 : j * 32 + lg * 8; };
     int rpos[NR];
     bf16x8 qf[QLDS ? 1 : NR][KSUB];
 #pragma unroll
@@ -205,9 +250,9 @@ k_attn(AttnArgs a) {
         int qrow, h;
         int64_t prow;
         if (row_src(r, qrow, h, prow)) {
-          const bf16_t* qp = a.q + (int64_t)qrow * a.q_stride + h * HD + lg * 8;
+          const bf16_t* qp = a.q + (int64_t)qrow * a.q_stride + h * HD;
 #pragma unroll
-          for (int j = 0; j < KSUB; ++j) qf[rt][j] = as_bf16x8(*reinterpret_cast<const uint4*>(qp + j * 32));
+          for (int j = 0; j < KSUB; ++j) qf[rt][j] = as_bf16x8(*reinterpret_cast<const uint4*>(qp + qdim(j)));
         } else {
 #pragma unroll
           for (int j = 0; j < KSUB; ++j) qf[rt][j] = as_bf16x8(make_uint4(0, 0, 0, 0));
@@ -216,7 +261,7 @@ k_attn(AttnArgs a) {
     }
     auto qfrag = [&](int rt, int j) -> bf16x8 {
       if constexpr (QLDS)
-        return as_bf16x8(*reinterpret_cast<const uint4*>(&s_q[(rt * 16 + ln) * QST + j * 32 + lg * 8]));
+        return as_bf16x8(*reinterpret_cast<const uint4*>(&s_q[(rt * 16 + ln) * QST + qdim(j)]));
       else
         return qf[rt][j];
     };
@@ -233,19 +278,35 @@ k_attn(AttnArgs a) {
 
     // MASK: the block holds keys above some row's position or past the
     // sequence end (only the last blocks of a request)
-    auto compute_block = [&](const KVFrag<HD>& fin, int kb, auto mask_tag) {
+    auto compute_block = [&](const KVFrag<HD, Q8>& fin, int kb, auto mask_tag) {
       constexpr bool MASK = decltype(mask_tag)::value;
       if constexpr (QLDS) asm volatile("" ::: "memory");  // re-read Q from LDS each block
       // phase 1: scores of every row tile (the K fragments die after this)
       float sc[NR][8];
+      [[maybe_unused]] bf16x8 kf[2][Q8 ? KSUB : 1];
+      if constexpr (Q8) {
+        const float ksc[2] = {scale_of<0>(fin.ks), scale_of<1>(fin.ks)};
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int j = 0; j < KSUB / 2; ++j) {
+            const uint4 c = fin.k[t][j];
+            kf[t][2 * j] = as_bf16x8(from_e4m3x8(c.x, c.y, ksc[t]));
+            kf[t][2 * j + 1] = as_bf16x8(from_e4m3x8(c.z, c.w, ksc[t]));
+          }
+      }
+      auto kfrag = [&](int t, int j) {
+        if constexpr (Q8) return kf[t][j];
+        else return as_bf16x8(fin.k[t][j]);
+      };
 #pragma unroll
       for (int rt = 0; rt < NR; ++rt) {
         f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < KSUB; ++j) {
           const bf16x8 q = qfrag(rt, j);
-          s0 = mfma16(as_bf16x8(fin.k[0][j]), q, s0);
-          s1 = mfma16(as_bf16x8(fin.k[1][j]), q, s1);
+          s0 = mfma16(kfrag(0, j), q, s0);
+          s1 = mfma16(kfrag(1, j), q, s1);
         }
         // lane holds S^T[key kb + lg*8 + 4t + i][row rt*16 + ln]
 #pragma unroll
@@ -255,13 +316,33 @@ k_attn(AttnArgs a) {
         }
       }
       uint4 vf[NDT];
+      [[maybe_unused]] float vsc[8];
+      if constexpr (Q8) {
+        uint2 vs = fin.vs;
+        int nvalid = 8;
+        if constexpr (MASK) nvalid = min(max(S - (kb + lg * 8), 0), 8);  // slots past the sequence end hold anything
+        auto codes = [&](uint32_t x, uint32_t y) {
+          const uint2 c = MASK ? keep_first8(make_uint2(x, y), nvalid) : make_uint2(x, y);
+          return from_e4m3x8(c.x, c.y, 1.f);
+        };
+        if constexpr (MASK) vs = keep_first8(vs, nvalid);
 #pragma unroll
-      for (int dt = 0; dt < NDT; ++dt) vf[dt] = fin.v[dt];
-      if constexpr (MASK) {
-        if (kb + 32 > S) {  // the sequence ends inside this block
-          const int nvalid = min(max(S - (kb + lg * 8), 0), 8);
+        for (int dt = 0; dt < NDT; dt += 2) {
+          const uint4 c = fin.v[dt / 2];
+          vf[dt] = codes(c.x, c.y);
+          vf[dt + 1] = codes(c.z, c.w);
+        }
+        vsc[0] = scale_of<0>(vs.x), vsc[1] = scale_of<1>(vs.x), vsc[2] = scale_of<2>(vs.x), vsc[3] = scale_of<3>(vs.x);
+        vsc[4] = scale_of<0>(vs.y), vsc[5] = scale_of<1>(vs.y), vsc[6] = scale_of<2>(vs.y), vsc[7] = scale_of<3>(vs.y);
+      } else {
 #pragma unroll
-          for (int dt = 0; dt < NDT; ++dt) vf[dt] = keep_first(vf[dt], nvalid);
+        for (int dt = 0; dt < NDT; ++dt) vf[dt] = fin.v[dt];
+        if constexpr (MASK) {
+          if (kb + 32 > S) {  // the sequence ends inside this block
+            const int nvalid = min(max(S - (kb + lg * 8), 0), 8);
+#pragma unroll
+            for (int dt = 0; dt < NDT; ++dt) vf[dt] = keep_first(vf[dt], nvalid);
+          }
         }
       }
       // phase 2: online softmax and O^T += V^T P^T per row tile
@@ -310,9 +391,13 @@ k_attn(AttnArgs a) {
         uint32_t hi[4], lo[4];
 #pragma unroll
         for (int e = 0; e < 8; e += 2) {
-          const float p0 = __builtin_amdgcn_exp2f(fmaf(sv[e], a.scale_log2, -m_use));
-          const float p1 = __builtin_amdgcn_exp2f(fmaf(sv[e + 1], a.scale_log2, -m_use));
+          float p0 = __builtin_amdgcn_exp2f(fmaf(sv[e], a.scale_log2, -m_use));
+          float p1 = __builtin_amdgcn_exp2f(fmaf(sv[e + 1], a.scale_log2, -m_use));
           sum += p0 + p1;
+          if constexpr (Q8) {
+            p0 *= vsc[e];
+            p1 *= vsc[e + 1];
+          }
           hi[e / 2] = pack2(p0, p1);
           lo[e / 2] = pack2(p0 - lo_f(hi[e / 2]), p1 - hi_f(hi[e / 2]));
         }
@@ -337,7 +422,7 @@ k_attn(AttnArgs a) {
       // at the top of every iteration f0 holds block i
       if constexpr (DEPTH == 1) {
         // one more block in flight while a block is computed
-        KVFrag<HD> f1;
+        KVFrag<HD, Q8> f1;
         for (; i + 1 < nfull; i += 2) {
           load_block(f1, wk0 + 32 * (i + 1));
           compute_block(f0, wk0 + 32 * i, NoMask{});
@@ -530,7 +615,7 @@ __global__ void __launch_bounds__(256) k_attn_combine(AttnArgs a) {
   const float inv = s_il[r];
   const int rr = r0 + r;
   const int ti = t0 + rr / a.G, h = kvh * a.G + rr % a.G;
-  bf16_t* dst = a.o + (int64_t)(a.meta.req_row0[b] + ti) * a.q_stride + h * HD + d4;
+  bf16_t* dst = a.o + (int64_t)(a.meta.req_row0[b] + ti) * a.o_stride + h * HD + d4;
   uint2 o;
   o.x = pack2(acc.x * inv, acc.y * inv);
   o.y = pack2(acc.z * inv, acc.w * inv);
@@ -545,17 +630,19 @@ void launch_attn_nr(const AttnArgs& a, int head_dim, int grid, hipStream_t st) {
   constexpr int DEPTH = NR == 1 ? 1 : 0;
   constexpr bool QLDS = NR > 1;
   const bool tree = a.meta.tmask != nullptr;
-  if (head_dim == 128) {
-    if (tree)
-      k_attn<NR, 128, DEPTH, QLDS, 2, true><<<grid, 256, 0, st>>>(a);
-    else
-      k_attn<NR, 128, DEPTH, QLDS, 2, false><<<grid, 256, 0, st>>>(a);
-  } else {
-    if (tree)
-      k_attn<NR, 64, DEPTH, QLDS, 2, true><<<grid, 256, 0, st>>>(a);
-    else
-      k_attn<NR, 64, DEPTH, QLDS, 2, false><<<grid, 256, 0, st>>>(a);
-  }
+  auto go = [&](auto hd, auto t, auto q8) {
+    k_attn<NR, decltype(hd)::value, DEPTH, QLDS, 2, decltype(t)::value, decltype(q8)::value><<<grid, 256, 0, st>>>(a);
+  };
+  auto by_dim = [&](auto t, auto q8) {
+    if (head_dim == 128) go(std::integral_constant<int, 128>{}, t, q8);
+    else go(std::integral_constant<int, 64>{}, t, q8);
+  };
+  auto by_tree = [&](auto q8) {
+    if (tree) by_dim(std::true_type{}, q8);
+    else by_dim(std::false_type{}, q8);
+  };
+  if (a.kv.q8) by_tree(std::true_type{});
+  else by_tree(std::false_type{});
 }
 
 template <int RB>

@@ -16,6 +16,10 @@
 //     lane order (each lane names its own 16 bytes), so that fragment reads are
 //     contiguous.  Four stages each, keys requested four steps and values two
 //     before the step that holds them: a load has two steps to arrive.
+// An e4m3 pool (Q8): the workgroup's threads take 16 codes each of a block's keys and
+// values to registers, two steps later to bf16 (exact: codes times their token's scale)
+// and to the same places in LDS, two steps before the block's scores.  So each code is
+// converted once a workgroup, and the products and softmax are the same.
 // 2048 rows of 32 heads over 25600 keys (head_dim 128): 1403 -> 1151-1162 us (the
 // kernel it replaces staged blocks through registers and took scores, softmax and
 // product one after the other).  Over an append of 16 x 2048 tokens to 8192-26624 keys
@@ -24,6 +28,7 @@
 // product 1.3-1.57).  Fewer VALU instructions (the low parts by v_dot2c_f32_bf16: 1185
 // us) or addresses (per-lane ones: 1151) change nothing.
 #include "attn.h"
+#include "e4m3.h"
 #include "lds_load.h"
 
 namespace {
@@ -70,7 +75,7 @@ WAR_DEV void wait_sync() {
   __builtin_amdgcn_sched_barrier(0);
 }
 
-template <int HD>
+template <int HD, bool Q8>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) k_attn_rows(AttnArgs a) {
   constexpr int KF = HD / 16;    // 1 KB fragments of a block's keys (MFMA k-steps), and of its values
   constexpr int NDT = HD / 32;   // 32-dim output tiles
@@ -97,6 +102,23 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
   }
   const int kread = (ln >> 4) * 1024 + g * 256 + (lane & 15) * 16, vread = ST * SB + lane * 16;
 
+  // Q8: 16-byte piece of a page that a thread takes, of the keys and of the values: all
+  // threads both at head_dim 128, the first half keys and the other values at 64.  A
+  // wave's key pieces are 1 KB of a page, dealt so that eight neighbouring lanes write
+  // eight key rows, which are neighbours in LDS.
+  constexpr int PP = HD;  // pieces of a page's keys
+  const int kid = tid & (2 * PP - 1);
+  const bool kmine = HD == 128 || tid < 128, vmine = HD == 128 || tid >= 128;
+  const int kpg = kid / PP, vpg = kpg;
+  const int s8 = lane & 7, sub = (lane >> 3) & 3;                   // key row member, 16 dims of its 64
+  const int rgrp = ((kid & (PP - 1)) >> 6) * 2 + (lane >> 5);       // (t, 64 dims) of the page
+  const int kt = rgrp / (HD / 64), kf = (rgrp % (HD / 64)) * 4 + sub;  // slot group, k-step
+  const int kpiece = (rgrp * 8 + s8) * 4 + sub, kscale = s8 * 2 + kt;
+  const int kdst = (kf >> 1) * 2048 + kpg * 1024 + (kf & 1) * 512 + (kt * 8 + s8) * 16;
+  const int vpiece = kid & (PP - 1), vp32 = vpiece >> 5, vhalf = (vpiece >> 4) & 1;
+  const int vscale = val_scale8(vhalf * 8);
+  const int vdst = (vpg * NDT + vp32) * 1024 + (vhalf * 32 + (vpiece & 15)) * 16;
+
   const UnitQueue uq(total);
   __shared__ int s_it;
   if (tid == 0) s_it = blockIdx.x;
@@ -114,7 +136,13 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
     // blocks before nfull lie at or below every row's position
     const int nfull = qpos0 - 31 - kbeg < 0 ? 0 : min(nb, (qpos0 - 31 - kbeg) / 32 + 1);
     const int64_t pstride = (int64_t)a.kv.n_kv_heads * 2 * P * HD;
-    const bf16_t* kvb = a.kv.kv + a.kv.page_elems(a.layer, 0, kvh, 0);
+    const bf16_t* kvb = a.kv.kv + (Q8 ? 0 : a.kv.page_elems(a.layer, 0, kvh, 0));
+    const uint8_t *q8b = nullptr, *scb = nullptr;
+    if constexpr (Q8) {
+      q8b = a.kv.q8 + a.kv.page_elems(a.layer, 0, kvh, 0);
+      scb = a.kv.scale + a.kv.scale_bytes(a.layer, 0, kvh);
+    }
+    const int64_t sstride = (int64_t)a.kv.n_kv_heads * 32;
 
     // Page ids: lane l of pv holds page 64 n + l of the chunk (the sequence's
     // last page beyond its end), pn those of the next n.
@@ -144,6 +172,45 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
       for (int i = 0; i < PW; ++i) {
         const int q = w * PW + i;
         load_lds16(lds0 + (ST + stage) * SB + q * 1024, kvb + (int64_t)(q / NDT ? p1 : p0) * pstride, voff[i]);
+      }
+    };
+
+    // Q8: this thread's 16 codes of a block's keys and values, with their scale bytes
+    struct Codes {
+      uint4 k, v;
+      uint32_t ks;
+      uint2 vs;
+    };
+    auto fetch = [&](Codes& c, int p0, int p1) __attribute__((always_inline)) {
+      const int pk = kpg ? p1 : p0, pv_ = vpg ? p1 : p0;
+      if (kmine) {
+        c.k = *reinterpret_cast<const uint4*>(q8b + (int64_t)pk * pstride + kpiece * 16);
+        c.ks = scb[(int64_t)pk * sstride + kscale];
+      }
+      if (vmine) {
+        c.v = *reinterpret_cast<const uint4*>(q8b + (int64_t)pv_ * pstride + P * HD + vpiece * 16);
+        c.vs = *reinterpret_cast<const uint2*>(scb + (int64_t)pv_ * sstride + vscale);
+      }
+    };
+    auto convert = [&](const Codes& c, int stage) __attribute__((always_inline)) {
+      if (kmine) {
+        const float f = scale_of<0>(c.ks);
+        unsigned char* d = smem + stage * SB + kdst;
+        *reinterpret_cast<uint4*>(d) = from_e4m3x8(c.k.x, c.k.y, f);
+        *reinterpret_cast<uint4*>(d + 256) = from_e4m3x8(c.k.z, c.k.w, f);
+      }
+      if (vmine) {
+        const float f[8] = {scale_of<0>(c.vs.x), scale_of<1>(c.vs.x), scale_of<2>(c.vs.x), scale_of<3>(c.vs.x),
+                            scale_of<0>(c.vs.y), scale_of<1>(c.vs.y), scale_of<2>(c.vs.y), scale_of<3>(c.vs.y)};
+        auto eight = [&](uint32_t w0, uint32_t w1) __attribute__((always_inline)) {
+          const auto a0 = __builtin_amdgcn_cvt_pk_f32_fp8(w0, false), a1 = __builtin_amdgcn_cvt_pk_f32_fp8(w0, true);
+          const auto a2 = __builtin_amdgcn_cvt_pk_f32_fp8(w1, false), a3 = __builtin_amdgcn_cvt_pk_f32_fp8(w1, true);
+          return make_uint4(pack2(a0[0] * f[0], a0[1] * f[1]), pack2(a1[0] * f[2], a1[1] * f[3]),
+                            pack2(a2[0] * f[4], a2[1] * f[5]), pack2(a3[0] * f[6], a3[1] * f[7]));
+        };
+        unsigned char* d = smem + (ST + stage) * SB + vdst;
+        *reinterpret_cast<uint4*>(d) = eight(c.v.x, c.v.y);
+        *reinterpret_cast<uint4*>(d + 256) = eight(c.v.z, c.v.w);
       }
     };
 
@@ -190,9 +257,15 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
     // softmax of block i makes its weights.  Past the end the requests repeat the
     // last block and S(i + 1) is of no use; block -1 has zero weights and zeros.
     auto step = [&](int i, f32x16& s, f32x16& snext, const Pw& pin, Pw& pout, int k0, int k1, int v0,
-                    int v1) __attribute__((always_inline)) {
-      load_k(i & 3, k0, k1);
-      load_v((i + 2) & 3, v0, v1);
+                    int v1, [[maybe_unused]] Codes& cd) __attribute__((always_inline)) {
+      if constexpr (Q8) {
+        // block i + 2 to LDS, block i + 4 requested in its place
+        convert(cd, (i + 2) & 3);
+        fetch(cd, k0, k1);
+      } else {
+        load_k(i & 3, k0, k1);
+        load_v((i + 2) & 3, v0, v1);
+      }
       if (i >= nfull) {  // keys above some row's position or past the sequence end
         const int kb = kbeg + 32 * i;
 #pragma unroll
@@ -269,24 +342,38 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
         m_run = m_new;
       }
       l_run += sum;
-      wait_sync<4 * PW>();  // K(i + 2) and V(i) are here; steps i - 1 and i may be in flight
+      wait_sync<Q8 ? 63 : 4 * PW>();  // K(i + 2) and V(i) are here; steps i - 1 and i may be in flight
     };
 
     if (nb > 0) {
       const int lb = nb - 1;
       int k0, k1, v0[2], v1[2];  // v: pages of the blocks whose values are requested next
-      pages(0, k0, k1);
-      load_k(0, k0, k1);
-      const int f0 = k0, f1 = k1;
-      pages(min(1, lb), k0, k1);
-      load_k(1, k0, k1);
-      const int g0 = k0, g1 = k1;
-      pages(min(2, lb), v0[0], v1[0]);
-      load_k(2, v0[0], v1[0]);
-      load_v(0, f0, f1);
-      pages(min(3, lb), v0[1], v1[1]);
-      load_k(3, v0[1], v1[1]);
-      load_v(1, g0, g1);
+      Codes ca{}, cb{};
+      if constexpr (Q8) {
+        pages(0, k0, k1);
+        fetch(ca, k0, k1);
+        pages(min(1, lb), k0, k1);
+        fetch(cb, k0, k1);
+        convert(ca, 0);
+        pages(min(2, lb), k0, k1);
+        fetch(ca, k0, k1);
+        convert(cb, 1);
+        pages(min(3, lb), k0, k1);
+        fetch(cb, k0, k1);
+      } else {
+        pages(0, k0, k1);
+        load_k(0, k0, k1);
+        const int f0 = k0, f1 = k1;
+        pages(min(1, lb), k0, k1);
+        load_k(1, k0, k1);
+        const int g0 = k0, g1 = k1;
+        pages(min(2, lb), v0[0], v1[0]);
+        load_k(2, v0[0], v1[0]);
+        load_v(0, f0, f1);
+        pages(min(3, lb), v0[1], v1[1]);
+        load_k(3, v0[1], v1[1]);
+        load_v(1, g0, g1);
+      }
       // block -1's values
       for (int e = tid; e < SB / 16; e += 256)
         *reinterpret_cast<uint4*>(smem + (ST + 3) * SB + e * 16) = make_uint4(0, 0, 0, 0);
@@ -294,12 +381,12 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
       Pw pa, pb;
 #pragma unroll
       for (int pg = 0; pg < 2; ++pg) pa.hi[pg] = pa.lo[pg] = make_uint4(0, 0, 0, 0);
-      wait_sync<5 * PW>();
+      wait_sync<Q8 ? 63 : 5 * PW>();
       scores(0, sa);
-      wait_sync<4 * PW>();
+      wait_sync<Q8 ? 63 : 4 * PW>();
       for (int i = 0;;) {
         pages(min(i + 4, lb), k0, k1);
-        step(i, sa, sb, pa, pb, k0, k1, v0[0], v1[0]);
+        step(i, sa, sb, pa, pb, k0, k1, v0[0], v1[0], ca);
         v0[0] = k0;
         v1[0] = k1;
         if (++i == nb) {
@@ -307,7 +394,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
           break;
         }
         pages(min(i + 4, lb), k0, k1);
-        step(i, sb, sa, pb, pa, k0, k1, v0[1], v1[1]);
+        step(i, sb, sa, pb, pa, k0, k1, v0[1], v1[1], cb);
         v0[1] = k0;
         v1[1] = k1;
         if (++i == nb) break;
@@ -349,6 +436,11 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
 }  // namespace
 
 void launch_attn_rows(const AttnArgs& a, int head_dim, int grid, hipStream_t st) {
-  if (head_dim == 128) k_attn_rows<128><<<grid, 256, 0, st>>>(a);
-  else k_attn_rows<64><<<grid, 256, 0, st>>>(a);
+  if (a.kv.q8) {
+    if (head_dim == 128) k_attn_rows<128, true><<<grid, 256, 0, st>>>(a);
+    else k_attn_rows<64, true><<<grid, 256, 0, st>>>(a);
+  } else {
+    if (head_dim == 128) k_attn_rows<128, false><<<grid, 256, 0, st>>>(a);
+    else k_attn_rows<64, false><<<grid, 256, 0, st>>>(a);
+  }
 }

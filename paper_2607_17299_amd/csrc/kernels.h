@@ -12,13 +12,23 @@
 // in the order the attention's MFMA fragments read it, so that every K load of
 // a wave reads 512 contiguous bytes of a page: key slot s, dim d sits at
 // key_elem(s, d) (below).
+//
+// A pool in e4m3 (q8 not null) has the same page regions in bytes, in the orders
+// key_elem8 and val_elem8, and 32 scale bytes a page and kv-head behind all pages:
+// the block of a scale is the head_dim keys (or values) of one token and kv-head, the
+// byte is e + 127 for the scale 2^e.
 struct KvGeom {
   bf16_t* kv;
+  uint8_t* q8;     // e4m3 pages, or nullptr: bf16 in kv
+  uint8_t* scale;  // scale bytes of the e4m3 pages
   int64_t num_pages;
   int n_kv_heads, head_dim, page_size;
   __host__ __device__ int64_t page_elems(int layer, int page, int kvh, int kind) const {
     return ((((int64_t)layer * num_pages + page) * n_kv_heads + kvh) * 2 + kind) *
            (int64_t)page_size * head_dim;
+  }
+  __host__ __device__ int64_t scale_bytes(int layer, int page, int kvh) const {
+    return (((int64_t)layer * num_pages + page) * n_kv_heads + kvh) * 32;
   }
 };
 
@@ -32,6 +42,23 @@ __host__ __device__ inline int key_elem(int s, int d, int head_dim) {
   const int t = (s >> 2) & 1, s8 = ((s >> 3) << 2) | (s & 3);
   return ((t * (head_dim >> 5) + (d >> 5)) * 8 + s8) * 32 + (d & 31);
 }
+
+// The same of an e4m3 page, whose 64-byte rows hold 64 dims: one load of 16 bytes a
+// lane covers two MFMA k-steps of a key.
+__host__ __device__ inline int key_elem8(int s, int d, int head_dim) {
+  const int t = (s >> 2) & 1, s8 = ((s >> 3) << 2) | (s & 3);
+  return ((t * (head_dim >> 6) + (d >> 6)) * 8 + s8) * 64 + (d & 63);
+}
+// Offset of value slot s, dim d in an e4m3 page's V region: 16-byte pieces of eight
+// slots of dims 32 p + r and 32 p + 16 + r, in the order p, slot half, r: one load of
+// 16 bytes a lane is its 8 keys of two 16-dim output tiles.
+__host__ __device__ inline int val_elem8(int s, int d) {
+  return (((d >> 5) * 2 + (s >> 3)) * 16 + (d & 15)) * 16 + ((d >> 4) & 1) * 8 + (s & 7);
+}
+// Offsets in the 32 scale bytes: a lane of the attention's score tiles reads the pair
+// (slot, slot + 4) of its two keys, and eight consecutive slots' value scales.
+__host__ __device__ inline int key_scale8(int s) { return (((s >> 3) << 2) | (s & 3)) * 2 + ((s >> 2) & 1); }
+__host__ __device__ inline int val_scale8(int s) { return 16 + s; }
 
 // The attention's eight work counters are a 128-byte line apart (in ints).
 constexpr int kCtrStride = 32;
@@ -76,7 +103,7 @@ enum { EPI_PARTIAL = 0, EPI_ARGMAX = 1, EPI_SWIGLU = 2 };
 
 struct AttnArgs {
   const bf16_t* q;  // [rows][n_q_heads * head_dim]
-  int q_stride;
+  int64_t q_stride;
   KvGeom kv;
   int layer;
   const int32_t* table;
@@ -89,6 +116,7 @@ struct AttnArgs {
   float* pl;         // [item][kvh][RB]
   float* po;         // [item][kvh][RB][head_dim]
   bf16_t* o;         // combine output [rows][n_q_heads * head_dim]
+  int64_t o_stride;  // elements between its rows
   int32_t* unit_ctr; // attention work counters; zero before each attention
                      // launch (the combine kernel resets them)
 };
@@ -99,6 +127,17 @@ void launch_grow(const PoolDev& p, int n, const int32_t* seq, const int32_t* a, 
                  int mode, hipStream_t st);
 void launch_verify_setup(const PoolDev& p, const VerifySetupArgs& a, const StepMeta& m,
                          hipStream_t st);
+// The attention plan of given rows (nothing is reserved): draft_lens holds the requests'
+// row counts, 0 .. k_max + 1; a request that its pages cannot hold fails the plan.
+void launch_attend_plan(const PoolDev& p, const VerifySetupArgs& a, const StepMeta& m, hipStream_t st);
+// The same in blocks of `TB` tokens (k_attn_rows): segment b * blocks + i is block i of
+// request b.
+struct RowPlanArgs {
+  int B, n_max, TB, blocks, chunk, items_fill;
+  const int32_t *seq_ids, *ctx_lens, *n_lens;
+  int32_t* unit_ctr;
+};
+void launch_attend_plan_rows(const PoolDev& p, const RowPlanArgs& a, const StepMeta& m, hipStream_t st);
 void launch_commit(const PoolDev& p, int B, const int32_t* seq, int32_t* ctx, const int32_t* acc,
                    uint32_t commit_seq, hipStream_t st);
 void launch_free(const PoolDev& p, int n, const int32_t* seq, hipStream_t st);
@@ -108,6 +147,17 @@ void launch_kv_load(const PoolDev& p, const KvGeom& g, int seq, int layer, int p
 void launch_append_read(const PoolDev& p, int n, const int32_t* seq, const int32_t* ctx, int64_t total,
                         const int32_t* tokens, int vocab, int flags, int32_t* out, hipStream_t st);
 void launch_add_ctx(int n, int32_t* ctx, const int32_t* add, hipStream_t st);
+
+// keys and values of given tokens into or out of the pages (kv8.hip)
+struct KvMove {
+  int layer, B, n_max;
+  const int32_t *seq, *pos, *n;  // [B]; null: seq0, pos0, n_max
+  int seq0, pos0;
+  bf16_t *k, *v;                 // row b * n_max + i: token pos[b] + i
+  int64_t k_stride, v_stride;    // elements between rows
+  int64_t head_stride;           // elements between a row's kv-heads
+};
+void launch_kv_move(bool write, const PoolDev& p, const KvGeom& g, const KvMove& m, hipStream_t st);
 
 // GEMM of few rows (gemm.hip): at most 80, or 96 where gemm_tiled says so
 void launch_gemm(const GemmArgs& g, int epi, int splits, hipStream_t st);

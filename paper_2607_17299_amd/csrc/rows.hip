@@ -6,6 +6,9 @@
 // matrix multiply (norm outputs, SwiGLU product) and the rotated q, k and the v
 // stored in the KV pages are rounded to bf16 (nearest even).  The residual
 // stream, norm statistics, rotation and SwiGLU arithmetic stay fp32.
+#include <type_traits>
+
+#include "e4m3.h"
 #include "kernels.h"
 
 namespace {
@@ -129,6 +132,34 @@ __global__ void __launch_bounds__(1024) k_residual_norm(int rows, int splits, co
   }
 }
 
+// Four pairs (x1[e], x2[e]), half a head apart, of a QKV row: the sums of its partials.
+WAR_DEV void pair_sums(const float* pr, int64_t pstride, int splits, int col, int half, float (&x1)[4], float (&x2)[4]) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) x1[e] = x2[e] = 0.f;
+#pragma unroll 4
+  for (int s = 0; s < splits; ++s) {
+    const float4 a1 = *reinterpret_cast<const float4*>(pr + s * pstride + col);
+    const float4 a2 = *reinterpret_cast<const float4*>(pr + s * pstride + col + half);
+    x1[0] += a1.x; x1[1] += a1.y; x1[2] += a1.z; x1[3] += a1.w;
+    x2[0] += a2.x; x2[1] += a2.y; x2[2] += a2.z; x2[3] += a2.w;
+  }
+}
+// rotate four pairs and round them
+WAR_DEV void rotate_pairs(const float (&x1)[4], const float (&x2)[4], const float* cos_r, const float* sin_r,
+                          bf16_t (&b1)[4], bf16_t (&b2)[4]) {
+  const float4 c = *reinterpret_cast<const float4*>(cos_r);
+  const float4 sn = *reinterpret_cast<const float4*>(sin_r);
+  const float cc[4] = {c.x, c.y, c.z, c.w}, ss[4] = {sn.x, sn.y, sn.z, sn.w};
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    b1[e] = f2bf(x1[e] * cc[e] - x2[e] * ss[e]);
+    b2[e] = f2bf(x2[e] * cc[e] + x1[e] * ss[e]);
+  }
+}
+WAR_DEV uint2 pack4(const bf16_t (&v)[4]) {
+  return make_uint2((uint32_t)v[0] | ((uint32_t)v[1] << 16), (uint32_t)v[2] | ((uint32_t)v[3] << 16));
+}
+
 // Sum the QKV partials of one row, rotate q and k (rotate-half pairs (j, j+D/2)),
 // round to bf16; q goes to its buffer, k and v of active rows into the KV page slot
 // of the row's position (a tree node's own slot, when the step has tree drafts).
@@ -170,24 +201,11 @@ __global__ void __launch_bounds__(64) k_qkv_rope(int rows, int splits, const flo
   }
   const int col = (region == 0 ? 0 : region == 1 ? md.nq * md.hd : (md.nq + md.nkv) * md.hd) +
                   head * md.hd + j;
-  float x1[4] = {0.f, 0.f, 0.f, 0.f}, x2[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-  for (int s = 0; s < splits; ++s) {
-    const float4 a1 = *reinterpret_cast<const float4*>(pr + s * pstride + col);
-    const float4 a2 = *reinterpret_cast<const float4*>(pr + s * pstride + col + half);
-    x1[0] += a1.x; x1[1] += a1.y; x1[2] += a1.z; x1[3] += a1.w;
-    x2[0] += a2.x; x2[1] += a2.y; x2[2] += a2.z; x2[3] += a2.w;
-  }
+  float x1[4], x2[4];
+  pair_sums(pr, pstride, splits, col, half, x1, x2);
   bf16_t b1[4], b2[4];
   if (region < 2) {
-    const float4 c = *reinterpret_cast<const float4*>(cos_t + r * half + j);
-    const float4 sn = *reinterpret_cast<const float4*>(sin_t + r * half + j);
-    const float cc[4] = {c.x, c.y, c.z, c.w}, ss[4] = {sn.x, sn.y, sn.z, sn.w};
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      b1[e] = f2bf(x1[e] * cc[e] - x2[e] * ss[e]);
-      b2[e] = f2bf(x2[e] * cc[e] + x1[e] * ss[e]);
-    }
+    rotate_pairs(x1, x2, cos_t + r * half + j, sin_t + r * half + j, b1, b2);
   } else {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -195,9 +213,6 @@ __global__ void __launch_bounds__(64) k_qkv_rope(int rows, int splits, const flo
       b2[e] = f2bf(x2[e]);
     }
   }
-  auto pack4 = [](const bf16_t* v) {
-    return make_uint2((uint32_t)v[0] | ((uint32_t)v[1] << 16), (uint32_t)v[2] | ((uint32_t)v[3] << 16));
-  };
   if (region == 0) {
     bf16_t* qr = q + (int64_t)r * md.nq * md.hd + head * md.hd;
     *reinterpret_cast<uint2*>(qr + j) = pack4(b1);
@@ -214,6 +229,83 @@ __global__ void __launch_bounds__(64) k_qkv_rope(int rows, int splits, const flo
         base[(j + e + half) * kv.page_size + slot] = b2[e];
       }
     }
+  }
+}
+
+// The same into e4m3 pages.  The numbers rounded to bf16 are the block's (e4m3.h), so a
+// step leaves what an import of its bf16 keys and values would leave.  A thread takes
+// four pairs of a query head, or of a key head and of its values: what marks a token
+// that is not finite is decided once for both (see k_kv_write).  A head is half / 4 (16
+// or 8) neighbouring threads of the wave.
+__global__ void __launch_bounds__(64) k_qkv_rope8(int rows, int splits, const float* P, ModelDims md,
+                                                  const float* cos_t, const float* sin_t, StepMeta meta,
+                                                  const int32_t* row_req, const int32_t* table, int max_pages,
+                                                  KvGeom kv, int layer, bf16_t* q) {
+  const int r = blockIdx.x;
+  const int half = md.hd / 2;
+  const int nq_pairs = md.nq * half;
+  const int p = (blockIdx.y * blockDim.x + threadIdx.x) * 4;
+  if (p >= nq_pairs + md.nkv * half) return;
+  const float* pr = P + (int64_t)r * md.qkv;
+  const int64_t pstride = (int64_t)rows * md.qkv;
+  const int col = p / half * md.hd + p % half, j = p % half;  // key heads follow the query heads
+  float x1[4], x2[4];
+  bf16_t b1[4], b2[4];
+  if (p < nq_pairs) {
+    pair_sums(pr, pstride, splits, col, half, x1, x2);
+    rotate_pairs(x1, x2, cos_t + r * half + j, sin_t + r * half + j, b1, b2);
+    bf16_t* qr = q + (int64_t)r * md.nq * md.hd + col;
+    *reinterpret_cast<uint2*>(qr) = pack4(b1);
+    *reinterpret_cast<uint2*>(qr + half) = pack4(b2);
+    return;
+  }
+  if (!meta.active[r]) return;
+  const int head = p / half - md.nq;
+  const int pos = meta.kvpos ? meta.kvpos[r] : meta.pos[r];
+  const int page = table[(int64_t)meta.req_seq[row_req[r]] * max_pages + pos / kv.page_size];
+  const int slot = pos % kv.page_size;
+  float v1[4], v2[4];
+  pair_sums(pr, pstride, splits, col, half, x1, x2);
+  pair_sums(pr, pstride, splits, col + md.nkv * md.hd, half, v1, v2);
+  rotate_pairs(x1, x2, cos_t + r * half + j, sin_t + r * half + j, b1, b2);
+  float ktop = 0.f, vtop = 0.f;
+  int any = 0;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    x1[e] = bf2f(b1[e]);
+    x2[e] = bf2f(b2[e]);
+    v1[e] = round_bf(v1[e]);
+    v2[e] = round_bf(v2[e]);
+    ktop = fmaxf(ktop, fmaxf(fabsf(x1[e]), fabsf(x2[e])));
+    vtop = fmaxf(vtop, fmaxf(fabsf(v1[e]), fabsf(v2[e])));
+    any |= !(fabsf(x1[e]) < INFINITY) | !(fabsf(x2[e]) < INFINITY) | !(fabsf(v1[e]) < INFINITY) |
+           !(fabsf(v2[e]) < INFINITY);
+  }
+  for (int o = 1; o < half / 4; o <<= 1) {
+    ktop = fmaxf(ktop, __shfl_xor(ktop, o, 64));
+    vtop = fmaxf(vtop, __shfl_xor(vtop, o, 64));
+    any |= __shfl_xor(any, o, 64);
+  }
+  const int ke = block_exp8(ktop), ve = block_exp8(vtop);
+  const float kf = exp2_int(-ke), vf = exp2_int(-ve);
+  const uint32_t nan4 = kNanCode8 * 0x01010101u;
+  const uint32_t k1 = any ? nan4 : to_e4m3x4(x1[0] * kf, x1[1] * kf, x1[2] * kf, x1[3] * kf);
+  const uint32_t k2 = any ? nan4 : to_e4m3x4(x2[0] * kf, x2[1] * kf, x2[2] * kf, x2[3] * kf);
+  const uint32_t w1 = any ? 0 : to_e4m3x4(v1[0] * vf, v1[1] * vf, v1[2] * vf, v1[3] * vf);
+  const uint32_t w2 = any ? 0 : to_e4m3x4(v2[0] * vf, v2[1] * vf, v2[2] * vf, v2[3] * vf);
+  uint8_t* kb = kv.q8 + kv.page_elems(layer, page, head, 0);
+  uint8_t* vb = kv.q8 + kv.page_elems(layer, page, head, 1);
+  *reinterpret_cast<uint32_t*>(kb + key_elem8(slot, j, md.hd)) = k1;
+  *reinterpret_cast<uint32_t*>(kb + key_elem8(slot, j + half, md.hd)) = k2;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    vb[val_elem8(slot, j + e)] = (uint8_t)(w1 >> (8 * e));
+    vb[val_elem8(slot, j + e + half)] = (uint8_t)(w2 >> (8 * e));
+  }
+  if (j == 0) {
+    uint8_t* sc = kv.scale + kv.scale_bytes(layer, page, head);
+    sc[key_scale8(slot)] = any ? 127 : (uint8_t)(ke + 127);
+    sc[val_scale8(slot)] = any ? 0 : (uint8_t)(ve + 127);
   }
 }
 
@@ -300,16 +392,24 @@ __global__ void __launch_bounds__(1024) k_argmax_accept(const int32_t* ntok, int
 // ctx + 1 .. ctx + a (node d of the path has index >= d, so a sequential copy
 // in depth order would also be safe; staging makes the order irrelevant).
 constexpr int kCompactMaxNodes = 31, kCompactMaxDim = 128;
+template <bool Q8>
 __global__ void __launch_bounds__(256) k_kv_compact(KvGeom kv, StepMeta meta, const int32_t* table,
                                                     int max_pages, const int32_t* accept_lens,
                                                     const int32_t* accept_path, int k_max) {
-  __shared__ bf16_t s_k[kCompactMaxNodes][kCompactMaxDim], s_v[kCompactMaxNodes][kCompactMaxDim];
+  using T = std::conditional_t<Q8, uint8_t, bf16_t>;  // e4m3: codes and scales move as they are
+  __shared__ T s_k[kCompactMaxNodes][kCompactMaxDim], s_v[kCompactMaxNodes][kCompactMaxDim];
+  __shared__ uint8_t s_sc[kCompactMaxNodes][2];
   __shared__ int s_src[kCompactMaxNodes];
   const int layer = blockIdx.x, kvh = blockIdx.y, b = blockIdx.z;
   const int n = meta.req_ntok[b];
   const int a = min(min(accept_lens[b], n - 1), k_max);
   if (a <= 0) return;
   const int D = kv.head_dim, P = kv.page_size;
+  T* base;
+  if constexpr (Q8) base = kv.q8;
+  else base = kv.kv;
+  auto key_at = [D](int s, int c) { return Q8 ? key_elem8(s, c, D) : key_elem(s, c, D); };
+  auto val_at = [P](int s, int c) { return Q8 ? val_elem8(s, c) : c * P + s; };
   const int ctx = meta.req_pos0[b];
   const int32_t* trow = table + (int64_t)meta.req_seq[b] * max_pages;
   if (threadIdx.x < a) {
@@ -321,16 +421,18 @@ __global__ void __launch_bounds__(256) k_kv_compact(KvGeom kv, StepMeta meta, co
     const int d = e / D, c = e % D;
     const int sp = ctx + s_src[d];
     const int pg = trow[sp / P], sl = sp % P;
-    s_k[d][c] = kv.kv[kv.page_elems(layer, pg, kvh, 0) + key_elem(sl, c, D)];
-    s_v[d][c] = kv.kv[kv.page_elems(layer, pg, kvh, 1) + (int64_t)c * P + sl];
+    s_k[d][c] = base[kv.page_elems(layer, pg, kvh, 0) + key_at(sl, c)];
+    s_v[d][c] = base[kv.page_elems(layer, pg, kvh, 1) + val_at(sl, c)];
+    if (Q8 && c < 2) s_sc[d][c] = kv.scale[kv.scale_bytes(layer, pg, kvh) + (c == 0 ? key_scale8(sl) : val_scale8(sl))];
   }
   __syncthreads();
   for (int e = threadIdx.x; e < a * D; e += blockDim.x) {
     const int d = e / D, c = e % D;
     const int dp = ctx + d + 1;
     const int pg = trow[dp / P], sl = dp % P;
-    kv.kv[kv.page_elems(layer, pg, kvh, 0) + key_elem(sl, c, D)] = s_k[d][c];
-    kv.kv[kv.page_elems(layer, pg, kvh, 1) + (int64_t)c * P + sl] = s_v[d][c];
+    base[kv.page_elems(layer, pg, kvh, 0) + key_at(sl, c)] = s_k[d][c];
+    base[kv.page_elems(layer, pg, kvh, 1) + val_at(sl, c)] = s_v[d][c];
+    if (Q8 && c < 2) kv.scale[kv.scale_bytes(layer, pg, kvh) + (c == 0 ? key_scale8(sl) : val_scale8(sl))] = s_sc[d][c];
   }
 }
 
@@ -355,6 +457,11 @@ void launch_qkv_rope(int rows, int splits, const float* P, const ModelDims& md,
                      const float* cos_t, const float* sin_t, const StepMeta& meta,
                      const int32_t* row_req, const int32_t* table, int max_pages, const KvGeom& kv,
                      int layer, bf16_t* q, hipStream_t st) {
+  if (kv.q8) {
+    dim3 grid(rows, cdiv_i((md.nq + md.nkv) * md.hd / 8, 64));
+    k_qkv_rope8<<<grid, 64, 0, st>>>(rows, splits, P, md, cos_t, sin_t, meta, row_req, table, max_pages, kv, layer, q);
+    return;
+  }
   dim3 grid(rows, cdiv_i(md.qkv / 8, 64));  // four pairs per thread, one wave per workgroup
   k_qkv_rope<<<grid, 64, 0, st>>>(rows, splits, P, md, cos_t, sin_t, meta, row_req, table,
                                    max_pages, kv, layer, q);
@@ -370,5 +477,6 @@ void launch_kv_compact(const KvGeom& kv, int n_layers, int B, const StepMeta& me
                        int max_pages, const int32_t* accept_lens, const int32_t* accept_path, int k_max,
                        hipStream_t st) {
   dim3 grid(n_layers, kv.n_kv_heads, B);
-  k_kv_compact<<<grid, 256, 0, st>>>(kv, meta, table, max_pages, accept_lens, accept_path, k_max);
+  if (kv.q8) k_kv_compact<true><<<grid, 256, 0, st>>>(kv, meta, table, max_pages, accept_lens, accept_path, k_max);
+  else k_kv_compact<false><<<grid, 256, 0, st>>>(kv, meta, table, max_pages, accept_lens, accept_path, k_max);
 }

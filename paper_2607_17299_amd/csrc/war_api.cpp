@@ -151,48 +151,61 @@ struct Workspace {
   }
 };
 
+// Hands out 256-byte aligned pieces of an allocation at `base` (nullptr: counts only).
+struct Pieces {
+  char* base;
+  size_t off = 0;
+  template <class T>
+  T* take(size_t bytes) {
+    char* at = base ? base + off : nullptr;
+    off += (bytes + 255) & ~size_t(255);
+    return reinterpret_cast<T*>(at);
+  }
+};
+
+// Step metadata, the attention work list and its partials, for R rows of n_req
+// requests in at most n_seg segments.
+void attn_layout(Workspace& v, Pieces& pc, int nkv, int hd, int R, int n_req, int n_seg, int64_t items, int rb) {
+  v.R = R;
+  v.n_req_cap = n_req;
+  v.n_seg_cap = n_seg;
+  v.items_cap = std::max<int64_t>(items, 1);
+  v.rb_cap = rb;
+  v.rows = pc.take<int32_t>((size_t)4 * R * 4);
+  v.tree = pc.take<int32_t>((size_t)2 * R * 4);
+  v.reqs = pc.take<int32_t>((size_t)4 * v.n_req_cap * 4);
+  v.segs = pc.take<int32_t>((size_t)4 * v.n_seg_cap * 4);
+  v.n_items = pc.take<int32_t>(16);
+  v.unit_ctr = pc.take<int32_t>(8 * kCtrStride * 4);
+  v.items = pc.take<int4>((size_t)v.items_cap * sizeof(int4));
+  v.udesc = pc.take<int4>((size_t)v.items_cap * 2 * sizeof(int4));
+  v.order = pc.take<int32_t>((size_t)v.items_cap * 4);
+  const size_t pr = (size_t)v.items_cap * nkv * rb;
+  v.pm = pc.take<float>(pr * 4);
+  v.pl = pc.take<float>(pr * 4);
+  v.po = pc.take<float>(pr * hd * 4);
+}
+
 // Lays a workspace out from `base` (nullptr: measure only); returns its bytes.
 size_t ws_layout(const ModelDims& md, int R, int64_t items, int rb, int64_t p_elems, char* base,
                  Workspace* w) {
-  size_t off = 0;
-  auto take = [&](size_t bytes) -> char* {
-    char* at = base ? base + off : nullptr;
-    off += (bytes + 255) & ~size_t(255);
-    return at;
-  };
+  Pieces pc{base};
   Workspace v;
-  v.R = R;
-  v.n_req_cap = std::max(R, kMaxBatch);
-  v.n_seg_cap = R + kMaxBatch;
-  v.items_cap = std::max<int64_t>(items, 1);
-  v.rb_cap = rb;
   v.p_elems = p_elems;
   const size_t nqhd = (size_t)md.nq * md.hd, nb = (size_t)md.V / 128;
-  v.h = reinterpret_cast<float*>(take((size_t)R * md.d * 4));
-  v.u = reinterpret_cast<bf16_t*>(take((size_t)R * md.d * 2));
-  v.q = reinterpret_cast<bf16_t*>(take((size_t)R * nqhd * 2));
-  v.o = reinterpret_cast<bf16_t*>(take((size_t)R * nqhd * 2));
-  v.y = reinterpret_cast<bf16_t*>(take((size_t)R * md.F * 2));
-  v.P = reinterpret_cast<float*>(take((size_t)p_elems * 4));
-  v.cos_t = reinterpret_cast<float*>(take((size_t)R * md.hd / 2 * 4));
-  v.sin_t = reinterpret_cast<float*>(take((size_t)R * md.hd / 2 * 4));
-  v.amax_v = reinterpret_cast<float*>(take((size_t)R * nb * 4));
-  v.amax_i = reinterpret_cast<int32_t*>(take((size_t)R * nb * 4));
-  v.rows = reinterpret_cast<int32_t*>(take((size_t)4 * R * 4));
-  v.tree = reinterpret_cast<int32_t*>(take((size_t)2 * R * 4));
-  v.reqs = reinterpret_cast<int32_t*>(take((size_t)4 * v.n_req_cap * 4));
-  v.segs = reinterpret_cast<int32_t*>(take((size_t)4 * v.n_seg_cap * 4));
-  v.n_items = reinterpret_cast<int32_t*>(take(16));
-  v.unit_ctr = reinterpret_cast<int32_t*>(take(8 * kCtrStride * 4));
-  v.items = reinterpret_cast<int4*>(take((size_t)v.items_cap * sizeof(int4)));
-  v.udesc = reinterpret_cast<int4*>(take((size_t)v.items_cap * 2 * sizeof(int4)));
-  v.order = reinterpret_cast<int32_t*>(take((size_t)v.items_cap * 4));
-  const size_t pr = (size_t)v.items_cap * md.nkv * rb;
-  v.pm = reinterpret_cast<float*>(take(pr * 4));
-  v.pl = reinterpret_cast<float*>(take(pr * 4));
-  v.po = reinterpret_cast<float*>(take(pr * md.hd * 4));
+  v.h = pc.take<float>((size_t)R * md.d * 4);
+  v.u = pc.take<bf16_t>((size_t)R * md.d * 2);
+  v.q = pc.take<bf16_t>((size_t)R * nqhd * 2);
+  v.o = pc.take<bf16_t>((size_t)R * nqhd * 2);
+  v.y = pc.take<bf16_t>((size_t)R * md.F * 2);
+  v.P = pc.take<float>((size_t)p_elems * 4);
+  v.cos_t = pc.take<float>((size_t)R * md.hd / 2 * 4);
+  v.sin_t = pc.take<float>((size_t)R * md.hd / 2 * 4);
+  v.amax_v = pc.take<float>((size_t)R * nb * 4);
+  v.amax_i = pc.take<int32_t>((size_t)R * nb * 4);
+  attn_layout(v, pc, md.nkv, md.hd, R, std::max(R, kMaxBatch), R + kMaxBatch, items, rb);
   if (w) *w = v;
-  return off;
+  return pc.off;
 }
 
 // ---- static device scratch (war_verify_step_noalloc)
@@ -268,6 +281,15 @@ struct war_model {
 //    commit j was issued, so fc_j - (total_need - need_at[j]) bounds the count
 //    after every step issued since.
 constexpr int kRing = 1024;
+
+struct war_attend {
+  war_kv_pool* pool;
+  int max_batch, max_rows;
+  DevBuf buf;
+  // the plan: its requests, rows a request, row block, segments and grid
+  int B = 0, n = 0, rb = 0, n_segs = 0, grid = 0;
+  Workspace ws;
+};
 
 struct war_kv_pool {
   war_model_config cfg;
@@ -557,6 +579,7 @@ AttnArgs attn_args(war_model* m, const Workspace& w, war_kv_pool* p, int TB) {
   a.pl = w.pl;
   a.po = w.po;
   a.o = w.o;
+  a.o_stride = a.q_stride;
   a.unit_ctr = w.unit_ctr;
   return a;
 }
@@ -754,18 +777,38 @@ void war_model_destroy(war_model* m) {
 war_status war_kv_pool_create(const war_model_config* cfg, void* kv_pages, int32_t num_pages,
                               int32_t* block_tables, int32_t max_seqs, int32_t max_pages_per_seq,
                               void* stream, war_kv_pool** out) {
+  return war_kv_pool_create_format(cfg, kv_pages, num_pages, WAR_KV_BF16, block_tables, max_seqs, max_pages_per_seq,
+                                   stream, out);
+}
+
+int64_t war_kv_pool_bytes(const war_model_config* cfg, int32_t num_pages, int32_t kv_format) {
+  if (check_config(cfg) != WAR_OK || num_pages < 1 || (kv_format != WAR_KV_BF16 && kv_format != WAR_KV_E4M3)) return -1;
+  const int64_t heads = (int64_t)cfg->n_layers * num_pages * cfg->n_kv_heads, numbers = 2 * cfg->page_size * cfg->head_dim;
+  return heads * (kv_format == WAR_KV_E4M3 ? numbers + 32 : 2 * numbers);
+}
+
+war_status war_kv_pool_create_format(const war_model_config* cfg, void* kv_pages, int32_t num_pages,
+                                     int32_t kv_format, int32_t* block_tables, int32_t max_seqs,
+                                     int32_t max_pages_per_seq, void* stream, war_kv_pool** out) {
   if (!out) return fail(WAR_ERR_INVALID_ARG, "null out");
   *out = nullptr;
   war_status s0 = check_config(cfg);
   if (s0 != WAR_OK) return s0;
   CHECK(kv_pages && block_tables, "null kv_pages or block_tables");
   CHECK(aligned16(kv_pages), "kv_pages must be 16-byte aligned");
+  CHECK(kv_format == WAR_KV_BF16 || kv_format == WAR_KV_E4M3, "unknown kv_format");
   CHECK(num_pages > 0 && max_seqs > 0 && max_pages_per_seq > 0, "non-positive pool size");
   CHECK((int64_t)max_pages_per_seq * cfg->page_size <= (1 << 24), "max_pages_per_seq too large");
   hipStream_t st = static_cast<hipStream_t>(stream);
   war_kv_pool* p = new war_kv_pool();
   p->cfg = *cfg;
-  p->geom.kv = static_cast<bf16_t*>(kv_pages);
+  p->geom = KvGeom{};
+  if (kv_format == WAR_KV_E4M3) {
+    p->geom.q8 = static_cast<uint8_t*>(kv_pages);
+    p->geom.scale = p->geom.q8 + (int64_t)cfg->n_layers * num_pages * cfg->n_kv_heads * 2 * cfg->page_size * cfg->head_dim;
+  } else {
+    p->geom.kv = static_cast<bf16_t*>(kv_pages);
+  }
   p->geom.num_pages = num_pages;
   p->geom.n_kv_heads = cfg->n_kv_heads;
   p->geom.head_dim = cfg->head_dim;
@@ -931,9 +974,66 @@ war_status war_kv_load(war_kv_pool* p, int32_t seq_id, int32_t layer, int32_t po
   HIPCHK(hipMemcpyAsync(&hs, p->dev.held + seq_id, 4, hipMemcpyDeviceToHost, st));
   HIPCHK(hipStreamSynchronize(st));
   CHECK((int64_t)pos0 + n <= (int64_t)hs * p->dev.page_size, "tokens beyond the sequence's pages");
-  launch_kv_load(p->dev, p->geom, seq_id, layer, pos0, n, static_cast<const bf16_t*>(src), st);
+  if (p->geom.q8) {
+    KvMove mv{};
+    mv.layer = layer;
+    mv.B = 1;
+    mv.n_max = n;
+    mv.seq0 = seq_id;
+    mv.pos0 = pos0;
+    mv.k = static_cast<bf16_t*>(const_cast<void*>(src));
+    mv.v = mv.k + (int64_t)p->geom.n_kv_heads * n * p->geom.head_dim;
+    mv.k_stride = mv.v_stride = p->geom.head_dim;
+    mv.head_stride = (int64_t)n * p->geom.head_dim;
+    launch_kv_move(true, p->dev, p->geom, mv, st);
+  } else {
+    launch_kv_load(p->dev, p->geom, seq_id, layer, pos0, n, static_cast<const bf16_t*>(src), st);
+  }
   HIPCHK(hipGetLastError());
   return WAR_OK;
+}
+
+static war_status kv_move(bool write, war_kv_pool* p, int32_t layer, int32_t B, const int32_t* seq_ids,
+                          const int32_t* pos0, int32_t n_max, const int32_t* n_lens, void* k, int64_t k_stride,
+                          void* v, int64_t v_stride, void* stream) {
+  CHECK(p, "null pool");
+  CHECK(layer >= 0 && layer < p->cfg.n_layers, "layer out of range");
+  CHECK(B >= 1 && B <= kMaxBatch, "B out of range [1, 1024]");
+  CHECK(n_max >= 0 && n_max <= 1 << 20, "n_max out of range [0, 2^20]");
+  CHECK(seq_ids && pos0 && k && v, "null array");
+  const int64_t row = (int64_t)p->geom.n_kv_heads * p->geom.head_dim;
+  CHECK(aligned16(k) && aligned16(v), "k and v must be 16-byte aligned");
+  CHECK(k_stride >= row && v_stride >= row && k_stride % 8 == 0 && v_stride % 8 == 0,
+        "strides must hold a row and be multiples of 8");
+  if (n_max == 0) return WAR_OK;
+  KvMove mv{};
+  mv.layer = layer;
+  mv.B = B;
+  mv.n_max = n_max;
+  mv.seq = seq_ids;
+  mv.pos = pos0;
+  mv.n = n_lens;
+  mv.k = static_cast<bf16_t*>(k);
+  mv.v = static_cast<bf16_t*>(v);
+  mv.k_stride = k_stride;
+  mv.v_stride = v_stride;
+  mv.head_stride = p->geom.head_dim;
+  launch_kv_move(write, p->dev, p->geom, mv, static_cast<hipStream_t>(stream));
+  HIPCHK(hipGetLastError());
+  return WAR_OK;
+}
+
+war_status war_kv_write(war_kv_pool* p, int32_t layer, int32_t B, const int32_t* seq_ids, const int32_t* pos0,
+                        int32_t n_max, const int32_t* n_lens, const void* k, int64_t k_stride, const void* v,
+                        int64_t v_stride, void* stream) {
+  return kv_move(true, p, layer, B, seq_ids, pos0, n_max, n_lens, const_cast<void*>(k), k_stride, const_cast<void*>(v),
+                 v_stride, stream);
+}
+
+war_status war_kv_read(war_kv_pool* p, int32_t layer, int32_t B, const int32_t* seq_ids, const int32_t* pos0,
+                       int32_t n_max, const int32_t* n_lens, void* k, int64_t k_stride, void* v,
+                       int64_t v_stride, void* stream) {
+  return kv_move(false, p, layer, B, seq_ids, pos0, n_max, n_lens, k, k_stride, v, v_stride, stream);
 }
 
 }  // extern "C"
@@ -1126,9 +1226,168 @@ war_status verify_impl(war_model* m, war_kv_pool* p, int32_t B, const int32_t* s
   return WAR_OK;
 }
 
+// How a plan of B requests with n rows each is laid out.  Few rows (a verify step's)
+// run in k_attn, more in blocks of 128 rows (k_attn_rows).
+struct AttendShape {
+  int rb, blocks, TB, chunk, items_fill, n_segs;
+  int64_t items;
+};
+AttendShape attend_shape(const war_kv_pool* p, int B, int n) {
+  const int G = p->cfg.n_q_heads / p->cfg.n_kv_heads, nkv = p->cfg.n_kv_heads, len = p->dev.max_pages * p->dev.page_size;
+  AttendShape s{};
+  if (G * n <= 48) {
+    s.rb = attn_rows_per_block(G, n);
+    s.blocks = 1;
+    s.TB = n;
+    s.chunk = 1024;
+    while (cdiv_i(len, s.chunk) > kMaxItemsPerSeq) s.chunk *= 2;
+    s.items = (int64_t)B * cdiv_i(len, s.chunk);
+    s.items_fill = (int)std::min<int64_t>(std::min(kMaxItemsPerSeq, std::max(1, kAttnFill / nkv)),
+                                          (int64_t)B * cdiv_i(len, 128));
+    s.n_segs = B;
+  } else {
+    s.rb = kPrefillRows;
+    s.TB = kPrefillRows / G;
+    s.blocks = cdiv_i(n, s.TB);
+    s.n_segs = B * s.blocks;
+    // chunks of kPrefillChunk keys, longer ones where there are units enough for 16
+    // rounds of the grid (each item has 128 rows of partial sums to write and merge)
+    s.chunk = kPrefillChunk;
+    while (cdiv_i(len, s.chunk) > kMaxItemsPerSeq) s.chunk *= 2;
+    const int64_t rounds = 16 * kAttnGrid / nkv, most = (int64_t)s.n_segs * cdiv_i(len, s.chunk);
+    while (s.chunk < len && (int64_t)s.n_segs * cdiv_i(len, s.chunk) > rounds) s.chunk *= 2;
+    s.items = std::min(most, std::max<int64_t>(s.n_segs, rounds));  // (grows with the segments, as a bound has to)
+    s.items_fill = std::max(1, kAttnGrid / nkv);
+  }
+  s.items = std::max<int64_t>(s.items, s.items_fill);
+  return s;
+}
+size_t attend_layout(const war_kv_pool* p, int B, int n, const AttendShape& s, char* base, Workspace* w) {
+  Pieces pc{base};
+  Workspace v{};
+  attn_layout(v, pc, p->cfg.n_kv_heads, p->cfg.head_dim, B * n, B, s.n_segs, s.items, s.rb);
+  if (w) *w = v;
+  return pc.off;
+}
+
 }  // namespace
 
 extern "C" {
+
+war_status war_attend_create(war_kv_pool* p, int32_t max_batch, int32_t max_rows, war_attend** out) {
+  CHECK(out, "null out");
+  *out = nullptr;
+  CHECK(p, "null pool");
+  CHECK(max_batch >= 1 && max_batch <= kMaxBatch, "max_batch out of range [1, 1024]");
+  CHECK(max_rows >= 1 && max_rows <= 65536 && (int64_t)max_batch * max_rows <= 1 << 20,
+        "max_rows out of range [1, 65536], or more than 2^20 rows");
+  const int G = p->cfg.n_q_heads / p->cfg.n_kv_heads;
+  size_t bytes = 0;  // the most of any plan: of each kind the one with the most requests and rows
+  for (int n : {std::min((int)max_rows, 48 / G), (int)max_rows})
+    bytes = std::max(bytes, attend_layout(p, max_batch, n, attend_shape(p, max_batch, n), nullptr, nullptr));
+  war_attend* a = new war_attend();
+  a->pool = p;
+  a->max_batch = max_batch;
+  a->max_rows = max_rows;
+  if (hipError_t e = a->buf.ensure(bytes); e != hipSuccess) {
+    delete a;
+    return fail(WAR_ERR_HIP, std::string("attention workspace: ") + hipGetErrorString(e));
+  }
+  *out = a;
+  return WAR_OK;
+}
+
+void war_attend_destroy(war_attend* a) {
+  if (!a) return;
+  a->buf.release();
+  delete a;
+}
+
+war_status war_attend_update(war_attend* a, int32_t B, int32_t n_max, const int32_t* seq_ids,
+                             const int32_t* ctx_lens, const int32_t* n_lens, const int32_t* draft_parents,
+                             void* stream) {
+  CHECK(a, "null attention");
+  CHECK(B >= 1 && B <= a->max_batch, "B out of range [1, max_batch]");
+  CHECK(n_max >= 1 && n_max <= a->max_rows, "n_max out of range [1, max_rows]");
+  CHECK(seq_ids && ctx_lens, "null array");
+  const war_kv_pool* p = a->pool;
+  const int G = p->cfg.n_q_heads / p->cfg.n_kv_heads;
+  const bool tree = draft_parents && n_max > 1;
+  if (tree && (G * n_max > 48 || n_max > 32))
+    return fail(WAR_ERR_UNSUPPORTED, "draft trees: n_q/n_kv * n_max must be <= 48 and n_max <= 32");
+  const AttendShape s = attend_shape(p, B, n_max);
+  if (attend_layout(p, B, n_max, s, nullptr, nullptr) > a->buf.bytes)
+    return fail(WAR_ERR_INVALID_ARG, "internal: attention plan exceeds its workspace");
+  attend_layout(p, B, n_max, s, a->buf.as<char>(), &a->ws);
+  a->ws.tree_step = tree;
+  a->B = B;
+  a->n = n_max;
+  a->rb = s.rb;
+  a->n_segs = s.n_segs;
+  a->grid = (int)std::min<int64_t>(s.items * p->cfg.n_kv_heads, kAttnGrid);
+  const StepMeta meta = a->ws.meta();
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  if (s.rb == kPrefillRows) {
+    RowPlanArgs ra{B, n_max, s.TB, s.blocks, s.chunk, s.items_fill, seq_ids, ctx_lens, n_lens, a->ws.unit_ctr};
+    launch_attend_plan_rows(p->dev, ra, meta, st);
+  } else {
+    VerifySetupArgs va{};
+    va.B = B;
+    va.k_max = n_max - 1;
+    va.vocab = p->cfg.vocab;
+    va.unit_ctr = a->ws.unit_ctr;
+    va.chunk = s.chunk;
+    va.items_double = cdiv_i(2 * kAttnGrid, p->cfg.n_kv_heads);
+    va.items_fill = s.items_fill;
+    va.seq_ids = seq_ids;
+    va.ctx_lens = ctx_lens;
+    va.draft_lens = n_lens;
+    va.G = G;
+    va.rb = s.rb;
+    va.cascade = p->forked && B > 1 ? 1 : 0;
+    va.draft_parents = tree ? draft_parents : nullptr;
+    launch_attend_plan(p->dev, va, meta, st);
+  }
+  HIPCHK(hipGetLastError());
+  return WAR_OK;
+}
+
+war_status war_attend_run(war_attend* a, int32_t layer, const void* q, int64_t q_stride, void* o, int64_t o_stride,
+                          void* stream) {
+  CHECK(a, "null attention");
+  CHECK(a->B > 0, "no plan (war_attend_update)");
+  const war_kv_pool* p = a->pool;
+  CHECK(layer >= 0 && layer < p->cfg.n_layers, "layer out of range");
+  CHECK(q && o, "null array");
+  CHECK(aligned16(q) && aligned16(o), "q and o must be 16-byte aligned");
+  const int64_t row = (int64_t)p->cfg.n_q_heads * p->cfg.head_dim;
+  CHECK(q_stride >= row && o_stride >= row && q_stride % 8 == 0 && o_stride % 8 == 0,
+        "strides must hold a row and be multiples of 8");
+  AttnArgs t{};
+  t.q = static_cast<const bf16_t*>(q);
+  t.q_stride = q_stride;
+  t.kv = p->geom;
+  t.layer = layer;
+  t.table = p->dev.table;
+  t.max_pages = p->dev.max_pages;
+  t.meta = a->ws.meta();
+  t.G = p->cfg.n_q_heads / p->cfg.n_kv_heads;
+  t.TB = a->rb == kPrefillRows ? kPrefillRows / t.G : a->n;
+  t.n_kv_heads = p->cfg.n_kv_heads;
+  t.prb = a->rb;
+  t.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)p->cfg.head_dim));
+  t.pm = a->ws.pm;
+  t.pl = a->ws.pl;
+  t.po = a->ws.po;
+  t.o = static_cast<bf16_t*>(o);
+  t.o_stride = o_stride;
+  t.unit_ctr = a->ws.unit_ctr;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  launch_attn(t, a->rb, p->cfg.head_dim, a->grid, st);
+  launch_attn_combine(t, a->rb, p->cfg.head_dim, a->n_segs, st);
+  HIPCHK(hipGetLastError());
+  return WAR_OK;
+}
 
 war_status war_verify_step(war_model* m, war_kv_pool* p, int32_t B, const int32_t* seq_ids,
                            const int32_t* ctx_lens, const int32_t* last_tokens, const int32_t* draft_tokens,

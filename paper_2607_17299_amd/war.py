@@ -27,7 +27,8 @@ EXPORTS = ["war_weight_count", "war_model_create", "war_model_destroy", "war_kv_
            "war_kv_pool_destroy", "war_kv_alloc", "war_kv_fork", "war_kv_free", "war_kv_load",
            "war_prefill_append", "war_verify_step", "war_verify_step_sampled", "war_verify_step_tree",
            "war_verify_step_noalloc",
-           "war_kv_commit", "war_pool_state",
+           "war_kv_commit", "war_pool_state", "war_kv_pool_bytes", "war_kv_pool_create_format", "war_kv_write",
+           "war_kv_read", "war_attend_create", "war_attend_destroy", "war_attend_update", "war_attend_run",
            "war_last_error", "war_debug_mfma16", "war_debug_workspace", "war_debug_sample",
            "war_debug_gemm", "war_debug_gemm_plan", "war_debug_pool_waits", "war_profile", "war_profile_read"]
 
@@ -68,6 +69,14 @@ def load_library(path: str = LIB_PATH) -> C.CDLL:
         "war_verify_step_noalloc": (i32, [vp, vp, i32, vp, vp, vp, vp, vp, i32, vp, vp, vp, vp]),
         "war_kv_commit": (i32, [vp, i32, vp, vp, vp, vp]),
         "war_pool_state": (i32, [vp, pi32, pi32, pi32, pi32, pi32, vp]),
+        "war_kv_pool_bytes": (C.c_int64, [C.POINTER(_Config), i32, i32]),
+        "war_kv_pool_create_format": (i32, [C.POINTER(_Config), vp, i32, i32, vp, i32, i32, vp, C.POINTER(vp)]),
+        "war_kv_write": (i32, [vp, i32, i32, vp, vp, i32, vp, vp, C.c_int64, vp, C.c_int64, vp]),
+        "war_kv_read": (i32, [vp, i32, i32, vp, vp, i32, vp, vp, C.c_int64, vp, C.c_int64, vp]),
+        "war_attend_create": (i32, [vp, i32, i32, C.POINTER(vp)]),
+        "war_attend_destroy": (None, [vp]),
+        "war_attend_update": (i32, [vp, i32, i32, vp, vp, vp, vp, vp]),
+        "war_attend_run": (i32, [vp, i32, vp, C.c_int64, vp, C.c_int64, vp]),
         "war_last_error": (C.c_char_p, []),
         "war_debug_sample": (i32, [vp, i32, i32, i32, vp, vp, vp, C.c_float, i32, vp, vp, vp]),
         "war_debug_mfma16": (i32, [vp, vp, vp, vp]),
@@ -147,26 +156,37 @@ class Model:
             pass
 
 
+KV_FORMATS = {"bf16": 0, "e4m3": 1}
+
+
 class Pool:
-    """A paged KV pool: caller-owned KV storage and block tables (torch tensors)."""
+    """A paged KV pool: caller-owned KV storage and block tables (torch tensors).
+    kv_format "e4m3" holds keys and values in 8 bits, with a power-of-two scale for
+    each token and kv-head (war.h)."""
 
     def __init__(self, cfg: ModelConfig, num_pages: int, max_seqs: int, max_pages_per_seq: int,
-                 device="cuda", stream=None):
-        self.cfg = cfg
+                 device="cuda", stream=None, kv_format: str = "bf16"):
+        self.cfg, self.kv_format = cfg, kv_format
         self.num_pages, self.max_seqs, self.max_pages = num_pages, max_seqs, max_pages_per_seq
+        if kv_format not in KV_FORMATS:
+            raise ValueError(f"kv_format must be one of {sorted(KV_FORMATS)}")
         n = cfg.n_layers * num_pages * cfg.n_kv_heads * 2 * cfg.page_size * cfg.head_dim
-        self.kv = torch.empty(n, dtype=torch.bfloat16, device=device)
-        self.block_tables = torch.empty((max_seqs, max_pages_per_seq), dtype=torch.int32, device=device)
         self._cfg = config_struct(cfg, 1)
+        if kv_format == "e4m3":
+            n = max(lib().war_kv_pool_bytes(C.byref(self._cfg), num_pages, KV_FORMATS[kv_format]), 0)
+        self.kv = torch.empty(n, dtype=torch.bfloat16 if kv_format == "bf16" else torch.uint8, device=device)
+        self.block_tables = torch.empty((max_seqs, max_pages_per_seq), dtype=torch.int32, device=device)
         h = C.c_void_p()
-        _check(lib().war_kv_pool_create(C.byref(self._cfg), _ptr(self.kv), num_pages,
-                                        _ptr(self.block_tables), max_seqs, max_pages_per_seq,
-                                        _stream(stream), C.byref(h)))
+        _check(lib().war_kv_pool_create_format(C.byref(self._cfg), _ptr(self.kv), num_pages, KV_FORMATS[kv_format],
+                                               _ptr(self.block_tables), max_seqs, max_pages_per_seq,
+                                               _stream(stream), C.byref(h)))
         self.handle = h
 
     # ---- layout helpers (views of the caller-owned storage)
     def kv_view(self) -> torch.Tensor:
+        """The bf16 pages."""
         c = self.cfg
+        assert self.kv_format == "bf16"
         return self.kv.view(c.n_layers, self.num_pages, c.n_kv_heads, 2, c.page_size, c.head_dim)
 
     def _key_order(self) -> torch.Tensor:
@@ -182,6 +202,12 @@ class Pool:
     def gather_kv(self, seq: int, n_tokens: int, layer: int) -> torch.Tensor:
         """[2, Hkv, n_tokens, D] keys/values of a sequence read back from its pages."""
         c = self.cfg
+        if self.kv_format != "bf16":
+            shape = (1, n_tokens, c.n_kv_heads, c.head_dim)
+            k, v = (torch.empty(shape, dtype=torch.bfloat16, device=self.kv.device) for _ in range(2))
+            ids = torch.tensor([seq, 0], dtype=torch.int32, device=self.kv.device)
+            kv_read(self, layer, ids[:1], ids[1:], k, v)
+            return torch.stack([k[0].transpose(0, 1), v[0].transpose(0, 1)])
         pages = self.block_tables[seq, : -(-n_tokens // c.page_size)].long()
         v = self.kv_view()[layer, pages]                       # [np, H, 2, P, D]
         kraw = v[:, :, 0].reshape(len(pages), c.n_kv_heads, c.page_size * c.head_dim)
@@ -300,6 +326,100 @@ def prefill_append(model: Model, pool: Pool, seq_ids: torch.Tensor, ctx_lens: to
     _check(lib().war_prefill_append(model.handle, pool.handle, n, _ptr(seq_ids), _ptr(ctx_lens),
                                     _host_i32(n_new), _ptr(new_tokens), _ptr(next_tokens),
                                     _ptr(last_logits), _stream(stream)))
+
+
+def _require(ok: bool, msg: str) -> None:
+    if not ok:
+        raise ValueError(msg)
+
+
+def _require_ids(device, **arrays) -> None:
+    """Device int32 arrays without gaps (None: absent)."""
+    for name, t in arrays.items():
+        _require(t is None or (t.dtype == torch.int32 and t.is_contiguous() and t.device == device),
+                 f"{name} must be a contiguous int32 tensor on {device}")
+
+
+def _rows_of(name: str, t: torch.Tensor, device, B: int, n: int, heads: int, dim: int) -> int:
+    """The row stride of bf16 [B, n, heads, dim] whose rows b * n + i lie at one stride."""
+    _require(t.dtype == torch.bfloat16 and t.device == device and tuple(t.shape) == (B, n, heads, dim),
+             f"{name} must be bf16 [{B}, {n}, {heads}, {dim}] on {device}")
+    row = t.stride(1) if n > 1 else t.stride(0) if B > 1 else heads * dim
+    _require(t.stride(3) == 1 and (heads == 1 or t.stride(2) == dim) and (n < 2 or B < 2 or t.stride(0) == n * row),
+             f"{name}: heads must lie one after the other, rows at one stride")
+    return row
+
+
+def _kv_args(pool: Pool, seq_ids, pos0, k, v, n_lens):
+    B, n, dev, c = seq_ids.numel(), k.shape[1], pool.kv.device, pool.cfg
+    _require_ids(dev, seq_ids=seq_ids, pos0=pos0, n_lens=n_lens)
+    _require(pos0.numel() == B and (n_lens is None or n_lens.numel() == B), "pos0 and n_lens must hold one entry a request")
+    ks, vs = (_rows_of(name, t, dev, B, n, c.n_kv_heads, c.head_dim) for name, t in (("k", k), ("v", v)))
+    return B, _ptr(seq_ids), _ptr(pos0), n, _ptr(n_lens), _ptr(k), ks, _ptr(v), vs
+
+
+def kv_write(pool: Pool, layer: int, seq_ids: torch.Tensor, pos0: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+             n_lens: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Keys (after RoPE) and values bf16 [B, n, Hkv, D] of tokens pos0[b] + i into their
+    pages; n_lens: live rows of each request."""
+    with torch.cuda.device(pool.kv.device):
+        _check(lib().war_kv_write(pool.handle, layer, *_kv_args(pool, seq_ids, pos0, k, v, n_lens), _stream(stream)))
+
+
+def kv_read(pool: Pool, layer: int, seq_ids: torch.Tensor, pos0: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+            n_lens: Optional[torch.Tensor] = None, stream=None) -> None:
+    """The same tokens' keys and values from their pages into k and v (8 bits: the
+    numbers the codes stand for); rows beyond n_lens stay as they are."""
+    with torch.cuda.device(pool.kv.device):
+        _check(lib().war_kv_read(pool.handle, layer, *_kv_args(pool, seq_ids, pos0, k, v, n_lens), _stream(stream)))
+
+
+class AttendPlan:
+    """Attention of given rows over a pool: owns the workspace of one plan, which
+    serves all layers of a step.  At most max_batch requests of max_rows rows."""
+
+    def __init__(self, pool: Pool, max_batch: int, max_rows: int):
+        self.pool, self.max_rows, self.shape = pool, max_rows, None
+        h = C.c_void_p()
+        with torch.cuda.device(pool.kv.device):
+            _check(lib().war_attend_create(pool.handle, max_batch, max_rows, C.byref(h)))
+        self.handle = h
+
+    def update(self, seq_ids: torch.Tensor, ctx_lens: torch.Tensor, n_lens: Optional[torch.Tensor] = None,
+               draft_parents: Optional[torch.Tensor] = None, n_rows: Optional[int] = None, stream=None) -> None:
+        """Plan the rows of these requests: n_rows (default max_rows) each, of which
+        n_lens are live; row 0 at position ctx_lens[b]."""
+        B, n, dev = seq_ids.numel(), self.max_rows if n_rows is None else n_rows, self.pool.kv.device
+        _require_ids(dev, seq_ids=seq_ids, ctx_lens=ctx_lens, n_lens=n_lens, draft_parents=draft_parents)
+        _require(ctx_lens.numel() == B and (n_lens is None or n_lens.numel() == B),
+                 "ctx_lens and n_lens must hold one entry a request")
+        _require(draft_parents is None or draft_parents.numel() == B * (n - 1), "draft_parents must be [B, n_rows - 1]")
+        with torch.cuda.device(dev):
+            _check(lib().war_attend_update(self.handle, B, n, _ptr(seq_ids), _ptr(ctx_lens), _ptr(n_lens),
+                                           _ptr(draft_parents), _stream(stream)))
+        self.shape = (B, n)
+
+    def close(self):
+        if getattr(self, "handle", None):
+            lib().war_attend_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def attend(plan: AttendPlan, layer: int, q: torch.Tensor, out: torch.Tensor, stream=None) -> torch.Tensor:
+    """Attention of the planned rows in one layer: q, out bf16 [B, n_rows, Hq, D]."""
+    _require(plan.shape is not None, "no plan: call update first")
+    pool, (B, n) = plan.pool, plan.shape
+    qs, os_ = (_rows_of(name, t, pool.kv.device, B, n, pool.cfg.n_q_heads, pool.cfg.head_dim)
+               for name, t in (("q", q), ("out", out)))
+    with torch.cuda.device(pool.kv.device):
+        _check(lib().war_attend_run(plan.handle, layer, _ptr(q), qs, _ptr(out), os_, _stream(stream)))
+    return out
 
 
 def debug_mfma16(A: torch.Tensor, B: torch.Tensor, stream=None) -> torch.Tensor:
