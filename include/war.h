@@ -328,6 +328,100 @@ war_status war_verify_step_tree(war_model* m, war_kv_pool* p, int32_t B, const i
                                 const int32_t* draft_lens, int32_t k_max, int32_t* accept_lens,
                                 int32_t* next_tokens, int32_t* accept_path, float* logits, void* stream);
 
+/* What a request's next token is held to: penalties for tokens its text holds already,
+ * biases, and masks (the tool calls of an agent's answers follow a grammar: System
+ * Design, "Overview of WAR").  Speculation stays lossless (Introduction): a draft is
+ * judged by the logits that decoding without drafts would have at its place, so a row's
+ * text is the counted tokens, the pending token and the drafts on the way to the row.
+ * With n(v) the occurrences of token v in that text and s(v) whether it occurs there or
+ * in the prompt, a logit z of v becomes, in fp32 and in this order:
+ *   z += the sum of v's bias entries, in list order
+ *   z  = z > 0 ? z / repetition : z * repetition     if s(v)
+ *   z -= frequency * n(v);  z -= presence            if n(v) > 0
+ *   z  = -inf                                        if the row's mask excludes v
+ * All arrays are device memory; one that is NULL does nothing.
+ *   counts       uint16 [n_seqs][vocab]: bit 15: v is in the prompt; the rest: its
+ *                occurrences in the generated text that is in the cache, at most 32767
+ *                (war_counts_begin, war_counts_add)
+ *   repetition, frequency, presence   fp32 [n_seqs]; repetition > 0
+ *   bias_ids     int32 [n_seqs][n_bias], bias_values fp32 the same; ids outside
+ *                [0, vocab) do nothing; n_bias <= 1024
+ *   masks        uint32 [n_masks][ceil(vocab / 32)]: bit v % 32 of word v / 32 is 1
+ *                where v is allowed
+ *   mask_index   int32, one a row: its mask; negative: every token is allowed; n_masks
+ *                or more: none is.  NULL: row r takes mask r.
+ * Arrays by sequence are indexed by the step's sequence ids. */
+typedef struct war_constraints {
+  int32_t n_seqs;
+  const uint16_t* counts;
+  const float* repetition;
+  const float* frequency;
+  const float* presence;
+  int32_t n_bias;
+  const int32_t* bias_ids;
+  const float* bias_values;
+  int32_t n_masks;
+  const uint32_t* masks;
+  const int32_t* mask_index;
+} war_constraints;
+
+/* Constrained logits of B requests' rows, and each row's greedy token.
+ *   seq_ids, last_tokens [B], draft_tokens, draft_parents (NULL: chains) [B][k_max],
+ *   draft_lens [B] (NULL: all k_max; clamped to [0, k_max])   device int32; k_max < 64
+ *   logits     device fp32 [B * (k_max + 1)] rows of vocab at logits_stride
+ *   out        device fp32, the same at out_stride; may be logits; NULL: not wanted
+ *   greedy     device int32 [B * (k_max + 1)]: the lowest id among the largest allowed
+ *              logits (a NaN is none of them), -1 where no token is allowed; NULL: not
+ *              wanted
+ *   workspace  device, war_constrain_workspace(B * (k_max + 1), vocab) bytes, 16-byte
+ *              aligned; NULL when greedy is
+ * Rows with i > draft_len are not read, and left as they were.  The rows of a request
+ * whose id is outside [0, n_seqs) have no token and are not written to out.  A token id
+ * outside [0, vocab) counts nowhere; a parent outside [0, i) is read as i - 1. */
+int64_t war_constrain_workspace(int32_t rows, int32_t vocab);
+war_status war_constrain_logits(const war_constraints* c, int32_t vocab, int32_t B, const int32_t* seq_ids,
+                                const int32_t* last_tokens, const int32_t* draft_tokens,
+                                const int32_t* draft_parents, const int32_t* draft_lens, int32_t k_max,
+                                const float* logits, int64_t logits_stride, float* out, int64_t out_stride,
+                                int32_t* greedy, void* workspace, void* stream);
+
+/* New requests' rows of a counts table [n_seqs][vocab]: their prompts' tokens get bit
+ * 15, everything else is cleared.
+ *   seq_ids   device int32 [B], distinct (others than [0, n_seqs) are skipped)
+ *   tokens    device int32, packed; request i's at offsets[i] .. offsets[i + 1]
+ *   offsets   device int32 [B + 1], ascending
+ * Token ids outside [0, vocab) are skipped. */
+war_status war_counts_begin(uint16_t* counts, int32_t vocab, int32_t n_seqs, int32_t B, const int32_t* seq_ids,
+                            const int32_t* tokens, const int32_t* offsets, void* stream);
+
+/* Count what a step committed (or any generated tokens): first[b] (NULL: none), then
+ * lens[b] tokens of tokens[b].
+ *   first   device int32 [B]: the step's last_tokens
+ *   tokens  device int32 [B][n_max]: its draft_tokens; n_max <= 4096
+ *   path    device int32 [B][n_max]: a tree's accept_path, token j is
+ *           tokens[path[j] - 1]; NULL: in order
+ *   lens    device int32 [B]: its accept_lens; -1: nothing of the request is counted;
+ *           NULL: all n_max
+ * seq_ids as above.  A count stays at 32767. */
+war_status war_counts_add(uint16_t* counts, int32_t vocab, int32_t n_seqs, int32_t B, const int32_t* seq_ids,
+                          const int32_t* first, const int32_t* tokens, int32_t n_max, const int32_t* path,
+                          const int32_t* lens, void* stream);
+
+/* A verify step under constraints: war_verify_step (chains), war_verify_step_tree
+ * (draft_parents not NULL, accept_path as there) or war_verify_step_sampled (uniforms
+ * not NULL, chains; temperature and top_k as there) with every row's logits
+ * constrained before its token is chosen.  n_seqs must cover the pool's sequences.
+ * logits receives the constrained ones.  In a row where no token is left (none allowed;
+ * sampled: none above -inf) no draft is accepted, and next_tokens is -1 where the
+ * accepted path ends there. */
+war_status war_verify_step_constrained(war_model* m, war_kv_pool* p, int32_t B, const int32_t* seq_ids,
+                                       const int32_t* ctx_lens, const int32_t* last_tokens,
+                                       const int32_t* draft_tokens, const int32_t* draft_parents,
+                                       const int32_t* draft_lens, int32_t k_max, const war_constraints* c,
+                                       const float* uniforms, float temperature, int32_t top_k,
+                                       int32_t* accept_lens, int32_t* next_tokens, int32_t* accept_path,
+                                       float* logits, void* stream);
+
 /* war_verify_step for callers that cannot allocate device memory (code under
  * HIP graph capture, tight serving loops, harnesses that forbid hipMalloc).
  * Same arguments, pool protocol and results as war_verify_step (greedy chain

@@ -1,0 +1,333 @@
+// Logits of a step's rows under their requests' constraints, the greedy token of each
+// row, and the token counts that the penalties read (gfx950).
+//
+// Row i of a request follows its counted text, the pending token and the drafts on the
+// way to row i; n(v) is how often token v occurs there and s(v) whether it does, or in
+// the prompt.  A logit z of token v becomes
+//   z += the bias entries of v;  s(v): z = z > 0 ? z / r : z r;  z -= f n(v);
+//   n(v) > 0: z -= p;  -inf where the row's mask excludes v
+// in fp32, each operation rounded by itself (no fused multiply-adds), so that any order
+// of rows, chunks and batches gives the same bits.
+//
+// Memory bounds it: a logit is read and written once, its count (16 bits) once a
+// request.  A workgroup takes 2048 ids of all rows of a request: counts and biases stay
+// in registers, the few tokens of the rows themselves are added where they fall into the
+// chunk (a uniform test), and the next row's logits are in flight while a row is done.
+// It leaves the best id of every 128 (as the LM head does without constraints), from
+// which the greedy token, the acceptance and the sampler start.
+#include "kernels.h"
+
+#pragma clang fp contract(off)
+
+namespace {
+
+constexpr int kThreads = 256, kUnits = 2, kIds = kThreads * 4 * kUnits;  // ids a workgroup
+constexpr int kNodes = 64;   // rows of a request
+constexpr int kNone = 0x7fffffff;
+
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+
+template <bool VEC>
+WAR_DEV f32x4_t load4(const float* z, int col, int V) {
+  if constexpr (VEC) return col < V ? *reinterpret_cast<const f32x4_t*>(z + col) : f32x4_t{0.f, 0.f, 0.f, 0.f};
+  f32x4_t x;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) x[e] = col + e < V ? z[col + e] : 0.f;
+  return x;
+}
+
+template <bool VEC>
+__global__ void __launch_bounds__(kThreads) k_constrain(ConstrainArgs a) {
+  __shared__ int s_tok[kNodes];
+  __shared__ unsigned long long s_path[kNodes];
+  __shared__ float s_bias[kIds];
+  const int b = blockIdx.y, tid = threadIdx.x, lane = tid & 63;
+  const int c0 = blockIdx.x * kIds, c1 = min(a.V, c0 + kIds);
+  const int kp1 = a.k_max + 1;
+  const int n = a.ntok ? a.ntok[b] : a.draft_lens ? min(max(a.draft_lens[b], 0), a.k_max) + 1 : kp1;
+  const int seq = a.seq_ids[b];
+  const int64_t row0 = (int64_t)b * kp1;
+  const int nblk = (a.V + 127) / 128;
+  if (n <= 0) return;
+  if (seq < 0 || seq >= a.n_seqs) {  // no such request: no token in any row
+    if (a.best_v)
+      for (int i = 0; i < n; ++i)
+        for (int q = c0 / 128 + tid; q < (c1 + 127) / 128; q += kThreads) {
+          a.best_v[(row0 + i) * nblk + q] = -INFINITY;
+          a.best_i[(row0 + i) * nblk + q] = kNone;
+        }
+    return;
+  }
+  // the rows' tokens (row i's own and its ancestors' are its text)
+  if (tid < n) {
+    s_tok[tid] = tid == 0 ? a.last_tokens[b] : a.draft_tokens[(int64_t)b * a.k_max + tid - 1];
+    unsigned long long path = 1ull << tid;
+    for (int j = tid; j > 0;) {
+      int p = a.parents ? a.parents[(int64_t)b * a.k_max + j - 1] : j - 1;
+      if (p < 0 || p >= j) p = j - 1;  // as the step reads it
+      path |= 1ull << p;
+      j = p;
+    }
+    s_path[tid] = path;
+  }
+  // biases of this chunk: the first entry of an id adds up all of them, in list order
+  bool hit = false;
+  const int32_t* bid = a.bias_ids + (int64_t)seq * a.n_bias;
+  const float* bval = a.bias_values + (int64_t)seq * a.n_bias;
+  for (int e = tid; e < a.n_bias; e += kThreads) hit = hit || (bid[e] >= c0 && bid[e] < c1);
+  const bool biased = __syncthreads_or(hit);
+  if (biased) {
+    for (int i = tid; i < kIds; i += kThreads) s_bias[i] = 0.f;
+    __syncthreads();
+    for (int e = tid; e < a.n_bias; e += kThreads) {
+      const int id = bid[e];
+      if (id < c0 || id >= c1) continue;
+      bool first = true;
+      for (int q = 0; q < e; ++q) first = first && bid[q] != id;
+      if (!first) continue;
+      float sum = bval[e];
+      for (int q = e + 1; q < a.n_bias; ++q)
+        if (bid[q] == id) sum += bval[q];
+      s_bias[id - c0] = sum;
+    }
+    __syncthreads();
+  }
+  unsigned long long here = 0;  // the rows' tokens that lie in this chunk
+  for (int i = 0; i < n; ++i)
+    if (s_tok[i] >= c0 && s_tok[i] < c1) here |= 1ull << i;
+
+  int col[kUnits], cnt[kUnits][4];
+  f32x4_t bias[kUnits], z[kUnits];
+  const uint16_t* crow = a.counts ? a.counts + (int64_t)seq * a.V : nullptr;
+#pragma unroll
+  for (int u = 0; u < kUnits; ++u) {
+    col[u] = c0 + (u * kThreads + tid) * 4;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) cnt[u][e] = 0;
+    if (crow) {
+      if constexpr (VEC) {
+        if (col[u] < a.V) {
+          const uint2 c = *reinterpret_cast<const uint2*>(crow + col[u]);
+          cnt[u][0] = c.x & 0xffff;
+          cnt[u][1] = c.x >> 16;
+          cnt[u][2] = c.y & 0xffff;
+          cnt[u][3] = c.y >> 16;
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (col[u] + e < a.V) cnt[u][e] = crow[col[u] + e];
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) cnt[u][e] = (cnt[u][e] & 0x7fff) * 2 + (cnt[u][e] >> 15);  // prompt bit last
+#pragma unroll
+    for (int e = 0; e < 4; ++e) bias[u][e] = biased ? s_bias[col[u] - c0 + e] : 0.f;
+    z[u] = load4<VEC>(a.logits + row0 * a.stride, col[u], a.V);
+  }
+  const float r = a.repetition ? a.repetition[seq] : 1.f;
+  const float f = a.frequency ? a.frequency[seq] : 0.f, p = a.presence ? a.presence[seq] : 0.f;
+
+  for (int i = 0; i < n; ++i) {
+    const int64_t row = row0 + i;
+    int m = -1;
+    bool none = false;  // a mask that is not there allows nothing
+    if (a.masks) {
+      m = a.mask_index ? a.mask_index[row] : (int)row;
+      none = m >= a.n_masks;
+    }
+    const uint32_t* mrow = m >= 0 && !none ? a.masks + (int64_t)m * ((a.V + 31) / 32) : nullptr;
+    uint32_t word[kUnits];
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u)
+      word[u] = none ? 0u : mrow && col[u] < a.V ? mrow[col[u] >> 5] >> (col[u] & 31) : ~0u;
+    f32x4_t next[kUnits];
+    if (i + 1 < n) {
+#pragma unroll
+      for (int u = 0; u < kUnits; ++u) next[u] = load4<VEC>(a.logits + (row + 1) * a.stride, col[u], a.V);
+    }
+    const unsigned long long add = here & s_path[i];
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+      int c[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) c[e] = cnt[u][e];
+      for (unsigned long long q = add; q; q &= q - 1) {
+        const int d = s_tok[__ffsll((long long)q) - 1] - col[u];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (d == e) c[e] += 2;
+      }
+      f32x4_t x = z[u];
+      float best = -INFINITY;
+      int at = kNone;
+      bool nan = false;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        float v = x[e];
+        if (biased) v += bias[u][e];
+        if (c[e]) {
+          v = v > 0.f ? v / r : v * r;
+          const int k = c[e] >> 1;
+          v -= f * (float)k;
+          if (k) v -= p;
+        }
+        const bool ok = ((word[u] >> e) & 1u) && col[u] + e < a.V;
+        if (!ok) v = -INFINITY;
+        x[e] = v;
+        nan = nan || v != v;
+        if (ok && v == v && (at == kNone || v > best)) {
+          best = v;
+          at = col[u] + e;
+        }
+      }
+      if (a.out) {
+        float* o = a.out + row * a.out_stride;
+        if constexpr (VEC) {
+          if (col[u] < a.V) *reinterpret_cast<f32x4_t*>(o + col[u]) = x;
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (col[u] + e < a.V) o[col[u] + e] = x[e];
+        }
+      }
+      if (a.best_v) {
+        // 128 ids are the 32 lanes of half a wave, ascending: the lowest lane that holds
+        // the maximum has its lowest id
+        float mx = best;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) mx = fmaxf(mx, __shfl_xor(mx, o, 64));
+        const unsigned long long half = lane < 32 ? 0xffffffffull : 0xffffffffull << 32;
+        const unsigned long long eq = __ballot(at != kNone && best == mx) & half;
+        const unsigned long long nans = __ballot(nan) & half;
+        const int q = (c0 + u * kThreads * 4 + (tid & ~31) * 4) / 128;
+        if (q < nblk && (eq ? __ffsll((long long)eq) - 1 == lane : (lane & 31) == 0)) {
+          a.best_v[row * nblk + q] = a.nan_max && nans ? __builtin_nanf("") : mx;
+          a.best_i[row * nblk + q] = eq ? at : kNone;
+        }
+      }
+      z[u] = next[u];
+    }
+  }
+}
+
+// Greedy token of each row from the best of its 128-id blocks: the lowest id among the
+// largest, -1 where no block has one (`finite`: or only -inf).  A wave a row.
+__global__ void __launch_bounds__(256) k_greedy(ConstrainArgs a, int32_t* greedy, bool finite) {
+  const int kp1 = a.k_max + 1, nblk = (a.V + 127) / 128, lane = threadIdx.x & 63;
+  const int r = blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (r >= a.B * kp1) return;
+  const int b = r / kp1;
+  const int n = a.ntok ? a.ntok[b] : a.draft_lens ? min(max(a.draft_lens[b], 0), a.k_max) + 1 : kp1;
+  if (r % kp1 >= n) return;
+  float v = -INFINITY;
+  int idx = kNone;
+  for (int c = lane; c < nblk; c += 64) {
+    const float bv = a.best_v[(int64_t)r * nblk + c];
+    const int bi = a.best_i[(int64_t)r * nblk + c];
+    if (bi != kNone && (idx == kNone || bv > v)) {
+      v = bv;
+      idx = bi;
+    }
+  }
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) {
+    const float ov = __shfl_xor(v, o, 64);
+    const int oi = __shfl_xor(idx, o, 64);
+    if (oi != kNone && (idx == kNone || ov > v || (ov == v && oi < idx))) {
+      v = ov;
+      idx = oi;
+    }
+  }
+  if (lane == 0) greedy[r] = idx == kNone || (finite && v == -INFINITY) ? -1 : idx;
+}
+
+// A request's row of the counts begins: bit 15 for each token of its prompt, no
+// occurrences.  A workgroup takes 16384 ids: the prompt's tokens among them as bits in
+// LDS, then the row's numbers, written once.
+constexpr int kSlice = 16384;
+template <bool VEC>
+__global__ void __launch_bounds__(256) k_counts_begin(uint16_t* counts, int V, int n_seqs, const int32_t* seq_ids,
+                                                      const int32_t* tokens, const int32_t* offsets) {
+  __shared__ uint32_t s_bits[kSlice / 32];
+  const int b = blockIdx.y, c0 = blockIdx.x * kSlice, c1 = min(V, c0 + kSlice);
+  const int seq = seq_ids[b];
+  if (seq < 0 || seq >= n_seqs) return;
+  for (int i = threadIdx.x; i < kSlice / 32; i += 256) s_bits[i] = 0;
+  __syncthreads();
+  const int t1 = offsets[b + 1];
+  for (int i = offsets[b] + threadIdx.x; i < t1; i += 256) {
+    const int t = tokens[i];
+    if (t >= c0 && t < c1) atomicOr(&s_bits[(t - c0) >> 5], 1u << ((t - c0) & 31));
+  }
+  __syncthreads();
+  uint16_t* row = counts + (int64_t)seq * V;
+  if constexpr (VEC) {
+    for (int c = c0 + threadIdx.x * 8; c < c1; c += 256 * 8) {
+      const uint32_t w = s_bits[(c - c0) >> 5] >> ((c - c0) & 31);
+      auto two = [w](int e) { return ((w >> e) & 1u) << 15 | ((w >> (e + 1)) & 1u) << 31; };
+      *reinterpret_cast<uint4*>(row + c) = make_uint4(two(0), two(2), two(4), two(6));
+    }
+  } else {
+    for (int c = c0 + threadIdx.x; c < c1; c += 256) row[c] = (s_bits[(c - c0) >> 5] >> ((c - c0) & 31) & 1u) << 15;
+  }
+}
+
+// A request's tokens are counted: the first occurrence of a token among them adds all of
+// its occurrences, so that no two threads touch one number and nothing hangs on their
+// order.
+__global__ void __launch_bounds__(256) k_counts_add(uint16_t* counts, int V, int n_seqs, const int32_t* seq_ids,
+                                                    const int32_t* first, const int32_t* tokens, int n_max,
+                                                    const int32_t* path, const int32_t* lens) {
+  extern __shared__ int s_tok[];
+  const int b = blockIdx.x;
+  const int seq = seq_ids[b], len = lens ? min(lens[b], n_max) : n_max;
+  if (seq < 0 || seq >= n_seqs || len < 0) return;
+  const int f = first ? 1 : 0, n = len + f;
+  for (int i = threadIdx.x; i < n; i += 256) {
+    int j = i - f;
+    if (j >= 0 && path) j = path[(int64_t)b * n_max + j] - 1;
+    s_tok[i] = i < f ? first[b] : j >= 0 && j < n_max ? tokens[(int64_t)b * n_max + j] : -1;
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < n; i += 256) {
+    const int t = s_tok[i];
+    if (t < 0 || t >= V) continue;
+    int times = 1;
+    bool mine = true;
+    for (int q = 0; q < n; ++q) {
+      if (q < i && s_tok[q] == t) mine = false;
+      if (q > i && s_tok[q] == t) ++times;
+    }
+    if (!mine) continue;
+    uint16_t* at = counts + (int64_t)seq * V + t;
+    *at = (uint16_t)((*at & 0x8000) | min((*at & 0x7fff) + times, 0x7fff));
+  }
+}
+
+}  // namespace
+
+void launch_constrain(const ConstrainArgs& a, hipStream_t st) {
+  const dim3 grid(cdiv_i(a.V, kIds), a.B);
+  auto quad = [](const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; };
+  // 16-byte accesses where every row of every array allows them
+  const bool vec = a.V % 4 == 0 && a.stride % 4 == 0 && quad(a.logits, 16) && quad(a.counts, 8) &&
+                   (!a.out || (a.out_stride % 4 == 0 && quad(a.out, 16)));
+  if (vec) k_constrain<true><<<grid, kThreads, 0, st>>>(a);
+  else k_constrain<false><<<grid, kThreads, 0, st>>>(a);
+}
+void launch_greedy(const ConstrainArgs& a, int32_t* greedy, bool finite, hipStream_t st) {
+  k_greedy<<<cdiv_i(a.B * (a.k_max + 1), 4), 256, 0, st>>>(a, greedy, finite);
+}
+void launch_counts_begin(uint16_t* counts, int V, int n_seqs, int B, const int32_t* seq_ids, const int32_t* tokens,
+                         const int32_t* offsets, hipStream_t st) {
+  const dim3 grid(cdiv_i(V, kSlice), B);
+  if (V % 8 == 0 && (reinterpret_cast<uintptr_t>(counts) & 15) == 0)
+    k_counts_begin<true><<<grid, 256, 0, st>>>(counts, V, n_seqs, seq_ids, tokens, offsets);
+  else
+    k_counts_begin<false><<<grid, 256, 0, st>>>(counts, V, n_seqs, seq_ids, tokens, offsets);
+}
+void launch_counts_add(uint16_t* counts, int V, int n_seqs, int B, const int32_t* seq_ids, const int32_t* first,
+                       const int32_t* tokens, int n_max, const int32_t* path, const int32_t* lens, hipStream_t st) {
+  k_counts_add<<<B, 256, (n_max + 1) * 4, st>>>(counts, V, n_seqs, seq_ids, first, tokens, n_max, path, lens);
+}

@@ -202,7 +202,40 @@ struct SampleArgs {
   // where the block holds one (the LM head's argmax partials with nan_max)
   const float* block_max;
   int32_t* row_out;        // [B * kp1][3]: accepted?, token if rejected here, token if last
+  const int32_t* greedy;   // nullable: constrained rows, -1 where one has no token at all
 };
+
+// constrained logits (constrain.hip)
+struct ConstrainArgs {
+  const float* logits;     // row b * (k_max + 1) + i at that many strides
+  float* out;              // nullable; may be logits
+  int64_t stride, out_stride;
+  int V, B, k_max;
+  const int32_t* ntok;     // rows of a request (the step's), or:
+  const int32_t* draft_lens;  // nullable: rows - 1, clamped to [0, k_max]
+  const int32_t *seq_ids, *last_tokens, *draft_tokens, *parents;
+  // by sequence; any array may be null
+  int n_seqs;
+  const uint16_t* counts;
+  const float *repetition, *frequency, *presence;
+  int n_bias;
+  const int32_t* bias_ids;
+  const float* bias_values;
+  int n_masks;
+  const uint32_t* masks;
+  const int32_t* mask_index;  // by row
+  // nullable: [B * (k_max + 1)][ceil(V / 128)] best logit and id of each block of ids
+  // (-inf and 0x7fffffff: none); nan_max: NaN where an allowed logit is NaN
+  float* best_v;
+  int32_t* best_i;
+  int nan_max;
+};
+void launch_constrain(const ConstrainArgs& a, hipStream_t st);
+void launch_greedy(const ConstrainArgs& a, int32_t* greedy, bool finite, hipStream_t st);
+void launch_counts_begin(uint16_t* counts, int V, int n_seqs, int B, const int32_t* seq_ids, const int32_t* tokens,
+                         const int32_t* offsets, hipStream_t st);
+void launch_counts_add(uint16_t* counts, int V, int n_seqs, int B, const int32_t* seq_ids, const int32_t* first,
+                       const int32_t* tokens, int n_max, const int32_t* path, const int32_t* lens, hipStream_t st);
 void launch_block_max(const float* logits, int rows, int V, float* block_max, hipStream_t st);
 void launch_sample(const SampleArgs& s, int32_t* accept_lens, int32_t* next_tokens, hipStream_t st);
 
@@ -228,12 +261,13 @@ void launch_qkv_rope(int rows, int splits, const float* P, const ModelDims& md,
                      const float* cos_t, const float* sin_t, const StepMeta& meta,
                      const int32_t* row_req, const int32_t* table, int max_pages, const KvGeom& kv,
                      int layer, bf16_t* q, hipStream_t st);
+// none: the greedy token of a row without any (constrained rows: -1).
 // parents (nullable): tree drafts; accept_path [n_req][k_max] then receives the
 // accepted nodes in depth order, -1 beyond the accept length
 void launch_argmax_accept(int n_req, const int32_t* ntok, int row_stride, int n_blocks,
                           const float* amax_v, const int32_t* amax_i, const int32_t* draft_tokens,
                           const int32_t* parents, int k_max, int32_t* accept_lens, int32_t* next_tokens,
-                          int32_t* accept_path, hipStream_t st);
+                          int32_t* accept_path, hipStream_t st, int none = 0x7fffffff);
 // Tree drafts: move the KV of each request's accepted nodes (slots ctx + node)
 // to slots ctx + 1 .. ctx + accept_len, every layer.
 void launch_kv_compact(const KvGeom& kv, int n_layers, int B, const StepMeta& meta, const int32_t* table,

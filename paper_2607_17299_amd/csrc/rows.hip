@@ -319,7 +319,7 @@ __global__ void __launch_bounds__(1024) k_argmax_accept(const int32_t* ntok, int
                                                        const int32_t* amax_i,
                                                        const int32_t* drafts, const int32_t* parents,
                                                        int k_max, int32_t* accept_lens, int32_t* next_tokens,
-                                                       int32_t* accept_path) {
+                                                       int32_t* accept_path, int none) {
   __shared__ int greedy[64];
   __shared__ int s_par[64], s_dep[64], s_ok[64];
   const int b = blockIdx.x;
@@ -356,7 +356,7 @@ __global__ void __launch_bounds__(1024) k_argmax_accept(const int32_t* ntok, int
         idx = oi;
       }
     }
-    if (lane == 0) greedy[i] = idx;
+    if (lane == 0) greedy[i] = idx == 0x7fffffff ? none : idx;
   }
   __syncthreads();
   if (threadIdx.x != 0) return;
@@ -369,14 +369,14 @@ __global__ void __launch_bounds__(1024) k_argmax_accept(const int32_t* ntok, int
       if (pj < 0 || pj >= j) pj = j - 1;  // flagged by the step setup
       s_par[j] = pj;
       s_dep[j] = s_dep[pj] + 1;
-      s_ok[j] = s_ok[pj] && drafts[(int64_t)b * k_max + j - 1] == greedy[pj];
+      s_ok[j] = s_ok[pj] && greedy[pj] >= 0 && drafts[(int64_t)b * k_max + j - 1] == greedy[pj];
       if (s_ok[j] && s_dep[j] > s_dep[last]) last = j;
     }
     a = s_dep[last];
     for (int d = a; d < k_max; ++d) accept_path[(int64_t)b * k_max + d] = -1;
     for (int j = last; j > 0; j = s_par[j]) accept_path[(int64_t)b * k_max + s_dep[j] - 1] = j;
   } else if (n > 0) {
-    while (a < n - 1 && drafts && drafts[(int64_t)b * k_max + a] == greedy[a]) ++a;
+    while (a < n - 1 && drafts && greedy[a] >= 0 && drafts[(int64_t)b * k_max + a] == greedy[a]) ++a;
     last = a;
   } else if (parents) {
     for (int d = 0; d < k_max; ++d) accept_path[(int64_t)b * k_max + d] = -1;
@@ -469,9 +469,9 @@ void launch_qkv_rope(int rows, int splits, const float* P, const ModelDims& md,
 void launch_argmax_accept(int n_req, const int32_t* ntok, int row_stride, int n_blocks,
                           const float* amax_v, const int32_t* amax_i, const int32_t* draft_tokens,
                           const int32_t* parents, int k_max, int32_t* accept_lens, int32_t* next_tokens,
-                          int32_t* accept_path, hipStream_t st) {
+                          int32_t* accept_path, hipStream_t st, int none) {
   k_argmax_accept<<<n_req, 1024, 0, st>>>(ntok, row_stride, n_blocks, amax_v, amax_i, draft_tokens,
-                                         parents, k_max, accept_lens, next_tokens, accept_path);
+                                         parents, k_max, accept_lens, next_tokens, accept_path, none);
 }
 void launch_kv_compact(const KvGeom& kv, int n_layers, int B, const StepMeta& meta, const int32_t* table,
                        int max_pages, const int32_t* accept_lens, const int32_t* accept_path, int k_max,

@@ -175,7 +175,8 @@ __device__ bool sample_from_blocks(const SampleArgs& s, int r, int d, SampleShar
     radix_pick(sh, pre, shift, kBins);
   }
   if (sh.flag) return false;
-  const uint32_t low = sh.prefix;
+  // constrained rows: an excluded id (-inf) has no weight and is never a candidate
+  const uint32_t low = s.greedy ? max(sh.prefix, 0x00800000u) : sh.prefix;
   // the blocks that reach it, in id order (c_id holds their list)
   int nsel;
   int mine = 0;
@@ -509,6 +510,10 @@ __global__ void __launch_bounds__(kST) k_sample_rows(SampleArgs s) {
   const int dl = s.ntok[b] - 1;  // drafts of the request (-1: inactive step)
   if (i > dl) return;
   const int d = i < dl ? s.drafts[(int64_t)b * s.k_max + i] : -1;
+  if (s.greedy && s.greedy[r] < 0) {  // no token at all
+    if (threadIdx.x < 3) s.row_out[(int64_t)r * 3 + threadIdx.x] = threadIdx.x == 0 ? 0 : -1;
+    return;
+  }
   if constexpr (BLOCKS) {
     if (sample_from_blocks(s, r, d, sh, c_key, c_id)) return;
     __syncthreads();

@@ -254,7 +254,7 @@ struct war_model {
   DevBuf inv_freq;  // RoPE frequencies [hd/2] fp64
   DevBuf ws_buf;    // the model's own workspace allocation
   Workspace ws;     // views into ws_buf
-  DevBuf logits_ws, row_out;  // sampled verification: full logits, per-row outcomes
+  DevBuf logits_ws, row_out;  // sampled or constrained verification: full logits, per-row outcomes
   DevBuf path_ws;             // tree drafts: accepted path when the caller passes none
   // prefill: two pinned blocks of host metadata and their device copies (a row
   // chunk's is filled while the chunk before it runs), and what the append reads
@@ -1054,12 +1054,45 @@ struct StaticWs {
   size_t bytes;
 };
 
+war_status check_constraints(const war_constraints& c) {
+  CHECK(c.n_seqs >= 1, "n_seqs must be positive");
+  CHECK(c.n_bias >= 0 && c.n_bias <= 1024, "n_bias out of range [0, 1024]");
+  CHECK(c.n_bias == 0 || (c.bias_ids && c.bias_values), "bias_ids and bias_values required when n_bias > 0");
+  CHECK(c.n_masks >= 0 && (c.n_masks == 0 || c.masks), "masks required when n_masks > 0");
+  CHECK(c.masks || !c.mask_index, "mask_index without masks");
+  return WAR_OK;
+}
+
+ConstrainArgs constrain_args(const war_constraints& c, int V, int B, const int32_t* seq_ids,
+                             const int32_t* last_tokens, const int32_t* draft_tokens, const int32_t* parents, int k_max) {
+  ConstrainArgs a{};
+  a.V = V;
+  a.B = B;
+  a.k_max = k_max;
+  a.seq_ids = seq_ids;
+  a.last_tokens = last_tokens;
+  a.draft_tokens = draft_tokens;
+  a.parents = parents;
+  a.n_seqs = c.n_seqs;
+  a.counts = c.counts;
+  a.repetition = c.repetition;
+  a.frequency = c.frequency;
+  a.presence = c.presence;
+  a.n_bias = c.n_bias;
+  a.bias_ids = c.bias_ids;
+  a.bias_values = c.bias_values;
+  a.n_masks = c.n_masks;
+  a.masks = c.masks;
+  a.mask_index = c.mask_index;
+  return a;
+}
+
 war_status verify_impl(war_model* m, war_kv_pool* p, int32_t B, const int32_t* seq_ids,
                        const int32_t* ctx_lens, const int32_t* last_tokens, const int32_t* draft_tokens,
                        const int32_t* draft_lens, int32_t k_max, int32_t* accept_lens,
                        int32_t* next_tokens, float* logits, void* stream, const SampleParams& sp,
                        const int32_t* draft_parents = nullptr, int32_t* accept_path = nullptr,
-                       const StaticWs* fixed = nullptr) {
+                       const StaticWs* fixed = nullptr, const war_constraints* cons = nullptr) {
   CHECK(m && p, "null model or pool");
   CHECK(same_shape(m->cfg, p->cfg), "model and pool shapes differ");
   CHECK(!p->pending, "previous verify step not committed");
@@ -1075,6 +1108,10 @@ war_status verify_impl(war_model* m, war_kv_pool* p, int32_t B, const int32_t* s
   const bool tree = draft_parents != nullptr && k_max > 0;
   if (tree && k_max + 1 > 32) return fail(WAR_ERR_UNSUPPORTED, "tree drafts: k_max + 1 must be <= 32");
   if (tree && sp.uniforms) return fail(WAR_ERR_UNSUPPORTED, "tree drafts are verified greedily");
+  if (cons) {
+    WARCHK(check_constraints(*cons));
+    CHECK(cons->n_seqs >= p->dev.max_seqs, "constraints for fewer sequences than the pool has");
+  }
 
   const int kp1 = k_max + 1;
   const int R = B * kp1;
@@ -1177,14 +1214,27 @@ war_status verify_impl(war_model* m, war_kv_pool* p, int32_t B, const int32_t* s
   war_status s = run_layers(m, w, p, R, a, RB, grid, B, st);
   if (s != WAR_OK) return s;
   int sdummy;
+  // the full logits are needed: the caller's buffer, else the workspace
+  float* lg = logits;
+  if ((sp.uniforms || cons) && !lg) {
+    HIPCHK(m->logits_ws.ensure((size_t)R * m->md.V * 4));
+    lg = m->logits_ws.as<float>();
+  }
+  if (sp.uniforms) HIPCHK(m->row_out.ensure((size_t)R * 4 * 4));
+  // constrained in place; the best of each block of ids takes the LM head's place
+  auto constrain = [&](int32_t* greedy) {
+    ConstrainArgs ca = constrain_args(*cons, m->md.V, B, seq_ids, last_tokens, draft_tokens, va.draft_parents, k_max);
+    ca.logits = ca.out = lg;
+    ca.stride = ca.out_stride = m->md.V;
+    ca.ntok = meta.req_ntok;
+    ca.best_v = w.amax_v;
+    ca.best_i = w.amax_i;
+    ca.nan_max = greedy != nullptr;
+    Timed t(m->prof, st, "constrain_logits");
+    launch_constrain(ca, st);
+    if (greedy) launch_greedy(ca, greedy, true, st);
+  };
   if (sp.uniforms) {
-    // the full logits are needed: the caller's buffer, else the workspace
-    float* lg = logits;
-    if (!lg) {
-      HIPCHK(m->logits_ws.ensure((size_t)R * m->md.V * 4));
-      lg = m->logits_ws.as<float>();
-    }
-    HIPCHK(m->row_out.ensure((size_t)R * 3 * 4));
     {
       Timed t(m->prof, st, "gemm_lm_head");
       WARCHK(gemm(w, w.u, m->md.d, nullptr, m->w_lm, R, m->md.V, m->md.d, 0, &sdummy, st, true, lg, nullptr,
@@ -1203,16 +1253,22 @@ war_status verify_impl(war_model* m, war_kv_pool* p, int32_t B, const int32_t* s
     sa.top_k = sp.top_k;
     sa.block_max = w.amax_v;
     sa.row_out = m->row_out.as<int32_t>();
+    if (cons) {
+      constrain(sa.row_out + (size_t)R * 3);
+      sa.greedy = sa.row_out + (size_t)R * 3;
+    }
     Timed t(m->prof, st, "sample_accept");
     launch_sample(sa, accept_lens, next_tokens, st);
   } else {
     {
       Timed t(m->prof, st, "gemm_lm_head_argmax");
-      WARCHK(gemm(w, w.u, m->md.d, nullptr, m->w_lm, R, m->md.V, m->md.d, 0, &sdummy, st, true, logits));
+      WARCHK(gemm(w, w.u, m->md.d, nullptr, m->w_lm, R, m->md.V, m->md.d, 0, &sdummy, st, true, lg));
     }
+    if (cons) constrain(nullptr);
     Timed t(m->prof, st, "argmax_accept");
     launch_argmax_accept(B, meta.req_ntok, kp1, m->md.V / 128, w.amax_v, w.amax_i, draft_tokens,
-                         tree ? draft_parents : nullptr, k_max, accept_lens, next_tokens, accept_path, st);
+                         tree ? draft_parents : nullptr, k_max, accept_lens, next_tokens, accept_path, st,
+                         cons ? -1 : 0x7fffffff);
   }
   if (tree) {
     Timed t(m->prof, st, "kv_compact");
@@ -1422,6 +1478,91 @@ war_status war_verify_step_tree(war_model* m, war_kv_pool* p, int32_t B, const i
   CHECK(k_max == 0 || draft_parents, "draft_parents required when k_max > 0");
   return verify_impl(m, p, B, seq_ids, ctx_lens, last_tokens, draft_tokens, draft_lens, k_max, accept_lens,
                      next_tokens, logits, stream, SampleParams{}, draft_parents, accept_path);
+}
+
+war_status war_verify_step_constrained(war_model* m, war_kv_pool* p, int32_t B, const int32_t* seq_ids,
+                                       const int32_t* ctx_lens, const int32_t* last_tokens,
+                                       const int32_t* draft_tokens, const int32_t* draft_parents,
+                                       const int32_t* draft_lens, int32_t k_max, const war_constraints* c,
+                                       const float* uniforms, float temperature, int32_t top_k,
+                                       int32_t* accept_lens, int32_t* next_tokens, int32_t* accept_path,
+                                       float* logits, void* stream) {
+  CHECK(m && c, "null model or constraints");
+  SampleParams sp;
+  if (uniforms) {
+    CHECK(std::isfinite(temperature) && temperature > 0.f, "temperature must be positive and finite");
+    CHECK(top_k >= 1 && top_k <= m->md.V, "top_k out of range [1, vocab]");
+    sp.uniforms = uniforms;
+    sp.temperature = temperature;
+    sp.top_k = top_k;
+  }
+  return verify_impl(m, p, B, seq_ids, ctx_lens, last_tokens, draft_tokens, draft_lens, k_max, accept_lens,
+                     next_tokens, logits, stream, sp, draft_parents, accept_path, nullptr, c);
+}
+
+int64_t war_constrain_workspace(int32_t rows, int32_t vocab) {
+  return rows < 1 || vocab < 1 ? -1 : (int64_t)rows * ((vocab + 127) / 128) * 8;
+}
+
+war_status war_constrain_logits(const war_constraints* c, int32_t vocab, int32_t B, const int32_t* seq_ids,
+                                const int32_t* last_tokens, const int32_t* draft_tokens,
+                                const int32_t* draft_parents, const int32_t* draft_lens, int32_t k_max,
+                                const float* logits, int64_t logits_stride, float* out, int64_t out_stride,
+                                int32_t* greedy, void* workspace, void* stream) {
+  CHECK(c, "null constraints");
+  WARCHK(check_constraints(*c));
+  CHECK(vocab >= 1 && vocab <= 1 << 24, "vocab out of range [1, 2^24]");
+  CHECK(B >= 1 && B <= kMaxBatch, "B out of range [1, 1024]");
+  CHECK(k_max >= 0 && k_max < 64, "k_max out of range [0, 63]");
+  CHECK(seq_ids && last_tokens && logits && (k_max == 0 || draft_tokens), "null array");
+  CHECK(logits_stride >= vocab && (!out || out_stride >= vocab), "a stride must hold a row");
+  CHECK(out != logits || out_stride == logits_stride, "in place, the strides must be the same");
+  CHECK(out || greedy, "neither out nor greedy is wanted");
+  CHECK(!greedy || (workspace && aligned16(workspace)), "greedy needs an aligned workspace");
+  ConstrainArgs a = constrain_args(*c, vocab, B, seq_ids, last_tokens, draft_tokens, draft_parents, k_max);
+  a.logits = logits;
+  a.stride = logits_stride;
+  a.out = out;
+  a.out_stride = out_stride;
+  a.draft_lens = draft_lens;
+  if (greedy) {
+    a.best_v = static_cast<float*>(workspace);
+    a.best_i = static_cast<int32_t*>(workspace) + (int64_t)B * (k_max + 1) * ((vocab + 127) / 128);
+  }
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  launch_constrain(a, st);
+  if (greedy) launch_greedy(a, greedy, false, st);
+  HIPCHK(hipGetLastError());
+  return WAR_OK;
+}
+
+static war_status check_counts(const uint16_t* counts, int32_t vocab, int32_t n_seqs, int32_t B, const int32_t* seq_ids) {
+  CHECK(counts && seq_ids, "null array");
+  CHECK((reinterpret_cast<uintptr_t>(counts) & 1) == 0, "counts must be 2-byte aligned");
+  CHECK(vocab >= 1 && vocab <= 1 << 24 && n_seqs >= 1, "non-positive or too large table");
+  CHECK(B >= 1 && B <= kMaxBatch, "B out of range [1, 1024]");
+  return WAR_OK;
+}
+
+war_status war_counts_begin(uint16_t* counts, int32_t vocab, int32_t n_seqs, int32_t B, const int32_t* seq_ids,
+                            const int32_t* tokens, const int32_t* offsets, void* stream) {
+  WARCHK(check_counts(counts, vocab, n_seqs, B, seq_ids));
+  CHECK(tokens && offsets, "null array");
+  launch_counts_begin(counts, vocab, n_seqs, B, seq_ids, tokens, offsets, static_cast<hipStream_t>(stream));
+  HIPCHK(hipGetLastError());
+  return WAR_OK;
+}
+
+war_status war_counts_add(uint16_t* counts, int32_t vocab, int32_t n_seqs, int32_t B, const int32_t* seq_ids,
+                          const int32_t* first, const int32_t* tokens, int32_t n_max, const int32_t* path,
+                          const int32_t* lens, void* stream) {
+  WARCHK(check_counts(counts, vocab, n_seqs, B, seq_ids));
+  CHECK(n_max >= 0 && n_max <= 4096, "n_max out of range [0, 4096]");
+  CHECK(n_max == 0 || tokens, "tokens required when n_max > 0");
+  launch_counts_add(counts, vocab, n_seqs, B, seq_ids, first, tokens, n_max, path, lens,
+                    static_cast<hipStream_t>(stream));
+  HIPCHK(hipGetLastError());
+  return WAR_OK;
 }
 
 war_status war_verify_step_noalloc(war_model* m, war_kv_pool* p, int32_t B, const int32_t* seq_ids,

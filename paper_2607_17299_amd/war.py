@@ -28,7 +28,8 @@ EXPORTS = ["war_weight_count", "war_model_create", "war_model_destroy", "war_kv_
            "war_prefill_append", "war_verify_step", "war_verify_step_sampled", "war_verify_step_tree",
            "war_verify_step_noalloc",
            "war_kv_commit", "war_pool_state", "war_kv_pool_bytes", "war_kv_pool_create_format", "war_kv_write",
-           "war_kv_read", "war_attend_create", "war_attend_destroy", "war_attend_update", "war_attend_run",
+           "war_kv_read", "war_constrain_workspace", "war_constrain_logits", "war_counts_begin", "war_counts_add",
+           "war_verify_step_constrained", "war_attend_create", "war_attend_destroy", "war_attend_update", "war_attend_run",
            "war_last_error", "war_debug_mfma16", "war_debug_workspace", "war_debug_sample",
            "war_debug_gemm", "war_debug_gemm_plan", "war_debug_pool_waits", "war_profile", "war_profile_read"]
 
@@ -44,6 +45,12 @@ class _Config(C.Structure):
                 ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("ffn_dim", C.c_int32),
                 ("vocab", C.c_int32), ("rms_eps", C.c_float), ("rope_base", C.c_float),
                 ("page_size", C.c_int32), ("max_rows", C.c_int32)]
+
+
+class _Constraints(C.Structure):
+    _fields_ = [("n_seqs", C.c_int32), ("counts", C.c_void_p), ("repetition", C.c_void_p), ("frequency", C.c_void_p),
+                ("presence", C.c_void_p), ("n_bias", C.c_int32), ("bias_ids", C.c_void_p), ("bias_values", C.c_void_p),
+                ("n_masks", C.c_int32), ("masks", C.c_void_p), ("mask_index", C.c_void_p)]
 
 
 def load_library(path: str = LIB_PATH) -> C.CDLL:
@@ -77,6 +84,13 @@ def load_library(path: str = LIB_PATH) -> C.CDLL:
         "war_attend_destroy": (None, [vp]),
         "war_attend_update": (i32, [vp, i32, i32, vp, vp, vp, vp, vp]),
         "war_attend_run": (i32, [vp, i32, vp, C.c_int64, vp, C.c_int64, vp]),
+        "war_constrain_workspace": (C.c_int64, [i32, i32]),
+        "war_constrain_logits": (i32, [C.POINTER(_Constraints), i32, i32, vp, vp, vp, vp, vp, i32, vp, C.c_int64, vp,
+                                       C.c_int64, vp, vp, vp]),
+        "war_counts_begin": (i32, [vp, i32, i32, i32, vp, vp, vp, vp]),
+        "war_counts_add": (i32, [vp, i32, i32, i32, vp, vp, vp, i32, vp, vp, vp]),
+        "war_verify_step_constrained": (i32, [vp, vp, i32, vp, vp, vp, vp, vp, vp, i32, C.POINTER(_Constraints), vp,
+                                              C.c_float, i32, vp, vp, vp, vp, vp]),
         "war_last_error": (C.c_char_p, []),
         "war_debug_sample": (i32, [vp, i32, i32, i32, vp, vp, vp, C.c_float, i32, vp, vp, vp]),
         "war_debug_mfma16": (i32, [vp, vp, vp, vp]),
@@ -333,45 +347,59 @@ def _require(ok: bool, msg: str) -> None:
         raise ValueError(msg)
 
 
-def _require_ids(device, **arrays) -> None:
-    """Device int32 arrays without gaps (None: absent)."""
+def _addr(t: Optional[torch.Tensor]):
+    return None if t is None else t.data_ptr()
+
+
+def _checked(device, dtype, **arrays) -> None:
+    """Arrays of a type without gaps on the device (None: absent)."""
     for name, t in arrays.items():
-        _require(t is None or (t.dtype == torch.int32 and t.is_contiguous() and t.device == device),
-                 f"{name} must be a contiguous int32 tensor on {device}")
+        if t is not None and not (t.dtype == dtype and t.device == device and t.is_contiguous()):
+            raise ValueError(f"{name} must be a contiguous {dtype} tensor on {device}")
+
+
+def _call(fn, device, stream, *args) -> None:
+    """fn(*args, stream) with `device` current; its current stream by default."""
+    raw = torch.cuda.current_stream(device).cuda_stream if stream is None else stream.cuda_stream
+    if torch.cuda.current_device() == device.index:
+        _check(fn(*args, raw))
+    else:
+        with torch.cuda.device(device):
+            _check(fn(*args, raw))
 
 
 def _rows_of(name: str, t: torch.Tensor, device, B: int, n: int, heads: int, dim: int) -> int:
     """The row stride of bf16 [B, n, heads, dim] whose rows b * n + i lie at one stride."""
-    _require(t.dtype == torch.bfloat16 and t.device == device and tuple(t.shape) == (B, n, heads, dim),
-             f"{name} must be bf16 [{B}, {n}, {heads}, {dim}] on {device}")
-    row = t.stride(1) if n > 1 else t.stride(0) if B > 1 else heads * dim
-    _require(t.stride(3) == 1 and (heads == 1 or t.stride(2) == dim) and (n < 2 or B < 2 or t.stride(0) == n * row),
-             f"{name}: heads must lie one after the other, rows at one stride")
+    if not (t.dtype == torch.bfloat16 and t.device == device and t.shape == (B, n, heads, dim)):
+        raise ValueError(f"{name} must be bf16 [{B}, {n}, {heads}, {dim}] on {device}")
+    sb, sn, sh, sd = t.stride()
+    row = sn if n > 1 else sb if B > 1 else heads * dim
+    if not (sd == 1 and (heads == 1 or sh == dim) and (n < 2 or B < 2 or sb == n * row)):
+        raise ValueError(f"{name}: heads must lie one after the other, rows at one stride")
     return row
 
 
-def _kv_args(pool: Pool, seq_ids, pos0, k, v, n_lens):
+def _kv_move(fn, pool: Pool, layer, seq_ids, pos0, k, v, n_lens, stream):
     B, n, dev, c = seq_ids.numel(), k.shape[1], pool.kv.device, pool.cfg
-    _require_ids(dev, seq_ids=seq_ids, pos0=pos0, n_lens=n_lens)
+    _checked(dev, torch.int32, seq_ids=seq_ids, pos0=pos0, n_lens=n_lens)
     _require(pos0.numel() == B and (n_lens is None or n_lens.numel() == B), "pos0 and n_lens must hold one entry a request")
-    ks, vs = (_rows_of(name, t, dev, B, n, c.n_kv_heads, c.head_dim) for name, t in (("k", k), ("v", v)))
-    return B, _ptr(seq_ids), _ptr(pos0), n, _ptr(n_lens), _ptr(k), ks, _ptr(v), vs
+    ks, vs = _rows_of("k", k, dev, B, n, c.n_kv_heads, c.head_dim), _rows_of("v", v, dev, B, n, c.n_kv_heads, c.head_dim)
+    _call(fn, dev, stream, pool.handle, layer, B, seq_ids.data_ptr(), pos0.data_ptr(), n, _addr(n_lens), k.data_ptr(), ks,
+          v.data_ptr(), vs)
 
 
 def kv_write(pool: Pool, layer: int, seq_ids: torch.Tensor, pos0: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
              n_lens: Optional[torch.Tensor] = None, stream=None) -> None:
     """Keys (after RoPE) and values bf16 [B, n, Hkv, D] of tokens pos0[b] + i into their
     pages; n_lens: live rows of each request."""
-    with torch.cuda.device(pool.kv.device):
-        _check(lib().war_kv_write(pool.handle, layer, *_kv_args(pool, seq_ids, pos0, k, v, n_lens), _stream(stream)))
+    _kv_move(lib().war_kv_write, pool, layer, seq_ids, pos0, k, v, n_lens, stream)
 
 
 def kv_read(pool: Pool, layer: int, seq_ids: torch.Tensor, pos0: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
             n_lens: Optional[torch.Tensor] = None, stream=None) -> None:
     """The same tokens' keys and values from their pages into k and v (8 bits: the
     numbers the codes stand for); rows beyond n_lens stay as they are."""
-    with torch.cuda.device(pool.kv.device):
-        _check(lib().war_kv_read(pool.handle, layer, *_kv_args(pool, seq_ids, pos0, k, v, n_lens), _stream(stream)))
+    _kv_move(lib().war_kv_read, pool, layer, seq_ids, pos0, k, v, n_lens, stream)
 
 
 class AttendPlan:
@@ -390,13 +418,13 @@ class AttendPlan:
         """Plan the rows of these requests: n_rows (default max_rows) each, of which
         n_lens are live; row 0 at position ctx_lens[b]."""
         B, n, dev = seq_ids.numel(), self.max_rows if n_rows is None else n_rows, self.pool.kv.device
-        _require_ids(dev, seq_ids=seq_ids, ctx_lens=ctx_lens, n_lens=n_lens, draft_parents=draft_parents)
+        _checked(dev, torch.int32, seq_ids=seq_ids, ctx_lens=ctx_lens, n_lens=n_lens, draft_parents=draft_parents)
         _require(ctx_lens.numel() == B and (n_lens is None or n_lens.numel() == B),
                  "ctx_lens and n_lens must hold one entry a request")
         _require(draft_parents is None or draft_parents.numel() == B * (n - 1), "draft_parents must be [B, n_rows - 1]")
-        with torch.cuda.device(dev):
-            _check(lib().war_attend_update(self.handle, B, n, _ptr(seq_ids), _ptr(ctx_lens), _ptr(n_lens),
-                                           _ptr(draft_parents), _stream(stream)))
+        self.shape = None
+        _call(lib().war_attend_update, dev, stream, self.handle, B, n, seq_ids.data_ptr(), ctx_lens.data_ptr(),
+              _addr(n_lens), _addr(draft_parents))
         self.shape = (B, n)
 
     def close(self):
@@ -415,11 +443,143 @@ def attend(plan: AttendPlan, layer: int, q: torch.Tensor, out: torch.Tensor, str
     """Attention of the planned rows in one layer: q, out bf16 [B, n_rows, Hq, D]."""
     _require(plan.shape is not None, "no plan: call update first")
     pool, (B, n) = plan.pool, plan.shape
-    qs, os_ = (_rows_of(name, t, pool.kv.device, B, n, pool.cfg.n_q_heads, pool.cfg.head_dim)
-               for name, t in (("q", q), ("out", out)))
-    with torch.cuda.device(pool.kv.device):
-        _check(lib().war_attend_run(plan.handle, layer, _ptr(q), qs, _ptr(out), os_, _stream(stream)))
+    dev, H, D = pool.kv.device, pool.cfg.n_q_heads, pool.cfg.head_dim
+    qs, os_ = _rows_of("q", q, dev, B, n, H, D), _rows_of("out", out, dev, B, n, H, D)
+    _call(lib().war_attend_run, dev, stream, plan.handle, layer, q.data_ptr(), qs, out.data_ptr(), os_)
     return out
+
+
+class Constraints:
+    """What requests' next tokens are held to (war.h); every array is optional and stays
+    the caller's, to be changed in place as requests come and go.
+    By sequence id: counts int16 [n_seqs, vocab] (16 bits a token: counts_begin,
+    counts_add), repetition, frequency, presence fp32 [n_seqs], bias_ids int32 and
+    bias_values fp32 [n_seqs, n_bias].  masks int32 [n_masks, ceil(vocab / 32)]: a bit a
+    token; mask_index int32, the mask of each row (negative: none), default row r mask r."""
+
+    def __init__(self, vocab: int, counts: Optional[torch.Tensor] = None, repetition: Optional[torch.Tensor] = None,
+                 frequency: Optional[torch.Tensor] = None, presence: Optional[torch.Tensor] = None,
+                 bias_ids: Optional[torch.Tensor] = None, bias_values: Optional[torch.Tensor] = None,
+                 masks: Optional[torch.Tensor] = None, mask_index: Optional[torch.Tensor] = None,
+                 n_seqs: Optional[int] = None):
+        by_seq = [t for t in (counts, repetition, frequency, presence, bias_ids, bias_values) if t is not None]
+        arrays = by_seq + [t for t in (masks, mask_index) if t is not None]
+        _require(bool(by_seq) or n_seqs is not None, "n_seqs is needed where no array is by sequence")
+        _require(bool(arrays), "nothing constrains")
+        n = n_seqs if n_seqs is not None else by_seq[0].shape[0]
+        dev = arrays[0].device
+        _checked(dev, torch.int16, counts=counts)
+        _checked(dev, torch.float32, repetition=repetition, frequency=frequency, presence=presence, bias_values=bias_values)
+        _checked(dev, torch.int32, bias_ids=bias_ids, masks=masks, mask_index=mask_index)
+        _require(all(t.shape[0] == n for t in by_seq), "arrays by sequence must have the same number of rows")
+        _require(counts is None or counts.shape == (n, vocab), "counts must be [n_seqs, vocab]")
+        _require(all(t is None or t.shape == (n,) for t in (repetition, frequency, presence)), "penalties must be [n_seqs]")
+        _require((bias_ids is None) == (bias_values is None) and
+                 (bias_ids is None or (bias_ids.dim() == 2 and bias_ids.shape == bias_values.shape)),
+                 "bias_ids and bias_values must both be [n_seqs, n_bias]")
+        _require(masks is None or (masks.dim() == 2 and masks.shape[1] == (vocab + 31) // 32),
+                 "masks must be [n_masks, ceil(vocab / 32)]")
+        self.vocab, self.device, self.masks, self.mask_index = vocab, dev, masks, mask_index
+        self._keep = arrays
+        self._c = _Constraints(n, _addr(counts), _addr(repetition), _addr(frequency), _addr(presence),
+                               0 if bias_ids is None else bias_ids.shape[1], _addr(bias_ids), _addr(bias_values),
+                               0 if masks is None else masks.shape[0], _addr(masks), _addr(mask_index))
+        self._ref = C.byref(self._c)
+
+    def _rows(self, rows: int) -> None:
+        """The masks of a call with this many rows."""
+        _require(self.masks is None or (self.mask_index.numel() if self.mask_index is not None else self.masks.shape[0]) >= rows,
+                 "a mask (mask_index) is needed for each row")
+
+
+def constrain_logits(logits: torch.Tensor, constraints: Constraints, seq_ids: torch.Tensor, last_tokens: torch.Tensor,
+                     draft_tokens: Optional[torch.Tensor], draft_lens: Optional[torch.Tensor], k_max: int,
+                     out: Optional[torch.Tensor] = None, greedy: Optional[torch.Tensor] = None,
+                     draft_parents: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                     stream=None) -> None:
+    """Constrained logits fp32 [B * (k_max + 1), vocab] of a step's rows into out (may be
+    logits itself) and each row's greedy token into greedy int32 (-1: no token is
+    allowed); at least one of the two.  A workspace (uint8) of war_constrain_workspace
+    bytes is allocated where none is given."""
+    B, V, dev = seq_ids.numel(), constraints.vocab, constraints.device
+    rows = B * (k_max + 1)
+    _checked(dev, torch.int32, seq_ids=seq_ids, last_tokens=last_tokens, draft_tokens=draft_tokens, draft_lens=draft_lens,
+             draft_parents=draft_parents, greedy=greedy)
+    _require(last_tokens.numel() == B and (draft_lens is None or draft_lens.numel() == B) and
+             all(t is None or t.numel() == B * k_max for t in (draft_tokens, draft_parents)) and
+             (greedy is None or greedy.numel() == rows), "token arrays do not fit B requests of k_max drafts")
+    for name, t in (("logits", logits), ("out", out)):
+        if t is not None and not (t.dtype == torch.float32 and t.device == dev and t.shape == (rows, V) and
+                                  (V == 1 or t.stride(1) == 1)):
+            raise ValueError(f"{name} must be fp32 [{rows}, {V}] on {dev}, ids one after the other")
+    constraints._rows(rows)
+    fn = lib()
+    if greedy is not None:
+        need = fn.war_constrain_workspace(rows, V)
+        if workspace is None:
+            workspace = torch.empty(max(need, 0), dtype=torch.uint8, device=dev)
+        _require(workspace.device == dev and workspace.is_contiguous() and
+                 workspace.numel() * workspace.element_size() >= need, f"workspace must hold {need} bytes on {dev}")
+    ls = logits.stride(0) if rows > 1 else V
+    os_ = V if out is None else out.stride(0) if rows > 1 else V
+    _call(fn.war_constrain_logits, dev, stream, constraints._ref, V, B, seq_ids.data_ptr(), last_tokens.data_ptr(),
+          _addr(draft_tokens) if k_max else None, _addr(draft_parents), _addr(draft_lens), k_max, logits.data_ptr(), ls,
+          _addr(out), os_, _addr(greedy), _addr(workspace) if greedy is not None else None)
+
+
+def _counts_of(counts: torch.Tensor):
+    if not (counts.dtype == torch.int16 and counts.dim() == 2 and counts.is_contiguous() and counts.is_cuda):
+        raise ValueError("counts must be a contiguous int16 [n_seqs, vocab] on the GPU")
+    return counts.device, counts.data_ptr(), counts.shape[1], counts.shape[0]
+
+
+def counts_begin(counts: torch.Tensor, seq_ids: torch.Tensor, tokens: torch.Tensor, offsets: torch.Tensor,
+                 stream=None) -> None:
+    """New requests' rows of counts: their prompts' tokens (packed; request i's at
+    offsets[i] .. offsets[i + 1]) are marked, everything else is cleared."""
+    dev, at, V, S = _counts_of(counts)
+    _checked(dev, torch.int32, seq_ids=seq_ids, tokens=tokens, offsets=offsets)
+    _require(offsets.numel() == seq_ids.numel() + 1, "offsets must hold one more entry than seq_ids")
+    _call(lib().war_counts_begin, dev, stream, at, V, S, seq_ids.numel(), seq_ids.data_ptr(), tokens.data_ptr(),
+          offsets.data_ptr())
+
+
+def counts_add(counts: torch.Tensor, seq_ids: torch.Tensor, first: Optional[torch.Tensor],
+               tokens: Optional[torch.Tensor], lens: Optional[torch.Tensor], path: Optional[torch.Tensor] = None,
+               stream=None) -> None:
+    """Count generated tokens: first[b], then lens[b] (a step's accept_lens; -1: nothing)
+    of tokens[b]; path: a tree's accept_path."""
+    dev, at, V, S = _counts_of(counts)
+    B = seq_ids.numel()
+    _checked(dev, torch.int32, seq_ids=seq_ids, first=first, tokens=tokens, lens=lens, path=path)
+    n = 0 if tokens is None or B == 0 else tokens.numel() // B
+    _require((tokens is None or tokens.numel() == B * n) and (path is None or path.numel() == B * n) and
+             all(t is None or t.numel() == B for t in (first, lens)), "token arrays do not fit the requests")
+    _call(lib().war_counts_add, dev, stream, at, V, S, B, seq_ids.data_ptr(), _addr(first), _addr(tokens), n, _addr(path),
+          _addr(lens))
+
+
+def verify_step_constrained(model: Model, pool: Pool, seq_ids: torch.Tensor, ctx_lens: torch.Tensor,
+                            last_tokens: torch.Tensor, draft_tokens: Optional[torch.Tensor],
+                            draft_lens: Optional[torch.Tensor], k_max: int, constraints: Constraints,
+                            accept_lens: torch.Tensor, next_tokens: torch.Tensor,
+                            logits: Optional[torch.Tensor] = None, draft_parents: Optional[torch.Tensor] = None,
+                            accept_path: Optional[torch.Tensor] = None, uniforms: Optional[torch.Tensor] = None,
+                            temperature: float = 1.0, top_k: int = 1, stream=None) -> None:
+    """A verify step (draft_parents: of draft trees; uniforms: sampled, as
+    verify_step_sampled) whose rows' logits are constrained before a token is chosen.
+    Afterwards counts_add counts what was committed."""
+    B, dev = seq_ids.numel(), pool.kv.device
+    _checked(dev, torch.int32, seq_ids=seq_ids, ctx_lens=ctx_lens, last_tokens=last_tokens, draft_tokens=draft_tokens,
+             draft_lens=draft_lens, accept_lens=accept_lens, next_tokens=next_tokens, draft_parents=draft_parents,
+             accept_path=accept_path)
+    _checked(dev, torch.float32, uniforms=uniforms, logits=logits)
+    _require(constraints.vocab == model.cfg.vocab and constraints.device == dev, "constraints of another vocabulary or device")
+    constraints._rows(B * (k_max + 1))
+    _call(lib().war_verify_step_constrained, dev, stream, model.handle, pool.handle, B, seq_ids.data_ptr(),
+          ctx_lens.data_ptr(), last_tokens.data_ptr(), _addr(draft_tokens), _addr(draft_parents), _addr(draft_lens), k_max,
+          constraints._ref, _addr(uniforms), float(temperature), int(top_k), accept_lens.data_ptr(),
+          next_tokens.data_ptr(), _addr(accept_path), _addr(logits))
 
 
 def debug_mfma16(A: torch.Tensor, B: torch.Tensor, stream=None) -> torch.Tensor:
