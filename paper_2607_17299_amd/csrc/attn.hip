@@ -267,11 +267,13 @@ k_attn(AttnArgs a) {
     };
 
     float m_run[NR], l_run[NR];
+    [[maybe_unused]] f32x4 l_acc[NR];
     f32x4 o_acc[NDT][NR];
 #pragma unroll
     for (int rt = 0; rt < NR; ++rt) {
       m_run[rt] = -INFINITY;
       l_run[rt] = 0.f;
+      l_acc[rt] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int dt = 0; dt < NDT; ++dt) o_acc[dt][rt] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
@@ -379,6 +381,7 @@ k_attn(AttnArgs a) {
           if (mx > m_run[rt] + 8.f) {
             const float alpha = exp2f(m_run[rt] - mx);
             l_run[rt] *= alpha;
+            if constexpr (Q8) l_acc[rt] *= alpha;
 #pragma unroll
             for (int dt = 0; dt < NDT; ++dt) o_acc[dt][rt] *= alpha;
             m_run[rt] = mx;
@@ -387,27 +390,37 @@ k_attn(AttnArgs a) {
         const float m_use = m_run[rt] == -INFINITY ? 0.f : m_run[rt];
         // P = hi + lo, both bf16: the product keeps ~16 bits of each weight.
         // v_exp_f32 directly: weights below 2^-126 of the running max flush to 0.
+        // Q8: one bf16 a weight (half a step is 2^-8 of it at most, a number of the
+        // cache is off by 2^-4 of it); the row sum is taken of the rounded weights, by
+        // the matrix core, so that what rounds alike cancels.  A scale is a power of
+        // two: the weights times scales round to the rounded weights times scales.
         float sum = 0.f;
         uint32_t hi[4], lo[4];
 #pragma unroll
         for (int e = 0; e < 8; e += 2) {
-          float p0 = __builtin_amdgcn_exp2f(fmaf(sv[e], a.scale_log2, -m_use));
-          float p1 = __builtin_amdgcn_exp2f(fmaf(sv[e + 1], a.scale_log2, -m_use));
-          sum += p0 + p1;
+          const float p0 = __builtin_amdgcn_exp2f(fmaf(sv[e], a.scale_log2, -m_use));
+          const float p1 = __builtin_amdgcn_exp2f(fmaf(sv[e + 1], a.scale_log2, -m_use));
           if constexpr (Q8) {
-            p0 *= vsc[e];
-            p1 *= vsc[e + 1];
+            lo[e / 2] = pack2(p0, p1);
+            hi[e / 2] = pack2(p0 * vsc[e], p1 * vsc[e + 1]);
+          } else {
+            sum += p0 + p1;
+            hi[e / 2] = pack2(p0, p1);
+            lo[e / 2] = pack2(p0 - lo_f(hi[e / 2]), p1 - hi_f(hi[e / 2]));
           }
-          hi[e / 2] = pack2(p0, p1);
-          lo[e / 2] = pack2(p0 - lo_f(hi[e / 2]), p1 - hi_f(hi[e / 2]));
         }
-        l_run[rt] += sum;
         const bf16x8 ph = as_bf16x8(make_uint4(hi[0], hi[1], hi[2], hi[3]));
         const bf16x8 pl = as_bf16x8(make_uint4(lo[0], lo[1], lo[2], lo[3]));
+        if constexpr (Q8) {
+          constexpr uint32_t one2 = 0x3f803f80u;
+          l_acc[rt] = mfma16(as_bf16x8(make_uint4(one2, one2, one2, one2)), pl, l_acc[rt]);
+        } else {
+          l_run[rt] += sum;
+        }
 #pragma unroll
         for (int dt = 0; dt < NDT; ++dt) {
           o_acc[dt][rt] = mfma16(as_bf16x8(vf[dt]), ph, o_acc[dt][rt]);
-          o_acc[dt][rt] = mfma16(as_bf16x8(vf[dt]), pl, o_acc[dt][rt]);
+          if constexpr (!Q8) o_acc[dt][rt] = mfma16(as_bf16x8(vf[dt]), pl, o_acc[dt][rt]);
         }
       }
     };
@@ -457,9 +470,11 @@ k_attn(AttnArgs a) {
     // ---- merge the 4 waves (fixed order) and write the item's partial
 #pragma unroll
     for (int rt = 0; rt < NR; ++rt) {
-      float l = l_run[rt];
-      l += __shfl_xor(l, 16, 64);
-      l += __shfl_xor(l, 32, 64);
+      float l = Q8 ? l_acc[rt][0] : l_run[rt];
+      if constexpr (!Q8) {
+        l += __shfl_xor(l, 16, 64);
+        l += __shfl_xor(l, 32, 64);
+      }
       if (lg == 0) {
         s_m[w][rt * 16 + ln] = m_run[rt];
         s_l[w][rt * 16 + ln] = l;

@@ -192,14 +192,14 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
         c.vs = *reinterpret_cast<const uint2*>(scb + (int64_t)pv_ * sstride + vscale);
       }
     };
-    auto convert = [&](const Codes& c, int stage) __attribute__((always_inline)) {
-      if (kmine) {
-        const float f = scale_of<0>(c.ks);
-        unsigned char* d = smem + stage * SB + kdst;
-        *reinterpret_cast<uint4*>(d) = from_e4m3x8(c.k.x, c.k.y, f);
-        *reinterpret_cast<uint4*>(d + 256) = from_e4m3x8(c.k.z, c.k.w, f);
+    // a quarter of it: keys (0, 1), values (2, 3), eight codes each
+    auto convert = [&](const Codes& c, int stage, int part) __attribute__((always_inline)) {
+      if (part < 2 && kmine) {
+        unsigned char* d = smem + stage * SB + kdst + part * 256;
+        *reinterpret_cast<uint4*>(d) = part ? from_e4m3x8(c.k.z, c.k.w, scale_of<0>(c.ks))
+                                            : from_e4m3x8(c.k.x, c.k.y, scale_of<0>(c.ks));
       }
-      if (vmine) {
+      if (part >= 2 && vmine) {
         const float f[8] = {scale_of<0>(c.vs.x), scale_of<1>(c.vs.x), scale_of<2>(c.vs.x), scale_of<3>(c.vs.x),
                             scale_of<0>(c.vs.y), scale_of<1>(c.vs.y), scale_of<2>(c.vs.y), scale_of<3>(c.vs.y)};
         auto eight = [&](uint32_t w0, uint32_t w1) __attribute__((always_inline)) {
@@ -208,10 +208,13 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
           return make_uint4(pack2(a0[0] * f[0], a0[1] * f[1]), pack2(a1[0] * f[2], a1[1] * f[3]),
                             pack2(a2[0] * f[4], a2[1] * f[5]), pack2(a3[0] * f[6], a3[1] * f[7]));
         };
-        unsigned char* d = smem + (ST + stage) * SB + vdst;
-        *reinterpret_cast<uint4*>(d) = eight(c.v.x, c.v.y);
-        *reinterpret_cast<uint4*>(d + 256) = eight(c.v.z, c.v.w);
+        unsigned char* d = smem + (ST + stage) * SB + vdst + (part - 2) * 256;
+        *reinterpret_cast<uint4*>(d) = part == 2 ? eight(c.v.x, c.v.y) : eight(c.v.z, c.v.w);
       }
+    };
+    auto convert_all = [&](const Codes& c, int stage) __attribute__((always_inline)) {
+#pragma unroll
+      for (int part = 0; part < 4; ++part) convert(c, stage, part);
     };
 
     // queries (B operand of S^T) and position of this lane's row
@@ -243,8 +246,10 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
       return as_bf16x8(*reinterpret_cast<const uint4*>(smem + stage * SB + f * 1024 + vread));
     };
     f32x16 zero;
+    [[maybe_unused]] f32x16 l_acc;
+    [[maybe_unused]] constexpr uint32_t one2 = 0x3f803f80u;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) zero[e] = 0.f;
+    for (int e = 0; e < 16; ++e) zero[e] = l_acc[e] = 0.f;
     auto scores = [&](int stage, f32x16& s) __attribute__((always_inline)) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) s[e] = 0.f;
@@ -258,11 +263,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
     // last block and S(i + 1) is of no use; block -1 has zero weights and zeros.
     auto step = [&](int i, f32x16& s, f32x16& snext, const Pw& pin, Pw& pout, int k0, int k1, int v0,
                     int v1, [[maybe_unused]] Codes& cd) __attribute__((always_inline)) {
-      if constexpr (Q8) {
-        // block i + 2 to LDS, block i + 4 requested in its place
-        convert(cd, (i + 2) & 3);
-        fetch(cd, k0, k1);
-      } else {
+      if constexpr (!Q8) {
         load_k(i & 3, k0, k1);
         load_v((i + 2) & 3, v0, v1);
       }
@@ -287,7 +288,10 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
       for (int f = 0; f < LOOK; ++f) read(f);
       float lm = 0.f, m_new = 0.f, m_use = 0.f, sum = 0.f, p0 = 0.f, p1 = 0.f;
       uint32_t hi[8], lo[8];
-      constexpr int SLOTS = 3 * KF, HEAD = 3 * KF / 8;  // the row maximum takes the first HEAD slots
+      // Q8: one product of a bf16 a weight (see k_attn), two of ones for the row sums, and
+      // a quarter of the conversion (block i + 2 to LDS) in each of four slots
+      constexpr int PV = Q8 ? 1 : 2;                                      // products of a value fragment
+      constexpr int SLOTS = (1 + PV) * KF + (Q8 ? 2 : 0), HEAD = 3 * KF / 8;  // the row maximum takes the first HEAD slots
       auto softmax = [&](int t) __attribute__((always_inline)) {  // task t of 16: half of the work of a pair of keys
         const int e = t / 2 * 2;
         if (t % 2 == 0) {
@@ -298,19 +302,27 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
           hi[e / 2] = pack2(p0, p1);
           asm volatile("" : "+v"(hi[e / 2]), "+v"(p0), "+v"(p1));
         } else {
-          sum += p0 + p1;
-          lo[e / 2] = pack2(p0 - lo_f(hi[e / 2]), p1 - hi_f(hi[e / 2]));
-          asm volatile("" : "+v"(lo[e / 2]), "+v"(sum));
+          if constexpr (!Q8) {
+            sum += p0 + p1;
+            lo[e / 2] = pack2(p0 - lo_f(hi[e / 2]), p1 - hi_f(hi[e / 2]));
+            asm volatile("" : "+v"(lo[e / 2]), "+v"(sum));
+          }
         }
       };
 #pragma unroll
       for (int z = 0; z < SLOTS; ++z) {
-        const int f = z / 3;
-        if (z % 3 == 0) {
+        const int f = z / (1 + PV);
+        if (z >= (1 + PV) * KF) {
+          l_acc = mfma32(as_bf16x8(make_uint4(one2, one2, one2, one2)), as_bf16x8(pin.hi[z - (1 + PV) * KF]), l_acc);
+        } else if (z % (1 + PV) == 0) {
           if (f + LOOK < KF) read(f + LOOK);
           snext = mfma32(rk[f % RING], qf[f], f == 0 ? zero : snext);
         } else {
-          o_acc[f % NDT] = mfma32(rv[f % RING], as_bf16x8(z % 3 == 1 ? pin.hi[f / NDT] : pin.lo[f / NDT]), o_acc[f % NDT]);
+          o_acc[f % NDT] = mfma32(rv[f % RING], as_bf16x8(z % (1 + PV) == 1 ? pin.hi[f / NDT] : pin.lo[f / NDT]), o_acc[f % NDT]);
+        }
+        if constexpr (Q8) {
+          constexpr int Q = SLOTS / 4;
+          if (z % Q == Q - 1 && z / Q < 4) convert(cd, (i + 2) & 3, z / Q);
         }
         if (z == 0) {
           lm = fmaxf(s[0], s[1]);
@@ -332,11 +344,13 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
 #pragma unroll
       for (int pg = 0; pg < 2; ++pg) {
         pout.hi[pg] = make_uint4(hi[pg * 4], hi[pg * 4 + 1], hi[pg * 4 + 2], hi[pg * 4 + 3]);
-        pout.lo[pg] = make_uint4(lo[pg * 4], lo[pg * 4 + 1], lo[pg * 4 + 2], lo[pg * 4 + 3]);
+        if constexpr (!Q8) pout.lo[pg] = make_uint4(lo[pg * 4], lo[pg * 4 + 1], lo[pg * 4 + 2], lo[pg * 4 + 3]);
       }
+      if constexpr (Q8) fetch(cd, k0, k1);  // block i + 4, in the place of the one just converted
       if (__any(m_new != m_run)) {
         const float alpha = m_new == m_run ? 1.f : exp2f(m_run - m_new);
         l_run *= alpha;
+        if constexpr (Q8) l_acc *= alpha;
 #pragma unroll
         for (int dt = 0; dt < NDT; ++dt) o_acc[dt] *= alpha;
         m_run = m_new;
@@ -354,10 +368,10 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
         fetch(ca, k0, k1);
         pages(min(1, lb), k0, k1);
         fetch(cb, k0, k1);
-        convert(ca, 0);
+        convert_all(ca, 0);
         pages(min(2, lb), k0, k1);
         fetch(ca, k0, k1);
-        convert(cb, 1);
+        convert_all(cb, 1);
         pages(min(3, lb), k0, k1);
         fetch(cb, k0, k1);
       } else {
@@ -402,20 +416,22 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
       // the last block's product; slots past the sequence end may hold anything
       const int kb = kbeg + 32 * lb;
 #pragma unroll
-      for (int pg = 0; pg < 2; ++pg)
+      for (int pg = 0; pg < 2; ++pg) {
+        if constexpr (Q8) l_acc = mfma32(as_bf16x8(make_uint4(one2, one2, one2, one2)), as_bf16x8(pa.hi[pg]), l_acc);
 #pragma unroll
         for (int dt = 0; dt < NDT; ++dt) {
           uint4 v = __builtin_bit_cast(uint4, vfrag(lb & 3, pg * NDT + dt));
           if (kb + 32 > S) v = keep_first(v, min(max(S - (kb + 16 * pg + 8 * g), 0), 8));
           o_acc[dt] = mfma32(as_bf16x8(v), as_bf16x8(pa.hi[pg]), o_acc[dt]);
-          o_acc[dt] = mfma32(as_bf16x8(v), as_bf16x8(pa.lo[pg]), o_acc[dt]);
+          if constexpr (!Q8) o_acc[dt] = mfma32(as_bf16x8(v), as_bf16x8(pa.lo[pg]), o_acc[dt]);
         }
+      }
     }
 
     int next_it = 0;
     if (tid == 0) next_it = uq.next(a.unit_ctr);
     // this wave's rows: partial O, running max and sum
-    const float l = l_run + __shfl_xor(l_run, 32, 64);
+    const float l = Q8 ? l_acc[0] : l_run + __shfl_xor(l_run, 32, 64);
     if (live) {
 #pragma unroll
       for (int dt = 0; dt < NDT; ++dt)

@@ -10,7 +10,7 @@
 // of rows, chunks and batches gives the same bits.
 //
 // Memory bounds it: a logit is read and written once, its count (16 bits) once a
-// request.  A workgroup takes 2048 ids of all rows of a request: counts and biases stay
+// request.  A workgroup takes 2048 ids of a request's rows: counts and biases stay
 // in registers, the few tokens of the rows themselves are added where they fall into the
 // chunk (a uniform test), and the next row's logits are in flight while a row is done.
 // It leaves the best id of every 128 (as the LM head does without constraints), from
@@ -38,7 +38,7 @@ WAR_DEV f32x4_t load4(const float* z, int col, int V) {
 
 template <bool VEC>
 __global__ void __launch_bounds__(kThreads) k_constrain(ConstrainArgs a) {
-  __shared__ int s_tok[kNodes];
+  __shared__ int s_tok[kNodes], s_mask[kNodes];
   __shared__ unsigned long long s_path[kNodes];
   __shared__ float s_bias[kIds];
   const int b = blockIdx.y, tid = threadIdx.x, lane = tid & 63;
@@ -47,61 +47,31 @@ __global__ void __launch_bounds__(kThreads) k_constrain(ConstrainArgs a) {
   const int n = a.ntok ? a.ntok[b] : a.draft_lens ? min(max(a.draft_lens[b], 0), a.k_max) + 1 : kp1;
   const int seq = a.seq_ids[b];
   const int64_t row0 = (int64_t)b * kp1;
-  const int nblk = (a.V + 127) / 128;
-  if (n <= 0) return;
+  const int nblk = (a.V + 127) / 128, words = (a.V + 31) / 32;
+  const int step = gridDim.z;  // this workgroup's rows: blockIdx.z, + step, ...
+  int i = blockIdx.z;
+  if (i >= n) return;
   if (seq < 0 || seq >= a.n_seqs) {  // no such request: no token in any row
     if (a.best_v)
-      for (int i = 0; i < n; ++i)
+      for (; i < n; i += step)
         for (int q = c0 / 128 + tid; q < (c1 + 127) / 128; q += kThreads) {
           a.best_v[(row0 + i) * nblk + q] = -INFINITY;
           a.best_i[(row0 + i) * nblk + q] = kNone;
         }
     return;
   }
-  // the rows' tokens (row i's own and its ancestors' are its text)
-  if (tid < n) {
-    s_tok[tid] = tid == 0 ? a.last_tokens[b] : a.draft_tokens[(int64_t)b * a.k_max + tid - 1];
-    unsigned long long path = 1ull << tid;
-    for (int j = tid; j > 0;) {
-      int p = a.parents ? a.parents[(int64_t)b * a.k_max + j - 1] : j - 1;
-      if (p < 0 || p >= j) p = j - 1;  // as the step reads it
-      path |= 1ull << p;
-      j = p;
-    }
-    s_path[tid] = path;
-  }
-  // biases of this chunk: the first entry of an id adds up all of them, in list order
-  bool hit = false;
-  const int32_t* bid = a.bias_ids + (int64_t)seq * a.n_bias;
-  const float* bval = a.bias_values + (int64_t)seq * a.n_bias;
-  for (int e = tid; e < a.n_bias; e += kThreads) hit = hit || (bid[e] >= c0 && bid[e] < c1);
-  const bool biased = __syncthreads_or(hit);
-  if (biased) {
-    for (int i = tid; i < kIds; i += kThreads) s_bias[i] = 0.f;
-    __syncthreads();
-    for (int e = tid; e < a.n_bias; e += kThreads) {
-      const int id = bid[e];
-      if (id < c0 || id >= c1) continue;
-      bool first = true;
-      for (int q = 0; q < e; ++q) first = first && bid[q] != id;
-      if (!first) continue;
-      float sum = bval[e];
-      for (int q = e + 1; q < a.n_bias; ++q)
-        if (bid[q] == id) sum += bval[q];
-      s_bias[id - c0] = sum;
-    }
-    __syncthreads();
-  }
-  unsigned long long here = 0;  // the rows' tokens that lie in this chunk
-  for (int i = 0; i < n; ++i)
-    if (s_tok[i] >= c0 && s_tok[i] < c1) here |= 1ull << i;
-
+  // everything that hangs on nothing else is requested first: the first row's logits, the
+  // counts, the penalties
   int col[kUnits], cnt[kUnits][4];
   f32x4_t bias[kUnits], z[kUnits];
   const uint16_t* crow = a.counts ? a.counts + (int64_t)seq * a.V : nullptr;
 #pragma unroll
   for (int u = 0; u < kUnits; ++u) {
     col[u] = c0 + (u * kThreads + tid) * 4;
+    z[u] = load4<VEC>(a.logits + (row0 + i) * a.stride, col[u], a.V);
+  }
+#pragma unroll
+  for (int u = 0; u < kUnits; ++u) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) cnt[u][e] = 0;
     if (crow) {
@@ -119,32 +89,76 @@ __global__ void __launch_bounds__(kThreads) k_constrain(ConstrainArgs a) {
           if (col[u] + e < a.V) cnt[u][e] = crow[col[u] + e];
       }
     }
-#pragma unroll
-    for (int e = 0; e < 4; ++e) cnt[u][e] = (cnt[u][e] & 0x7fff) * 2 + (cnt[u][e] >> 15);  // prompt bit last
-#pragma unroll
-    for (int e = 0; e < 4; ++e) bias[u][e] = biased ? s_bias[col[u] - c0 + e] : 0.f;
-    z[u] = load4<VEC>(a.logits + row0 * a.stride, col[u], a.V);
   }
   const float r = a.repetition ? a.repetition[seq] : 1.f;
   const float f = a.frequency ? a.frequency[seq] : 0.f, p = a.presence ? a.presence[seq] : 0.f;
-
-  for (int i = 0; i < n; ++i) {
-    const int64_t row = row0 + i;
-    int m = -1;
-    bool none = false;  // a mask that is not there allows nothing
+  // the rows' tokens (row j's own and its ancestors' are its text) and masks
+  if (tid < n) {
+    s_tok[tid] = tid == 0 ? a.last_tokens[b] : a.draft_tokens[(int64_t)b * a.k_max + tid - 1];
+    int m = -1;  // (a mask that is not there allows nothing: -2)
     if (a.masks) {
-      m = a.mask_index ? a.mask_index[row] : (int)row;
-      none = m >= a.n_masks;
+      m = a.mask_index ? a.mask_index[row0 + tid] : (int)(row0 + tid);
+      m = m >= a.n_masks ? -2 : max(m, -1);
     }
-    const uint32_t* mrow = m >= 0 && !none ? a.masks + (int64_t)m * ((a.V + 31) / 32) : nullptr;
-    uint32_t word[kUnits];
+    s_mask[tid] = m;
+    unsigned long long path = a.parents ? 1ull << tid : ~0ull >> (63 - tid);
+    if (a.parents)
+      for (int j = tid; j > 0;) {
+        int q = a.parents[(int64_t)b * a.k_max + j - 1];
+        if (q < 0 || q >= j) q = j - 1;  // as the step reads it
+        path |= 1ull << q;
+        j = q;
+      }
+    s_path[tid] = path;
+  }
+  // biases of this chunk: the first entry of an id adds up all of them, in list order
+  bool hit = false;
+  const int32_t* bid = a.bias_ids + (int64_t)seq * a.n_bias;
+  const float* bval = a.bias_values + (int64_t)seq * a.n_bias;
+  for (int e = tid; e < a.n_bias; e += kThreads) hit = hit || (bid[e] >= c0 && bid[e] < c1);
+  const bool biased = __syncthreads_or(hit);
+  if (biased) {
+    for (int j = tid; j < kIds; j += kThreads) s_bias[j] = 0.f;
+    __syncthreads();
+    for (int e = tid; e < a.n_bias; e += kThreads) {
+      const int id = bid[e];
+      if (id < c0 || id >= c1) continue;
+      bool first = true;
+      for (int q = 0; q < e; ++q) first = first && bid[q] != id;
+      if (!first) continue;
+      float sum = bval[e];
+      for (int q = e + 1; q < a.n_bias; ++q)
+        if (bid[q] == id) sum += bval[q];
+      s_bias[id - c0] = sum;
+    }
+    __syncthreads();
+  }
+  // the rows' tokens that lie in this chunk (n <= 64: lane j looks at token j)
+  const unsigned long long here = __ballot(lane < n && s_tok[min(lane, n - 1)] >= c0 && s_tok[min(lane, n - 1)] < c1);
+  auto mask_words = [&](int j, uint32_t (&w)[kUnits]) {
+    const int m = __builtin_amdgcn_readfirstlane(s_mask[j]);
+    const uint32_t* mrow = a.masks + (int64_t)max(m, 0) * words;
 #pragma unroll
-    for (int u = 0; u < kUnits; ++u)
-      word[u] = none ? 0u : mrow && col[u] < a.V ? mrow[col[u] >> 5] >> (col[u] & 31) : ~0u;
+    for (int u = 0; u < kUnits; ++u) w[u] = m == -2 ? 0u : m >= 0 && col[u] < a.V ? mrow[col[u] >> 5] : ~0u;
+  };
+  uint32_t word[kUnits];
+  mask_words(i, word);
+#pragma unroll
+  for (int u = 0; u < kUnits; ++u)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      cnt[u][e] = (cnt[u][e] & 0x7fff) * 2 + (cnt[u][e] >> 15);  // prompt bit last
+      bias[u][e] = biased ? s_bias[col[u] - c0 + e] : 0.f;
+    }
+
+  for (; i < n; i += step) {
+    const int64_t row = row0 + i;
     f32x4_t next[kUnits];
-    if (i + 1 < n) {
+    uint32_t next_word[kUnits];
+    if (i + step < n) {
 #pragma unroll
-      for (int u = 0; u < kUnits; ++u) next[u] = load4<VEC>(a.logits + (row + 1) * a.stride, col[u], a.V);
+      for (int u = 0; u < kUnits; ++u) next[u] = load4<VEC>(a.logits + (row + step) * a.stride, col[u], a.V);
+      mask_words(i + step, next_word);
     }
     const unsigned long long add = here & s_path[i];
 #pragma unroll
@@ -159,6 +173,7 @@ __global__ void __launch_bounds__(kThreads) k_constrain(ConstrainArgs a) {
           if (d == e) c[e] += 2;
       }
       f32x4_t x = z[u];
+      const uint32_t allow = word[u] >> (col[u] & 31);
       float best = -INFINITY;
       int at = kNone;
       bool nan = false;
@@ -172,7 +187,7 @@ __global__ void __launch_bounds__(kThreads) k_constrain(ConstrainArgs a) {
           v -= f * (float)k;
           if (k) v -= p;
         }
-        const bool ok = ((word[u] >> e) & 1u) && col[u] + e < a.V;
+        const bool ok = ((allow >> e) & 1u) && col[u] + e < a.V;
         if (!ok) v = -INFINITY;
         x[e] = v;
         nan = nan || v != v;
@@ -207,39 +222,51 @@ __global__ void __launch_bounds__(kThreads) k_constrain(ConstrainArgs a) {
         }
       }
       z[u] = next[u];
+      word[u] = next_word[u];
     }
   }
 }
 
 // Greedy token of each row from the best of its 128-id blocks: the lowest id among the
-// largest, -1 where no block has one (`finite`: or only -inf).  A wave a row.
+// largest, -1 where no block has one (`finite`: or only -inf).  A workgroup a row; a
+// thread's blocks ascend, so that the first of equals has the lowest id.
 __global__ void __launch_bounds__(256) k_greedy(ConstrainArgs a, int32_t* greedy, bool finite) {
+  __shared__ float s_v[4];
+  __shared__ int s_i[4];
   const int kp1 = a.k_max + 1, nblk = (a.V + 127) / 128, lane = threadIdx.x & 63;
-  const int r = blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (r >= a.B * kp1) return;
-  const int b = r / kp1;
+  const int r = blockIdx.x, b = r / kp1;
   const int n = a.ntok ? a.ntok[b] : a.draft_lens ? min(max(a.draft_lens[b], 0), a.k_max) + 1 : kp1;
   if (r % kp1 >= n) return;
   float v = -INFINITY;
   int idx = kNone;
-  for (int c = lane; c < nblk; c += 64) {
-    const float bv = a.best_v[(int64_t)r * nblk + c];
-    const int bi = a.best_i[(int64_t)r * nblk + c];
-    if (bi != kNone && (idx == kNone || bv > v)) {
-      v = bv;
-      idx = bi;
-    }
-  }
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) {
-    const float ov = __shfl_xor(v, o, 64);
-    const int oi = __shfl_xor(idx, o, 64);
+  auto better = [&](float ov, int oi) {
     if (oi != kNone && (idx == kNone || ov > v || (ov == v && oi < idx))) {
       v = ov;
       idx = oi;
     }
+  };
+  for (int c0 = threadIdx.x; c0 < nblk; c0 += 256 * 8) {
+    float bv[8];
+    int bi[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const int c = c0 + 256 * u;
+      bv[u] = c < nblk ? a.best_v[(int64_t)r * nblk + c] : 0.f;
+      bi[u] = c < nblk ? a.best_i[(int64_t)r * nblk + c] : kNone;
+    }
+#pragma unroll
+    for (int u = 0; u < 8; ++u) better(bv[u], bi[u]);
   }
-  if (lane == 0) greedy[r] = idx == kNone || (finite && v == -INFINITY) ? -1 : idx;
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) better(__shfl_xor(v, o, 64), __shfl_xor(idx, o, 64));
+  if (lane == 0) {
+    s_v[threadIdx.x >> 6] = v;
+    s_i[threadIdx.x >> 6] = idx;
+  }
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+  for (int w = 1; w < 4; ++w) better(s_v[w], s_i[w]);
+  greedy[r] = idx == kNone || (finite && v == -INFINITY) ? -1 : idx;
 }
 
 // A request's row of the counts begins: bit 15 for each token of its prompt, no
@@ -308,7 +335,11 @@ __global__ void __launch_bounds__(256) k_counts_add(uint16_t* counts, int V, int
 }  // namespace
 
 void launch_constrain(const ConstrainArgs& a, hipStream_t st) {
-  const dim3 grid(cdiv_i(a.V, kIds), a.B);
+  // a workgroup takes all of a request's rows where that fills the chip (its counts are read
+  // once), fewer otherwise
+  const int chunks = cdiv_i(a.V, kIds), most = std::min(a.k_max + 1, 65535);
+  int rows = std::max(1, std::min(most, cdiv_i(2048, chunks * a.B)));
+  const dim3 grid(chunks, a.B, rows);
   auto quad = [](const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; };
   // 16-byte accesses where every row of every array allows them
   const bool vec = a.V % 4 == 0 && a.stride % 4 == 0 && quad(a.logits, 16) && quad(a.counts, 8) &&
@@ -317,7 +348,7 @@ void launch_constrain(const ConstrainArgs& a, hipStream_t st) {
   else k_constrain<false><<<grid, kThreads, 0, st>>>(a);
 }
 void launch_greedy(const ConstrainArgs& a, int32_t* greedy, bool finite, hipStream_t st) {
-  k_greedy<<<cdiv_i(a.B * (a.k_max + 1), 4), 256, 0, st>>>(a, greedy, finite);
+  k_greedy<<<a.B * (a.k_max + 1), 256, 0, st>>>(a, greedy, finite);
 }
 void launch_counts_begin(uint16_t* counts, int V, int n_seqs, int B, const int32_t* seq_ids, const int32_t* tokens,
                          const int32_t* offsets, hipStream_t st) {

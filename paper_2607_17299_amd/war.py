@@ -359,8 +359,9 @@ def _checked(device, dtype, **arrays) -> None:
 
 
 def _call(fn, device, stream, *args) -> None:
-    """fn(*args, stream) with `device` current; its current stream by default."""
-    raw = torch.cuda.current_stream(device).cuda_stream if stream is None else stream.cuda_stream
+    """fn(*args, stream) with `device` current; its current stream by default (read raw:
+    a Stream object is made in 2 us, a third of a small call)."""
+    raw = torch._C._cuda_getCurrentRawStream(device.index) if stream is None else stream.cuda_stream
     if torch.cuda.current_device() == device.index:
         _check(fn(*args, raw))
     else:
