@@ -477,25 +477,30 @@ __global__ void __launch_bounds__(kBT) k_attend_plan_rows(PoolDev p, RowPlanArgs
     if (s_bad) atomicOr(&p.scalars[1], ERR_BAD_TOKEN);
     if (s_dup) atomicOr(&p.scalars[1], ERR_DUP_SEQ);
   }
-  if (fail) n = 0;
+  if (fail) s = ctx = n = 0;  // (what was refused may be any number)
   const int len = n > 0 ? ctx + n : 0, blocks = (n + a.TB - 1) / a.TB;
+  // (lengths are at most 2^24; every block reaches the chunks that begin before the
+  // first block's end, so only those behind take a division)
   auto first = [&](int ctx_, int c, int chunk) {
-    const int64_t before = (int64_t)c * chunk - ctx_;
-    return before < a.TB ? 0 : (int)(before / a.TB);
+    const int before = c * chunk - ctx_;
+    return before < a.TB ? 0 : before / a.TB;
   };
   auto items_of = [&](int chunk) {
-    int k = 0;
-    for (int c = 0; c * chunk < len; ++c) k += blocks - first(ctx, c, chunk);
+    int c = min((len + chunk - 1) / chunk, (ctx + a.TB + chunk - 1) / chunk);
+    int k = c * blocks;
+    for (; c * chunk < len; ++c) k += blocks - first(ctx, c, chunk);
     return k;
   };
-  if (t < a.B && n > 0)
-    for (int i = 1, ch = a.chunk / 2; i < kChunks && ch >= kMinChunk; ++i, ch /= 2)
-      atomicAdd(&s_cnt[i], min(items_of(ch), 1 << 20));
-  __syncthreads();
-  int chunk = a.chunk;
-  for (int i = 1; i < kChunks && chunk / 2 >= kMinChunk && s_cnt[i] <= a.items_fill; ++i) chunk /= 2;
-  int n_items;
-  const int off = block_excl_scan(t < a.B ? items_of(chunk) : 0, &n_items);
+  int chunk = a.chunk, n_items;
+  int off = block_excl_scan(t < a.B ? items_of(chunk) : 0, &n_items);
+  if (2 * n_items <= a.items_fill) {  // (the same for all threads)
+    if (t < a.B && n > 0)
+      for (int i = 1, ch = a.chunk / 2; i < kChunks && ch >= kMinChunk; ++i, ch /= 2)
+        atomicAdd(&s_cnt[i], min(items_of(ch), 1 << 20));
+    __syncthreads();
+    for (int i = 1; i < kChunks && chunk / 2 >= kMinChunk && s_cnt[i] <= a.items_fill; ++i) chunk /= 2;
+    off = block_excl_scan(t < a.B ? items_of(chunk) : 0, &n_items);
+  }
   if (t < a.B) {
     s_ctx[t] = ctx;
     s_n[t] = n;
@@ -520,8 +525,10 @@ __global__ void __launch_bounds__(kBT) k_attend_plan_rows(PoolDev p, RowPlanArgs
     m.seg_begin[i] = m.seg_count[i] = 0;
     if (rb >= nb) continue;
     const int ntk = min(a.TB, s_n[b] - rb * a.TB), S = s_ctx[b] + rb * a.TB + ntk;
-    int begin = s_off[b];  // items block by block: the chunks of the blocks before this one
-    for (int c = 0; c * chunk < s_ctx[b] + s_n[b]; ++c) begin += max(0, rb - first(s_ctx[b], c, chunk));
+    // items block by block: the chunks of the blocks before this one
+    int c0 = (s_ctx[b] + a.TB + chunk - 1) / chunk;
+    int begin = s_off[b] + c0 * rb;
+    for (int c = c0; c * chunk < S; ++c) begin += max(0, rb - first(s_ctx[b], c, chunk));
     m.seg_begin[i] = begin;
     m.seg_count[i] = (S + chunk - 1) / chunk;
     int slot = s_off[b];  // work order chunk by chunk

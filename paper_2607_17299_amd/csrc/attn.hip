@@ -165,41 +165,56 @@ k_attn(AttnArgs a) {
     auto ntload = [](const Elem* p) {
       return __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(p)));
     };
-    auto load_block = [&](KVFrag<HD, Q8>& f, int kb) {
-      const int pg0 = trow[kb / P];
-      const int pg1 = (kb + 16 < S) ? trow[kb / P + 1] : pg0;
+    auto pages_of = [&](int kb, int& pg0, int& pg1) {
+      pg0 = trow[kb / P];
+      pg1 = (kb + 16 < S) ? trow[kb / P + 1] : pg0;
+    };
+    auto load_k = [&](KVFrag<HD, Q8>& f, int pg0, int pg1) {
+      const int64_t pg = k_second ? pg1 : pg0;
+      const Elem* kp = kvb + pg * pstride;
       if constexpr (Q8) {
-        const uint8_t* kp = kvb + (int64_t)(k_second ? pg1 : pg0) * pstride;
-        const uint8_t* vp = kvb + (int64_t)(v_second ? pg1 : pg0) * pstride + voff;
-        const int64_t sstride = (int64_t)a.kv.n_kv_heads * 32;
-        f.ks = *reinterpret_cast<const uint16_t*>(scb + (int64_t)(k_second ? pg1 : pg0) * sstride + key_scale8(kk0 & 15));
-        f.vs = *reinterpret_cast<const uint2*>(scb + (int64_t)(v_second ? pg1 : pg0) * sstride + val_scale8((lg & 1) * 8));
+        f.ks = *reinterpret_cast<const uint16_t*>(scb + pg * a.kv.n_kv_heads * 32 + key_scale8(kk0 & 15));
 #pragma unroll
         for (int j = 0; j < KSUB / 2; ++j) {
           f.k[0][j] = ntload(kp + koff0 + j * 512);
           f.k[1][j] = ntload(kp + koff1 + j * 512);
         }
+      } else {
+#pragma unroll
+        for (int j = 0; j < KSUB; ++j) {
+          f.k[0][j] = ntload(kp + koff0 + j * 256);
+          f.k[1][j] = ntload(kp + koff1 + j * 256);
+        }
+      }
+    };
+    auto load_v = [&](KVFrag<HD, Q8>& f, int pg0, int pg1) {
+      const int64_t pg = v_second ? pg1 : pg0;
+      const Elem* vp = kvb + pg * pstride + voff;
+      if constexpr (Q8) {
+        f.vs = *reinterpret_cast<const uint2*>(scb + pg * a.kv.n_kv_heads * 32 + val_scale8((lg & 1) * 8));
 #pragma unroll
         for (int dt = 0; dt < NDT / 2; ++dt) f.v[dt] = ntload(vp + dt * 512);
-        return;
       } else {
-      const bf16_t* kp = kvb + (int64_t)(k_second ? pg1 : pg0) * pstride;
 #pragma unroll
-      for (int j = 0; j < KSUB; ++j) {
-        f.k[0][j] = ntload(kp + koff0 + j * 256);
-        f.k[1][j] = ntload(kp + koff1 + j * 256);
+        for (int dt = 0; dt < NDT; ++dt) f.v[dt] = ntload(vp + dt * 16 * P);
       }
-      const bf16_t* vp = kvb + (int64_t)(v_second ? pg1 : pg0) * pstride + voff;
-#pragma unroll
-      for (int dt = 0; dt < NDT; ++dt) f.v[dt] = ntload(vp + dt * 16 * P);
-      }
+    };
+    auto load_block = [&](KVFrag<HD, Q8>& f, int kb) {
+      int pg0, pg1;
+      pages_of(kb, pg0, pg1);
+      load_k(f, pg0, pg1);
+      load_v(f, pg0, pg1);
     };
 
     // The first block is requested before the queries are staged, and each
     // next block as soon as the current one is computed -- except with three
     // row tiles, which lack the registers for a block held across those points
     // and load each block right before computing it.
-    constexpr bool kEarlyLoad = NR < 3;
+    constexpr bool kEarlyLoad = Q8 || NR < 3;
+    // Q8 with more than one row tile: the next block's codes are requested as soon as
+    // this one's are converted (compute_block does it), keys before the softmax, values
+    // behind their products, into the same registers.
+    constexpr bool kRefill = Q8 && DEPTH == 0;
     KVFrag<HD, Q8> f0;
     if (kEarlyLoad && nb > 0) load_block(f0, wk0);
 
@@ -278,37 +293,63 @@ k_attn(AttnArgs a) {
       for (int dt = 0; dt < NDT; ++dt) o_acc[dt][rt] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
 
-    // MASK: the block holds keys above some row's position or past the
-    // sequence end (only the last blocks of a request)
-    auto compute_block = [&](const KVFrag<HD, Q8>& fin, int kb, auto mask_tag) {
+    // Masks and maxima of one row tile's scores (MASK: the block holds keys above some
+    // row's position or past the sequence end, only the last blocks of a request);
+    // returns the maximum to subtract.
+    auto tile_max = [&](float* sv, int rt, int kb, auto mask_tag) {
+      constexpr bool MASK = decltype(mask_tag)::value;
+      if constexpr (MASK) {
+        if constexpr (TREE) {
+          // a tree row sees the step slot pos0 + i only when node i is on its path
+          const uint32_t tm = s_tm[rt * 16 + ln];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const int dd = rpos[rt] - (kb + lg * 8 + e);
+            if (dd < 0 || !((tm >> min(dd, 31)) & 1u)) sv[e] = -INFINITY;
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (kb + lg * 8 + e > rpos[rt]) sv[e] = -INFINITY;
+        }
+      }
+      float lm = sv[0];
+#pragma unroll
+      for (int e = 1; e < 8; ++e) lm = fmaxf(lm, sv[e]);
+      lm *= a.scale_log2;
+      // Lazy rescaling: a row's running max only moves when one of its scores
+      // exceeds it by more than 2^8 (weights stay below 256, exact in fp32).
+      // Each row decides from its own maximum (the 4 lanes of a row agree), so
+      // a row's result never depends on the other rows of its tile; the wave
+      // skips the row maxima when no lane needs them.
+      if (__any(lm > m_run[rt] + 8.f)) {
+        float mx = fmaxf(lm, __shfl_xor(lm, 16, 64));
+        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+        if (mx > m_run[rt] + 8.f) {
+          const float alpha = exp2f(m_run[rt] - mx);
+          l_run[rt] *= alpha;
+          if constexpr (Q8) l_acc[rt] *= alpha;
+#pragma unroll
+          for (int dt = 0; dt < NDT; ++dt) o_acc[dt][rt] *= alpha;
+          m_run[rt] = mx;
+        }
+      }
+      return m_run[rt] == -INFINITY ? 0.f : m_run[rt];
+    };
+
+    auto compute_bf16 = [&](const auto& fin, int kb, auto mask_tag) {
       constexpr bool MASK = decltype(mask_tag)::value;
       if constexpr (QLDS) asm volatile("" ::: "memory");  // re-read Q from LDS each block
       // phase 1: scores of every row tile (the K fragments die after this)
       float sc[NR][8];
-      [[maybe_unused]] bf16x8 kf[2][Q8 ? KSUB : 1];
-      if constexpr (Q8) {
-        const float ksc[2] = {scale_of<0>(fin.ks), scale_of<1>(fin.ks)};
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-          for (int j = 0; j < KSUB / 2; ++j) {
-            const uint4 c = fin.k[t][j];
-            kf[t][2 * j] = as_bf16x8(from_e4m3x8(c.x, c.y, ksc[t]));
-            kf[t][2 * j + 1] = as_bf16x8(from_e4m3x8(c.z, c.w, ksc[t]));
-          }
-      }
-      auto kfrag = [&](int t, int j) {
-        if constexpr (Q8) return kf[t][j];
-        else return as_bf16x8(fin.k[t][j]);
-      };
 #pragma unroll
       for (int rt = 0; rt < NR; ++rt) {
         f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < KSUB; ++j) {
           const bf16x8 q = qfrag(rt, j);
-          s0 = mfma16(kfrag(0, j), q, s0);
-          s1 = mfma16(kfrag(1, j), q, s1);
+          s0 = mfma16(as_bf16x8(fin.k[0][j]), q, s0);
+          s1 = mfma16(as_bf16x8(fin.k[1][j]), q, s1);
         }
         // lane holds S^T[key kb + lg*8 + 4t + i][row rt*16 + ln]
 #pragma unroll
@@ -318,111 +359,115 @@ k_attn(AttnArgs a) {
         }
       }
       uint4 vf[NDT];
-      [[maybe_unused]] float vsc[8];
-      if constexpr (Q8) {
-        uint2 vs = fin.vs;
-        int nvalid = 8;
-        if constexpr (MASK) nvalid = min(max(S - (kb + lg * 8), 0), 8);  // slots past the sequence end hold anything
-        auto codes = [&](uint32_t x, uint32_t y) {
-          const uint2 c = MASK ? keep_first8(make_uint2(x, y), nvalid) : make_uint2(x, y);
-          return from_e4m3x8(c.x, c.y, 1.f);
-        };
-        if constexpr (MASK) vs = keep_first8(vs, nvalid);
 #pragma unroll
-        for (int dt = 0; dt < NDT; dt += 2) {
-          const uint4 c = fin.v[dt / 2];
-          vf[dt] = codes(c.x, c.y);
-          vf[dt + 1] = codes(c.z, c.w);
-        }
-        vsc[0] = scale_of<0>(vs.x), vsc[1] = scale_of<1>(vs.x), vsc[2] = scale_of<2>(vs.x), vsc[3] = scale_of<3>(vs.x);
-        vsc[4] = scale_of<0>(vs.y), vsc[5] = scale_of<1>(vs.y), vsc[6] = scale_of<2>(vs.y), vsc[7] = scale_of<3>(vs.y);
-      } else {
+      for (int dt = 0; dt < NDT; ++dt) vf[dt] = fin.v[dt];
+      if constexpr (MASK) {
+        if (kb + 32 > S) {  // the sequence ends inside this block
+          const int nvalid = min(max(S - (kb + lg * 8), 0), 8);
 #pragma unroll
-        for (int dt = 0; dt < NDT; ++dt) vf[dt] = fin.v[dt];
-        if constexpr (MASK) {
-          if (kb + 32 > S) {  // the sequence ends inside this block
-            const int nvalid = min(max(S - (kb + lg * 8), 0), 8);
-#pragma unroll
-            for (int dt = 0; dt < NDT; ++dt) vf[dt] = keep_first(vf[dt], nvalid);
-          }
+          for (int dt = 0; dt < NDT; ++dt) vf[dt] = keep_first(vf[dt], nvalid);
         }
       }
       // phase 2: online softmax and O^T += V^T P^T per row tile
 #pragma unroll
       for (int rt = 0; rt < NR; ++rt) {
         float* sv = sc[rt];
-        if constexpr (MASK) {
-          if constexpr (TREE) {
-            // a tree row sees the step slot pos0 + i only when node i is on its path
-            const uint32_t tm = s_tm[rt * 16 + ln];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const int dd = rpos[rt] - (kb + lg * 8 + e);
-              if (dd < 0 || !((tm >> min(dd, 31)) & 1u)) sv[e] = -INFINITY;
-            }
-          } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-              if (kb + lg * 8 + e > rpos[rt]) sv[e] = -INFINITY;
-          }
-        }
-        float lm = sv[0];
-#pragma unroll
-        for (int e = 1; e < 8; ++e) lm = fmaxf(lm, sv[e]);
-        lm *= a.scale_log2;
-        // Lazy rescaling: a row's running max only moves when one of its scores
-        // exceeds it by more than 2^8 (weights stay below 256, exact in fp32).
-        // Each row decides from its own maximum (the 4 lanes of a row agree), so
-        // a row's result never depends on the other rows of its tile; the wave
-        // skips the row maxima when no lane needs them.
-        if (__any(lm > m_run[rt] + 8.f)) {
-          float mx = fmaxf(lm, __shfl_xor(lm, 16, 64));
-          mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-          if (mx > m_run[rt] + 8.f) {
-            const float alpha = exp2f(m_run[rt] - mx);
-            l_run[rt] *= alpha;
-            if constexpr (Q8) l_acc[rt] *= alpha;
-#pragma unroll
-            for (int dt = 0; dt < NDT; ++dt) o_acc[dt][rt] *= alpha;
-            m_run[rt] = mx;
-          }
-        }
-        const float m_use = m_run[rt] == -INFINITY ? 0.f : m_run[rt];
+        const float m_use = tile_max(sv, rt, kb, mask_tag);
         // P = hi + lo, both bf16: the product keeps ~16 bits of each weight.
         // v_exp_f32 directly: weights below 2^-126 of the running max flush to 0.
-        // Q8: one bf16 a weight (half a step is 2^-8 of it at most, a number of the
-        // cache is off by 2^-4 of it); the row sum is taken of the rounded weights, by
-        // the matrix core, so that what rounds alike cancels.  A scale is a power of
-        // two: the weights times scales round to the rounded weights times scales.
         float sum = 0.f;
         uint32_t hi[4], lo[4];
 #pragma unroll
         for (int e = 0; e < 8; e += 2) {
           const float p0 = __builtin_amdgcn_exp2f(fmaf(sv[e], a.scale_log2, -m_use));
           const float p1 = __builtin_amdgcn_exp2f(fmaf(sv[e + 1], a.scale_log2, -m_use));
-          if constexpr (Q8) {
-            lo[e / 2] = pack2(p0, p1);
-            hi[e / 2] = pack2(p0 * vsc[e], p1 * vsc[e + 1]);
-          } else {
-            sum += p0 + p1;
-            hi[e / 2] = pack2(p0, p1);
-            lo[e / 2] = pack2(p0 - lo_f(hi[e / 2]), p1 - hi_f(hi[e / 2]));
-          }
+          sum += p0 + p1;
+          hi[e / 2] = pack2(p0, p1);
+          lo[e / 2] = pack2(p0 - lo_f(hi[e / 2]), p1 - hi_f(hi[e / 2]));
         }
+        l_run[rt] += sum;
         const bf16x8 ph = as_bf16x8(make_uint4(hi[0], hi[1], hi[2], hi[3]));
         const bf16x8 pl = as_bf16x8(make_uint4(lo[0], lo[1], lo[2], lo[3]));
-        if constexpr (Q8) {
-          constexpr uint32_t one2 = 0x3f803f80u;
-          l_acc[rt] = mfma16(as_bf16x8(make_uint4(one2, one2, one2, one2)), pl, l_acc[rt]);
-        } else {
-          l_run[rt] += sum;
-        }
 #pragma unroll
         for (int dt = 0; dt < NDT; ++dt) {
           o_acc[dt][rt] = mfma16(as_bf16x8(vf[dt]), ph, o_acc[dt][rt]);
-          if constexpr (!Q8) o_acc[dt][rt] = mfma16(as_bf16x8(vf[dt]), pl, o_acc[dt][rt]);
+          o_acc[dt][rt] = mfma16(as_bf16x8(vf[dt]), pl, o_acc[dt][rt]);
         }
       }
+    };
+
+    // The same from codes.  nkb >= 0 (kRefill): the block to request next, into f.
+    auto compute_e4m3 = [&](auto& f, int kb, int nkb, auto mask_tag) {
+      constexpr bool MASK = decltype(mask_tag)::value;
+      if constexpr (QLDS) asm volatile("" ::: "memory");
+      int npg0 = 0, npg1 = 0;
+      if (kRefill && nkb >= 0) pages_of(nkb, npg0, npg1);
+      f32x4 s0[NR], s1[NR];
+#pragma unroll
+      for (int rt = 0; rt < NR; ++rt) s0[rt] = s1[rt] = f32x4{0.f, 0.f, 0.f, 0.f};
+      const float ks0 = scale_of<0>(f.ks), ks1 = scale_of<1>(f.ks);
+#pragma unroll
+      for (int j = 0; j < KSUB; ++j) {
+        const uint4 c0 = f.k[0][j / 2], c1 = f.k[1][j / 2];
+        const bf16x8 k0 = as_bf16x8(j & 1 ? from_e4m3x8(c0.z, c0.w, ks0) : from_e4m3x8(c0.x, c0.y, ks0));
+        const bf16x8 k1 = as_bf16x8(j & 1 ? from_e4m3x8(c1.z, c1.w, ks1) : from_e4m3x8(c1.x, c1.y, ks1));
+#pragma unroll
+        for (int rt = 0; rt < NR; ++rt) {
+          const bf16x8 q = qfrag(rt, j);
+          s0[rt] = mfma16(k0, q, s0[rt]);
+          s1[rt] = mfma16(k1, q, s1[rt]);
+        }
+      }
+      if (kRefill && nkb >= 0) load_k(f, npg0, npg1);
+      uint2 vs = f.vs;
+      int nvalid = 8;  // slots past the sequence end hold anything
+      if constexpr (MASK) {
+        nvalid = min(max(S - (kb + lg * 8), 0), 8);
+        vs = keep_first8(vs, nvalid);
+      }
+      const float vsc[8] = {scale_of<0>(vs.x), scale_of<1>(vs.x), scale_of<2>(vs.x), scale_of<3>(vs.x),
+                            scale_of<0>(vs.y), scale_of<1>(vs.y), scale_of<2>(vs.y), scale_of<3>(vs.y)};
+      // One bf16 a weight (half a step is 2^-8 of it at most, a number of the cache is off
+      // by 2^-4 of it); the row sum is taken of the rounded weights, by the matrix core, so
+      // that what rounds alike cancels.  A scale is a power of two: the weights times
+      // scales round to the rounded weights times scales.
+      bf16x8 pw[NR];
+#pragma unroll
+      for (int rt = 0; rt < NR; ++rt) {
+        float sv[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          sv[i] = s0[rt][i];
+          sv[4 + i] = s1[rt][i];
+        }
+        const float m_use = tile_max(sv, rt, kb, mask_tag);
+        uint32_t w[4], ws[4];
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) {
+          const float p0 = __builtin_amdgcn_exp2f(fmaf(sv[e], a.scale_log2, -m_use));
+          const float p1 = __builtin_amdgcn_exp2f(fmaf(sv[e + 1], a.scale_log2, -m_use));
+          w[e / 2] = pack2(p0, p1);
+          ws[e / 2] = pack2(p0 * vsc[e], p1 * vsc[e + 1]);
+        }
+        constexpr uint32_t one2 = 0x3f803f80u;
+        l_acc[rt] = mfma16(as_bf16x8(make_uint4(one2, one2, one2, one2)), as_bf16x8(make_uint4(w[0], w[1], w[2], w[3])),
+                           l_acc[rt]);
+        pw[rt] = as_bf16x8(make_uint4(ws[0], ws[1], ws[2], ws[3]));
+      }
+#pragma unroll
+      for (int dt = 0; dt < NDT; ++dt) {
+        const uint4 c = f.v[dt / 2];
+        uint2 cv = dt & 1 ? make_uint2(c.z, c.w) : make_uint2(c.x, c.y);
+        if constexpr (MASK) cv = keep_first8(cv, nvalid);
+        const bf16x8 v = as_bf16x8(from_e4m3x8(cv.x, cv.y, 1.f));
+#pragma unroll
+        for (int rt = 0; rt < NR; ++rt) o_acc[dt][rt] = mfma16(v, pw[rt], o_acc[dt][rt]);
+      }
+      if (kRefill && nkb >= 0) load_v(f, npg0, npg1);
+    };
+    auto compute_block = [&](KVFrag<HD, Q8>& f, int kb, auto mask_tag, [[maybe_unused]] int nkb) {
+      if constexpr (Q8) compute_e4m3(f, kb, nkb, mask_tag);
+      else compute_bf16(f, kb, mask_tag);
     };
     using NoMask = std::integral_constant<bool, false>;
     using Mask = std::integral_constant<bool, true>;
@@ -431,35 +476,38 @@ k_attn(AttnArgs a) {
     // masked tail (at most the last two blocks of a request) run in separate
     // loops, so that each loop body holds one instantiation of the block code.
     int i = 0;
-    if constexpr (kEarlyLoad) {
+    if constexpr (kRefill) {
+      for (; i < nfull; ++i) compute_block(f0, wk0 + 32 * i, NoMask{}, i + 1 < nb ? wk0 + 32 * (i + 1) : -1);
+      for (; i < nb; ++i) compute_block(f0, wk0 + 32 * i, Mask{}, i + 1 < nb ? wk0 + 32 * (i + 1) : -1);
+    } else if constexpr (kEarlyLoad) {
       // at the top of every iteration f0 holds block i
       if constexpr (DEPTH == 1) {
         // one more block in flight while a block is computed
         KVFrag<HD, Q8> f1;
         for (; i + 1 < nfull; i += 2) {
           load_block(f1, wk0 + 32 * (i + 1));
-          compute_block(f0, wk0 + 32 * i, NoMask{});
+          compute_block(f0, wk0 + 32 * i, NoMask{}, -1);
           if (i + 2 < nb) load_block(f0, wk0 + 32 * (i + 2));
-          compute_block(f1, wk0 + 32 * (i + 1), NoMask{});
+          compute_block(f1, wk0 + 32 * (i + 1), NoMask{}, -1);
         }
       }
       for (; i < nfull; ++i) {
-        compute_block(f0, wk0 + 32 * i, NoMask{});
+        compute_block(f0, wk0 + 32 * i, NoMask{}, -1);
         if (i + 1 < nb) load_block(f0, wk0 + 32 * (i + 1));
       }
       for (; i < nb; ++i) {
-        compute_block(f0, wk0 + 32 * i, Mask{});
+        compute_block(f0, wk0 + 32 * i, Mask{}, -1);
         if (i + 1 < nb) load_block(f0, wk0 + 32 * (i + 1));
       }
     } else {
       static_assert(DEPTH == 0, "a block in flight needs the early first load");
       for (; i < nfull; ++i) {
         load_block(f0, wk0 + 32 * i);
-        compute_block(f0, wk0 + 32 * i, NoMask{});
+        compute_block(f0, wk0 + 32 * i, NoMask{}, -1);
       }
       for (; i < nb; ++i) {
         load_block(f0, wk0 + 32 * i);
-        compute_block(f0, wk0 + 32 * i, Mask{});
+        compute_block(f0, wk0 + 32 * i, Mask{}, -1);
       }
     }
 
