@@ -27,6 +27,29 @@ constexpr int kNone = 0x7fffffff;
 
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 
+// A request's penalties.  z / r is the quotient from the reciprocal with one residual step
+// (Markstein 1990: correctly rounded where nothing over- or underflows, which the ranges
+// here exclude), a third of a division's instructions.
+struct Penalty {
+  float r, rinv, f, p;
+  bool plain;  // r in [2^-40, 2^40]
+  __device__ void set(const ConstrainArgs& a, int seq) {
+    r = a.repetition ? a.repetition[seq] : 1.f;
+    f = a.frequency ? a.frequency[seq] : 0.f;
+    p = a.presence ? a.presence[seq] : 0.f;
+    rinv = 1.f / r;
+    plain = r >= 0x1p-40f && r <= 0x1p40f;
+  }
+  // c: twice the occurrences, plus one for the prompt; not 0
+  __device__ float operator()(float v, int c) const {
+    const float q = v * rinv;
+    float d = fmaf(fmaf(-q, r, v), rinv, q);
+    if (!(plain && v >= 0x1p-60f && v <= 0x1p60f)) d = v > 0.f ? v / r : v * r;
+    d -= f * (float)(c >> 1);
+    return c > 1 ? d - p : d;
+  }
+};
+
 template <bool VEC>
 WAR_DEV f32x4_t load4(const float* z, int col, int V) {
   if constexpr (VEC) return col < V ? *reinterpret_cast<const f32x4_t*>(z + col) : f32x4_t{0.f, 0.f, 0.f, 0.f};
@@ -90,8 +113,8 @@ __global__ void __launch_bounds__(kThreads) k_constrain(ConstrainArgs a) {
       }
     }
   }
-  const float r = a.repetition ? a.repetition[seq] : 1.f;
-  const float f = a.frequency ? a.frequency[seq] : 0.f, p = a.presence ? a.presence[seq] : 0.f;
+  Penalty pen;
+  pen.set(a, seq);
   // the rows' tokens (row j's own and its ancestors' are its text) and masks
   if (tid < n) {
     s_tok[tid] = tid == 0 ? a.last_tokens[b] : a.draft_tokens[(int64_t)b * a.k_max + tid - 1];
@@ -173,28 +196,21 @@ __global__ void __launch_bounds__(kThreads) k_constrain(ConstrainArgs a) {
           if (d == e) c[e] += 2;
       }
       f32x4_t x = z[u];
-      const uint32_t allow = word[u] >> (col[u] & 31);
+      uint32_t allow = word[u] >> (col[u] & 31);
+      if constexpr (VEC)
+        allow = col[u] < a.V ? allow : 0u;
+      else
+        allow &= col[u] + 4 <= a.V ? 15u : col[u] < a.V ? (1u << (a.V - col[u])) - 1u : 0u;
       float best = -INFINITY;
-      int at = kNone;
-      bool nan = false;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         float v = x[e];
         if (biased) v += bias[u][e];
-        if (c[e]) {
-          v = v > 0.f ? v / r : v * r;
-          const int k = c[e] >> 1;
-          v -= f * (float)k;
-          if (k) v -= p;
-        }
-        const bool ok = ((allow >> e) & 1u) && col[u] + e < a.V;
-        if (!ok) v = -INFINITY;
-        x[e] = v;
-        nan = nan || v != v;
-        if (ok && v == v && (at == kNone || v > best)) {
-          best = v;
-          at = col[u] + e;
-        }
+        if (c[e]) v = pen(v, c[e]);
+        // excluded: -inf, by a mask of the id's bit
+        const uint32_t keep = (uint32_t)((int)(allow << (31 - e)) >> 31);
+        x[e] = __uint_as_float((__float_as_uint(v) & keep) | (0xff800000u & ~keep));
+        best = fmaxf(best, x[e]);  // (drops NaN)
       }
       if (a.out) {
         float* o = a.out + row * a.out_stride;
@@ -208,17 +224,22 @@ __global__ void __launch_bounds__(kThreads) k_constrain(ConstrainArgs a) {
       }
       if (a.best_v) {
         // 128 ids are the 32 lanes of half a wave, ascending: the lowest lane that holds
-        // the maximum has its lowest id
+        // the maximum has its lowest id; a maximum of -inf counts where an id is allowed
         float mx = best;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) mx = fmaxf(mx, __shfl_xor(mx, o, 64));
+        int at = kNone;
+#pragma unroll
+        for (int e = 3; e >= 0; --e)
+          if (x[e] == mx && (mx > -INFINITY || ((allow >> e) & 1u))) at = col[u] + e;
         const unsigned long long half = lane < 32 ? 0xffffffffull : 0xffffffffull << 32;
-        const unsigned long long eq = __ballot(at != kNone && best == mx) & half;
-        const unsigned long long nans = __ballot(nan) & half;
+        const unsigned long long eq = __ballot(at != kNone) & half;
+        bool nan = false;
+        if (a.nan_max) nan = (__ballot(x[0] != x[0] || x[1] != x[1] || x[2] != x[2] || x[3] != x[3]) & half) != 0;
         const int q = (c0 + u * kThreads * 4 + (tid & ~31) * 4) / 128;
         if (q < nblk && (eq ? __ffsll((long long)eq) - 1 == lane : (lane & 31) == 0)) {
-          a.best_v[row * nblk + q] = a.nan_max && nans ? __builtin_nanf("") : mx;
-          a.best_i[row * nblk + q] = eq ? at : kNone;
+          a.best_v[row * nblk + q] = nan ? __builtin_nanf("") : mx;
+          a.best_i[row * nblk + q] = at;
         }
       }
       z[u] = next[u];
@@ -283,9 +304,13 @@ __global__ void __launch_bounds__(256) k_counts_begin(uint16_t* counts, int V, i
   for (int i = threadIdx.x; i < kSlice / 32; i += 256) s_bits[i] = 0;
   __syncthreads();
   const int t1 = offsets[b + 1];
-  for (int i = offsets[b] + threadIdx.x; i < t1; i += 256) {
-    const int t = tokens[i];
-    if (t >= c0 && t < c1) atomicOr(&s_bits[(t - c0) >> 5], 1u << ((t - c0) & 31));
+  for (int i0 = offsets[b] + threadIdx.x; i0 < t1; i0 += 256 * 16) {
+    int t[16];
+#pragma unroll
+    for (int u = 0; u < 16; ++u) t[u] = i0 + 256 * u < t1 ? tokens[i0 + 256 * u] : -1;
+#pragma unroll
+    for (int u = 0; u < 16; ++u)
+      if (t[u] >= c0 && t[u] < c1) atomicOr(&s_bits[(t[u] - c0) >> 5], 1u << ((t[u] - c0) & 31));
   }
   __syncthreads();
   uint16_t* row = counts + (int64_t)seq * V;

@@ -86,7 +86,10 @@ struct Profiler {
     return pool[used++];
   }
 };
-constexpr int kPrefillChunk = 4096;  // keys per attention item when prefilling (chunk-major: L2 serves the row blocks)
+// keys per attention item when prefilling (chunk-major: L2 serves the row blocks); twice
+// as many in half the bytes
+constexpr int kPrefillChunk = 4096;
+inline int prefill_chunk(const KvGeom& g) { return g.q8 ? 2 * kPrefillChunk : kPrefillChunk; }
 constexpr int kPrefillRows = 128;    // attention rows per prefill row block (k_attn_rows)
 constexpr size_t kStageInts = 16384;  // least size of a prefill chunk's metadata block (64 KiB)
 constexpr int kMaxItemsPerSeq = 512;  // attention chunks one combine merges
@@ -1306,9 +1309,9 @@ AttendShape attend_shape(const war_kv_pool* p, int B, int n) {
     s.TB = kPrefillRows / G;
     s.blocks = cdiv_i(n, s.TB);
     s.n_segs = B * s.blocks;
-    // chunks of kPrefillChunk keys, longer ones where there are units enough for 16
+    // chunks of prefill_chunk keys, longer ones where there are units enough for 16
     // rounds of the grid (each item has 128 rows of partial sums to write and merge)
-    s.chunk = kPrefillChunk;
+    s.chunk = prefill_chunk(p->geom);
     while (cdiv_i(len, s.chunk) > kMaxItemsPerSeq) s.chunk *= 2;
     const int64_t rounds = 16 * kAttnGrid / nkv, most = (int64_t)s.n_segs * cdiv_i(len, s.chunk);
     while (s.chunk < len && (int64_t)s.n_segs * cdiv_i(len, s.chunk) > rounds) s.chunk *= 2;
@@ -1645,7 +1648,7 @@ war_status war_prefill_append(war_model* m, war_kv_pool* p, int32_t n, const int
   const int RB = kPrefillRows;
   CHECK(RB % G == 0, "internal: query heads per kv head must divide the prefill row block");
   const int TB = RB / G;
-  int chunk = kPrefillChunk;
+  int chunk = prefill_chunk(p->geom);
   while (cdiv_i(p->dev.max_pages * P, chunk) > kMaxItemsPerSeq) chunk *= 2;
   std::vector<int64_t> cu(n + 1, 0);
   for (int i = 0; i < n; ++i) cu[i + 1] = cu[i] + n_new_host[i];

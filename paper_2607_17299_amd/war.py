@@ -354,7 +354,7 @@ def _addr(t: Optional[torch.Tensor]):
 def _checked(device, dtype, **arrays) -> None:
     """Arrays of a type without gaps on the device (None: absent)."""
     for name, t in arrays.items():
-        if t is not None and not (t.dtype == dtype and t.device == device and t.is_contiguous()):
+        if t is not None and not (t.dtype is dtype and t.device == device and t.is_contiguous()):
             raise ValueError(f"{name} must be a contiguous {dtype} tensor on {device}")
 
 
@@ -362,17 +362,21 @@ def _call(fn, device, stream, *args) -> None:
     """fn(*args, stream) with `device` current; its current stream by default (read raw:
     a Stream object is made in 2 us, a third of a small call)."""
     raw = torch._C._cuda_getCurrentRawStream(device.index) if stream is None else stream.cuda_stream
-    if torch.cuda.current_device() == device.index:
-        _check(fn(*args, raw))
+    if torch._C._cuda_getDevice() == device.index:
+        status = fn(*args, raw)
     else:
         with torch.cuda.device(device):
-            _check(fn(*args, raw))
+            status = fn(*args, raw)
+    if status:
+        _check(status)
 
 
 def _rows_of(name: str, t: torch.Tensor, device, B: int, n: int, heads: int, dim: int) -> int:
     """The row stride of bf16 [B, n, heads, dim] whose rows b * n + i lie at one stride."""
-    if not (t.dtype == torch.bfloat16 and t.device == device and t.shape == (B, n, heads, dim)):
+    if not (t.dtype is torch.bfloat16 and t.device == device and t.shape == (B, n, heads, dim)):
         raise ValueError(f"{name} must be bf16 [{B}, {n}, {heads}, {dim}] on {device}")
+    if t.is_contiguous():
+        return heads * dim
     sb, sn, sh, sd = t.stride()
     row = sn if n > 1 else sb if B > 1 else heads * dim
     if not (sd == 1 and (heads == 1 or sh == dim) and (n < 2 or B < 2 or sb == n * row)):
