@@ -192,14 +192,14 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
         c.vs = *reinterpret_cast<const uint2*>(scb + (int64_t)pv_ * sstride + vscale);
       }
     };
-    // a quarter of it: keys (0, 1), values (2, 3), eight codes each
+    // a part of it: eight codes of the keys (0, 1), all of the values (2)
     auto convert = [&](const Codes& c, int stage, int part) __attribute__((always_inline)) {
       if (part < 2 && kmine) {
         unsigned char* d = smem + stage * SB + kdst + part * 256;
         *reinterpret_cast<uint4*>(d) = part ? from_e4m3x8(c.k.z, c.k.w, scale_of<0>(c.ks))
                                             : from_e4m3x8(c.k.x, c.k.y, scale_of<0>(c.ks));
       }
-      if (part >= 2 && vmine) {
+      if (part == 2 && vmine) {
         const float f[8] = {scale_of<0>(c.vs.x), scale_of<1>(c.vs.x), scale_of<2>(c.vs.x), scale_of<3>(c.vs.x),
                             scale_of<0>(c.vs.y), scale_of<1>(c.vs.y), scale_of<2>(c.vs.y), scale_of<3>(c.vs.y)};
         auto eight = [&](uint32_t w0, uint32_t w1) __attribute__((always_inline)) {
@@ -208,13 +208,14 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
           return make_uint4(pack2(a0[0] * f[0], a0[1] * f[1]), pack2(a1[0] * f[2], a1[1] * f[3]),
                             pack2(a2[0] * f[4], a2[1] * f[5]), pack2(a3[0] * f[6], a3[1] * f[7]));
         };
-        unsigned char* d = smem + (ST + stage) * SB + vdst + (part - 2) * 256;
-        *reinterpret_cast<uint4*>(d) = part == 2 ? eight(c.v.x, c.v.y) : eight(c.v.z, c.v.w);
+        unsigned char* d = smem + (ST + stage) * SB + vdst;
+        *reinterpret_cast<uint4*>(d) = eight(c.v.x, c.v.y);
+        *reinterpret_cast<uint4*>(d + 256) = eight(c.v.z, c.v.w);
       }
     };
     auto convert_all = [&](const Codes& c, int stage) __attribute__((always_inline)) {
 #pragma unroll
-      for (int part = 0; part < 4; ++part) convert(c, stage, part);
+      for (int part = 0; part < 3; ++part) convert(c, stage, part);
     };
 
     // queries (B operand of S^T) and position of this lane's row
@@ -278,7 +279,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
       // (hi, lo) of value fragment f, whose operands are read LOOK triples
       // ahead; the softmax of block i is dealt over the slots.
       // Lane holds S^T[key kb + 16 (e / 8) + 8 g + e % 8][row].
-      constexpr int LOOK = 2, RING = 3;
+      constexpr int LOOK = Q8 ? 1 : 2, RING = LOOK + 1;  // (Q8 has not the registers for two)
       bf16x8 rk[RING], rv[RING];
       auto read = [&](int f) __attribute__((always_inline)) {
         rk[f % RING] = kfrag((i + 1) & 3, f);
@@ -289,7 +290,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
       float lm = 0.f, m_new = 0.f, m_use = 0.f, sum = 0.f, p0 = 0.f, p1 = 0.f;
       uint32_t hi[8], lo[8];
       // Q8: one product of a bf16 a weight (see k_attn), two of ones for the row sums, and
-      // a quarter of the conversion (block i + 2 to LDS) in each of four slots
+      // a part of the conversion (block i + 2 to LDS) in each of three slots
       constexpr int PV = Q8 ? 1 : 2;                                      // products of a value fragment
       constexpr int SLOTS = (1 + PV) * KF + (Q8 ? 2 : 0), HEAD = 3 * KF / 8;  // the row maximum takes the first HEAD slots
       auto softmax = [&](int t) __attribute__((always_inline)) {  // task t of 16: half of the work of a pair of keys
@@ -321,8 +322,8 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
           o_acc[f % NDT] = mfma32(rv[f % RING], as_bf16x8(z % (1 + PV) == 1 ? pin.hi[f / NDT] : pin.lo[f / NDT]), o_acc[f % NDT]);
         }
         if constexpr (Q8) {
-          constexpr int Q = SLOTS / 4;
-          if (z % Q == Q - 1 && z / Q < 4) convert(cd, (i + 2) & 3, z / Q);
+          constexpr int Q = SLOTS / 3;
+          if (z % Q == Q - 1 && z / Q < 3) convert(cd, (i + 2) & 3, z / Q);
         }
         if (z == 0) {
           lm = fmaxf(s[0], s[1]);

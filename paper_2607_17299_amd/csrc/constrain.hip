@@ -22,7 +22,8 @@
 namespace {
 
 constexpr int kThreads = 256, kUnits = 2, kIds = kThreads * 4 * kUnits;  // ids a workgroup
-constexpr int kNodes = 64;   // rows of a request
+constexpr int kNodes = 64;      // rows of a request
+constexpr int kMaxBias = 1024;  // its bias entries
 constexpr int kNone = 0x7fffffff;
 
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
@@ -63,7 +64,8 @@ template <bool VEC>
 __global__ void __launch_bounds__(kThreads) k_constrain(ConstrainArgs a) {
   __shared__ int s_tok[kNodes], s_mask[kNodes];
   __shared__ unsigned long long s_path[kNodes];
-  __shared__ float s_bias[kIds];
+  __shared__ int s_hits, s_entry[kMaxBias], s_at[kMaxBias];
+  __shared__ float s_sum[kMaxBias];
   const int b = blockIdx.y, tid = threadIdx.x, lane = tid & 63;
   const int c0 = blockIdx.x * kIds, c1 = min(a.V, c0 + kIds);
   const int kp1 = a.k_max + 1;
@@ -83,6 +85,8 @@ __global__ void __launch_bounds__(kThreads) k_constrain(ConstrainArgs a) {
         }
     return;
   }
+  if (tid == 0) s_hits = 0;
+  __syncthreads();
   // everything that hangs on nothing else is requested first: the first row's logits, the
   // counts, the penalties
   int col[kUnits], cnt[kUnits][4];
@@ -91,6 +95,7 @@ __global__ void __launch_bounds__(kThreads) k_constrain(ConstrainArgs a) {
 #pragma unroll
   for (int u = 0; u < kUnits; ++u) {
     col[u] = c0 + (u * kThreads + tid) * 4;
+    bias[u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     z[u] = load4<VEC>(a.logits + (row0 + i) * a.stride, col[u], a.V);
   }
 #pragma unroll
@@ -134,27 +139,47 @@ __global__ void __launch_bounds__(kThreads) k_constrain(ConstrainArgs a) {
       }
     s_path[tid] = path;
   }
-  // biases of this chunk: the first entry of an id adds up all of them, in list order
-  bool hit = false;
+  // the bias entries of this chunk, in any order (few of them: the same id twice is looked
+  // for among them alone)
   const int32_t* bid = a.bias_ids + (int64_t)seq * a.n_bias;
   const float* bval = a.bias_values + (int64_t)seq * a.n_bias;
-  for (int e = tid; e < a.n_bias; e += kThreads) hit = hit || (bid[e] >= c0 && bid[e] < c1);
-  const bool biased = __syncthreads_or(hit);
-  if (biased) {
-    for (int j = tid; j < kIds; j += kThreads) s_bias[j] = 0.f;
-    __syncthreads();
-    for (int e = tid; e < a.n_bias; e += kThreads) {
-      const int id = bid[e];
-      if (id < c0 || id >= c1) continue;
-      bool first = true;
-      for (int q = 0; q < e; ++q) first = first && bid[q] != id;
-      if (!first) continue;
-      float sum = bval[e];
-      for (int q = e + 1; q < a.n_bias; ++q)
-        if (bid[q] == id) sum += bval[q];
-      s_bias[id - c0] = sum;
+  for (int e = tid; e < a.n_bias; e += kThreads) {
+    const int id = bid[e];
+    if (id >= c0 && id < c1) {
+      const int at = atomicAdd(&s_hits, 1);
+      s_entry[at] = e;
+      s_at[at] = id - c0;
+    }
+  }
+  __syncthreads();
+  const int hits = s_hits;
+  if (hits) {
+    // an id's first entry adds up all of them, in list order
+    for (int h = tid; h < hits; h += kThreads) {
+      const int e = s_entry[h], id = s_at[h];
+      bool first = true, more = false;
+      for (int q = 0; q < hits; ++q)
+        if (s_at[q] == id) {
+          first = first && s_entry[q] >= e;
+          more = more || s_entry[q] > e;
+        }
+      float sum = first ? bval[e] : 0.f;
+      if (first && more)
+        for (int q = e + 1; q < a.n_bias; ++q)
+          if (bid[q] == c0 + id) sum += bval[q];
+      s_sum[h] = sum;
     }
     __syncthreads();
+    for (int h = 0; h < hits; ++h) {
+      const int d = s_at[h];
+      if (((d >> 2) & (kThreads - 1)) == tid) {
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (d == (u * kThreads + tid) * 4 + e) bias[u][e] += s_sum[h];
+      }
+    }
   }
   // the rows' tokens that lie in this chunk (n <= 64: lane j looks at token j)
   const unsigned long long here = __ballot(lane < n && s_tok[min(lane, n - 1)] >= c0 && s_tok[min(lane, n - 1)] < c1);
@@ -171,7 +196,6 @@ __global__ void __launch_bounds__(kThreads) k_constrain(ConstrainArgs a) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       cnt[u][e] = (cnt[u][e] & 0x7fff) * 2 + (cnt[u][e] >> 15);  // prompt bit last
-      bias[u][e] = biased ? s_bias[col[u] - c0 + e] : 0.f;
     }
 
   for (; i < n; i += step) {
@@ -205,7 +229,7 @@ __global__ void __launch_bounds__(kThreads) k_constrain(ConstrainArgs a) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         float v = x[e];
-        if (biased) v += bias[u][e];
+        v += bias[u][e];
         if (c[e]) v = pen(v, c[e]);
         // excluded: -inf, by a mask of the id's bit
         const uint32_t keep = (uint32_t)((int)(allow << (31 - e)) >> 31);

@@ -1227,7 +1227,8 @@ war_status verify_impl(war_model* m, war_kv_pool* p, int32_t B, const int32_t* s
   // constrained in place; the best of each block of ids takes the LM head's place
   auto constrain = [&](int32_t* greedy) {
     ConstrainArgs ca = constrain_args(*cons, m->md.V, B, seq_ids, last_tokens, draft_tokens, va.draft_parents, k_max);
-    ca.logits = ca.out = lg;
+    ca.logits = lg;
+    ca.out = logits || greedy ? lg : nullptr;  // (greedy steps take the blocks' best alone)
     ca.stride = ca.out_stride = m->md.V;
     ca.ntok = meta.req_ntok;
     ca.best_v = w.amax_v;
