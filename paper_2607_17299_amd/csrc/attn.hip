@@ -103,7 +103,8 @@ k_attn(AttnArgs a) {
   if (tid == 0) s_it = blockIdx.x;
   __syncthreads();
   for (;;) {
-    const int it = s_it;
+    int it = s_it;
+    if constexpr (Q8) it = __builtin_amdgcn_readfirstlane(it);  // (scalar: so are the unit's addresses)
     if (it >= total) break;
     const int kvh = it % a.n_kv_heads;
     const int4 u0 = a.meta.udesc[2 * (it / a.n_kv_heads)], u1 = a.meta.udesc[2 * (it / a.n_kv_heads) + 1];
@@ -152,6 +153,7 @@ k_attn(AttnArgs a) {
     const Elem* kvb;
     if constexpr (Q8) kvb = a.kv.q8 + a.kv.page_elems(a.layer, 0, kvh, 0);
     else kvb = a.kv.kv + a.kv.page_elems(a.layer, 0, kvh, 0);
+    [[maybe_unused]] const int64_t sstride = (int64_t)a.kv.n_kv_heads * 32;
     const uint8_t* scb = nullptr;  // this kv-head's scales of page 0
     if constexpr (Q8) scb = a.kv.scale + a.kv.scale_bytes(a.layer, 0, kvh);
 
@@ -165,15 +167,39 @@ k_attn(AttnArgs a) {
     auto ntload = [](const Elem* p) {
       return __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(p)));
     };
-    auto pages_of = [&](int kb, int& pg0, int& pg1) {
-      pg0 = trow[kb / P];
-      pg1 = (kb + 16 < S) ? trow[kb / P + 1] : pg0;
+    // Q8: page ids of 64 pages at a time, one a lane, the next 64 on their way, so that a
+    // block's ids are there when its codes are requested: loaded one by one they wait
+    // behind the codes in flight (8 requests x 9 rows at 32k keys 110 us, @@ so).
+    const int32_t* wrow = trow + wk0 / P;
+    const int plast = (S - 1) / P - wk0 / P;
+    auto page_vec = [&](int n) { return wrow[min(n * 64 + lane, plast)]; };
+    [[maybe_unused]] int pv = 0, pn = 0, pgrp = 0;
+    if constexpr (Q8) {
+      if (nb > 0) {
+        pv = page_vec(0);
+        pn = page_vec(1);
+      }
+    }
+    auto pages_of = [&](int kb, int& pg0, int& pg1) {  // (kb: a block of the wave, no earlier than the last)
+      if constexpr (Q8) {
+        const int i = (kb - wk0) / P;
+        if ((i >> 6) != pgrp) {
+          pgrp = i >> 6;
+          pv = pn;
+          pn = page_vec(pgrp + 1);
+        }
+        pg0 = __builtin_amdgcn_readlane(pv, i & 63);
+        pg1 = __builtin_amdgcn_readlane(pv, (i + 1) & 63);
+      } else {
+        pg0 = trow[kb / P];
+        pg1 = (kb + 16 < S) ? trow[kb / P + 1] : pg0;
+      }
     };
     auto load_k = [&](KVFrag<HD, Q8>& f, int pg0, int pg1) {
-      const int64_t pg = k_second ? pg1 : pg0;
-      const Elem* kp = kvb + pg * pstride;
+      const Elem *kp0 = kvb + pg0 * pstride, *kp1 = kvb + pg1 * pstride, *kp = k_second ? kp1 : kp0;
       if constexpr (Q8) {
-        f.ks = *reinterpret_cast<const uint16_t*>(scb + pg * a.kv.n_kv_heads * 32 + key_scale8(kk0 & 15));
+        const uint8_t *sp0 = scb + pg0 * sstride, *sp1 = scb + pg1 * sstride;
+        f.ks = *reinterpret_cast<const uint16_t*>((k_second ? sp1 : sp0) + key_scale8(kk0 & 15));
 #pragma unroll
         for (int j = 0; j < KSUB / 2; ++j) {
           f.k[0][j] = ntload(kp + koff0 + j * 512);
@@ -188,10 +214,10 @@ k_attn(AttnArgs a) {
       }
     };
     auto load_v = [&](KVFrag<HD, Q8>& f, int pg0, int pg1) {
-      const int64_t pg = v_second ? pg1 : pg0;
-      const Elem* vp = kvb + pg * pstride + voff;
+      const Elem *vp0 = kvb + pg0 * pstride, *vp1 = kvb + pg1 * pstride, *vp = (v_second ? vp1 : vp0) + voff;
       if constexpr (Q8) {
-        f.vs = *reinterpret_cast<const uint2*>(scb + pg * a.kv.n_kv_heads * 32 + val_scale8((lg & 1) * 8));
+        const uint8_t *sp0 = scb + pg0 * sstride, *sp1 = scb + pg1 * sstride;
+        f.vs = *reinterpret_cast<const uint2*>((v_second ? sp1 : sp0) + val_scale8((lg & 1) * 8));
 #pragma unroll
         for (int dt = 0; dt < NDT / 2; ++dt) f.v[dt] = ntload(vp + dt * 512);
       } else {
