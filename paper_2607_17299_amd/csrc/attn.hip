@@ -167,26 +167,26 @@ k_attn(AttnArgs a) {
     auto ntload = [](const Elem* p) {
       return __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(p)));
     };
-    // Q8: page ids of 64 pages at a time, one a lane, the next 64 on their way, so that a
-    // block's ids are there when its codes are requested: loaded one by one they wait
-    // behind the codes in flight (8 requests x 9 rows at 32k keys 110 us, @@ so).
+    // Q8: page ids of 64 pages at a time, one a lane, so that a block's ids are there when
+    // its codes are requested (loaded one by one they wait behind the codes in flight).
+    // The wait for them stays with their load, once in 32 blocks: where the compiler
+    // places it, every block waits for all codes in flight.
     const int32_t* wrow = trow + wk0 / P;
     const int plast = (S - 1) / P - wk0 / P;
-    auto page_vec = [&](int n) { return wrow[min(n * 64 + lane, plast)]; };
-    [[maybe_unused]] int pv = 0, pn = 0, pgrp = 0;
+    [[maybe_unused]] int pv = 0, pgrp = 0;
+    auto page_vec = [&](int n) {
+      pv = wrow[min(n * 64 + lane, plast)];
+      asm volatile("" : "+v"(pv));
+    };
     if constexpr (Q8) {
-      if (nb > 0) {
-        pv = page_vec(0);
-        pn = page_vec(1);
-      }
+      if (nb > 0) page_vec(0);
     }
     auto pages_of = [&](int kb, int& pg0, int& pg1) {  // (kb: a block of the wave, no earlier than the last)
       if constexpr (Q8) {
-        const int i = (kb - wk0) / P;
+        const int i = (kb - wk0) >> 4;
         if ((i >> 6) != pgrp) {
           pgrp = i >> 6;
-          pv = pn;
-          pn = page_vec(pgrp + 1);
+          page_vec(pgrp);
         }
         pg0 = __builtin_amdgcn_readlane(pv, i & 63);
         pg1 = __builtin_amdgcn_readlane(pv, (i + 1) & 63);
@@ -237,11 +237,8 @@ k_attn(AttnArgs a) {
     // row tiles, which lack the registers for a block held across those points
     // and load each block right before computing it.
     constexpr bool kEarlyLoad = Q8 || NR < 3;
-    // Q8 with more than one row tile: the next block's codes are requested as soon as
-    // this one's are converted (compute_block does it), keys before the softmax, values
-    // behind their products, into the same registers.
-    constexpr bool kRefill = Q8 && DEPTH == 0;
     KVFrag<HD, Q8> f0;
+    [[maybe_unused]] KVFrag<HD, Q8> f1;  // one more block in flight while a block is computed
     if (kEarlyLoad && nb > 0) load_block(f0, wk0);
 
     // row r -> (query row, query head) and its partial row; false if r is not live
@@ -422,29 +419,48 @@ k_attn(AttnArgs a) {
       }
     };
 
-    // The same from codes.  nkb >= 0 (kRefill): the block to request next, into f.
-    auto compute_e4m3 = [&](auto& f, int kb, int nkb, auto mask_tag) {
+    // The same from codes.  REFILL: block nkb is requested into f's registers as soon as
+    // its codes are converted, keys before the softmax, values behind their products.
+    // (Without a branch: behind one, a wait for older loads waits for these too.)
+    auto compute_e4m3 = [&](auto& f, int kb, auto mask_tag, auto refill_tag, int nkb) {
+      constexpr bool REFILL = decltype(refill_tag)::value;
       constexpr bool MASK = decltype(mask_tag)::value;
       if constexpr (QLDS) asm volatile("" ::: "memory");
       int npg0 = 0, npg1 = 0;
-      if (kRefill && nkb >= 0) pages_of(nkb, npg0, npg1);
+      if constexpr (REFILL) pages_of(nkb, npg0, npg1);
       f32x4 s0[NR], s1[NR];
 #pragma unroll
       for (int rt = 0; rt < NR; ++rt) s0[rt] = s1[rt] = f32x4{0.f, 0.f, 0.f, 0.f};
+      // HS k-steps a time (one of three row tiles: registers); their queries (from LDS) are
+      // read as many ahead, the first before the wait for the codes
+      constexpr int HS = NR == 3 ? 1 : 2;
+      bf16x8 q[2][NR][HS];
+      auto read_q = [&](int h) {
+#pragma unroll
+        for (int rt = 0; rt < NR; ++rt)
+#pragma unroll
+          for (int j = 0; j < HS; ++j) q[h & 1][rt][j] = qfrag(rt, HS * h + j);
+        if constexpr (QLDS) __builtin_amdgcn_sched_barrier(0);
+      };
+      read_q(0);
       const float ks0 = scale_of<0>(f.ks), ks1 = scale_of<1>(f.ks);
 #pragma unroll
-      for (int j = 0; j < KSUB; ++j) {
-        const uint4 c0 = f.k[0][j / 2], c1 = f.k[1][j / 2];
-        const bf16x8 k0 = as_bf16x8(j & 1 ? from_e4m3x8(c0.z, c0.w, ks0) : from_e4m3x8(c0.x, c0.y, ks0));
-        const bf16x8 k1 = as_bf16x8(j & 1 ? from_e4m3x8(c1.z, c1.w, ks1) : from_e4m3x8(c1.x, c1.y, ks1));
+      for (int h = 0; h < KSUB / HS; ++h) {
+        if (h + 1 < KSUB / HS) read_q(h + 1);
 #pragma unroll
-        for (int rt = 0; rt < NR; ++rt) {
-          const bf16x8 q = qfrag(rt, j);
-          s0[rt] = mfma16(k0, q, s0[rt]);
-          s1[rt] = mfma16(k1, q, s1[rt]);
+        for (int j = 0; j < HS; ++j) {
+          const int js = HS * h + j;
+          const uint4 c0 = f.k[0][js / 2], c1 = f.k[1][js / 2];
+          const bf16x8 k0 = as_bf16x8(js & 1 ? from_e4m3x8(c0.z, c0.w, ks0) : from_e4m3x8(c0.x, c0.y, ks0));
+          const bf16x8 k1 = as_bf16x8(js & 1 ? from_e4m3x8(c1.z, c1.w, ks1) : from_e4m3x8(c1.x, c1.y, ks1));
+#pragma unroll
+          for (int rt = 0; rt < NR; ++rt) {
+            s0[rt] = mfma16(k0, q[h & 1][rt][j], s0[rt]);
+            s1[rt] = mfma16(k1, q[h & 1][rt][j], s1[rt]);
+          }
         }
       }
-      if (kRefill && nkb >= 0) load_k(f, npg0, npg1);
+      if constexpr (REFILL) load_k(f, npg0, npg1);
       uint2 vs = f.vs;
       int nvalid = 8;  // slots past the sequence end hold anything
       if constexpr (MASK) {
@@ -489,11 +505,7 @@ k_attn(AttnArgs a) {
 #pragma unroll
         for (int rt = 0; rt < NR; ++rt) o_acc[dt][rt] = mfma16(v, pw[rt], o_acc[dt][rt]);
       }
-      if (kRefill && nkb >= 0) load_v(f, npg0, npg1);
-    };
-    auto compute_block = [&](KVFrag<HD, Q8>& f, int kb, auto mask_tag, [[maybe_unused]] int nkb) {
-      if constexpr (Q8) compute_e4m3(f, kb, nkb, mask_tag);
-      else compute_bf16(f, kb, mask_tag);
+      if constexpr (REFILL) load_v(f, npg0, npg1);
     };
     using NoMask = std::integral_constant<bool, false>;
     using Mask = std::integral_constant<bool, true>;
@@ -502,38 +514,55 @@ k_attn(AttnArgs a) {
     // masked tail (at most the last two blocks of a request) run in separate
     // loops, so that each loop body holds one instantiation of the block code.
     int i = 0;
-    if constexpr (kRefill) {
-      for (; i < nfull; ++i) compute_block(f0, wk0 + 32 * i, NoMask{}, i + 1 < nb ? wk0 + 32 * (i + 1) : -1);
-      for (; i < nb; ++i) compute_block(f0, wk0 + 32 * i, Mask{}, i + 1 < nb ? wk0 + 32 * (i + 1) : -1);
+    auto key = [&](int b) { return wk0 + 32 * b; };
+    if constexpr (Q8) {
+      // The last blocks, and all that take masks, are few: they run the masked code, which
+      // is right for any block.
+      const std::true_type yes;
+      const std::false_type no;
+      if constexpr (DEPTH == 1) {
+        for (; i + 1 < nfull; i += 2) {
+          load_block(f1, key(i + 1));
+          compute_e4m3(f0, key(i), NoMask{}, no, 0);
+          if (i + 2 < nb) load_block(f0, key(i + 2));
+          compute_e4m3(f1, key(i + 1), NoMask{}, no, 0);
+        }
+        for (; i < nb; ++i) {
+          compute_e4m3(f0, key(i), Mask{}, no, 0);
+          if (i + 1 < nb) load_block(f0, key(i + 1));
+        }
+      } else {
+        for (; i < min(nfull, nb - 1); ++i) compute_e4m3(f0, key(i), NoMask{}, yes, key(i + 1));
+        for (; i < nb - 1; ++i) compute_e4m3(f0, key(i), Mask{}, yes, key(i + 1));
+        if (i < nb) compute_e4m3(f0, key(i), Mask{}, no, 0);
+      }
     } else if constexpr (kEarlyLoad) {
       // at the top of every iteration f0 holds block i
       if constexpr (DEPTH == 1) {
-        // one more block in flight while a block is computed
-        KVFrag<HD, Q8> f1;
         for (; i + 1 < nfull; i += 2) {
-          load_block(f1, wk0 + 32 * (i + 1));
-          compute_block(f0, wk0 + 32 * i, NoMask{}, -1);
-          if (i + 2 < nb) load_block(f0, wk0 + 32 * (i + 2));
-          compute_block(f1, wk0 + 32 * (i + 1), NoMask{}, -1);
+          load_block(f1, key(i + 1));
+          compute_bf16(f0, key(i), NoMask{});
+          if (i + 2 < nb) load_block(f0, key(i + 2));
+          compute_bf16(f1, key(i + 1), NoMask{});
         }
       }
       for (; i < nfull; ++i) {
-        compute_block(f0, wk0 + 32 * i, NoMask{}, -1);
-        if (i + 1 < nb) load_block(f0, wk0 + 32 * (i + 1));
+        compute_bf16(f0, key(i), NoMask{});
+        if (i + 1 < nb) load_block(f0, key(i + 1));
       }
       for (; i < nb; ++i) {
-        compute_block(f0, wk0 + 32 * i, Mask{}, -1);
-        if (i + 1 < nb) load_block(f0, wk0 + 32 * (i + 1));
+        compute_bf16(f0, key(i), Mask{});
+        if (i + 1 < nb) load_block(f0, key(i + 1));
       }
     } else {
       static_assert(DEPTH == 0, "a block in flight needs the early first load");
       for (; i < nfull; ++i) {
-        load_block(f0, wk0 + 32 * i);
-        compute_block(f0, wk0 + 32 * i, NoMask{}, -1);
+        load_block(f0, key(i));
+        compute_bf16(f0, key(i), NoMask{});
       }
       for (; i < nb; ++i) {
-        load_block(f0, wk0 + 32 * i);
-        compute_block(f0, wk0 + 32 * i, Mask{}, -1);
+        load_block(f0, key(i));
+        compute_bf16(f0, key(i), Mask{});
       }
     }
 
