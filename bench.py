@@ -48,6 +48,8 @@ def parse():
     ap.add_argument("--workload", default=None,
                     choices=["low_load", "high_load", "high_load_k2", "multi_turn"],
                     help="only this workload (default: all four, headline high_load_k2)")
+    ap.add_argument("--kv-format", default="bf16", choices=["bf16", "e4m3"],
+                    help="what the KV pools hold (default: bf16, which the headline is)")
     ap.add_argument("--no-cpu-baseline", action="store_true")
     ap.add_argument("--no-variants", action="store_true")
     ap.add_argument("--sweep", action="store_true",
@@ -257,7 +259,8 @@ def run_workload(name, model, weights, cfg, args, war, want_cpu, want_variants):
         st = harness.low_load_step()
     elif name == "multi_turn":
         mt = harness.multi_turn_inputs(vocab=cfg.vocab)
-        pool = harness.multi_turn_pool(cfg, mt, 4, extra_pages=64 + max(40, args.steps + 8) * 16)
+        pool = harness.multi_turn_pool(cfg, mt, 4, extra_pages=64 + max(40, args.steps + 8) * 16,
+                                       kv_format=args.kv_format)
         log("multi_turn: loading cached prefixes (forked) and private contexts")
         harness.load_multi_turn(pool, cfg, mt, kv_seed)
         log("multi_turn: prefill-append")
@@ -274,7 +277,8 @@ def run_workload(name, model, weights, cfg, args, war, want_cpu, want_variants):
         k_res = 2 if name == "high_load_k2" else st.k_max
         in_flight = max(40, args.steps + 8)
         pool = harness.make_pool(cfg, st.ctx_lens, max(k_res, 2) + 8,
-                                 extra_pages=64 + in_flight * st.B * harness.cdiv(k_res + 1, cfg.page_size))
+                                 extra_pages=64 + in_flight * st.B * harness.cdiv(k_res + 1, cfg.page_size),
+                                 kv_format=args.kv_format)
         log(f"{name}: loading cached contexts")
         harness.load_contexts(pool, cfg, st.ctx_lens, st.seq_ids, kv_seed)
     if name == "high_load_k2":
@@ -298,9 +302,9 @@ def run_workload(name, model, weights, cfg, args, war, want_cpu, want_variants):
     prof = kernel_profile(ds, model, pool, war)
     attn = prof.get("attention", {"calls": 0, "ms": 0.0})
     per_launch_ms = attn["ms"] / max(attn["calls"], 1)
-    kv_bytes = harness.step_kv_bytes(cfg, st, mt)
+    kv_bytes = harness.step_kv_bytes(cfg, st, mt, args.kv_format)
     attn_gbps = kv_bytes / (per_launch_ms * 1e-3) / 1e9
-    total_bytes = harness.step_bytes(cfg, st, shared_prefix=mt)
+    total_bytes = harness.step_bytes(cfg, st, shared_prefix=mt, kv_format=args.kv_format)
     step_gbps = total_bytes / (ms * 1e-3) / 1e9
     entry = {
         "workload": WORKLOADS[name], "batch": st.B, "k": st.k_max, "rows": st.rows(),
@@ -315,7 +319,7 @@ def run_workload(name, model, weights, cfg, args, war, want_cpu, want_variants):
         "roofline": {"kernel": "attention (k_attn)", "bound": "hbm", "achieved": round(attn_gbps, 1),
                      "peak": HBM_PEAK_GBPS, "unit": "GB/s", "frac": round(attn_gbps / HBM_PEAK_GBPS, 4),
                      "bytes_per_launch": kv_bytes, "mean_launch_ms": round(per_launch_ms, 5),
-                     "traffic": measured_traffic(name)},
+                     "traffic": measured_traffic(name) if args.kv_format == "bf16" else None},
         "step_ms_events": dist, "host_waits_for_free_count": waits, "kernels_ms_per_step": prof,
     }
     if prefill is not None:
@@ -470,7 +474,7 @@ def main():
         "higher_is_better": True, "scaling": "weak", "vs_baseline": None, "dtype": "bf16",
         "data": "synthetic (seeded random-init weights, seeded cached KV, motif-built token streams)",
         "config": {"workload": e["workload"], "batch": e["batch"], "k": e["k"], "rows": e["rows"],
-                   "sum_ctx": e["sum_ctx"], "parallelism": "single GPU"},
+                   "sum_ctx": e["sum_ctx"], "parallelism": "single GPU", "kv_format": args.kv_format},
         "hbm": e["hbm"], "roofline": e["roofline"], "cpu_baseline": e.get("cpu_baseline"),
         "verified_positions_per_s": e["verified_positions_per_s"], "step_ms_events": e["step_ms_events"],
         "kernels_ms_per_step": e["kernels_ms_per_step"],

@@ -123,11 +123,11 @@ class DeviceStep:
 
 
 def make_pool(cfg: synth.ModelConfig, ctx_lens, k_max: int, extra_pages: int = 64,
-              max_seqs: Optional[int] = None) -> war.Pool:
+              max_seqs: Optional[int] = None, kv_format: str = "bf16") -> war.Pool:
     P = cfg.page_size
     need = sum(cdiv(int(c) + k_max + 1, P) for c in ctx_lens) + extra_pages
     max_pages = cdiv(int(max(ctx_lens)) + max(k_max, 64) + 1, P)
-    return war.Pool(cfg, need, max_seqs or len(ctx_lens), max_pages)
+    return war.Pool(cfg, need, max_seqs or len(ctx_lens), max_pages, kv_format=kv_format)
 
 
 def load_contexts(pool: war.Pool, cfg: synth.ModelConfig, ctx_lens, seq_ids, kv_seed: int,
@@ -303,12 +303,13 @@ def multi_turn_inputs(seed: int = 5, groups: int = 4, per_group: int = 4, prefix
     return MultiTurn(groups, per_group, prefix, private, n_new, obs)
 
 
-def multi_turn_pool(cfg: synth.ModelConfig, mt: MultiTurn, k_max: int, extra_pages: int = 64) -> war.Pool:
+def multi_turn_pool(cfg: synth.ModelConfig, mt: MultiTurn, k_max: int, extra_pages: int = 64,
+                    kv_format: str = "bf16") -> war.Pool:
     P = cfg.page_size
     assert mt.prefix % P == 0, "shared prefixes are whole pages"
     own = cdiv(mt.cached + mt.n_new + k_max + 1, P) - mt.prefix // P
     need = mt.groups * (mt.prefix // P) + mt.n * own + extra_pages
-    return war.Pool(cfg, need, mt.n, cdiv(mt.cached + mt.n_new + max(k_max, 64) + 1, P))
+    return war.Pool(cfg, need, mt.n, cdiv(mt.cached + mt.n_new + max(k_max, 64) + 1, P), kv_format=kv_format)
 
 
 def load_multi_turn(pool: war.Pool, cfg: synth.ModelConfig, mt: MultiTurn, kv_seed: int) -> None:
@@ -367,11 +368,18 @@ def multi_turn_step(mt: MultiTurn, next_tokens, k: int = 4,
     return Step(mt.seq_ids, np.full(mt.n, mt.cached + mt.n_new, np.int32), nxt, drafts, k)
 
 
-def step_kv_bytes(cfg: synth.ModelConfig, st: Step, shared_prefix: Optional[MultiTurn] = None) -> int:
+def kv_token_bytes(cfg: synth.ModelConfig, kv_format: str = "bf16") -> int:
+    """Bytes of one token's keys and values in one layer of a pool (e4m3: codes and scales)."""
+    per_head = 2 * cfg.head_dim if kv_format == "bf16" else cfg.head_dim + 1
+    return 2 * cfg.n_kv_heads * per_head
+
+
+def step_kv_bytes(cfg: synth.ModelConfig, st: Step, shared_prefix: Optional[MultiTurn] = None,
+                  kv_format: str = "bf16") -> int:
     """KV bytes one layer's attention must read: every visible key and value.
     With ``shared_prefix`` (forked siblings) a group's common prefix counts
     once: the unique bytes."""
-    per_tok = 2 * cfg.n_kv_heads * cfg.head_dim * 2
+    per_tok = kv_token_bytes(cfg, kv_format)
     toks = int(sum(int(c) + len(d) + 1 for c, d in zip(st.ctx_lens, st.drafts)))
     if shared_prefix is not None:
         mt = shared_prefix
@@ -380,12 +388,12 @@ def step_kv_bytes(cfg: synth.ModelConfig, st: Step, shared_prefix: Optional[Mult
 
 
 def step_bytes(cfg: synth.ModelConfig, st: Step, logits: bool = False,
-               shared_prefix: Optional[MultiTurn] = None) -> int:
+               shared_prefix: Optional[MultiTurn] = None, kv_format: str = "bf16") -> int:
     """Algorithmic HBM bytes of one verify step: streamed weights, KV read and
     KV written (every layer), logits if written."""
-    kv_tok = cfg.kv_bytes_per_token()
+    kv_tok = cfg.n_layers * kv_token_bytes(cfg, kv_format)
     T = st.rows()
-    b = cfg.streamed_weight_bytes() + cfg.n_layers * step_kv_bytes(cfg, st, shared_prefix) + T * kv_tok
+    b = cfg.streamed_weight_bytes() + cfg.n_layers * step_kv_bytes(cfg, st, shared_prefix, kv_format) + T * kv_tok
     if logits:
         b += 4 * T * cfg.vocab
     return b
