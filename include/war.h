@@ -205,8 +205,9 @@ war_status war_kv_read(war_kv_pool* p, int32_t layer, int32_t B, const int32_t* 
  *   max_batch, max_rows   the most requests and rows a request: max_batch <= 1024,
  *                         max_rows <= 65536, their product <= 2^20
  * The pool must outlive the object.  Only war_attend_create and _destroy allocate and
- * wait, so update and run may be captured into a graph; an object holds one plan at a
- * time, so graphs that may run at the same time take an object each. */
+ * wait, so update and run may be captured into a graph, both together (a plan made
+ * outside describes the pool as it was then); an object holds one plan at a time, so
+ * graphs that may run at the same time take an object each. */
 typedef struct war_attend war_attend;
 war_status war_attend_create(war_kv_pool* p, int32_t max_batch, int32_t max_rows, war_attend** out);
 void war_attend_destroy(war_attend* a);
@@ -221,7 +222,8 @@ void war_attend_destroy(war_attend* a);
  * The keys and values of positions 0 .. ctx + n_lens - 1 (a tree's node i: ctx + i) must
  * be in the pool when the attention runs.  A bad id, position or count, an id twice, or
  * rows beyond a sequence's pages are flagged (war_pool_state), and war_attend_run then
- * writes nothing. */
+ * writes nothing.  A plan ends when the pool gives pages back (war_kv_free,
+ * war_kv_commit): war_attend_run then asks for the next update. */
 war_status war_attend_update(war_attend* a, int32_t B, int32_t n_max, const int32_t* seq_ids,
                              const int32_t* ctx_lens, const int32_t* n_lens, const int32_t* draft_parents,
                              void* stream);
@@ -388,11 +390,12 @@ war_status war_constrain_logits(const war_constraints* c, int32_t vocab, int32_t
 /* New requests' rows of a counts table [n_seqs][vocab]: their prompts' tokens get bit
  * 15, everything else is cleared.
  *   seq_ids   device int32 [B], distinct (others than [0, n_seqs) are skipped)
- *   tokens    device int32, packed; request i's at offsets[i] .. offsets[i + 1]
+ *   tokens    device int32 [n_tokens], packed; request i's at offsets[i] ..
+ *             offsets[i + 1] (what lies outside [0, n_tokens) is not read)
  *   offsets   device int32 [B + 1], ascending
  * Token ids outside [0, vocab) are skipped. */
 war_status war_counts_begin(uint16_t* counts, int32_t vocab, int32_t n_seqs, int32_t B, const int32_t* seq_ids,
-                            const int32_t* tokens, const int32_t* offsets, void* stream);
+                            const int32_t* tokens, int32_t n_tokens, const int32_t* offsets, void* stream);
 
 /* Count what a step committed (or any generated tokens): first[b] (NULL: none), then
  * lens[b] tokens of tokens[b].

@@ -320,15 +320,15 @@ __global__ void __launch_bounds__(256) k_greedy(ConstrainArgs a, int32_t* greedy
 constexpr int kSlice = 16384;
 template <bool VEC>
 __global__ void __launch_bounds__(256) k_counts_begin(uint16_t* counts, int V, int n_seqs, const int32_t* seq_ids,
-                                                      const int32_t* tokens, const int32_t* offsets) {
+                                                      const int32_t* tokens, int n_tokens, const int32_t* offsets) {
   __shared__ uint32_t s_bits[kSlice / 32];
   const int b = blockIdx.y, c0 = blockIdx.x * kSlice, c1 = min(V, c0 + kSlice);
   const int seq = seq_ids[b];
   if (seq < 0 || seq >= n_seqs) return;
   for (int i = threadIdx.x; i < kSlice / 32; i += 256) s_bits[i] = 0;
   __syncthreads();
-  const int t1 = offsets[b + 1];
-  for (int i0 = offsets[b] + threadIdx.x; i0 < t1; i0 += 256 * 16) {
+  const int t1 = min(offsets[b + 1], n_tokens);
+  for (int i0 = max(offsets[b], 0) + threadIdx.x; i0 < t1; i0 += 256 * 16) {
     int t[16];
 #pragma unroll
     for (int u = 0; u < 16; ++u) t[u] = i0 + 256 * u < t1 ? tokens[i0 + 256 * u] : -1;
@@ -400,12 +400,12 @@ void launch_greedy(const ConstrainArgs& a, int32_t* greedy, bool finite, hipStre
   k_greedy<<<a.B * (a.k_max + 1), 256, 0, st>>>(a, greedy, finite);
 }
 void launch_counts_begin(uint16_t* counts, int V, int n_seqs, int B, const int32_t* seq_ids, const int32_t* tokens,
-                         const int32_t* offsets, hipStream_t st) {
+                         int n_tokens, const int32_t* offsets, hipStream_t st) {
   const dim3 grid(cdiv_i(V, kSlice), B);
   if (V % 8 == 0 && (reinterpret_cast<uintptr_t>(counts) & 15) == 0)
-    k_counts_begin<true><<<grid, 256, 0, st>>>(counts, V, n_seqs, seq_ids, tokens, offsets);
+    k_counts_begin<true><<<grid, 256, 0, st>>>(counts, V, n_seqs, seq_ids, tokens, n_tokens, offsets);
   else
-    k_counts_begin<false><<<grid, 256, 0, st>>>(counts, V, n_seqs, seq_ids, tokens, offsets);
+    k_counts_begin<false><<<grid, 256, 0, st>>>(counts, V, n_seqs, seq_ids, tokens, n_tokens, offsets);
 }
 void launch_counts_add(uint16_t* counts, int V, int n_seqs, int B, const int32_t* seq_ids, const int32_t* first,
                        const int32_t* tokens, int n_max, const int32_t* path, const int32_t* lens, hipStream_t st) {

@@ -233,7 +233,7 @@ struct ConstrainArgs {
 void launch_constrain(const ConstrainArgs& a, hipStream_t st);
 void launch_greedy(const ConstrainArgs& a, int32_t* greedy, bool finite, hipStream_t st);
 void launch_counts_begin(uint16_t* counts, int V, int n_seqs, int B, const int32_t* seq_ids, const int32_t* tokens,
-                         const int32_t* offsets, hipStream_t st);
+                         int n_tokens, const int32_t* offsets, hipStream_t st);
 void launch_counts_add(uint16_t* counts, int V, int n_seqs, int B, const int32_t* seq_ids, const int32_t* first,
                        const int32_t* tokens, int n_max, const int32_t* path, const int32_t* lens, hipStream_t st);
 void launch_block_max(const float* logits, int rows, int V, float* block_max, hipStream_t st);

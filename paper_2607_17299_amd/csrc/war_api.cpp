@@ -291,6 +291,7 @@ struct war_attend {
   DevBuf buf;
   // the plan: its requests, rows a request, row block, segments and grid
   int B = 0, n = 0, rb = 0, n_segs = 0, grid = 0;
+  int64_t releases = 0;  // the pool's, when it was made
   Workspace ws;
 };
 
@@ -310,6 +311,7 @@ struct war_kv_pool {
   int64_t exact_waits = 0;  // verify steps that read the exact count
   bool pending = false;
   int pending_B = 0;
+  int64_t releases = 0;  // calls that give pages back
   bool forked = false;  // some sequences may share pages (war_kv_fork was called)
 };
 
@@ -959,6 +961,7 @@ war_status war_kv_free(war_kv_pool* p, int32_t n, const int32_t* seq_ids_host, v
   hipStream_t st = static_cast<hipStream_t>(stream);
   s = upload_ids(p, n, seq_ids_host, nullptr, st);
   if (s != WAR_OK) return s;
+  ++p->releases;
   launch_free(p->dev, n, p->tmp.as<int32_t>(), st);
   HIPCHK(hipGetLastError());
   int32_t fc;
@@ -1350,6 +1353,7 @@ war_status war_attend_create(war_kv_pool* p, int32_t max_batch, int32_t max_rows
   a->max_batch = max_batch;
   a->max_rows = max_rows;
   if (hipError_t e = a->buf.ensure(bytes); e != hipSuccess) {
+    (void)hipGetLastError();  // reported here, not by the next call
     delete a;
     return fail(WAR_ERR_HIP, std::string("attention workspace: ") + hipGetErrorString(e));
   }
@@ -1382,6 +1386,7 @@ war_status war_attend_update(war_attend* a, int32_t B, int32_t n_max, const int3
   a->ws.tree_step = tree;
   a->B = B;
   a->n = n_max;
+  a->releases = p->releases;
   a->rb = s.rb;
   a->n_segs = s.n_segs;
   a->grid = (int)std::min<int64_t>(s.items * p->cfg.n_kv_heads, kAttnGrid);
@@ -1417,6 +1422,7 @@ war_status war_attend_run(war_attend* a, int32_t layer, const void* q, int64_t q
   CHECK(a, "null attention");
   CHECK(a->B > 0, "no plan (war_attend_update)");
   const war_kv_pool* p = a->pool;
+  CHECK(a->releases == p->releases, "the pool gave pages back since the plan was made (war_attend_update)");
   CHECK(layer >= 0 && layer < p->cfg.n_layers, "layer out of range");
   CHECK(q && o, "null array");
   CHECK(aligned16(q) && aligned16(o), "q and o must be 16-byte aligned");
@@ -1549,10 +1555,10 @@ static war_status check_counts(const uint16_t* counts, int32_t vocab, int32_t n_
 }
 
 war_status war_counts_begin(uint16_t* counts, int32_t vocab, int32_t n_seqs, int32_t B, const int32_t* seq_ids,
-                            const int32_t* tokens, const int32_t* offsets, void* stream) {
+                            const int32_t* tokens, int32_t n_tokens, const int32_t* offsets, void* stream) {
   WARCHK(check_counts(counts, vocab, n_seqs, B, seq_ids));
-  CHECK(tokens && offsets, "null array");
-  launch_counts_begin(counts, vocab, n_seqs, B, seq_ids, tokens, offsets, static_cast<hipStream_t>(stream));
+  CHECK(n_tokens >= 0 && (n_tokens == 0 || tokens) && offsets, "null array or negative n_tokens");
+  launch_counts_begin(counts, vocab, n_seqs, B, seq_ids, tokens, n_tokens, offsets, static_cast<hipStream_t>(stream));
   HIPCHK(hipGetLastError());
   return WAR_OK;
 }
@@ -1593,6 +1599,7 @@ war_status war_kv_commit(war_kv_pool* p, int32_t B, const int32_t* seq_ids, int3
   CHECK(B == p->pending_B, "B differs from the verify step's");
   CHECK(seq_ids && ctx_lens && accept_lens, "null array");
   const uint32_t seq = p->commit_issued + 1;
+  ++p->releases;
   launch_commit(p->dev, B, seq_ids, ctx_lens, accept_lens, seq, static_cast<hipStream_t>(stream));
   HIPCHK(hipGetLastError());
   p->commit_issued = seq;

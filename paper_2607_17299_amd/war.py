@@ -87,7 +87,7 @@ def load_library(path: str = LIB_PATH) -> C.CDLL:
         "war_constrain_workspace": (C.c_int64, [i32, i32]),
         "war_constrain_logits": (i32, [C.POINTER(_Constraints), i32, i32, vp, vp, vp, vp, vp, i32, vp, C.c_int64, vp,
                                        C.c_int64, vp, vp, vp]),
-        "war_counts_begin": (i32, [vp, i32, i32, i32, vp, vp, vp, vp]),
+        "war_counts_begin": (i32, [vp, i32, i32, i32, vp, vp, i32, vp, vp]),
         "war_counts_add": (i32, [vp, i32, i32, i32, vp, vp, vp, i32, vp, vp, vp]),
         "war_verify_step_constrained": (i32, [vp, vp, i32, vp, vp, vp, vp, vp, vp, i32, C.POINTER(_Constraints), vp,
                                               C.c_float, i32, vp, vp, vp, vp, vp]),
@@ -523,6 +523,8 @@ def constrain_logits(logits: torch.Tensor, constraints: Constraints, seq_ids: to
         need = fn.war_constrain_workspace(rows, V)
         if workspace is None:
             workspace = torch.empty(max(need, 0), dtype=torch.uint8, device=dev)
+            if stream is not None:
+                workspace.record_stream(stream)  # its memory is free once that stream is done
         _require(workspace.device == dev and workspace.is_contiguous() and
                  workspace.numel() * workspace.element_size() >= need, f"workspace must hold {need} bytes on {dev}")
     ls = logits.stride(0) if rows > 1 else V
@@ -546,7 +548,7 @@ def counts_begin(counts: torch.Tensor, seq_ids: torch.Tensor, tokens: torch.Tens
     _checked(dev, torch.int32, seq_ids=seq_ids, tokens=tokens, offsets=offsets)
     _require(offsets.numel() == seq_ids.numel() + 1, "offsets must hold one more entry than seq_ids")
     _call(lib().war_counts_begin, dev, stream, at, V, S, seq_ids.numel(), seq_ids.data_ptr(), tokens.data_ptr(),
-          offsets.data_ptr())
+          tokens.numel(), offsets.data_ptr())
 
 
 def counts_add(counts: torch.Tensor, seq_ids: torch.Tensor, first: Optional[torch.Tensor],
@@ -580,7 +582,13 @@ def verify_step_constrained(model: Model, pool: Pool, seq_ids: torch.Tensor, ctx
              accept_path=accept_path)
     _checked(dev, torch.float32, uniforms=uniforms, logits=logits)
     _require(constraints.vocab == model.cfg.vocab and constraints.device == dev, "constraints of another vocabulary or device")
-    constraints._rows(B * (k_max + 1))
+    rows = B * (k_max + 1)
+    constraints._rows(rows)
+    _require(all(t.numel() == B for t in (ctx_lens, last_tokens, accept_lens, next_tokens)) and
+             (draft_lens is None or draft_lens.numel() == B) and
+             all(t is None or t.numel() >= B * k_max for t in (draft_tokens, draft_parents, accept_path)) and
+             (uniforms is None or uniforms.numel() == 2 * rows) and
+             (logits is None or logits.numel() == rows * model.cfg.vocab), "arrays do not fit B requests of k_max drafts")
     _call(lib().war_verify_step_constrained, dev, stream, model.handle, pool.handle, B, seq_ids.data_ptr(),
           ctx_lens.data_ptr(), last_tokens.data_ptr(), _addr(draft_tokens), _addr(draft_parents), _addr(draft_lens), k_max,
           constraints._ref, _addr(uniforms), float(temperature), int(top_k), accept_lens.data_ptr(),

@@ -251,6 +251,30 @@ def test_counts_begin_and_add(V):
     np.testing.assert_array_equal(gpu.cpu().numpy().view(np.uint16), table)
 
 
+def test_counts_begin_reads_no_token_outside_its_array():
+    war = _war()
+    V, toks = 64, [1, 2, 3, 4, 5]
+    for off, want in (([-7, 2], [1, 2]), ([3, 2**31 - 1], [4, 5]), ([5, 9], []), ([4, 1], []), ([0, 5], toks)):
+        gpu = torch.full((1, V), 77, dtype=torch.int16, device=DEV)
+        war.counts_begin(gpu, t32([0]), t32(toks), t32(off))
+        assert (gpu[0] != 0).nonzero().flatten().tolist() == want and (gpu[0, want] == -32768).all()
+
+
+def test_another_stream():
+    """The calls go to the given stream, in order there; their temporary memory lives as long."""
+    war = _war()
+    c = Case(50257, 4, 3, 9)
+    want, g0 = run_case(c)
+    s = torch.cuda.Stream()
+    z, cons, args = f32(c.z), c.constraints(), (t32(c.seq), t32(c.last), t32(c.drafts[:, :3]), t32(c.lens))
+    out, greedy = torch.full_like(z, 123.0), torch.full((16,), 77, dtype=torch.int32, device=DEV)
+    torch.cuda.synchronize()
+    war.constrain_logits(z, cons, *args, 3, out=out, greedy=greedy, stream=s)
+    junk = [torch.full((1 << 20,), -1, dtype=torch.uint8, device=DEV) for _ in range(8)]   # on the current stream
+    s.synchronize()
+    assert torch.equal(torch.nan_to_num(out, 1e9), torch.nan_to_num(want, 1e9)) and greedy.tolist() == g0.tolist() and junk
+
+
 # ------------------------------------------------------------------- whole steps
 CFG = synth.TINY
 

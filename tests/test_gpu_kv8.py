@@ -343,6 +343,25 @@ def test_refusals():
         war.AttendPlan(pool, 1025, 1)
 
 
+def test_a_plan_ends_when_pages_are_given_back():
+    war = _war()
+    cfg = cfg_of(8, 2, 64)
+    pool = scattered_pool(cfg, [64, 64], "e4m3")
+    ids, ctx = t32([0, 1]), t32([3, 3])
+    war.kv_write(pool, 0, ids, t32([0, 0]), *torch.ones((2, 2, 64, 2, 64), dtype=torch.bfloat16, device=DEV))
+    plan = war.AttendPlan(pool, 2, 2)
+    q = torch.ones((2, 2, 8, 64), dtype=torch.bfloat16, device=DEV)
+    out = torch.zeros_like(q)
+    plan.update(ids, ctx)
+    pool.free([1])
+    with pytest.raises(war.WarError) as e:
+        war.attend(plan, 0, q, out)
+    assert e.value.status == -1
+    plan.update(ids[:1], ctx[:1])
+    war.attend(plan, 0, q[:1], out[:1])
+    assert pool.state()["status"] == 0 and (out[0] == 1.0).all() and (out[1] == 0.0).all()
+
+
 def test_captured_plans_replay_and_follow_their_inputs():
     war = _war()
     cfg = cfg_of(8, 2, 64)
@@ -391,13 +410,20 @@ def near_codes(got, want):
         assert (np.abs(x - w) <= bound).all()
 
 
-def test_a_step_stores_the_bytes_of_its_bf16_keys_and_values(tiny):
+WIDE = synth.ModelConfig(n_layers=2, d_model=512, n_q_heads=8, n_kv_heads=2, head_dim=128, ffn_dim=512, vocab=1024)
+
+
+@pytest.mark.parametrize("wide", [False, True])
+def test_a_step_stores_the_bytes_of_its_bf16_keys_and_values(tiny, wide):
     """Layer 0's keys and values do not hang on the cache: a bf16 pool's, written with
     war_kv_write, are an 8-bit pool's bit for bit (an append, and a step's rows)."""
-    war, model = _war(), tiny["model"]
-    pools = {name: war.Pool(CFG, 32, 2, 16, device=DEV, kv_format=f)
+    war, cfg, model = _war(), CFG, tiny["model"]
+    if wide:
+        cfg = WIDE
+        model = war.Model(cfg, {k: v.to(DEV) for k, v in synth.model_weights(cfg, seed=2, norm_std=0.1).items()}, max_rows=128)
+    pools = {name: war.Pool(cfg, 32, 2, 16, device=DEV, kv_format=f)
              for name, f in (("bf16", "bf16"), ("e4m3", "e4m3"), ("copy", "e4m3"))}
-    toks = t32(np.concatenate([synth.uniform_tokens(31, 61, CFG.vocab), synth.uniform_tokens(32, 7, CFG.vocab)]))
+    toks = t32(np.concatenate([synth.uniform_tokens(31, 61, cfg.vocab), synth.uniform_tokens(32, 7, cfg.vocab)]))
     for f in ("bf16", "e4m3"):
         seq, ctx, nxt, acc = t32([0, 1]), t32([0, 0]), t32([0, 0]), t32([0, 0])
         war.prefill_append(model, pools[f], seq, ctx, [61, 7], toks, nxt)

@@ -38,12 +38,13 @@ def test_constrain_logits_refuses():
 
 def test_counts_refuse():
     lib = war.lib()
-    begin = lambda counts=A, V=10, S=2, B=1, seq=A, tok=A, off=A: lib.war_counts_begin(counts, V, S, B, seq, tok, off, None)
+    begin = lambda counts=A, V=10, S=2, B=1, seq=A, tok=A, m=5, off=A: lib.war_counts_begin(counts, V, S, B, seq, tok, m, off,
+                                                                                             None)
     add = lambda counts=A, V=10, S=2, B=1, seq=A, first=A, tok=A, n=3: lib.war_counts_add(counts, V, S, B, seq, first, tok, n,
                                                                                       None, None, None)
     for bad in (dict(counts=None), dict(counts=A + 1), dict(V=0), dict(S=0), dict(B=0), dict(B=1025), dict(seq=None)):
         assert begin(**bad) == INVALID and add(**bad) == INVALID, bad
-    for bad in (dict(tok=None), dict(off=None)):
+    for bad in (dict(tok=None), dict(off=None), dict(m=-1)):
         assert begin(**bad) == INVALID, bad
     for bad in (dict(tok=None), dict(n=-1), dict(n=4097)):
         assert add(**bad) == INVALID, bad
