@@ -185,12 +185,13 @@ war_status war_kv_load(war_kv_pool* p, int32_t seq_id, int32_t layer, int32_t po
  * cache-aware scheduler).  Unlike war_kv_load nothing waits for the device.
  *   seq_ids   device int32 [B], distinct
  *   pos0      device int32 [B]: the first token's position
- *   n_max     row b * n_max + i of k and v is token pos0[b] + i
+ *   n_max     row b * n_max + i of k and v is token pos0[b] + i; B * n_max <= 2^26
  *   n_lens    device int32 [B] in [0, n_max], or NULL: all n_max.  Rows beyond are not
  *             read (written: left as they were).
  *   k, v      device bf16 rows of n_kv_heads * head_dim, keys after RoPE; strides in
  *             elements, multiples of 8, at least a row; 16-byte aligned
- * The tokens must lie within the sequence's pages (war_kv_alloc).  A request that does
+ * The tokens must lie within the sequence's pages (war_kv_alloc; a page that forked
+ * sequences share changes for all of them, as under war_kv_load).  A request that does
  * not (or has a bad id, position or count) is flagged (war_pool_state) and left out. */
 war_status war_kv_write(war_kv_pool* p, int32_t layer, int32_t B, const int32_t* seq_ids, const int32_t* pos0,
                         int32_t n_max, const int32_t* n_lens, const void* k, int64_t k_stride, const void* v,
@@ -414,7 +415,8 @@ war_status war_counts_add(uint16_t* counts, int32_t vocab, int32_t n_seqs, int32
  * (draft_parents not NULL, accept_path as there) or war_verify_step_sampled (uniforms
  * not NULL, chains; temperature and top_k as there) with every row's logits
  * constrained before its token is chosen.  n_seqs must cover the pool's sequences.
- * logits receives the constrained ones.  In a row where no token is left (none allowed;
+ * logits receives the constrained ones; where it is NULL the model holds as many itself,
+ * in memory that grows at need (like every step's, so not under a graph capture).  In a row where no token is left (none allowed;
  * sampled: none above -inf) no draft is accepted, and next_tokens is -1 where the
  * accepted path ends there. */
 war_status war_verify_step_constrained(war_model* m, war_kv_pool* p, int32_t B, const int32_t* seq_ids,

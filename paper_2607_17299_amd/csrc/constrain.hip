@@ -328,7 +328,7 @@ __global__ void __launch_bounds__(256) k_counts_begin(uint16_t* counts, int V, i
   for (int i = threadIdx.x; i < kSlice / 32; i += 256) s_bits[i] = 0;
   __syncthreads();
   const int t1 = min(offsets[b + 1], n_tokens);
-  for (int i0 = max(offsets[b], 0) + threadIdx.x; i0 < t1; i0 += 256 * 16) {
+  for (int64_t i0 = max(offsets[b], 0) + (int64_t)threadIdx.x; i0 < t1; i0 += 256 * 16) {
     int t[16];
 #pragma unroll
     for (int u = 0; u < 16; ++u) t[u] = i0 + 256 * u < t1 ? tokens[i0 + 256 * u] : -1;

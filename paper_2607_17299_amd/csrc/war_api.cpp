@@ -1005,8 +1005,8 @@ static war_status kv_move(bool write, war_kv_pool* p, int32_t layer, int32_t B, 
   CHECK(p, "null pool");
   CHECK(layer >= 0 && layer < p->cfg.n_layers, "layer out of range");
   CHECK(B >= 1 && B <= kMaxBatch, "B out of range [1, 1024]");
-  CHECK(n_max >= 0 && n_max <= 1 << 20, "n_max out of range [0, 2^20]");
-  CHECK(seq_ids && pos0 && k && v, "null array");
+  CHECK(n_max >= 0 && (int64_t)B * n_max <= 1 << 26, "n_max negative, or more than 2^26 rows");
+  CHECK(seq_ids && pos0 && (n_max == 0 || (k && v)), "null array");
   const int64_t row = (int64_t)p->geom.n_kv_heads * p->geom.head_dim;
   CHECK(aligned16(k) && aligned16(v), "k and v must be 16-byte aligned");
   CHECK(k_stride >= row && v_stride >= row && k_stride % 8 == 0 && v_stride % 8 == 0,

@@ -422,6 +422,7 @@ class AttendPlan:
                draft_parents: Optional[torch.Tensor] = None, n_rows: Optional[int] = None, stream=None) -> None:
         """Plan the rows of these requests: n_rows (default max_rows) each, of which
         n_lens are live; row 0 at position ctx_lens[b]."""
+        _require(bool(self.pool.handle), "the pool is closed")
         B, n, dev = seq_ids.numel(), self.max_rows if n_rows is None else n_rows, self.pool.kv.device
         _checked(dev, torch.int32, seq_ids=seq_ids, ctx_lens=ctx_lens, n_lens=n_lens, draft_parents=draft_parents)
         _require(ctx_lens.numel() == B and (n_lens is None or n_lens.numel() == B),
@@ -446,7 +447,7 @@ class AttendPlan:
 
 def attend(plan: AttendPlan, layer: int, q: torch.Tensor, out: torch.Tensor, stream=None) -> torch.Tensor:
     """Attention of the planned rows in one layer: q, out bf16 [B, n_rows, Hq, D]."""
-    _require(plan.shape is not None, "no plan: call update first")
+    _require(plan.shape is not None and bool(plan.pool.handle), "no plan: call update first (the pool must be open)")
     pool, (B, n) = plan.pool, plan.shape
     dev, H, D = pool.kv.device, pool.cfg.n_q_heads, pool.cfg.head_dim
     qs, os_ = _rows_of("q", q, dev, B, n, H, D), _rows_of("out", out, dev, B, n, H, D)

@@ -1,5 +1,7 @@
 """Constrained logits, their greedy tokens, token counts and verify steps under
 constraints, against the float64 oracle."""
+import gc
+
 import numpy as np
 import pytest
 import torch
@@ -273,6 +275,44 @@ def test_another_stream():
     junk = [torch.full((1 << 20,), -1, dtype=torch.uint8, device=DEV) for _ in range(8)]   # on the current stream
     s.synchronize()
     assert torch.equal(torch.nan_to_num(out, 1e9), torch.nan_to_num(want, 1e9)) and greedy.tolist() == g0.tolist() and junk
+
+
+def test_captured_constraints_and_counts_replay():
+    """Constrain, count what was taken, constrain again: replays against eager calls."""
+    war = _war()
+    c = Case(5000, 3, 4, 21, odd=False)
+    kw = dict(repetition=f32(c.rep), frequency=f32(c.freq), presence=f32(c.pres), bias_ids=t32(c.bid), bias_values=f32(c.bval),
+              masks=bits_of(c.allowed), mask_index=t32(c.index))
+    prompt, off = t32([1, 2, 3, 4999, 0, 7]), t32([0, 2, 2, 6])
+    seq, last, drafts, lens = t32(c.seq), t32(c.last), t32(c.drafts), t32([4, 0, 3])
+    z = f32(c.z)
+    tables = [torch.full((c.S, c.V), 5, dtype=torch.int16, device=DEV) for _ in range(2)]
+    cons = [war.Constraints(c.V, counts=t, **kw) for t in tables]
+    outs = [torch.full((15, c.V), 123.0, device=DEV) for _ in range(2)]
+    greedy = [torch.full((15,), 77, dtype=torch.int32, device=DEV) for _ in range(2)]
+    work = torch.empty(war.lib().war_constrain_workspace(15, c.V), dtype=torch.uint8, device=DEV)
+
+    def step(i, workspace=None):
+        war.counts_add(tables[i], seq, last, drafts, lens)
+        war.constrain_logits(z, cons[i], seq, last, drafts, lens, 4, out=outs[i], greedy=greedy[i], workspace=workspace)
+
+    for i in range(2):
+        war.counts_begin(tables[i], seq, prompt, off)
+    graph = torch.cuda.CUDAGraph()
+    gc.collect()
+    with torch.cuda.graph(graph):
+        step(0, work)
+    g = torch.Generator(device=DEV).manual_seed(2)
+    for _ in range(5):
+        z.copy_(torch.randn(z.shape, device=DEV, generator=g) * 4)
+        drafts.copy_(torch.randint(0, 40, drafts.shape, device=DEV, generator=g))
+        lens.copy_(torch.randint(-1, 5, (3,), device=DEV, generator=g))
+        graph.replay()
+        step(1)
+        assert torch.equal(tables[0], tables[1]) and torch.equal(outs[0], outs[1]) and torch.equal(greedy[0], greedy[1])
+    counted = (tables[0].long() & 0x7FFF).sum(1)                # (the rows that began started at 0)
+    rest = [s for s in range(c.S) if s not in c.seq]
+    assert (counted[seq.long()] > 0).all() and (counted[rest] == 5 * c.V).all()
 
 
 # ------------------------------------------------------------------- whole steps

@@ -394,6 +394,153 @@ def test_captured_plans_replay_and_follow_their_inputs():
         assert pool.state()["status"] == 0
 
 
+@pytest.mark.parametrize("fmt", ["e4m3", "bf16"])
+def test_pages_past_32_bit_offsets(fmt):
+    """A sequence's pages at both ends of a pool of more than 2^32 bytes (bf16: elements)."""
+    war = _war()
+    cfg, far = cfg_of(32, 8, 128, layers=2), 70000
+    pool = war.Pool(cfg, far, 2, 69990, device=DEV, kv_format=fmt)
+    assert 2 * far * 8 * 2 * 16 * 128 > 2 ** 32
+    n_ctx, n = 300, 3
+    pool.alloc([0], [160])
+    pool.alloc([1], [69960 * 16])
+    pool.alloc([0], [n_ctx + n])
+    used = pool.block_tables[0, :19].tolist()
+    assert max(used) - min(used) > 65000
+    g = torch.Generator(device=DEV).manual_seed(8)
+    kv = torch.randn((2, 1, n_ctx + n, 8, 128), device=DEV, generator=g).bfloat16()
+    q = torch.randn((1, 40, 32, 128), device=DEV, generator=g).bfloat16()
+    for layer in range(2):
+        war.kv_write(pool, layer, t32([0]), t32([0]), *kv.roll(layer, 0))
+    back = torch.empty_like(kv)
+    want_kv = [e4m3.store_kv(as64(x[0]), as64(y[0])) if fmt == "e4m3" else (as64(x[0]), as64(y[0])) for x, y in
+               (kv, kv.roll(1, 0))]
+    for rows in (n, 40):
+        plan = war.AttendPlan(pool, 1, rows)
+        plan.update(t32([0]), t32([n_ctx + n - rows]))
+        for layer in range(2):
+            war.kv_read(pool, layer, t32([0]), t32([0]), *back)
+            for x, w in zip(back, want_kv[layer]):
+                np.testing.assert_array_equal(as64(x[0]), w)
+            out = torch.full((1, rows, 32, 128), 7.0, dtype=torch.bfloat16, device=DEV)
+            war.attend(plan, layer, q[:, :rows].contiguous(), out)
+            want, tol = np.zeros((rows, 32, 128)), np.zeros((rows, 32, 128))
+            reference(fmt, as64(q[0, :rows]), *want_kv[layer], n_ctx + n - rows, rows, None, want, tol)
+            check(as64(out[0]), want, tol)
+    assert pool.state()["status"] == 0
+
+
+def test_the_most_rows_of_a_request_and_the_most_requests():
+    war = _war()
+    cfg = cfg_of(2, 1, 64)
+    g = torch.Generator(device=DEV).manual_seed(12)
+    n, ctx = 65536, 37
+    pool = war.Pool(cfg, (ctx + n) // 16 + 3, 1, (ctx + n) // 16 + 2, device=DEV, kv_format="e4m3")
+    pool.alloc([0], [ctx + n])
+    kv = torch.randn((2, 1, ctx + n, 1, 64), device=DEV, generator=g).bfloat16()
+    war.kv_write(pool, 0, t32([0]), t32([0]), *kv)
+    q = torch.randn((1, n, 2, 64), device=DEV, generator=g).bfloat16()
+    plan, out = war.AttendPlan(pool, 1, n), torch.empty_like(q)
+    plan.update(t32([0]), t32([ctx]))
+    war.attend(plan, 0, q, out)
+    k, v = e4m3.store_kv(as64(kv[0, 0]), as64(kv[1, 0]))
+    for i in (0, 1, 63, 64, 4095, 40000, 65535):
+        want, tol = np.zeros((1, 2, 64)), np.zeros((1, 2, 64))
+        reference("e4m3", as64(q[0, i:i + 1]), k, v, ctx + i, 1, None, want, tol)
+        check(as64(out[0, i:i + 1]), want, tol)
+    B = 1024
+    pool = war.Pool(cfg, 3 * B, B, 3, device=DEV, kv_format="e4m3")
+    ctx = np.random.default_rng(4).integers(0, 40, B)
+    pool.alloc(list(range(B)), [48] * B)
+    ids, kv = t32(np.random.default_rng(5).permutation(B)), torch.randn((2, B, 45, 1, 64), device=DEV, generator=g).bfloat16()
+    war.kv_write(pool, 0, ids, t32(np.zeros(B)), *kv)
+    war.kv_write(pool, 0, ids, t32(np.zeros(B)), *kv[:, :, :0])                  # no rows: nothing
+    plan = war.AttendPlan(pool, B, 30)
+    rows = np.random.default_rng(6).integers(0, 6, B)
+    for m in (5, 30):                                                             # few rows, blocks of rows
+        q = torch.randn((B, m, 2, 64), device=DEV, generator=g).bfloat16()
+        out = torch.full_like(q, 7.0)
+        plan.update(ids, t32(ctx), t32(rows), n_rows=m)
+        war.attend(plan, 0, q, out)
+        assert pool.state()["status"] == 0
+        for b in range(0, B, 73):
+            want, tol = np.full((m, 2, 64), 7.0), np.zeros((m, 2, 64))
+            reference("e4m3", as64(q[b]), *e4m3.store_kv(as64(kv[0, b]), as64(kv[1, b])), ctx[b], rows[b], None, want, tol)
+            check(as64(out[b]), want, tol)
+
+
+def test_an_object_serves_smaller_plans_and_another_stream():
+    war = _war()
+    cfg = cfg_of(8, 2, 64)
+    g = torch.Generator(device=DEV).manual_seed(10)
+    pool = scattered_pool(cfg, [200] * 4, "e4m3")
+    kv = torch.randn((2, 4, 150, 2, 64), device=DEV, generator=g).bfloat16()
+    stream, plan = torch.cuda.Stream(), war.AttendPlan(pool, 4, 50)
+    ids, zero = t32(range(4)), t32([0] * 4)
+    torch.cuda.synchronize()
+    war.kv_write(pool, 0, ids, zero, *kv, stream=stream)
+    for B, n in ((4, 50), (1, 1), (2, 13), (3, 12), (4, 2), (1, 50)):            # both kinds of plans in turn
+        pos = t32([99] * B)
+        q = torch.randn((B, n, 8, 64), device=DEV, generator=g).bfloat16()
+        out = torch.zeros_like(q)
+        torch.cuda.synchronize()
+        plan.update(ids[:B], pos, n_rows=n, stream=stream)
+        war.attend(plan, 0, q, out, stream=stream)
+        stream.synchronize()
+        for b in range(B):
+            want, tol = np.zeros((n, 8, 64)), np.zeros((n, 8, 64))
+            reference("e4m3", as64(q[b]), *e4m3.store_kv(as64(kv[0, b]), as64(kv[1, b])), 99, n, None, want, tol)
+            check(as64(out[b]), want, tol)
+    back = torch.zeros_like(kv)
+    torch.cuda.synchronize()
+    war.kv_read(pool, 0, ids, zero, *back, stream=stream)
+    stream.synchronize()
+    for b in range(4):
+        for x, w in zip(back[:, b], e4m3.store_kv(as64(kv[0, b]), as64(kv[1, b]))):
+            np.testing.assert_array_equal(as64(x), w)
+    pool.close()
+    with pytest.raises(ValueError):
+        plan.update(ids, zero)
+    with pytest.raises(ValueError):
+        war.attend(plan, 0, q, out)
+
+
+def test_captured_write_attend_and_read_replay():
+    """A step of somebody's decoder as one graph, replayed on changing inputs."""
+    war = _war()
+    cfg = cfg_of(8, 2, 64, layers=2)
+    g = torch.Generator(device=DEV).manual_seed(13)
+    B, n = 3, 4
+    pools = [scattered_pool(cfg, [120] * B, "e4m3") for _ in range(2)]            # replayed, eager
+    plans = [war.AttendPlan(p, B, n) for p in pools]
+    ids, pos, lens = t32([2, 0, 1]), t32([0] * B), t32([4, 2, 3])
+    kv = torch.empty((2, 2, B, n, 2, 64), dtype=torch.bfloat16, device=DEV)
+    q = torch.empty((B, n, 8, 64), dtype=torch.bfloat16, device=DEV)
+    outs = [torch.zeros((2, B, n, 8, 64), dtype=torch.bfloat16, device=DEV) for _ in pools]
+    backs = [torch.zeros_like(kv) for _ in pools]
+
+    def step(i):
+        plans[i].update(ids, pos, lens)
+        for layer in range(2):
+            war.kv_write(pools[i], layer, ids, pos, *kv[layer], lens)
+            war.attend(plans[i], layer, q, outs[i][layer])
+            war.kv_read(pools[i], layer, ids, pos, *backs[i][layer], lens)
+
+    graph = torch.cuda.CUDAGraph()
+    gc.collect()
+    with torch.cuda.graph(graph):
+        step(0)
+    for _ in range(6):
+        kv.copy_(torch.randn(kv.shape, device=DEV, generator=g))
+        q.copy_(torch.randn(q.shape, device=DEV, generator=g))
+        graph.replay()
+        step(1)
+        assert torch.equal(outs[0], outs[1]) and torch.equal(backs[0], backs[1])
+        pos += lens
+        lens.copy_(torch.randint(0, n + 1, (B,), device=DEV, generator=g))
+    assert [p.state()["status"] for p in pools] == [0, 0]
+
+
 # ------------------------------------------------------------------- whole steps
 CFG = synth.TINY
 
