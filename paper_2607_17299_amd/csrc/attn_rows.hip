@@ -19,7 +19,12 @@
 // An e4m3 pool (Q8): the workgroup's threads take 16 codes each of a block's keys and
 // values to registers, two steps later to bf16 (exact: codes times their token's scale)
 // and to the same places in LDS, two steps before the block's scores.  So each code is
-// converted once a workgroup, and the products and softmax are the same.
+// converted once a workgroup, and the products and softmax are the same.  A wave's
+// pieces are of one page, so that the addresses are scalar (1355 -> 1325 us), the row sums
+// are v_dot2 of the weights (two products of ones before) and operands are read three
+// fragments ahead instead of two (1307).  2048 and 2011 rows of 32 heads behind 9001 and
+// 24576 tokens, the merge among it: 1279 us, 921 TFLOP/s; the matrix pipes are busy 43% of
+// all cycles, the VALU 57%, and two waves a SIMD wait for neither most of the rest.
 // 2048 rows of 32 heads over 25600 keys (head_dim 128): 1403 -> 1151-1162 us (the
 // kernel it replaces staged blocks through registers and took scores, softmax and
 // product one after the other).  Over an append of 16 x 2048 tokens to 8192-26624 keys
@@ -37,6 +42,12 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 WAR_DEV f32x16 mfma32(bf16x8 a, bf16x8 b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+
+// c + the two bf16 of a times those of b
+WAR_DEV float dot2(uint32_t a, uint32_t b, float c) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, a), __builtin_bit_cast(bf16x2, b), c, false);
 }
 
 // One unit's rows and keys, decoded from its work-order descriptor (the fields
@@ -108,8 +119,8 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
   // eight key rows, which are neighbours in LDS.
   constexpr int PP = HD;  // pieces of a page's keys
   const int kid = tid & (2 * PP - 1);
-  const bool kmine = HD == 128 || tid < 128, vmine = HD == 128 || tid >= 128;
-  const int kpg = kid / PP, vpg = kpg;
+  const bool kmine = HD == 128 || w < 2, vmine = HD == 128 || w >= 2;
+  const int kpg = __builtin_amdgcn_readfirstlane(kid / PP), vpg = kpg;  // (a wave's pieces are of one page)
   const int s8 = lane & 7, sub = (lane >> 3) & 3;                   // key row member, 16 dims of its 64
   const int rgrp = ((kid & (PP - 1)) >> 6) * 2 + (lane >> 5);       // (t, 64 dims) of the page
   const int kt = rgrp / (HD / 64), kf = (rgrp % (HD / 64)) * 4 + sub;  // slot group, k-step
@@ -182,14 +193,15 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
       uint2 vs;
     };
     auto fetch = [&](Codes& c, int p0, int p1) __attribute__((always_inline)) {
-      const int pk = kpg ? p1 : p0, pv_ = vpg ? p1 : p0;
+      const int pg = kpg ? p1 : p0;  // (scalar, and so are the page's addresses)
+      const uint8_t *codes = q8b + pg * pstride, *scales = scb + pg * sstride;
       if (kmine) {
-        c.k = *reinterpret_cast<const uint4*>(q8b + (int64_t)pk * pstride + kpiece * 16);
-        c.ks = scb[(int64_t)pk * sstride + kscale];
+        c.k = *reinterpret_cast<const uint4*>(codes + (uint32_t)(kpiece * 16));
+        c.ks = scales[(uint32_t)kscale];
       }
       if (vmine) {
-        c.v = *reinterpret_cast<const uint4*>(q8b + (int64_t)pv_ * pstride + P * HD + vpiece * 16);
-        c.vs = *reinterpret_cast<const uint2*>(scb + (int64_t)pv_ * sstride + vscale);
+        c.v = *reinterpret_cast<const uint4*>(codes + (uint32_t)(P * HD + vpiece * 16));
+        c.vs = *reinterpret_cast<const uint2*>(scales + (uint32_t)vscale);
       }
     };
     // a part of it: eight codes of the keys (0, 1), all of the values (2)
@@ -203,10 +215,8 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
         const float f[8] = {scale_of<0>(c.vs.x), scale_of<1>(c.vs.x), scale_of<2>(c.vs.x), scale_of<3>(c.vs.x),
                             scale_of<0>(c.vs.y), scale_of<1>(c.vs.y), scale_of<2>(c.vs.y), scale_of<3>(c.vs.y)};
         auto eight = [&](uint32_t w0, uint32_t w1) __attribute__((always_inline)) {
-          const auto a0 = __builtin_amdgcn_cvt_pk_f32_fp8(w0, false), a1 = __builtin_amdgcn_cvt_pk_f32_fp8(w0, true);
-          const auto a2 = __builtin_amdgcn_cvt_pk_f32_fp8(w1, false), a3 = __builtin_amdgcn_cvt_pk_f32_fp8(w1, true);
-          return make_uint4(pack2(a0[0] * f[0], a0[1] * f[1]), pack2(a1[0] * f[2], a1[1] * f[3]),
-                            pack2(a2[0] * f[4], a2[1] * f[5]), pack2(a3[0] * f[6], a3[1] * f[7]));
+          return make_uint4(pack2(from_e4m3<0>(w0, f[0]), from_e4m3<1>(w0, f[1])), pack2(from_e4m3<2>(w0, f[2]), from_e4m3<3>(w0, f[3])),
+                            pack2(from_e4m3<0>(w1, f[4]), from_e4m3<1>(w1, f[5])), pack2(from_e4m3<2>(w1, f[6]), from_e4m3<3>(w1, f[7])));
         };
         unsigned char* d = smem + (ST + stage) * SB + vdst;
         *reinterpret_cast<uint4*>(d) = eight(c.v.x, c.v.y);
@@ -247,10 +257,9 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
       return as_bf16x8(*reinterpret_cast<const uint4*>(smem + stage * SB + f * 1024 + vread));
     };
     f32x16 zero;
-    [[maybe_unused]] f32x16 l_acc;
     [[maybe_unused]] constexpr uint32_t one2 = 0x3f803f80u;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) zero[e] = l_acc[e] = 0.f;
+    for (int e = 0; e < 16; ++e) zero[e] = 0.f;
     auto scores = [&](int stage, f32x16& s) __attribute__((always_inline)) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) s[e] = 0.f;
@@ -279,7 +288,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
       // (hi, lo) of value fragment f, whose operands are read LOOK triples
       // ahead; the softmax of block i is dealt over the slots.
       // Lane holds S^T[key kb + 16 (e / 8) + 8 g + e % 8][row].
-      constexpr int LOOK = Q8 ? 1 : 2, RING = LOOK + 1;  // (Q8 has not the registers for two)
+      constexpr int LOOK = 2, RING = LOOK + 1;
       bf16x8 rk[RING], rv[RING];
       auto read = [&](int f) __attribute__((always_inline)) {
         rk[f % RING] = kfrag((i + 1) & 3, f);
@@ -289,21 +298,26 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
       for (int f = 0; f < LOOK; ++f) read(f);
       float lm = 0.f, m_new = 0.f, m_use = 0.f, sum = 0.f, p0 = 0.f, p1 = 0.f;
       uint32_t hi[8], lo[8];
-      // Q8: one product of a bf16 a weight (see k_attn), two of ones for the row sums, and
-      // a part of the conversion (block i + 2 to LDS) in each of three slots
+      // Q8: one product of a bf16 a weight (see k_attn), the row sum taken of the rounded
+      // weights, and a part of the conversion (block i + 2 to LDS) in each of three slots.
+      // The compiler may move work between these slots, held by the pairs' order alone
+      // (1307 us with barriers between the slots, 1279 without, at the size above)
       constexpr int PV = Q8 ? 1 : 2;                                      // products of a value fragment
-      constexpr int SLOTS = (1 + PV) * KF + (Q8 ? 2 : 0), HEAD = 3 * KF / 8;  // the row maximum takes the first HEAD slots
+      constexpr int SLOTS = (1 + PV) * KF, HEAD = 3 * KF / 8;  // the row maximum takes the first HEAD slots
       auto softmax = [&](int t) __attribute__((always_inline)) {  // task t of 16: half of the work of a pair of keys
         const int e = t / 2 * 2;
         if (t % 2 == 0) {
           float s0 = s[e], s1 = s[e + 1];
-          asm volatile("" : "+v"(s0), "+v"(s1));  // (the empty asm keep the work in its slot)
+          if constexpr (!Q8) asm volatile("" : "+v"(s0), "+v"(s1));  // (the empty asm keep the work in its slot)
           p0 = __builtin_amdgcn_exp2f(fmaf(s0, a.scale_log2, -m_use));
           p1 = __builtin_amdgcn_exp2f(fmaf(s1, a.scale_log2, -m_use));
           hi[e / 2] = pack2(p0, p1);
           asm volatile("" : "+v"(hi[e / 2]), "+v"(p0), "+v"(p1));
         } else {
-          if constexpr (!Q8) {
+          if constexpr (Q8) {
+            sum = dot2(hi[e / 2], one2, sum);
+            asm volatile("" : "+v"(sum));
+          } else {
             sum += p0 + p1;
             lo[e / 2] = pack2(p0 - lo_f(hi[e / 2]), p1 - hi_f(hi[e / 2]));
             asm volatile("" : "+v"(lo[e / 2]), "+v"(sum));
@@ -313,9 +327,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
 #pragma unroll
       for (int z = 0; z < SLOTS; ++z) {
         const int f = z / (1 + PV);
-        if (z >= (1 + PV) * KF) {
-          l_acc = mfma32(as_bf16x8(make_uint4(one2, one2, one2, one2)), as_bf16x8(pin.hi[z - (1 + PV) * KF]), l_acc);
-        } else if (z % (1 + PV) == 0) {
+        if (z % (1 + PV) == 0) {
           if (f + LOOK < KF) read(f + LOOK);
           snext = mfma32(rk[f % RING], qf[f], f == 0 ? zero : snext);
         } else {
@@ -340,7 +352,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
 #pragma unroll
         for (int t = 0; t < 16; ++t)
           if (z >= HEAD && t * (SLOTS - HEAD) / 16 == z - HEAD) softmax(t);
-        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (!Q8) __builtin_amdgcn_sched_barrier(0);
       }
 #pragma unroll
       for (int pg = 0; pg < 2; ++pg) {
@@ -351,7 +363,6 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
       if (__any(m_new != m_run)) {
         const float alpha = m_new == m_run ? 1.f : exp2f(m_run - m_new);
         l_run *= alpha;
-        if constexpr (Q8) l_acc *= alpha;
 #pragma unroll
         for (int dt = 0; dt < NDT; ++dt) o_acc[dt] *= alpha;
         m_run = m_new;
@@ -418,7 +429,6 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
       const int kb = kbeg + 32 * lb;
 #pragma unroll
       for (int pg = 0; pg < 2; ++pg) {
-        if constexpr (Q8) l_acc = mfma32(as_bf16x8(make_uint4(one2, one2, one2, one2)), as_bf16x8(pa.hi[pg]), l_acc);
 #pragma unroll
         for (int dt = 0; dt < NDT; ++dt) {
           uint4 v = __builtin_bit_cast(uint4, vfrag(lb & 3, pg * NDT + dt));
@@ -432,7 +442,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
     int next_it = 0;
     if (tid == 0) next_it = uq.next(a.unit_ctr);
     // this wave's rows: partial O, running max and sum
-    const float l = Q8 ? l_acc[0] : l_run + __shfl_xor(l_run, 32, 64);
+    const float l = l_run + __shfl_xor(l_run, 32, 64);
     if (live) {
 #pragma unroll
       for (int dt = 0; dt < NDT; ++dt)

@@ -36,8 +36,13 @@ WAR_DEV uint4 from_e4m3x8(uint32_t w0, uint32_t w1, float scale) {
   return make_uint4(from_e4m3x2<false>(w0, scale), from_e4m3x2<true>(w0, scale), from_e4m3x2<false>(w1, scale),
                     from_e4m3x2<true>(w1, scale));
 }
+// code I of a word times a power of two
+template <int I>
+WAR_DEV float from_e4m3(uint32_t w, float scale) {
+  return __builtin_amdgcn_cvt_scalef32_f32_fp8((int)w, scale, I);
+}
 // the scale of byte I of a word of scale bytes (byte 0: 0)
 template <int I>
 WAR_DEV float scale_of(uint32_t w) {
-  return __uint_as_float((I == 0 ? w << 23 : I == 3 ? w >> 1 : w << (23 - 8 * I)) & 0x7f800000u);
+  return __uint_as_float(((w >> (8 * I)) & 0xff) << 23);
 }
