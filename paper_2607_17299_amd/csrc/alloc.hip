@@ -143,8 +143,10 @@ __global__ void __launch_bounds__(kBT) k_verify_setup(PoolDev p, VerifySetupArgs
   // 8000-120000 tokens, attention and merge against twice the chunk: 39 partials 0.90,
   // 62 1.05, 125 1.10, 250 1.26.
   constexpr int kMergeMax = 64;
+  constexpr int kEvenFree = 2048;  // longer even cuts have to be nearly even (below)
   auto chunks_of = [](int n, int shift) { return (n + (1 << shift) - 1) >> shift; };
-  __shared__ int s_cnt[kChunks];
+  constexpr int kCuts = 8;  // even cuts tried (a.even)
+  __shared__ int s_cnt[kChunks], s_total, s_cut[kCuts];
   const int t = threadIdx.x, lane = t & 63, w = t >> 6, nt = blockDim.x, nw = nt >> 6;
   const int kp1 = a.k_max + 1;
   const int R = a.B * kp1;
@@ -164,6 +166,7 @@ __global__ void __launch_bounds__(kBT) k_verify_setup(PoolDev p, VerifySetupArgs
   if (t == 0) {
     s_bad = 0;
     s_dup = 0;
+    s_total = 0;
   }
   // the attention launches of this step start their work counters at zero
   if (t < 8) a.unit_ctr[t * kCtrStride] = 0;
@@ -233,6 +236,20 @@ __global__ void __launch_bounds__(kBT) k_verify_setup(PoolDev p, VerifySetupArgs
   __syncthreads();
   const int len = (t < a.B && !fail && (!PLAN || dl >= 0)) ? ctx + dl + 1 : 0;
   int csh = 31 - __clz(a.chunk);  // log2 of the chunk (a power of two)
+  // Even cuts: the shortest chunk of a multiple of 128 keys that leaves no more units
+  // than workgroups, so that all of them run at once and end together; one a CU where
+  // chunks stay short (a.even: 128 KB of codes), which draws the memory's rate as well
+  // and has half the starts and merges.  In 8 bits, with the merge: 24 requests of
+  // 501-9001 tokens, 64-wide heads 25.9 -> 22.6 us; 8 of 4000-12000, 3 kv-heads 18.6 ->
+  // 16.4; 4 of 40-900, 2 kv-heads 11.3 -> 8.9; 8 of 32001-32768 with 36 rows 109 -> 103.
+  // Cuts that leave workgroups idle lose to several units each in any order (16 of
+  // 2000-40000: 78 us, even 87), so long ones have to be nearly even.
+  const int u128 = (len + 127) / 128;
+  if (t < a.B) s_mis[t] = u128;
+  if (w * 64 < a.B) {
+    const int n = wave_scan(u128);
+    if (lane == 63) atomicAdd(&s_total, n);
+  }
   if (w * 64 < a.B)
     for (int c = 0; c < kChunks; ++c) {
       int n = chunks_of(len, max(csh + 1 - c, kMinShift));
@@ -241,14 +258,38 @@ __global__ void __launch_bounds__(kBT) k_verify_setup(PoolDev p, VerifySetupArgs
       if (lane == 63) atomicAdd(&s_cnt[c], n);
     }
   __syncthreads();
+  int cut = 0, cut_m = 1, cut_step = kCuts;  // items at most, shortest chunk (in 128 keys), 1 / step to the next
+  if (a.even && !a.cascade) {
+    cut = a.items_fill;
+    if (s_total < cut * a.even) cut = (cut + 1) / 2;
+    cut_m = cut > 0 ? max(1, (s_total + cut - 1) / cut) : 1;
+    if (cut_m > kEvenFree / 128) cut_step = 4 * kCuts;
+    for (int c = w; cut > 0 && c < kCuts; c += nw) {
+      const int m128 = cut_m + cut_m * c / cut_step;
+      int n = 0;
+      for (int q = lane; q < a.B; q += 64) {
+        const int nq = (s_mis[q] + m128 - 1) / m128;
+        n += nq > kMergeMax ? 1 << 20 : nq;
+      }
+      n = wave_scan(n);
+      if (lane == 63) s_cut[c] = n;
+    }
+  }
+  __syncthreads();
+  int even = 0;
+  if (cut > 0) {  // (the same for all threads)
+    const bool fits = lane < (cut_step == kCuts ? kCuts : 3) && s_cut[lane % kCuts] <= cut;
+    const int c = __ffsll((long long)__ballot(fits)) - 1;
+    if (c >= 0) even = 128 * (cut_m + cut_m * c / cut_step);
+  }
   if (!a.cascade) {
     if (s_cnt[0] >= a.items_double) ++csh;
     else if (s_cnt[1] > a.B)
 #pragma unroll 1
       for (int c = 2; c < kChunks && csh > kMinShift && s_cnt[c] <= a.items_fill; ++c) --csh;
   }
-  const int chunk = 1 << csh;
-  const int nch = chunks_of(len, csh);
+  const int chunk = even > 0 ? even : 1 << csh;
+  const int nch = (len + chunk - 1) / chunk;
   int n_items;
   const int ioff = block_excl_scan(nch, &n_items);
   if (t < a.B) {
@@ -329,14 +370,14 @@ __global__ void __launch_bounds__(kBT) k_verify_setup(PoolDev p, VerifySetupArgs
   }
   __syncthreads();
   int nsc = 0;
-  if (t < a.B && a.cascade && g > 1 && nch > 0 && s_shr[L] >= chunk) nsc = min(s_shr[L] >> csh, nch);
+  if (t < a.B && a.cascade && g > 1 && nch > 0 && s_shr[L] >= chunk) nsc = min(s_shr[L] / chunk, nch);
   const int j = t - L;
   const int run = nsc > 0 ? s_run[t] : 0;  // members of the run this request owns (0: not an owner)
   // A batch without forked siblings takes every request's whole chunks first,
   // in request order, then the partial last chunks, longest first: the
   // persistent grid then ends on its shortest units (s_mis is free by now and
   // holds each request's partial length).
-  const int n_whole = len >> csh, rem = len & (chunk - 1);
+  const int n_whole = len / chunk, rem = len - n_whole * chunk;
   if (t < a.B) s_mis[t] = rem;
   const bool lpt = !__syncthreads_or(t < a.B && g > 1);
   // Work order otherwise.  A group without shared units whose members have equal

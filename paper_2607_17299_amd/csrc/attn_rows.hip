@@ -21,8 +21,8 @@
 // and to the same places in LDS, two steps before the block's scores.  So each code is
 // converted once a workgroup, and the products and softmax are the same.  A wave's
 // pieces are of one page, so that the addresses are scalar (1355 -> 1325 us), the row sums
-// are v_dot2 of the weights (two products of ones before) and operands are read three
-// fragments ahead instead of two (1307).  2048 and 2011 rows of 32 heads behind 9001 and
+// are v_dot2 of the weights (two products of ones before) and operands are read two
+// fragments ahead instead of one (1307).  2048 and 2011 rows of 32 heads behind 9001 and
 // 24576 tokens, the merge among it: 1279 us, 921 TFLOP/s; the matrix pipes are busy 43% of
 // all cycles, the VALU 57%, and two waves a SIMD wait for neither most of the rest.
 // 2048 rows of 32 heads over 25600 keys (head_dim 128): 1403 -> 1151-1162 us (the

@@ -71,6 +71,7 @@ struct VerifySetupArgs {
   int items_fill;    // halved while that leaves at most this many and no request too many partials
   int G;        // query heads per kv-head
   int rb;       // attention row block of the step (rows per unit)
+  int even;     // even cuts are tried first, two units a CU from chunks of 128 times this on (0: not)
   int cascade;  // 1: plan shared-prefix attention units for forked siblings
   const int32_t* seq_ids;
   const int32_t* ctx_lens;

@@ -1201,6 +1201,7 @@ war_status verify_impl(war_model* m, war_kv_pool* p, int32_t B, const int32_t* s
   va.draft_lens = draft_lens;
   va.G = G;
   va.rb = RB;
+  va.even = p->geom.q8 ? m->md.hd / 16 : 0;  // (the sums of bf16 pools keep their order)
   va.cascade = p->forked && B > 1 ? 1 : 0;  // shared-prefix units for forked siblings
   va.draft_parents = tree ? draft_parents : nullptr;
   if (tree && !accept_path) {
@@ -1409,6 +1410,7 @@ war_status war_attend_update(war_attend* a, int32_t B, int32_t n_max, const int3
     va.draft_lens = n_lens;
     va.G = G;
     va.rb = s.rb;
+    va.even = p->cfg.head_dim / 16;
     va.cascade = p->forked && B > 1 ? 1 : 0;
     va.draft_parents = tree ? draft_parents : nullptr;
     launch_attend_plan(p->dev, va, meta, st);

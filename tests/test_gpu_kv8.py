@@ -235,6 +235,15 @@ def test_chunks_of_row_blocks_merge():
     check(*attend_case("e4m3", (4, 1, 128), 100, [470, 200], [100, 100]))
 
 
+@pytest.mark.parametrize("heads,n,ctx", [
+    ((32, 8, 128), 1, [5000, 3000, 4100]),       # cut into chunks of 384 or so keys
+    ((8, 8, 64), 7, [2500, 1, 6300, 0, 700]),    # 640
+    ((2, 2, 64), 3, [9000, 64]),                 # one request takes most of them
+])
+def test_even_cuts(heads, n, ctx):
+    check(*attend_case("e4m3", heads, n, ctx, [n] * len(ctx)))
+
+
 @pytest.mark.parametrize("fmt", ["e4m3", "bf16"])
 def test_attention_of_draft_trees(fmt):
     parents = [[0, 0, 1, 1, 3, 0, 6], [0, 1, 2, 3, 4, 5, 6], [0] * 7]
