@@ -15,6 +15,8 @@
 // chunk (a uniform test), and the next row's logits are in flight while a row is done.
 // It leaves the best id of every 128 (as the LM head does without constraints), from
 // which the greedy token, the acceptance and the sampler start.
+// 192 rows of 151,936 ids under everything (255 MB): 46 us, 5.5 TB/s, and 4.6 for the
+// greedy tokens.  The divisions as such, and each row looking through the biases, took 76.
 #include "kernels.h"
 
 #pragma clang fp contract(off)
@@ -316,7 +318,9 @@ __global__ void __launch_bounds__(256) k_greedy(ConstrainArgs a, int32_t* greedy
 
 // A request's row of the counts begins: bit 15 for each token of its prompt, no
 // occurrences.  A workgroup takes 16384 ids: the prompt's tokens among them as bits in
-// LDS, then the row's numbers, written once.
+// LDS, then the row's numbers, written once.  Every workgroup of a request reads its whole
+// prompt (from L2): 64 prompts of 8192 tokens into 151,936 ids 8.1 us, of which the 19 MB
+// written are 4.
 constexpr int kSlice = 16384;
 template <bool VEC>
 __global__ void __launch_bounds__(256) k_counts_begin(uint16_t* counts, int V, int n_seqs, const int32_t* seq_ids,
