@@ -480,17 +480,29 @@ __global__ void __launch_bounds__(kBT) k_verify_setup(PoolDev p, VerifySetupArgs
 // cut into chunks; the work order is a request's chunks, each with all blocks that reach
 // it, so that the units which read a chunk run together and find it in L2.  With first(c)
 // the first block that reaches chunk c, a request has sum_c (blocks - first(c)) items.
-// Few units (less than half the grid's) take shorter chunks, down to 256 keys.  One
-// workgroup: 5.2 us for two requests of 2048 rows.
+//
+// The chunk is the one of 20 with the least estimated time, in keys a workgroup: a unit
+// costs its keys and kUnitKeys for its start, its end and the merge of its partials.
+// Units of one length run in rounds of the grid, others fill in behind each other and
+// end half a unit apart, and nothing ends before the longest.  (Every number is an
+// integer sum, so that a plan repeats itself.)  Against 8192 keys, halved only where
+// half the grid idles, over e4m3: 4 requests of 500 rows behind 1000-9000 tokens 285 ->
+// 233 us, 2 of 300 behind 16000 293 -> 251, 4096 rows of 8 64-wide heads 85 -> 73; the worst
+// of 20 shapes 8 of 256 behind 2000-20000, 394 -> 414.  One workgroup: 7.7 us.
 __global__ void __launch_bounds__(kBT) k_attend_plan_rows(PoolDev p, RowPlanArgs a, StepMeta m) {
   __shared__ int s_ctx[kBT], s_n[kBT], s_off[kBT], s_seq[kBT];
-  constexpr int kChunks = 5, kMinChunk = 256;
-  __shared__ int s_cnt[kChunks];
+  constexpr int kCuts = 20;
+  constexpr float kUnitKeys = 1000.f;
+  auto cut = [](int c) { return (4 + c % 4) << (c / 4 + 7); };  // 512, 640, 768, 896, 1024, ... 14336 keys
+  __shared__ int s_cnt[kCuts], s_long;
+  __shared__ unsigned long long s_keys;
   __shared__ int s_hash[2 * kBT], s_bad, s_dup;
-  const int t = threadIdx.x;
+  const int t = threadIdx.x, lane = t & 63, w = t >> 6;
   if (t < 8) a.unit_ctr[t * kCtrStride] = 0;
-  if (t < kChunks) s_cnt[t] = 0;
-  if (t == 0) s_bad = s_dup = 0;
+  if (t == 0) {
+    s_bad = s_dup = s_long = 0;
+    s_keys = 0;
+  }
   for (int i = t; i < 2 * kBT; i += kBT) s_hash[i] = -1;
   __syncthreads();
   int s = 0, ctx = 0, n = 0;
@@ -520,32 +532,62 @@ __global__ void __launch_bounds__(kBT) k_attend_plan_rows(PoolDev p, RowPlanArgs
     if (s_dup) atomicOr(&p.scalars[1], ERR_DUP_SEQ);
   }
   if (fail) s = ctx = n = 0;  // (what was refused may be any number)
-  const int len = n > 0 ? ctx + n : 0, blocks = (n + a.TB - 1) / a.TB;
   // (lengths are at most 2^24; every block reaches the chunks that begin before the
   // first block's end, so only those behind take a division)
   auto first = [&](int ctx_, int c, int chunk) {
     const int before = c * chunk - ctx_;
     return before < a.TB ? 0 : before / a.TB;
   };
-  auto items_of = [&](int chunk) {
-    int c = min((len + chunk - 1) / chunk, (ctx + a.TB + chunk - 1) / chunk);
-    int k = c * blocks;
-    for (; c * chunk < len; ++c) k += blocks - first(ctx, c, chunk);
-    return k;
+  auto items_of = [&](int ctx_, int n_, int chunk) {
+    const int len_ = ctx_ + n_, blocks_ = (n_ + a.TB - 1) / a.TB;
+    int c = min((len_ + chunk - 1) / chunk, (ctx_ + a.TB + chunk - 1) / chunk);
+    int k = c * blocks_;
+    for (; c * chunk < len_; ++c) k += blocks_ - first(ctx_, c, chunk);
+    return n_ > 0 ? k : 0;
   };
-  int chunk = a.chunk, n_items;
-  int off = block_excl_scan(t < a.B ? items_of(chunk) : 0, &n_items);
-  if (2 * n_items <= a.items_fill) {  // (the same for all threads)
-    if (t < a.B && n > 0)
-      for (int i = 1, ch = a.chunk / 2; i < kChunks && ch >= kMinChunk; ++i, ch /= 2)
-        atomicAdd(&s_cnt[i], min(items_of(ch), 1 << 20));
-    __syncthreads();
-    for (int i = 1; i < kChunks && chunk / 2 >= kMinChunk && s_cnt[i] <= a.items_fill; ++i) chunk /= 2;
-    off = block_excl_scan(t < a.B ? items_of(chunk) : 0, &n_items);
-  }
   if (t < a.B) {
     s_ctx[t] = ctx;
     s_n[t] = n;
+    if (n > 0) {
+      atomicMax(&s_long, ctx + n);
+      atomicAdd(&s_keys, (unsigned long long)((n + a.TB - 1) / a.TB) * (unsigned)(ctx + (n + a.TB) / 2));
+    }
+  }
+  __syncthreads();
+  for (int c = w; c < kCuts; c += kBT / 64) {
+    const int ch = cut(c);
+    int k = 0;
+    if ((s_long + ch - 1) / ch <= a.most_chunks)  // (else k may overflow)
+      for (int b = lane; b < a.B; b += 64) k += items_of(s_ctx[b], s_n[b], ch);
+    else
+      k = a.items_cap;
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) k += __shfl_xor(k, o, 64);
+    if (lane == 0) s_cnt[c] = k;
+  }
+  __syncthreads();
+  int chunk = a.chunk, n_items;
+  {
+    const int c = min(lane, kCuts - 1);
+    const float slots = (float)a.items_fill, keys = (float)s_keys, k = (float)s_cnt[c];
+    const float unit = (float)min(cut(c), s_long) + kUnitKeys;
+    const float rounds = ceilf(k / slots) * unit;
+    const float filled = fmaxf((keys + k * kUnitKeys) / slots + keys / (2.f * fmaxf(k, 1.f)), unit);
+    float est = lane < kCuts && s_cnt[c] <= a.items_cap ? fminf(rounds, filled) : INFINITY;
+    int at = c;
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) {
+      const float oe = __shfl_xor(est, o, 64);
+      const int oa = __shfl_xor(at, o, 64);
+      if (oe < est || (oe == est && oa < at)) {
+        est = oe;
+        at = oa;
+      }
+    }
+    if (est < INFINITY) chunk = cut(at);
+  }
+  const int off = block_excl_scan(t < a.B ? items_of(ctx, n, chunk) : 0, &n_items);
+  if (t < a.B) {
     s_off[t] = off;
     s_seq[t] = s;
     m.req_seq[t] = s;

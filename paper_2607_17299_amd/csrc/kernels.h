@@ -134,7 +134,11 @@ void launch_attend_plan(const PoolDev& p, const VerifySetupArgs& a, const StepMe
 // The same in blocks of `TB` tokens (k_attn_rows): segment b * blocks + i is block i of
 // request b.
 struct RowPlanArgs {
-  int B, n_max, TB, blocks, chunk, items_fill;
+  int B, n_max, TB, blocks;
+  int chunk;        // keys per item that fit items_cap whatever the lengths
+  int items_fill;   // items (of a kv-head) of one round of the grid
+  int items_cap;    // items at most,
+  int most_chunks;  // of a segment
   const int32_t *seq_ids, *ctx_lens, *n_lens;
   int32_t* unit_ctr;
 };

@@ -1314,14 +1314,17 @@ AttendShape attend_shape(const war_kv_pool* p, int B, int n) {
     s.TB = kPrefillRows / G;
     s.blocks = cdiv_i(n, s.TB);
     s.n_segs = B * s.blocks;
-    // chunks of prefill_chunk keys, longer ones where there are units enough for 16
-    // rounds of the grid (each item has 128 rows of partial sums to write and merge)
+    // room for chunks of prefill_chunk keys, of longer ones where there are units enough
+    // for 16 rounds of the grid (each item has 128 rows of partial sums to write and
+    // merge); the plan cuts as the lengths at hand want it
     s.chunk = prefill_chunk(p->geom);
     while (cdiv_i(len, s.chunk) > kMaxItemsPerSeq) s.chunk *= 2;
     const int64_t rounds = 16 * kAttnGrid / nkv, most = (int64_t)s.n_segs * cdiv_i(len, s.chunk);
     while (s.chunk < len && (int64_t)s.n_segs * cdiv_i(len, s.chunk) > rounds) s.chunk *= 2;
     s.items = std::min(most, std::max<int64_t>(s.n_segs, rounds));  // (grows with the segments, as a bound has to)
     s.items_fill = std::max(1, kAttnGrid / nkv);
+    // (short contexts are cut finer, up to four rounds of the grid)
+    s.items = std::max(s.items, std::min<int64_t>((int64_t)s.n_segs * cdiv_i(len, 512), 4 * s.items_fill));
   }
   s.items = std::max<int64_t>(s.items, s.items_fill);
   return s;
@@ -1394,7 +1397,8 @@ war_status war_attend_update(war_attend* a, int32_t B, int32_t n_max, const int3
   const StepMeta meta = a->ws.meta();
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (s.rb == kPrefillRows) {
-    RowPlanArgs ra{B, n_max, s.TB, s.blocks, s.chunk, s.items_fill, seq_ids, ctx_lens, n_lens, a->ws.unit_ctr};
+    RowPlanArgs ra{B, n_max, s.TB, s.blocks, s.chunk, s.items_fill, (int)s.items, kMaxItemsPerSeq,
+                   seq_ids, ctx_lens, n_lens, a->ws.unit_ctr};
     launch_attend_plan_rows(p->dev, ra, meta, st);
   } else {
     VerifySetupArgs va{};

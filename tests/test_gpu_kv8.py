@@ -235,6 +235,15 @@ def test_chunks_of_row_blocks_merge():
     check(*attend_case("e4m3", (4, 1, 128), 100, [470, 200], [100, 100]))
 
 
+@pytest.mark.parametrize("fmt", ["e4m3", "bf16"])
+@pytest.mark.parametrize("heads,n,ctx,rows", [
+    ((32, 32, 64), 50, [14000], [50]),              # 16 items fill the grid: chunks of 896 or so keys
+    ((16, 16, 64), 130, [3000, 0, 1000], [60, 130, 0]),
+])
+def test_cuts_of_row_blocks(fmt, heads, n, ctx, rows):
+    check(*attend_case(fmt, heads, n, ctx, rows))
+
+
 @pytest.mark.parametrize("heads,n,ctx", [
     ((32, 8, 128), 1, [5000, 3000, 4100]),       # cut into chunks of 384 or so keys
     ((8, 8, 64), 7, [2500, 1, 6300, 0, 700]),    # 640
