@@ -243,7 +243,8 @@ __global__ void __launch_bounds__(kBT) k_verify_setup(PoolDev p, VerifySetupArgs
   // 501-9001 tokens, 64-wide heads 25.9 -> 22.6 us; 8 of 4000-12000, 3 kv-heads 18.6 ->
   // 16.4; 4 of 40-900, 2 kv-heads 11.3 -> 8.9; 8 of 32001-32768 with 36 rows 109 -> 103.
   // Cuts that leave workgroups idle lose to several units each in any order (16 of
-  // 2000-40000: 78 us, even 87), so long ones have to be nearly even.
+  // 2000-40000: 78 us, even 87), so long ones have to be nearly even.  (bf16 pools, in
+  // plans: 0.59-1.08 of the other rule's time over 40 shapes.)
   const int u128 = (len + 127) / 128;
   if (t < a.B) s_mis[t] = u128;
   if (w * 64 < a.B) {
@@ -560,7 +561,7 @@ __global__ void __launch_bounds__(kBT) k_attend_plan_rows(PoolDev p, RowPlanArgs
     if ((s_long + ch - 1) / ch <= a.most_chunks)  // (else k may overflow)
       for (int b = lane; b < a.B; b += 64) k += items_of(s_ctx[b], s_n[b], ch);
     else
-      k = a.items_cap;
+      k = lane == 0 ? a.items_cap + 1 : 0;  // not taken
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) k += __shfl_xor(k, o, 64);
     if (lane == 0) s_cnt[c] = k;

@@ -487,6 +487,29 @@ def test_the_most_rows_of_a_request_and_the_most_requests():
             check(as64(out[b]), want, tol)
 
 
+def test_contexts_of_more_chunks_than_a_merge_takes():
+    """300000 tokens: 512-key chunks would be 587 partials of a row block, 512 are merged."""
+    war = _war()
+    cfg, ctx = cfg_of(8, 1, 64), 300000
+    pool = war.Pool(cfg, ctx // 16 + 3, 1, ctx // 16 + 3, device=DEV, kv_format="e4m3")
+    pool.alloc([0], [ctx + 30])
+    g = torch.Generator(device=DEV).manual_seed(14)
+    kv = torch.randn((2, 1, ctx + 30, 1, 64), device=DEV, generator=g).bfloat16()
+    kv[0, 0, ::50000] *= 6                                                     # keys that stand out in some chunks
+    war.kv_write(pool, 0, t32([0]), t32([0]), *kv)
+    k, v = e4m3.store_kv(as64(kv[0, 0]), as64(kv[1, 0]))
+    for n in (1, 6, 30):
+        q = torch.randn((1, n, 8, 64), device=DEV, generator=g).bfloat16()
+        plan, out = war.AttendPlan(pool, 1, n), torch.zeros_like(q)
+        plan.update(t32([0]), t32([ctx]))
+        war.attend(plan, 0, q, out)
+        assert pool.state()["status"] == 0
+        for i in {0, n - 1}:
+            want, tol = np.zeros((1, 8, 64)), np.zeros((1, 8, 64))
+            reference("e4m3", as64(q[0, i:i + 1]), k, v, ctx + i, 1, None, want, tol)
+            check(as64(out[0, i:i + 1]), want, tol)
+
+
 def test_an_object_serves_smaller_plans_and_another_stream():
     war = _war()
     cfg = cfg_of(8, 2, 64)
