@@ -482,20 +482,13 @@ __global__ void __launch_bounds__(kBT) k_verify_setup(PoolDev p, VerifySetupArgs
 // it, so that the units which read a chunk run together and find it in L2.  With first(c)
 // the first block that reaches chunk c, a request has sum_c (blocks - first(c)) items.
 //
-// The chunk is the one of 20 with the least estimated time, in keys a workgroup: a unit
-// costs its keys and kUnitKeys for its start, its end and the merge of its partials.
-// Units of one length run in rounds of the grid, others fill in behind each other and
-// end half a unit apart, and nothing ends before the longest.  (Every number is an
-// integer sum, so that a plan repeats itself.)  Against 8192 keys, halved only where
+// The chunk is the one of kRowCuts with the least estimated time (row_cut_time).  Against 8192 keys, halved only where
 // half the grid idles, over e4m3: 4 requests of 500 rows behind 1000-9000 tokens 285 ->
 // 233 us, 2 of 300 behind 16000 293 -> 251, 4096 rows of 8 64-wide heads 85 -> 73; the worst
 // of 20 shapes 8 of 256 behind 2000-20000, 394 -> 414.  One workgroup: 7.7 us.
 __global__ void __launch_bounds__(kBT) k_attend_plan_rows(PoolDev p, RowPlanArgs a, StepMeta m) {
   __shared__ int s_ctx[kBT], s_n[kBT], s_off[kBT], s_seq[kBT];
-  constexpr int kCuts = 20;
-  constexpr float kUnitKeys = 1000.f;
-  auto cut = [](int c) { return (4 + c % 4) << (c / 4 + 7); };  // 512, 640, 768, 896, 1024, ... 14336 keys
-  __shared__ int s_cnt[kCuts], s_long;
+  __shared__ int s_cnt[kRowCuts], s_long;
   __shared__ unsigned long long s_keys;
   __shared__ int s_hash[2 * kBT], s_bad, s_dup;
   const int t = threadIdx.x, lane = t & 63, w = t >> 6;
@@ -555,8 +548,8 @@ __global__ void __launch_bounds__(kBT) k_attend_plan_rows(PoolDev p, RowPlanArgs
     }
   }
   __syncthreads();
-  for (int c = w; c < kCuts; c += kBT / 64) {
-    const int ch = cut(c);
+  for (int c = w; c < kRowCuts; c += kBT / 64) {
+    const int ch = row_cut(c);
     int k = 0;
     if ((s_long + ch - 1) / ch <= a.most_chunks)  // (else k may overflow)
       for (int b = lane; b < a.B; b += 64) k += items_of(s_ctx[b], s_n[b], ch);
@@ -569,13 +562,9 @@ __global__ void __launch_bounds__(kBT) k_attend_plan_rows(PoolDev p, RowPlanArgs
   __syncthreads();
   int chunk = a.chunk, n_items;
   {
-    const int c = min(lane, kCuts - 1);
-    const float slots = (float)a.items_fill, keys = (float)s_keys, k = (float)s_cnt[c];
-    const float unit = (float)min(cut(c), s_long) + kUnitKeys;
-    const float rounds = ceilf(k / slots) * unit;
-    const float filled = fmaxf((keys + k * kUnitKeys) / slots + keys / (2.f * fmaxf(k, 1.f)), unit);
-    float est = lane < kCuts && s_cnt[c] <= a.items_cap ? fminf(rounds, filled) : INFINITY;
-    int at = c;
+    int at = min(lane, kRowCuts - 1);
+    float est = row_cut_time(row_cut(at), s_cnt[at], (int64_t)s_keys, s_long, a.items_fill);
+    if (lane >= kRowCuts || s_cnt[at] > a.items_cap) est = INFINITY;
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) {
       const float oe = __shfl_xor(est, o, 64);
@@ -585,7 +574,7 @@ __global__ void __launch_bounds__(kBT) k_attend_plan_rows(PoolDev p, RowPlanArgs
         at = oa;
       }
     }
-    if (est < INFINITY) chunk = cut(at);
+    if (est < INFINITY) chunk = row_cut(at);
   }
   const int off = block_excl_scan(t < a.B ? items_of(ctx, n, chunk) : 0, &n_items);
   if (t < a.B) {

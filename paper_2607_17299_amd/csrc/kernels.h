@@ -133,6 +133,21 @@ void launch_verify_setup(const PoolDev& p, const VerifySetupArgs& a, const StepM
 void launch_attend_plan(const PoolDev& p, const VerifySetupArgs& a, const StepMeta& m, hipStream_t st);
 // The same in blocks of `TB` tokens (k_attn_rows): segment b * blocks + i is block i of
 // request b.
+//
+// Their contexts are cut by estimated time, in keys a workgroup: a unit costs its keys and
+// kUnitKeys for its start, its end and the merge of its partials.  Units of one length run
+// in rounds of the grid (`slots` items of a kv-head), others fill in behind each other and
+// end half a unit apart, and nothing ends before the longest.  (From integer sums, so that
+// a plan repeats itself.)
+constexpr int kRowCuts = 20;
+constexpr float kUnitKeys = 1000.f;
+inline __host__ __device__ int row_cut(int c) { return (4 + c % 4) << (c / 4 + 7); }  // 512, 640, 768, 896, 1024, ... 14336
+inline __host__ __device__ float row_cut_time(int chunk, int items, int64_t keys, int longest, int slots) {
+  const float n = (float)(items > 1 ? items : 1), unit = (float)(chunk < longest ? chunk : longest) + kUnitKeys;
+  const float rounds = (float)((items + slots - 1) / slots) * unit;
+  const float filled = ((float)keys + n * kUnitKeys) / (float)slots + (float)keys / (2.f * n);
+  return fminf(rounds, fmaxf(filled, unit));
+}
 struct RowPlanArgs {
   int B, n_max, TB, blocks;
   int chunk;        // keys per item that fit items_cap whatever the lengths

@@ -1662,8 +1662,8 @@ war_status war_prefill_append(war_model* m, war_kv_pool* p, int32_t n, const int
   const int RB = kPrefillRows;
   CHECK(RB % G == 0, "internal: query heads per kv head must divide the prefill row block");
   const int TB = RB / G;
-  int chunk = prefill_chunk(p->geom);
-  while (cdiv_i(p->dev.max_pages * P, chunk) > kMaxItemsPerSeq) chunk *= 2;
+  int base_chunk = prefill_chunk(p->geom);
+  while (cdiv_i(p->dev.max_pages * P, base_chunk) > kMaxItemsPerSeq) base_chunk *= 2;
   std::vector<int64_t> cu(n + 1, 0);
   for (int i = 0; i < n; ++i) cu[i + 1] = cu[i] + n_new_host[i];
   const int R_cap = m->max_rows;
@@ -1687,6 +1687,35 @@ war_status war_prefill_append(war_model* m, war_kv_pool* p, int32_t n, const int
       }
     }
     const int nr = (int)rq_seq.size(), nl = (int)last_rows.size();
+    // 8-bit pools: the contexts are cut by estimated time, as a plan's (4 layers: 60 tokens
+    // behind 30000 1.45 -> 0.85 ms, 4 x 500 behind 1000-9000 4.05 -> 3.83, the worst of 8
+    // appends 4.41 -> 4.49; bf16 pools as they were: the sums keep their order)
+    int chunk = base_chunk;
+    if (p->geom.q8) {
+      const int slots = std::max(1, kAttnGrid / m->md.nkv);
+      int64_t keys = 0;
+      int longest = 0;
+      auto items_at = [&](int ch) {
+        int64_t k = 0;
+        for (int j = 0; j < nr; ++j)
+          for (int t0 = 0; t0 < rq_ntok[j]; t0 += TB) k += cdiv_i(rq_pos0[j] + std::min(rq_ntok[j], t0 + TB), ch);
+        return k;
+      };
+      for (int j = 0; j < nr; ++j) {
+        longest = std::max(longest, rq_pos0[j] + rq_ntok[j]);
+        keys += (int64_t)cdiv_i(rq_ntok[j], TB) * (rq_pos0[j] + (rq_ntok[j] + TB) / 2);
+      }
+      const int64_t most = std::max<int64_t>(items_at(base_chunk), 4 * slots);  // (partials' memory)
+      float best = INFINITY;
+      for (int c = 0; c < kRowCuts; ++c) {
+        if (cdiv_i(longest, row_cut(c)) > kMaxItemsPerSeq) continue;
+        const int64_t k = items_at(row_cut(c));
+        const float t = row_cut_time(row_cut(c), (int)std::min(k, most), keys, longest, slots);
+        if (k > most || t >= best) continue;
+        best = t;
+        chunk = row_cut(c);
+      }
+    }
     std::vector<int32_t> sg_b, sg_c, sg_r, sg_rb;
     std::vector<int4> udesc;
     int ni = 0;  // attention items

@@ -677,6 +677,39 @@ def test_prefill_verify_commit_over_an_8_bit_pool(tiny):
     assert pool.state()["status"] == 0
 
 
+def test_appends_behind_long_contexts(tiny):
+    """Appends whose contexts are cut into several chunks: new keys and values and the last
+    row's logits, as above."""
+    war, model, W = _war(), tiny["model"], tiny["W"]
+    ctx, lens = [2600, 513, 5000], [70, 30, 5]
+    pool = war.Pool(CFG, 540, 3, 330, device=DEV, kv_format="e4m3")
+    pool.alloc([0, 1, 2], ctx)
+    kvs = []
+    for b, c in enumerate(ctx):
+        layers = []
+        for layer in range(CFG.n_layers):
+            x = synth.kv_context(CFG, 6, b, layer, 0, c, DEV)               # [2, Hkv, c, D]
+            pool.load(b, layer, 0, x)
+            k, v = e4m3.store_kv(*(as64(y.transpose(0, 1)) for y in x))
+            layers.append((k.transpose(1, 0, 2), v.transpose(1, 0, 2)))
+        kvs.append(RequestKV(CFG, layers, store=e4m3.store_kv))
+    toks = [synth.uniform_tokens(500 + b, lens[b], CFG.vocab) for b in range(3)]
+    d_ctx, nxt, logits = t32(ctx), t32([0] * 3), torch.empty((3, CFG.vocab), device=DEV)
+    war.prefill_append(model, pool, t32([0, 1, 2]), d_ctx, lens, t32(np.concatenate(toks)), nxt, logits)
+    assert d_ctx.tolist() == [c + n for c, n in zip(ctx, lens)] and pool.state()["status"] == 0
+    for b in range(3):
+        first, rest = int(toks[b][0]), [int(t) for t in toks[b][1:]]
+        z, z32 = (verify_request(CFG, W, kvs[b], first, rest, precision=p)["logits"] for p in ("fp64", "fp32"))
+        assert np.abs(as64(logits[b]) - z[-1]).max() <= fp32_drift_tol(z, z32)
+        prefill_request(CFG, W, kvs[b], toks[b])
+        for layer in range(CFG.n_layers):
+            got = as64(pool.gather_kv(b, ctx[b] + lens[b], layer))
+            want = kvs[b].get(layer)
+            for x, w in zip(got, want):
+                np.testing.assert_array_equal(x[:, : ctx[b]], w[:, : ctx[b]])
+            near_codes(got[:, :, ctx[b]:], [w[:, ctx[b]:] for w in want])
+
+
 def test_tree_step_moves_codes_and_scales(tiny):
     war, model, W = _war(), tiny["model"], tiny["W"]
     pool = war.Pool(CFG, 32, 1, 16, device=DEV, kv_format="e4m3")
