@@ -141,7 +141,8 @@ void launch_attend_plan(const PoolDev& p, const VerifySetupArgs& a, const StepMe
 // a plan repeats itself.)
 constexpr int kRowCuts = 20;
 constexpr float kUnitKeys = 1000.f;
-inline __host__ __device__ int row_cut(int c) { return (4 + c % 4) << (c / 4 + 7); }  // 512, 640, 768, 896, 1024, ... 14336
+// 512 keys times 1, 9/8, 11/8, 13/8, 2, ... 26
+inline __host__ __device__ int row_cut(int c) { return (0xdb98 >> (4 * (c % 4)) & 15) << (c / 4 + 6); }
 inline __host__ __device__ float row_cut_time(int chunk, int items, int64_t keys, int longest, int slots) {
   const float n = (float)(items > 1 ? items : 1), unit = (float)(chunk < longest ? chunk : longest) + kUnitKeys;
   const float rounds = (float)((items + slots - 1) / slots) * unit;
