@@ -487,7 +487,7 @@ __global__ void __launch_bounds__(kBT) k_verify_setup(PoolDev p, VerifySetupArgs
 // 233 us, 2 of 300 behind 16000 293 -> 251, 4096 rows of 8 64-wide heads 85 -> 73; the worst
 // of 20 shapes 8 of 256 behind 2000-20000, 394 -> 414.  One workgroup: 7.7 us.
 __global__ void __launch_bounds__(kBT) k_attend_plan_rows(PoolDev p, RowPlanArgs a, StepMeta m) {
-  __shared__ int s_ctx[kBT], s_n[kBT], s_off[kBT], s_seq[kBT];
+  __shared__ int s_ctx[kBT], s_n[kBT], s_off[kBT], s_seq[kBT], s_whole[kBT], s_part[kBT];
   __shared__ int s_cnt[kRowCuts], s_long;
   __shared__ unsigned long long s_keys;
   __shared__ int s_hash[2 * kBT], s_bad, s_dup;
@@ -576,9 +576,17 @@ __global__ void __launch_bounds__(kBT) k_attend_plan_rows(PoolDev p, RowPlanArgs
     }
     if (est < INFINITY) chunk = row_cut(at);
   }
-  const int off = block_excl_scan(t < a.B ? items_of(ctx, n, chunk) : 0, &n_items);
+  const int mine = t < a.B ? items_of(ctx, n, chunk) : 0;
+  const int off = block_excl_scan(mine, &n_items);
+  // work order: every request's whole chunks, then what is left of each, so that the last
+  // units are short
+  const int whole = t < a.B ? (ctx + min(a.TB, n)) / chunk * ((n + a.TB - 1) / a.TB) : 0;
+  int n_whole, n_part;
+  const int woff = block_excl_scan(whole, &n_whole), poff = block_excl_scan(mine - whole, &n_part);
   if (t < a.B) {
     s_off[t] = off;
+    s_whole[t] = woff;
+    s_part[t] = n_whole + poff;
     s_seq[t] = s;
     m.req_seq[t] = s;
     m.req_pos0[t] = ctx;
@@ -605,8 +613,10 @@ __global__ void __launch_bounds__(kBT) k_attend_plan_rows(PoolDev p, RowPlanArgs
     for (int c = c0; c * chunk < S; ++c) begin += max(0, rb - first(s_ctx[b], c, chunk));
     m.seg_begin[i] = begin;
     m.seg_count[i] = (S + chunk - 1) / chunk;
-    int slot = s_off[b];  // work order chunk by chunk
+    const int nwc = (s_ctx[b] + min(a.TB, s_n[b])) / chunk;
+    int slot = s_whole[b];  // chunk by chunk
     for (int c = 0; c * chunk < S; ++c) {
+      if (c == nwc) slot = s_part[b];
       const int f = first(s_ctx[b], c, chunk);
       m.udesc[2 * (slot + rb - f)] = make_int4(begin + c, b, c, (rb * a.TB) | (ntk << 16));
       m.udesc[2 * (slot + rb - f) + 1] = make_int4(0, s_seq[b], s_ctx[b], b * a.n_max);
