@@ -482,10 +482,11 @@ __global__ void __launch_bounds__(kBT) k_verify_setup(PoolDev p, VerifySetupArgs
 // it, so that the units which read a chunk run together and find it in L2.  With first(c)
 // the first block that reaches chunk c, a request has sum_c (blocks - first(c)) items.
 //
-// The chunk is the one of kRowCuts with the least estimated time (row_cut_time).  Against 8192 keys, halved only where
-// half the grid idles, over e4m3: 4 requests of 500 rows behind 1000-9000 tokens 285 ->
-// 233 us, 2 of 300 behind 16000 293 -> 251, 4096 rows of 8 64-wide heads 85 -> 73; the worst
-// of 20 shapes 8 of 256 behind 2000-20000, 394 -> 414.  One workgroup: 7.7 us.
+// The chunk is the one of kRowCuts with the least estimated time (row_cut_time).  Against
+// 8192 keys, halved only where half the grid idles, over e4m3: 4 requests of 500 rows
+// behind 1000-9000 tokens 281 -> 224 us, 2 of 300 behind 16000 287 -> 234, 4096 rows of 8
+// 64-wide heads 85 -> 76; the worst of 20 shapes 8 of 256 behind 2000-20000, 390 -> 423.
+// One workgroup: 8 us.
 __global__ void __launch_bounds__(kBT) k_attend_plan_rows(PoolDev p, RowPlanArgs a, StepMeta m) {
   __shared__ int s_ctx[kBT], s_n[kBT], s_off[kBT], s_seq[kBT], s_whole[kBT], s_part[kBT];
   __shared__ int s_cnt[kRowCuts], s_long;
