@@ -485,7 +485,7 @@ __global__ void __launch_bounds__(kBT) k_verify_setup(PoolDev p, VerifySetupArgs
 // The chunk is the one of kRowCuts with the least estimated time (row_cut_time).  Against
 // 8192 keys, halved only where half the grid idles, over e4m3: 4 requests of 500 rows
 // behind 1000-9000 tokens 281 -> 224 us, 2 of 300 behind 16000 287 -> 234, 4096 rows of 8
-// 64-wide heads 85 -> 76; the worst of 20 shapes 8 of 256 behind 2000-20000, 390 -> 423.
+// 64-wide heads 85 -> 76; the worst of 20 shapes 2048 behind 8000, 379 -> 390.
 // One workgroup: 8 us.
 __global__ void __launch_bounds__(kBT) k_attend_plan_rows(PoolDev p, RowPlanArgs a, StepMeta m) {
   __shared__ int s_ctx[kBT], s_n[kBT], s_off[kBT], s_seq[kBT], s_whole[kBT], s_part[kBT];
@@ -563,19 +563,14 @@ __global__ void __launch_bounds__(kBT) k_attend_plan_rows(PoolDev p, RowPlanArgs
   __syncthreads();
   int chunk = a.chunk, n_items;
   {
-    int at = min(lane, kRowCuts - 1);
+    const int at = min(lane, kRowCuts - 1);
     float est = row_cut_time(row_cut(at), s_cnt[at], (int64_t)s_keys, s_long, a.items_fill);
     if (lane >= kRowCuts || s_cnt[at] > a.items_cap) est = INFINITY;
+    float least = est;
 #pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) {
-      const float oe = __shfl_xor(est, o, 64);
-      const int oa = __shfl_xor(at, o, 64);
-      if (oe < est || (oe == est && oa < at)) {
-        est = oe;
-        at = oa;
-      }
-    }
-    if (est < INFINITY) chunk = row_cut(at);
+    for (int o = 32; o >= 1; o >>= 1) least = fminf(least, __shfl_xor(least, o, 64));
+    const unsigned long long near = __ballot(est < INFINITY && est <= least * kCutNear);
+    if (near) chunk = row_cut(63 - __clzll((long long)near));
   }
   const int mine = t < a.B ? items_of(ctx, n, chunk) : 0;
   const int off = block_excl_scan(mine, &n_items);

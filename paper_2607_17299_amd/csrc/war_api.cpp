@@ -1706,15 +1706,14 @@ war_status war_prefill_append(war_model* m, war_kv_pool* p, int32_t n, const int
         keys += (int64_t)cdiv_i(rq_ntok[j], TB) * (rq_pos0[j] + (rq_ntok[j] + TB) / 2);
       }
       const int64_t most = std::max<int64_t>(items_at(base_chunk), 4 * slots);  // (partials' memory)
-      float best = INFINITY;
+      float time[kRowCuts], least = INFINITY;
       for (int c = 0; c < kRowCuts; ++c) {
-        if (cdiv_i(longest, row_cut(c)) > kMaxItemsPerSeq) continue;
-        const int64_t k = items_at(row_cut(c));
-        const float t = row_cut_time(row_cut(c), (int)std::min(k, most), keys, longest, slots);
-        if (k > most || t >= best) continue;
-        best = t;
-        chunk = row_cut(c);
+        const int64_t k = cdiv_i(longest, row_cut(c)) > kMaxItemsPerSeq ? most + 1 : items_at(row_cut(c));
+        time[c] = k > most ? INFINITY : row_cut_time(row_cut(c), (int)k, keys, longest, slots);
+        least = std::min(least, time[c]);
       }
+      for (int c = 0; c < kRowCuts; ++c)
+        if (time[c] < INFINITY && time[c] <= least * kCutNear) chunk = row_cut(c);
     }
     std::vector<int32_t> sg_b, sg_c, sg_r, sg_rb;
     std::vector<int4> udesc;
