@@ -86,8 +86,8 @@ struct Profiler {
     return pool[used++];
   }
 };
-// keys per attention item when prefilling (chunk-major: L2 serves the row blocks); twice
-// as many in half the bytes
+// keys per attention item when prefilling (chunk-major: L2 serves the row blocks); in 8
+// bits twice as many, and only the length that room is made for (row_cut_time)
 constexpr int kPrefillChunk = 4096;
 inline int prefill_chunk(const KvGeom& g) { return g.q8 ? 2 * kPrefillChunk : kPrefillChunk; }
 constexpr int kPrefillRows = 128;    // attention rows per prefill row block (k_attn_rows)
