@@ -486,7 +486,7 @@ __global__ void __launch_bounds__(kBT) k_verify_setup(PoolDev p, VerifySetupArgs
 // 8192 keys, halved only where half the grid idles, over e4m3: 4 requests of 500 rows
 // behind 1000-9000 tokens 281 -> 224 us, 2 of 300 behind 16000 287 -> 234, 4096 rows of 8
 // 64-wide heads 85 -> 76; the worst of 20 shapes 2048 behind 8000, 379 -> 390.
-// One workgroup: 8 us.
+// One workgroup: 9 us.
 __global__ void __launch_bounds__(kBT) k_attend_plan_rows(PoolDev p, RowPlanArgs a, StepMeta m) {
   __shared__ int s_ctx[kBT], s_n[kBT], s_off[kBT], s_seq[kBT], s_whole[kBT], s_part[kBT];
   __shared__ int s_cnt[kRowCuts], s_long;
