@@ -230,7 +230,9 @@ war_status war_attend_update(war_attend* a, int32_t B, int32_t n_max, const int3
                              void* stream);
 
 /* o = softmax(q k / sqrt(head_dim)) v of the planned rows in one layer; row i of request
- * b sees the keys 0 .. ctx_b + i (a tree's node the context and its root path).
+ * b sees the keys 0 .. ctx_b + i (a tree's node the context and its root path).  Over
+ * either kind of pool the weights keep 16 bits for the product with the values, and the
+ * sums are fp32.
  *   q, o   device bf16, row b * n_max + i at that many strides, n_q_heads * head_dim
  *          elements; strides in elements, multiples of 8; 16-byte aligned.  Rows of o
  *          beyond n_lens are left as they were. */

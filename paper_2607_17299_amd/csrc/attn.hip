@@ -25,7 +25,9 @@
 // An e4m3 pool (Q8) halves the bytes.  A block's codes are converted to bf16 in
 // registers, which is exact: keys with their token's scale by the conversion itself,
 // values without, their scales multiply the weights (a lane holds the weights of eight
-// tokens of one row), whose sum stays without them.  16 bytes of a lane are two k-steps
+// tokens of one row), whose sum stays without them.  One bf16 a weight in place of hi + lo
+// would save 1-4% of the time (8 requests of 32001-32768 tokens, nine rows each, with the
+// merge: 108.0 against 109.5 us).  16 bytes of a lane are two k-steps
 // of a key (k-step j covers dims 64 (j / 2) + 16 g + 8 (j % 2) + 0..7 of lane group g)
 // or its eight keys in two output tiles.
 // HBM bounds it with one row tile (64 requests of 1024-65536 tokens, 32 / 8 heads of 128:
@@ -237,9 +239,9 @@ k_attn(AttnArgs a) {
     };
 
     // The first block is requested before the queries are staged, and each
-    // next block as soon as the current one is computed -- except with three
-    // row tiles, which lack the registers for a block held across those points
-    // and load each block right before computing it.
+    // next block as soon as the current one is computed -- except in bf16 with
+    // three row tiles, which lack the registers for a block held across those
+    // points and load each block right before computing it.
     constexpr bool kEarlyLoad = Q8 || NR < 3;
     KVFrag<HD, Q8> f0;
     [[maybe_unused]] KVFrag<HD, Q8> f1;  // one more block in flight while a block is computed
@@ -309,13 +311,11 @@ k_attn(AttnArgs a) {
     };
 
     float m_run[NR], l_run[NR];
-    [[maybe_unused]] f32x4 l_acc[NR];
     f32x4 o_acc[NDT][NR];
 #pragma unroll
     for (int rt = 0; rt < NR; ++rt) {
       m_run[rt] = -INFINITY;
       l_run[rt] = 0.f;
-      l_acc[rt] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int dt = 0; dt < NDT; ++dt) o_acc[dt][rt] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
@@ -355,7 +355,6 @@ k_attn(AttnArgs a) {
         if (mx > m_run[rt] + 8.f) {
           const float alpha = exp2f(m_run[rt] - mx);
           l_run[rt] *= alpha;
-          if constexpr (Q8) l_acc[rt] *= alpha;
 #pragma unroll
           for (int dt = 0; dt < NDT; ++dt) o_acc[dt][rt] *= alpha;
           m_run[rt] = mx;
@@ -473,11 +472,9 @@ k_attn(AttnArgs a) {
       }
       const float vsc[8] = {scale_of<0>(vs.x), scale_of<1>(vs.x), scale_of<2>(vs.x), scale_of<3>(vs.x),
                             scale_of<0>(vs.y), scale_of<1>(vs.y), scale_of<2>(vs.y), scale_of<3>(vs.y)};
-      // One bf16 a weight (half a step is 2^-8 of it at most, a number of the cache is off
-      // by 2^-4 of it); the row sum is taken of the rounded weights, by the matrix core, so
-      // that what rounds alike cancels.  A scale is a power of two: the weights times
-      // scales round to the rounded weights times scales.
-      bf16x8 pw[NR];
+      // The weights times the values' scales (powers of two: exact) as bf16 hi + lo, as over
+      // bf16 pools; their sum is of the weights themselves.
+      bf16x8 ph[NR], pl[NR];
 #pragma unroll
       for (int rt = 0; rt < NR; ++rt) {
         float sv[8];
@@ -487,18 +484,21 @@ k_attn(AttnArgs a) {
           sv[4 + i] = s1[rt][i];
         }
         const float m_use = tile_max(sv, rt, kb, mask_tag);
-        uint32_t w[4], ws[4];
+        float sum = 0.f;
+        uint32_t hi[4], lo[4];
 #pragma unroll
         for (int e = 0; e < 8; e += 2) {
-          const float p0 = __builtin_amdgcn_exp2f(fmaf(sv[e], a.scale_log2, -m_use));
-          const float p1 = __builtin_amdgcn_exp2f(fmaf(sv[e + 1], a.scale_log2, -m_use));
-          w[e / 2] = pack2(p0, p1);
-          ws[e / 2] = pack2(p0 * vsc[e], p1 * vsc[e + 1]);
+          float p0 = __builtin_amdgcn_exp2f(fmaf(sv[e], a.scale_log2, -m_use));
+          float p1 = __builtin_amdgcn_exp2f(fmaf(sv[e + 1], a.scale_log2, -m_use));
+          sum += p0 + p1;
+          p0 *= vsc[e];
+          p1 *= vsc[e + 1];
+          hi[e / 2] = pack2(p0, p1);
+          lo[e / 2] = pack2(p0 - lo_f(hi[e / 2]), p1 - hi_f(hi[e / 2]));
         }
-        constexpr uint32_t one2 = 0x3f803f80u;
-        l_acc[rt] = mfma16(as_bf16x8(make_uint4(one2, one2, one2, one2)), as_bf16x8(make_uint4(w[0], w[1], w[2], w[3])),
-                           l_acc[rt]);
-        pw[rt] = as_bf16x8(make_uint4(ws[0], ws[1], ws[2], ws[3]));
+        l_run[rt] += sum;
+        ph[rt] = as_bf16x8(make_uint4(hi[0], hi[1], hi[2], hi[3]));
+        pl[rt] = as_bf16x8(make_uint4(lo[0], lo[1], lo[2], lo[3]));
       }
 #pragma unroll
       for (int dt = 0; dt < NDT; ++dt) {
@@ -507,7 +507,10 @@ k_attn(AttnArgs a) {
         if constexpr (MASK) cv = keep_first8(cv, nvalid);
         const bf16x8 v = as_bf16x8(from_e4m3x8(cv.x, cv.y, 1.f));
 #pragma unroll
-        for (int rt = 0; rt < NR; ++rt) o_acc[dt][rt] = mfma16(v, pw[rt], o_acc[dt][rt]);
+        for (int rt = 0; rt < NR; ++rt) {
+          o_acc[dt][rt] = mfma16(v, ph[rt], o_acc[dt][rt]);
+          o_acc[dt][rt] = mfma16(v, pl[rt], o_acc[dt][rt]);
+        }
       }
       if constexpr (REFILL) load_v(f, npg0, npg1);
     };
@@ -577,11 +580,9 @@ k_attn(AttnArgs a) {
     // ---- merge the 4 waves (fixed order) and write the item's partial
 #pragma unroll
     for (int rt = 0; rt < NR; ++rt) {
-      float l = Q8 ? l_acc[rt][0] : l_run[rt];
-      if constexpr (!Q8) {
-        l += __shfl_xor(l, 16, 64);
-        l += __shfl_xor(l, 32, 64);
-      }
+      float l = l_run[rt];
+      l += __shfl_xor(l, 16, 64);
+      l += __shfl_xor(l, 32, 64);
       if (lg == 0) {
         s_m[w][rt * 16 + ln] = m_run[rt];
         s_l[w][rt * 16 + ln] = l;

@@ -19,12 +19,12 @@
 // An e4m3 pool (Q8): the workgroup's threads take 16 codes each of a block's keys and
 // values to registers, two steps later to bf16 (exact: codes times their token's scale)
 // and to the same places in LDS, two steps before the block's scores.  So each code is
-// converted once a workgroup, and the products and softmax are the same.  A wave's
-// pieces are of one page, so that the addresses are scalar (1355 -> 1325 us), the row sums
-// are v_dot2 of the weights (two products of ones before) and operands are read two
-// fragments ahead instead of one (1307).  2048 and 2011 rows of 32 heads behind 9001 and
-// 24576 tokens, the merge among it: 1279 us, 921 TFLOP/s; the matrix pipes are busy 43% of
-// all cycles, the VALU 57%, and two waves a SIMD wait for neither most of the rest.
+// converted once a workgroup, and the products and softmax are the same, weights in hi + lo
+// among them.  A wave's pieces are of one page, so that the addresses are scalar; the
+// compiler may order the work of the slots (barriers between them cost 1% and spill).
+// 2048 and 2011 rows of 32 heads behind 9001 and 24576 tokens, the merge among it: 1681 us
+// against 1677 over a bf16 pool on the same box.  (One bf16 a weight: 1311 us, a third fewer
+// matrix instructions, and results off by 2^-9 of every weight.)
 // 2048 rows of 32 heads over 25600 keys (head_dim 128): 1403 -> 1151-1162 us (the
 // kernel it replaces staged blocks through registers and took scores, softmax and
 // product one after the other).  Over an append of 16 x 2048 tokens to 8192-26624 keys
@@ -42,12 +42,6 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 WAR_DEV f32x16 mfma32(bf16x8 a, bf16x8 b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
-}
-
-// c + the two bf16 of a times those of b
-WAR_DEV float dot2(uint32_t a, uint32_t b, float c) {
-  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, a), __builtin_bit_cast(bf16x2, b), c, false);
 }
 
 // One unit's rows and keys, decoded from its work-order descriptor (the fields
@@ -257,7 +251,6 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
       return as_bf16x8(*reinterpret_cast<const uint4*>(smem + stage * SB + f * 1024 + vread));
     };
     f32x16 zero;
-    [[maybe_unused]] constexpr uint32_t one2 = 0x3f803f80u;
 #pragma unroll
     for (int e = 0; e < 16; ++e) zero[e] = 0.f;
     auto scores = [&](int stage, f32x16& s) __attribute__((always_inline)) {
@@ -298,12 +291,9 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
       for (int f = 0; f < LOOK; ++f) read(f);
       float lm = 0.f, m_new = 0.f, m_use = 0.f, sum = 0.f, p0 = 0.f, p1 = 0.f;
       uint32_t hi[8], lo[8];
-      // Q8: one product of a bf16 a weight (see k_attn), the row sum taken of the rounded
-      // weights, and a part of the conversion (block i + 2 to LDS) in each of three slots.
-      // The compiler may move work between these slots, held by the pairs' order alone
-      // (1307 us with barriers between the slots, 1279 without, at the size above)
-      constexpr int PV = Q8 ? 1 : 2;                                      // products of a value fragment
-      constexpr int SLOTS = (1 + PV) * KF, HEAD = 3 * KF / 8;  // the row maximum takes the first HEAD slots
+      // Q8: a part of the conversion (block i + 2 to LDS) in each of three slots, and no
+      // barriers between the slots.
+      constexpr int SLOTS = 3 * KF, HEAD = 3 * KF / 8;  // the row maximum takes the first HEAD slots
       auto softmax = [&](int t) __attribute__((always_inline)) {  // task t of 16: half of the work of a pair of keys
         const int e = t / 2 * 2;
         if (t % 2 == 0) {
@@ -314,24 +304,19 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
           hi[e / 2] = pack2(p0, p1);
           asm volatile("" : "+v"(hi[e / 2]), "+v"(p0), "+v"(p1));
         } else {
-          if constexpr (Q8) {
-            sum = dot2(hi[e / 2], one2, sum);
-            asm volatile("" : "+v"(sum));
-          } else {
-            sum += p0 + p1;
-            lo[e / 2] = pack2(p0 - lo_f(hi[e / 2]), p1 - hi_f(hi[e / 2]));
-            asm volatile("" : "+v"(lo[e / 2]), "+v"(sum));
-          }
+          sum += p0 + p1;
+          lo[e / 2] = pack2(p0 - lo_f(hi[e / 2]), p1 - hi_f(hi[e / 2]));
+          asm volatile("" : "+v"(lo[e / 2]), "+v"(sum));
         }
       };
 #pragma unroll
       for (int z = 0; z < SLOTS; ++z) {
-        const int f = z / (1 + PV);
-        if (z % (1 + PV) == 0) {
+        const int f = z / 3;
+        if (z % 3 == 0) {
           if (f + LOOK < KF) read(f + LOOK);
           snext = mfma32(rk[f % RING], qf[f], f == 0 ? zero : snext);
         } else {
-          o_acc[f % NDT] = mfma32(rv[f % RING], as_bf16x8(z % (1 + PV) == 1 ? pin.hi[f / NDT] : pin.lo[f / NDT]), o_acc[f % NDT]);
+          o_acc[f % NDT] = mfma32(rv[f % RING], as_bf16x8(z % 3 == 1 ? pin.hi[f / NDT] : pin.lo[f / NDT]), o_acc[f % NDT]);
         }
         if constexpr (Q8) {
           constexpr int Q = SLOTS / 3;
@@ -357,7 +342,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
 #pragma unroll
       for (int pg = 0; pg < 2; ++pg) {
         pout.hi[pg] = make_uint4(hi[pg * 4], hi[pg * 4 + 1], hi[pg * 4 + 2], hi[pg * 4 + 3]);
-        if constexpr (!Q8) pout.lo[pg] = make_uint4(lo[pg * 4], lo[pg * 4 + 1], lo[pg * 4 + 2], lo[pg * 4 + 3]);
+        pout.lo[pg] = make_uint4(lo[pg * 4], lo[pg * 4 + 1], lo[pg * 4 + 2], lo[pg * 4 + 3]);
       }
       if constexpr (Q8) fetch(cd, k0, k1);  // block i + 4, in the place of the one just converted
       if (__any(m_new != m_run)) {
@@ -434,7 +419,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
           uint4 v = __builtin_bit_cast(uint4, vfrag(lb & 3, pg * NDT + dt));
           if (kb + 32 > S) v = keep_first(v, min(max(S - (kb + 16 * pg + 8 * g), 0), 8));
           o_acc[dt] = mfma32(as_bf16x8(v), as_bf16x8(pa.hi[pg]), o_acc[dt]);
-          if constexpr (!Q8) o_acc[dt] = mfma32(as_bf16x8(v), as_bf16x8(pa.lo[pg]), o_acc[dt]);
+          o_acc[dt] = mfma32(as_bf16x8(v), as_bf16x8(pa.lo[pg]), o_acc[dt]);
         }
       }
     }
