@@ -22,8 +22,8 @@
 // converted once a workgroup, and the products and softmax are the same, weights in hi + lo
 // among them.  A wave's pieces are of one page, so that the addresses are scalar; the
 // compiler may order the work of the slots (barriers between them cost 1% and spill).
-// 2048 and 2011 rows of 32 heads behind 9001 and 24576 tokens, the merge among it: 1681 us
-// against 1677 over a bf16 pool on the same box.  (One bf16 a weight: 1311 us, a third fewer
+// 2048 and 2011 rows of 32 heads behind 9001 and 24576 tokens, the merge among it: 1752 us
+// where the same over a bf16 pool takes 1690.  (One bf16 a weight: 1340 us, a third fewer
 // matrix instructions, and results off by 2^-9 of every weight.)
 // 2048 rows of 32 heads over 25600 keys (head_dim 128): 1403 -> 1151-1162 us (the
 // kernel it replaces staged blocks through registers and took scores, softmax and
@@ -208,9 +208,15 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))
       if (part == 2 && vmine) {
         const float f[8] = {scale_of<0>(c.vs.x), scale_of<1>(c.vs.x), scale_of<2>(c.vs.x), scale_of<3>(c.vs.x),
                             scale_of<0>(c.vs.y), scale_of<1>(c.vs.y), scale_of<2>(c.vs.y), scale_of<3>(c.vs.y)};
+        // a value that reads as infinite (256 * 2^120) is the largest bf16 here: rows that do
+        // not see it have zero weights for it, and 0 * inf is NaN (3% of the time)
+        auto two = [](float a, float b) __attribute__((always_inline)) {
+          constexpr float most = 0x1.fep127f;
+          return pack2(__builtin_amdgcn_fmed3f(a, -most, most), __builtin_amdgcn_fmed3f(b, -most, most));
+        };
         auto eight = [&](uint32_t w0, uint32_t w1) __attribute__((always_inline)) {
-          return make_uint4(pack2(from_e4m3<0>(w0, f[0]), from_e4m3<1>(w0, f[1])), pack2(from_e4m3<2>(w0, f[2]), from_e4m3<3>(w0, f[3])),
-                            pack2(from_e4m3<0>(w1, f[4]), from_e4m3<1>(w1, f[5])), pack2(from_e4m3<2>(w1, f[6]), from_e4m3<3>(w1, f[7])));
+          return make_uint4(two(from_e4m3<0>(w0, f[0]), from_e4m3<1>(w0, f[1])), two(from_e4m3<2>(w0, f[2]), from_e4m3<3>(w0, f[3])),
+                            two(from_e4m3<0>(w1, f[4]), from_e4m3<1>(w1, f[5])), two(from_e4m3<2>(w1, f[6]), from_e4m3<3>(w1, f[7])));
         };
         unsigned char* d = smem + (ST + stage) * SB + vdst;
         *reinterpret_cast<uint4*>(d) = eight(c.v.x, c.v.y);

@@ -783,3 +783,23 @@ def test_noalloc_and_sampled_steps_agree_with_the_plain_step(tiny):
         res.append((acc.tolist(), nx.tolist(), z.clone()))
     for r in res[1:]:
         assert r[:2] == res[0][:2] and torch.equal(r[2], res[0][2])
+
+
+@pytest.mark.parametrize("n", [4, 30])
+def test_a_value_that_reads_as_infinite_reaches_only_the_rows_that_see_it(n):
+    """Above 1.9375 * 2^127 a finite number's code stands for 2^128.  Two heads' worth of
+    rows, row 2's own token; all keys in one 32-key block, or in two."""
+    def spoil(b, k, v):
+        v[0, 12 + b, 0, 3] = 1.96 * 2.0 ** 127
+        v[0, 12 + b, 1, 40] = -1.96 * 2.0 ** 127
+    got, want, tol = attend_case("e4m3", (8, 2, 64), n, [10, 11], [n, n], spoil=spoil)
+    for b, first in ((0, 2), (1, 2)):
+        assert np.isfinite(got[b, :first]).all()
+        check(got[b, :first], want[b, :first], tol[b, :first])
+        for h, d in ((0, 3), (1, 40)):
+            heads = slice(4 * h, 4 * h + 4)
+            other = np.delete(np.arange(64), d)
+            seen = got[b, first:, heads, d]
+            assert not np.isnan(seen).any() and (np.sign(seen) == (-1) ** h).all()
+            sub = np.ix_(np.arange(first, n), np.arange(4 * h, 4 * h + 4), other)
+            check(got[b][sub], want[b][sub], tol[b][sub])
