@@ -523,9 +523,12 @@ def constrain_logits(logits: torch.Tensor, constraints: Constraints, seq_ids: to
     if greedy is not None:
         need = fn.war_constrain_workspace(rows, V)
         if workspace is None:
-            workspace = torch.empty(max(need, 0), dtype=torch.uint8, device=dev)
-            if stream is not None:
-                workspace.record_stream(stream)  # its memory is free once that stream is done
+            make = lambda: torch.empty(max(need, 0), dtype=torch.uint8, device=dev)
+            if stream is None:
+                workspace = make()
+            else:  # that stream's own memory: what another one freed may still be in use there
+                with torch.cuda.stream(stream):
+                    workspace = make()
         _require(workspace.device == dev and workspace.is_contiguous() and
                  workspace.numel() * workspace.element_size() >= need, f"workspace must hold {need} bytes on {dev}")
     ls = logits.stride(0) if rows > 1 else V

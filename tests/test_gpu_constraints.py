@@ -520,3 +520,32 @@ def test_refusals(tiny):
     step(good)                                                                   # nothing above left a step behind
     war.kv_commit(pool, seq, ctx, acc)
     assert pool.state()["status"] == 0
+
+
+def test_a_workspace_made_for_a_stream_is_that_streams_memory():
+    """Memory that the current stream still reads, freed and free to be reused there, is
+    not written by a call on another stream."""
+    war = _war()
+    c = Case(4096, 64, 3, 5, odd=False)
+    cons, z = c.constraints(), f32(c.z)
+    R = c.B * (c.k + 1)
+    seq, last, drafts, lens = t32(c.seq), t32(c.last), t32(c.drafts[:, : c.k]), t32(c.lens)
+    greedy, want = torch.empty(R, dtype=torch.int32, device=DEV), torch.empty(R, dtype=torch.int32, device=DEV)
+    want.fill_(77), greedy.fill_(77)
+    war.constrain_logits(z, cons, seq, last, drafts, lens, c.k, greedy=want)
+    other = torch.cuda.Stream()
+    n = war.lib().war_constrain_workspace(R, c.V)
+    gc.collect()
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    for _ in range(4):
+        x = torch.full((n,), 9, dtype=torch.uint8, device=DEV)
+        y = torch.empty_like(x)
+        torch.cuda.synchronize()
+        torch.cuda._sleep(20_000_000)
+        y.copy_(x)                                     # waits behind the sleep
+        del x
+        war.constrain_logits(z, cons, seq, last, drafts, lens, c.k, greedy=greedy, stream=other)
+        torch.cuda.synchronize()
+        assert (y == 9).all()
+        assert torch.equal(greedy, want)
