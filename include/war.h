@@ -171,7 +171,8 @@ war_status war_kv_free(war_kv_pool* p, int32_t n, const int32_t* seq_ids_host, v
 
 /* Write precomputed keys/values of tokens [pos0, pos0 + n) of one layer of one
  * sequence into its pages (capacity must already be there, e.g. war_kv_alloc).
- * src: bf16 [2][n_kv_heads][n][head_dim] (0 = keys after RoPE, 1 = values).
+ * src: bf16 [2][n_kv_heads][n][head_dim] (0 = keys after RoPE, 1 = values), 2-byte
+ * aligned.
  * Imports a cached context computed elsewhere: the scheduler places a
  * request on the replica whose cache already holds its prefix, and a
  * trajectory's KV is reused across turns instead of recomputed (System

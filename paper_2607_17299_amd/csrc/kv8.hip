@@ -66,17 +66,13 @@ __device__ bool span_of(const KvMoveArgs& a, Span& s) {
   return true;
 }
 
-// R numbers (8, or 4 at head_dim 64) of a row
+// R numbers (8, or 4 at head_dim 64) of a row, which may begin at any element (an import's
+// source): still one load, which the hardware takes at any address
 template <int R>
 WAR_DEV void load_row(const bf16_t* p, float* x) {
-  uint32_t w[R / 2];
-  if constexpr (R == 8) {
-    const uint4 u = *reinterpret_cast<const uint4*>(p);
-    w[0] = u.x, w[1] = u.y, w[2] = u.z, w[3] = u.w;
-  } else {
-    const uint2 u = *reinterpret_cast<const uint2*>(p);
-    w[0] = u.x, w[1] = u.y;
-  }
+  typedef uint32_t words_t __attribute__((ext_vector_type(R / 2)));
+  typedef words_t any_t __attribute__((aligned(2), may_alias));
+  const words_t w = *reinterpret_cast<const any_t*>(p);
 #pragma unroll
   for (int i = 0; i < R / 2; ++i) x[2 * i] = lo_f(w[i]), x[2 * i + 1] = hi_f(w[i]);
 }

@@ -803,3 +803,19 @@ def test_a_value_that_reads_as_infinite_reaches_only_the_rows_that_see_it(n):
             assert not np.isnan(seen).any() and (np.sign(seen) == (-1) ** h).all()
             sub = np.ix_(np.arange(first, n), np.arange(4 * h, 4 * h + 4), other)
             check(got[b][sub], want[b][sub], tol[b][sub])
+
+
+@pytest.mark.parametrize("heads", [(4, 2, 64), (16, 2, 128)])
+@pytest.mark.parametrize("fmt", ["e4m3", "bf16"])
+def test_an_import_may_begin_at_any_element(heads, fmt):
+    cfg = cfg_of(*heads)
+    n = 37
+    g = torch.Generator(device=DEV).manual_seed(4)
+    flat = torch.randn(2 * cfg.n_kv_heads * n * cfg.head_dim + 8, device=DEV, generator=g).bfloat16()
+    for at in (0, 1, 2, 3, 5, 7):
+        src = flat[at: at + flat.numel() - 8].view(2, cfg.n_kv_heads, n, cfg.head_dim)
+        assert src.data_ptr() % 16 == 2 * at
+        pools = [scattered_pool(cfg, [n + 5], fmt) for _ in range(2)]
+        pools[0].load(0, 0, 5, src)
+        pools[1].load(0, 0, 5, src.clone())
+        assert torch.equal(pools[0].kv.view(torch.uint8), pools[1].kv.view(torch.uint8))
