@@ -176,10 +176,9 @@ __global__ void __launch_bounds__(kBT) k_verify_setup(PoolDev p, VerifySetupArgs
   if (t < a.B) {
     if constexpr (!PLAN) dl = min(max(dl, 0), a.k_max);
     // a bad id, a negative length or a request beyond its block-table row
-    // fails the whole step (no page moves, no row is active)
-    if (s < 0 || s >= p.max_seqs || ctx < 0 ||
-        (PLAN ? dl < -1 || dl > a.k_max || (int64_t)ctx + dl + 1 > (int64_t)p.held[s] * kPage
-              : cdiv_i(ctx + dl + 1, kPage) > p.max_pages)) {
+    // fails the whole step (no page moves, no row is active); lengths may be any number
+    if (s < 0 || s >= p.max_seqs || ctx < 0 || (PLAN && (dl < -1 || dl > a.k_max)) ||
+        (int64_t)ctx + dl + 1 > (int64_t)(PLAN ? p.held[s] : p.max_pages) * kPage) {
       s = 0;
       ctx = 0;
       atomicOr(&s_bad, 1);

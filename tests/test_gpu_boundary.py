@@ -138,3 +138,35 @@ def test_steady_loop_never_waits_for_the_free_count(tiny):
         torch.cuda.synchronize()
     assert pool.waits() == w0
     assert pool.state()["stack"].size == free0
+
+
+@pytest.mark.parametrize("far", [2**31 - 1, 2**31 - 2, 2**31 - 5, 2**31 - 17, 2**30])
+@pytest.mark.parametrize("k", [0, 3])
+def test_the_largest_context_lengths_fail_the_step(tiny, far, k):
+    """ctx + drafts + 1 passes 2^31: chain, tree, sampled, noalloc and constrained steps."""
+    war, model = tiny
+    pool, ctx, nxt = _prefilled(war, model, [20, 30])
+    before = _snapshot(pool)
+    seq, bad = _t([0, 1]), _t([20, far])
+    drafts = _t(np.arange(2 * k).reshape(2, k) % CFG.vocab) if k else None
+    parents = _t([list(range(k))] * 2) if k else None
+    u = torch.zeros((2 * (k + 1), 2), device=DEV)
+    cons = war.Constraints(CFG.vocab, repetition=torch.ones(3, device=DEV))
+    steps = {
+        "chain": lambda acc, out: war.verify_step(model, pool, seq, bad, nxt, drafts, None, k, acc, out),
+        "sampled": lambda acc, out: war.verify_step_sampled(model, pool, seq, bad, nxt, drafts, None, k, u, 1.0, 5, acc, out),
+        "noalloc": lambda acc, out: war.verify_step_noalloc(model, pool, seq, bad, nxt, drafts, None, k, acc, out),
+        "constrained": lambda acc, out: war.verify_step_constrained(model, pool, seq, bad, nxt, drafts, None, k, cons, acc, out),
+    }
+    if k:
+        steps["tree"] = lambda acc, out: war.verify_step_tree(model, pool, seq, bad, nxt, drafts, parents, None, k, acc, out,
+                                                              _t(np.zeros((2, k))))
+    for name, step in steps.items():
+        acc, out = _t([7, 7]), _t([7, 7])
+        step(acc, out)
+        war.kv_commit(pool, seq, bad, acc)
+        torch.cuda.synchronize()
+        assert acc.cpu().tolist() == [-1, -1] and out.cpu().tolist() == [-1, -1], name
+        assert bad.cpu().tolist() == [20, far], name
+        _flagged(war, pool, "context length")
+        _same(before, _snapshot(pool))
