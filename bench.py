@@ -62,6 +62,11 @@ def parse():
     return ap.parse_args()
 
 
+def result_dtype(kv_format: str) -> str:
+    """What a line's figures are computed in: bf16 throughout, or bf16 on 8-bit caches."""
+    return "bf16" if kv_format == "bf16" else f"bf16, keys and values {kv_format}"
+
+
 def log(msg):
     print(f"[bench] {msg}", file=sys.stderr, flush=True)
 
@@ -471,7 +476,8 @@ def main():
     out = {
         "metric": METRIC, "value": e["accepted_tokens_per_s"], "unit": "accepted tokens/s", "n_gpus": 1,
         "steps": args.steps, "warmup": args.warmup, "ms_per_step": e["ms_per_step"],
-        "higher_is_better": True, "scaling": "weak", "vs_baseline": None, "dtype": "bf16",
+        "higher_is_better": True, "scaling": "weak", "vs_baseline": None,
+        "dtype": result_dtype(args.kv_format),
         "data": "synthetic (seeded random-init weights, seeded cached KV, motif-built token streams)",
         "config": {"workload": e["workload"], "batch": e["batch"], "k": e["k"], "rows": e["rows"],
                    "sum_ctx": e["sum_ctx"], "parallelism": "single GPU", "kv_format": args.kv_format},

@@ -30,3 +30,9 @@ def test_another_format_is_refused_by_name():
     assert r.returncode == 2 and "kv-format" in r.stderr
     with pytest.raises(ValueError):
         war.Pool(synth.TINY, 4, 1, 4, device="cpu", kv_format="int8")
+
+
+def test_a_line_over_8_bit_pools_does_not_call_itself_bf16():
+    import bench
+    assert bench.result_dtype("bf16") == "bf16"
+    assert bench.result_dtype("e4m3") != "bf16" and "e4m3" in bench.result_dtype("e4m3")
