@@ -59,7 +59,10 @@ def parse():
                          "at 72 and 192 rows, weights rotated past the memory-side cache, and exit")
     ap.add_argument("--copy-probe", action="store_true",
                     help="only time a plain 2 GiB device copy (counter calibration)")
-    return ap.parse_args()
+    args = ap.parse_args()
+    if args.sweep and args.kv_format != "bf16":
+        ap.error("--sweep measures bf16 pools, not --kv-format " + args.kv_format)
+    return args
 
 
 def result_dtype(kv_format: str) -> str:

@@ -36,3 +36,9 @@ def test_a_line_over_8_bit_pools_does_not_call_itself_bf16():
     import bench
     assert bench.result_dtype("bf16") == "bf16"
     assert bench.result_dtype("e4m3") != "bf16" and "e4m3" in bench.result_dtype("e4m3")
+
+
+def test_the_sweep_refuses_a_format_it_does_not_measure():
+    r = subprocess.run([sys.executable, os.path.join(ROOT, "bench.py"), "--sweep", "--kv-format", "e4m3"], capture_output=True,
+                       text=True, timeout=60, cwd=ROOT)
+    assert r.returncode == 2 and "--kv-format" in r.stderr
