@@ -206,6 +206,11 @@ war_status war_kv_read(war_kv_pool* p, int32_t layer, int32_t B, const int32_t* 
  * once a step and serves all its layers.
  *   max_batch, max_rows   the most requests and rows a request: max_batch <= 1024,
  *                         max_rows <= 65536, their product <= 2^20
+ * The workspace is mostly partial sums, 4 * (head_dim + 2) bytes a row and kv-head.  With
+ * G = n_q_heads / n_kv_heads: 16, 32 or 48 rows (the least that holds G * max_rows, 48 at
+ * most) for every request and 1024 tokens of max_pages_per_seq; where G * max_rows > 48
+ * also 128 rows for each of up to max(max_batch * ceil(max_rows / (128 / G)),
+ * 8192 / n_kv_heads) units, whichever is more: 17 GB for 2^20 rows of 32 heads of 128.
  * The pool must outlive the object.  Only war_attend_create and _destroy allocate and
  * wait, so update and run may be captured into a graph, both together (a plan made
  * outside describes the pool as it was then); an object holds one plan at a time, so

@@ -239,11 +239,12 @@ __global__ void __launch_bounds__(kBT) k_verify_setup(PoolDev p, VerifySetupArgs
   // than workgroups, so that all of them run at once and end together; one a CU where
   // chunks stay short (a.even: 128 KB of codes), which draws the memory's rate as well
   // and has half the starts and merges.  In 8 bits, with the merge: 24 requests of
-  // 501-9001 tokens, 64-wide heads 25.9 -> 22.6 us; 8 of 4000-12000, 3 kv-heads 18.6 ->
-  // 16.4; 4 of 40-900, 2 kv-heads 11.3 -> 8.9; 8 of 32001-32768 with 36 rows 109 -> 103.
+  // 501-9001 tokens, 64-wide heads 26.9 -> 23.4 us; 8 of 4000-12000, 3 kv-heads 18.9 ->
+  // 16.8; 4 of 40-900, 2 kv-heads 11.9 -> 9.0; 8 of 32001-32768 with 36 rows 116 -> 105.
   // Cuts that leave workgroups idle lose to several units each in any order (16 of
-  // 2000-40000: 78 us, even 87), so long ones have to be nearly even.  (bf16 pools, in
-  // plans: 0.59-1.08 of the other rule's time over 40 shapes.)
+  // 2000-40000: 78 us, even 87), so long ones have to be nearly even.  Over 40 shapes 0.66
+  // to 1.04 of the other rule's time; bf16 pools, in plans, 0.59 to 1.07.  (a.cascade: a
+  // pool that has ever forked cuts neither way, for batches without siblings too.)
   const int u128 = (len + 127) / 128;
   if (t < a.B) s_mis[t] = u128;
   if (w * 64 < a.B) {
@@ -481,10 +482,11 @@ __global__ void __launch_bounds__(kBT) k_verify_setup(PoolDev p, VerifySetupArgs
 // it, so that the units which read a chunk run together and find it in L2.  With first(c)
 // the first block that reaches chunk c, a request has sum_c (blocks - first(c)) items.
 //
-// The chunk is the one of kRowCuts with the least estimated time (row_cut_time).  Against
-// 8192 keys, halved only where half the grid idles, over e4m3: 4 requests of 500 rows
-// behind 1000-9000 tokens 281 -> 224 us, 2 of 300 behind 16000 287 -> 234, 4096 rows of 8
-// 64-wide heads 85 -> 76; the worst of 20 shapes 2048 behind 8000, 379 -> 390.
+// The chunk is the longest of kRowCuts within 2% of the least estimated time
+// (row_cut_time), for pools of either format.  Against chunks of 8192 keys (bf16: 4096)
+// throughout, 20 shapes: e4m3 0.29 to 1.02 of the time, bf16 0.42 to 1.04 (8 requests of 49
+// rows behind 500-8000 tokens 221 -> 67 us, bf16 114 -> 61; 4 of 500 behind 1000-9000 302
+// -> 278, 262 -> 255; worst 2 of 2048 behind 9001-24576, bf16 1612 -> 1682).
 // One workgroup: 9 us.
 __global__ void __launch_bounds__(kBT) k_attend_plan_rows(PoolDev p, RowPlanArgs a, StepMeta m) {
   __shared__ int s_ctx[kBT], s_n[kBT], s_off[kBT], s_seq[kBT], s_whole[kBT], s_part[kBT];

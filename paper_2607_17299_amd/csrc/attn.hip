@@ -26,14 +26,14 @@
 // registers, which is exact: keys with their token's scale by the conversion itself,
 // values without, their scales multiply the weights (a lane holds the weights of eight
 // tokens of one row), whose sum stays without them.  One bf16 a weight in place of hi + lo
-// would save 1-4% of the time (8 requests of 32001-32768 tokens, nine rows each, with the
-// merge: 108.0 against 109.5 us).  16 bytes of a lane are two k-steps
+// would save 0-7% of the time (8 requests of 32001-32768 tokens, nine rows each, two layers
+// with plan and merges: 227 against 243 us).  16 bytes of a lane are two k-steps
 // of a key (k-step j covers dims 64 (j / 2) + 16 g + 8 (j % 2) + 0..7 of lane group g)
 // or its eight keys in two output tiles.
 // HBM bounds it with one row tile (64 requests of 1024-65536 tokens, 32 / 8 heads of 128:
-// 2.09 GB in 317 us, 6.6 TB/s, bf16 6.6-6.7 of twice the bytes); with three the issue of
+// 2.09 GB in 319 us, 6.6 TB/s, bf16 6.6-6.7 of twice the bytes); with three the issue of
 // conversions, weights and products at two waves a SIMD (8 requests of 32001-32768 tokens,
-// nine rows each: 536 MB in 97 us, 5.5 TB/s, VALU 40% and matrix pipes 22% busy).
+// nine rows each: 536 MB in 96-111 us, 4.8-5.6 TB/s, VALU 49% and matrix pipes 31% busy).
 // The waves' (max, sum, O) are merged through LDS in a fixed order and one
 // partial per item goes to global memory; the combine kernel merges a
 // request's chunks in item order (deterministic).

@@ -22,9 +22,10 @@
 // converted once a workgroup, and the products and softmax are the same, weights in hi + lo
 // among them.  A wave's pieces are of one page, so that the addresses are scalar; the
 // compiler may order the work of the slots (barriers between them cost 1% and spill).
-// 2048 and 2011 rows of 32 heads behind 9001 and 24576 tokens, the merge among it: 1752 us
-// where the same over a bf16 pool takes 1690.  (One bf16 a weight: 1340 us, a third fewer
-// matrix instructions, and results off by 2^-9 of every weight.)
+// 2048 and 2011 rows of 32 heads behind 9001 and 24576 tokens, the merge among it: 1714 us
+// where the same over a bf16 pool takes 1672; matrix pipes 50% and VALU 62% of all cycles.
+// (One bf16 a weight: 1317 us, a third fewer matrix instructions, and results off by 2^-9
+// of every weight.)
 // 2048 rows of 32 heads over 25600 keys (head_dim 128): 1403 -> 1151-1162 us (the
 // kernel it replaces staged blocks through registers and took scores, softmax and
 // product one after the other).  Over an append of 16 x 2048 tokens to 8192-26624 keys

@@ -394,7 +394,8 @@ void launch_constrain(const ConstrainArgs& a, hipStream_t st) {
   int rows = std::max(1, std::min(most, cdiv_i(2048, chunks * a.B)));
   const dim3 grid(chunks, a.B, rows);
   auto quad = [](const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; };
-  // 16-byte accesses where every row of every array allows them
+  // 16-byte accesses where every row of every array allows them (192 rows of 151,936 ids 46
+  // us, of 151,937 ids 66)
   const bool vec = a.V % 4 == 0 && a.stride % 4 == 0 && quad(a.logits, 16) && quad(a.counts, 8) &&
                    (!a.out || (a.out_stride % 4 == 0 && quad(a.out, 16)));
   if (vec) k_constrain<true><<<grid, kThreads, 0, st>>>(a);

@@ -139,8 +139,10 @@ void launch_attend_plan(const PoolDev& p, const VerifySetupArgs& a, const StepMe
 // in rounds of the grid (`slots` items of a kv-head), others fill in behind each other and
 // end half a unit apart, and nothing ends before the longest.  (From integer sums, so that
 // a plan repeats itself.)  Of the cuts within kCutNear of the least time the longest is
-// taken: the estimate is no better than that (8 of 256 rows behind 2000-20000 tokens 425 ->
-// 389 us, the others of 20 shapes within 2%).
+// taken: the estimate is no better than that (against the least, 8 of 256 rows behind
+// 2000-20000 tokens 484 -> 472 us, bf16 461 -> 447, 4 of 500 behind 1000-9000 265 -> 278,
+// 248 -> 255, the others of 20 shapes within 2%).  A kUnitKeys of 600 or 1500 moves no
+// shape of either format by more than 6%.
 constexpr int kRowCuts = 20;
 constexpr float kUnitKeys = 1000.f, kCutNear = 1.02f;
 // 512 keys times 1, 9/8, 11/8, 13/8, 2, ... 26

@@ -7,8 +7,9 @@
 // exchanges within a wave, and the page passes through LDS in its own order, so that
 // both sides move 16-byte pieces.  A page's other slots hold other tokens: of a piece
 // that covers some of them only the new tokens' bytes are written.
-// 28,300 tokens of 16 requests, 8 heads of 128, e4m3 (175 MB): written in 34 us (5.1 TB/s),
-// read in 31.5 (5.5); 64 requests' three tokens 4.3 and 3.4 us, a launch.
+// 28,300 tokens of 16 requests, 8 heads of 128, e4m3 (175 MB): written in 33 us (5.3 TB/s),
+// read in 31.5 (5.5); bf16 (232 MB): 40 us (5.8) and 48 (4.8); 64 requests' three tokens
+// 4.3 and 3.5 us, a launch.  (A copy kernel of that size reaches 6.4 TB/s.)
 #include <type_traits>
 
 #include "e4m3.h"

@@ -236,7 +236,8 @@ __global__ void __launch_bounds__(64) k_qkv_rope(int rows, int splits, const flo
 // step leaves what an import of its bf16 keys and values would leave.  A thread takes
 // four pairs of a query head, or of a key head and of its values: what marks a token
 // that is not finite is decided once for both (see k_kv_write).  A head is half / 4 (16
-// or 8) neighbouring threads of the wave.
+// or 8) neighbouring threads of the wave.  2048 rows of 32 / 8 heads of 128 (71 MB): 23 us,
+// 3.1 TB/s, values a byte a store (bf16 pages 25); 72 rows 5.6 us, a launch.
 __global__ void __launch_bounds__(64) k_qkv_rope8(int rows, int splits, const float* P, ModelDims md,
                                                   const float* cos_t, const float* sin_t, StepMeta meta,
                                                   const int32_t* row_req, const int32_t* table, int max_pages,

@@ -1688,8 +1688,8 @@ war_status war_prefill_append(war_model* m, war_kv_pool* p, int32_t n, const int
     }
     const int nr = (int)rq_seq.size(), nl = (int)last_rows.size();
     // 8-bit pools: the contexts are cut by estimated time, as a plan's (4 layers: 60 tokens
-    // behind 30000 1.45 -> 0.85 ms, 4 x 500 behind 1000-9000 4.05 -> 3.83, the worst of 8
-    // appends 4.41 -> 4.49; bf16 pools as they were: the sums keep their order)
+    // behind 30000 1.52 -> 0.88 ms, 4 x 500 behind 1000-9000 4.17 -> 3.99, the worst of 8
+    // appends 11.7 -> 12.0; bf16 pools as they were: the sums keep their order)
     int chunk = base_chunk;
     if (p->geom.q8) {
       const int slots = std::max(1, kAttnGrid / m->md.nkv);
