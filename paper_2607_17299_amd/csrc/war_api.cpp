@@ -49,6 +49,7 @@ struct DevBuf {
     }
     hipError_t e = hipMalloc(&p, n);
     if (e == hipSuccess) bytes = n;
+    else (void)hipGetLastError();  // reported here, not by the next call
     return e;
   }
   void release() {
@@ -1208,6 +1209,14 @@ war_status verify_impl(war_model* m, war_kv_pool* p, int32_t B, const int32_t* s
     HIPCHK(m->path_ws.ensure((size_t)B * k_max * 4));
     accept_path = m->path_ws.as<int32_t>();
   }
+  // the full logits are needed: the caller's buffer, else the workspace (before the setup,
+  // which reserves pages: a step that has no memory changes nothing)
+  float* lg = logits;
+  if ((sp.uniforms || cons) && !lg) {
+    HIPCHK(m->logits_ws.ensure((size_t)R * m->md.V * 4));
+    lg = m->logits_ws.as<float>();
+  }
+  if (sp.uniforms) HIPCHK(m->row_out.ensure((size_t)R * 4 * 4));
   const StepMeta meta = w.meta();
   {
     Timed t(m->prof, st, "verify_setup");
@@ -1221,13 +1230,6 @@ war_status verify_impl(war_model* m, war_kv_pool* p, int32_t B, const int32_t* s
   war_status s = run_layers(m, w, p, R, a, RB, grid, B, st);
   if (s != WAR_OK) return s;
   int sdummy;
-  // the full logits are needed: the caller's buffer, else the workspace
-  float* lg = logits;
-  if ((sp.uniforms || cons) && !lg) {
-    HIPCHK(m->logits_ws.ensure((size_t)R * m->md.V * 4));
-    lg = m->logits_ws.as<float>();
-  }
-  if (sp.uniforms) HIPCHK(m->row_out.ensure((size_t)R * 4 * 4));
   // constrained in place; the best of each block of ids takes the LM head's place
   auto constrain = [&](int32_t* greedy) {
     ConstrainArgs ca = constrain_args(*cons, m->md.V, B, seq_ids, last_tokens, draft_tokens, va.draft_parents, k_max);
@@ -1357,7 +1359,6 @@ war_status war_attend_create(war_kv_pool* p, int32_t max_batch, int32_t max_rows
   a->max_batch = max_batch;
   a->max_rows = max_rows;
   if (hipError_t e = a->buf.ensure(bytes); e != hipSuccess) {
-    (void)hipGetLastError();  // reported here, not by the next call
     delete a;
     return fail(WAR_ERR_HIP, std::string("attention workspace: ") + hipGetErrorString(e));
   }

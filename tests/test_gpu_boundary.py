@@ -170,3 +170,40 @@ def test_the_largest_context_lengths_fail_the_step(tiny, far, k):
         assert bad.cpu().tolist() == [20, far], name
         _flagged(war, pool, "context length")
         _same(before, _snapshot(pool))
+
+
+@pytest.mark.parametrize("sampled", [False, True])
+def test_a_step_without_memory_for_its_logits_leaves_the_pool_alone(sampled):
+    """1024 requests of 16 rows, 8,000,000 ids: 524 GB of logits that the caller does not
+    bring; no page is reserved, and the next step runs."""
+    war = _war()
+    cfg = synth.ModelConfig(n_layers=1, d_model=128, n_q_heads=2, n_kv_heads=2, head_dim=64, ffn_dim=128, vocab=8000000)
+    w = {name: torch.zeros(shape, dtype=torch.bfloat16, device=DEV) for name, shape in synth.weight_shapes(cfg)}
+    model = war.Model(cfg, w, max_rows=16384)
+    del w
+    B, k = 1024, 15
+    pool = war.Pool(cfg, B + 1, B, 2)
+    before = _snapshot(pool)
+    cons = war.Constraints(cfg.vocab, repetition=torch.ones(B, device=DEV))
+
+    def step(B, k):
+        seq, ctx, last, drafts = _t(np.arange(B)), _t([0] * B), _t([1] * B), _t(np.ones((B, k)))
+        acc, nxt = _t([7] * B), _t([7] * B)
+        u = torch.zeros((B * (k + 1), 2), device=DEV)
+        if sampled:
+            war.verify_step_sampled(model, pool, seq, ctx, last, drafts, None, k, u, 1.0, 1, acc, nxt)
+        else:
+            war.verify_step_constrained(model, pool, seq, ctx, last, drafts, None, k, cons, acc, nxt)
+        return seq, ctx, acc
+
+    with pytest.raises(war.WarError, match="memory"):
+        step(B, k)
+    torch.cuda.synchronize()
+    _same(before, _snapshot(pool))
+    seq, ctx, acc = step(1, 0)
+    war.kv_commit(pool, seq, ctx, acc)
+    assert acc.cpu().tolist() == [0] and ctx.cpu().tolist() == [1]
+    assert pool.state()["status"] == 0
+    pool.close()
+    model.close()
+    torch.cuda.empty_cache()
