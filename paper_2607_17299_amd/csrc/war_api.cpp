@@ -601,6 +601,7 @@ war_status ensure_ws(war_model* m, int64_t n_items, int RB) {
   const int64_t pel = std::max<int64_t>(kPartialCap, partials_needed(m->md, m->max_rows));
   const size_t bytes = ws_layout(m->md, m->max_rows, items, rb, pel, nullptr, nullptr);
   const bool tree = w.tree_step;
+  w = Workspace{};  // (the old memory goes first: without new memory there is none)
   HIPCHK(m->ws_buf.ensure(bytes));
   ws_layout(m->md, m->max_rows, items, rb, pel, m->ws_buf.as<char>(), &w);
   w.tree_step = tree;

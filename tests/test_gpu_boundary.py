@@ -207,3 +207,31 @@ def test_a_step_without_memory_for_its_logits_leaves_the_pool_alone(sampled):
     pool.close()
     model.close()
     torch.cuda.empty_cache()
+
+
+def test_a_step_whose_workspace_does_not_fit_leaves_the_model_usable():
+    """1024 requests of 48 rows over block tables of 2^24 tokens want 412 GB of partial sums."""
+    war = _war()
+    cfg = synth.ModelConfig(n_layers=1, d_model=128, n_q_heads=32, n_kv_heads=32, head_dim=128, ffn_dim=128, vocab=128)
+    w = {name: t.to(DEV) for name, t in synth.model_weights(cfg, seed=0, norm_std=0.1).items()}
+    model = war.Model(cfg, w, max_rows=1024 * 48)
+    small = war.Pool(cfg, 8, 1, 4)
+
+    def step(pool, B, k):
+        acc, nxt = _t([7] * B), _t([7] * B)
+        logits = torch.empty((B * (k + 1), cfg.vocab), device=DEV)
+        war.verify_step(model, pool, _t(np.arange(B)), _t([0] * B), _t([1] * B), _t(np.ones((B, k))), None, k, acc, nxt, logits)
+        war.kv_commit(pool, _t(np.arange(B)), _t([0] * B), _t([-1] * B))
+        return logits
+
+    first = step(small, 1, 3)
+    large = war.Pool(cfg, 1024 * 3, 1024, 1 << 20)
+    with pytest.raises(war.WarError, match="memory"):
+        step(large, 1024, 47)
+    assert bool((large.block_tables == -1).all())                     # no page moved
+    assert torch.equal(first, step(small, 1, 3))
+    large.close()
+    small.close()
+    model.close()
+    del large
+    torch.cuda.empty_cache()
