@@ -190,6 +190,8 @@ class Pool:
             n = max(lib().war_kv_pool_bytes(C.byref(self._cfg), num_pages, KV_FORMATS[kv_format]), 0)
         self.kv = torch.empty(n, dtype=torch.bfloat16 if kv_format == "bf16" else torch.uint8, device=device)
         self.block_tables = torch.empty((max_seqs, max_pages_per_seq), dtype=torch.int32, device=device)
+        if stream is not None:  # memory that the current stream freed may be in use there still
+            stream.wait_stream(torch.cuda.current_stream(self.kv.device))
         h = C.c_void_p()
         _check(lib().war_kv_pool_create_format(C.byref(self._cfg), _ptr(self.kv), num_pages, KV_FORMATS[kv_format],
                                                _ptr(self.block_tables), max_seqs, max_pages_per_seq,
