@@ -241,7 +241,7 @@ def test_a_pool_made_on_another_stream_waits_for_its_memory():
     """Memory that the current stream still reads, freed there and taken for the pool's block
     tables, is not cleared before that reading."""
     war = _war()
-    n = 4096 * 1024                                          # int32: as large as the block tables below
+    n = 4096 * 32768                                         # int32: as large as the block tables below
     other = torch.cuda.Stream()
     for _ in range(3):
         torch.cuda.synchronize()
@@ -253,9 +253,9 @@ def test_a_pool_made_on_another_stream_waits_for_its_memory():
         y.copy_(x)                                           # waits behind the sleep
         at = x.data_ptr()
         del x
-        pool = war.Pool(CFG, 8, 4096, 1024, stream=other)
+        pool = war.Pool(CFG, 8, 4096, 32768, stream=other)
         torch.cuda.synchronize()
         assert pool.block_tables.data_ptr() == at            # (the allocator gave it that memory)
         assert (y == 9).all()
         pool.close()
-        del pool
+        del pool, y
