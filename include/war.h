@@ -130,6 +130,8 @@ void war_kv_pool_destroy(war_kv_pool* p);
  * a step, an append, an import and war_kv_write of the same bf16 numbers store the
  * same bytes.  Where any key or value of a token and kv-head is not finite, all of
  * them read as NaN, and rows that see the token get NaN; others do not.
+ * (A finite value that reads as infinite reaches only the rows that see it, too; it
+ * counts as 2^128 or as the largest bf16 there.)
  *   kv_format     WAR_KV_BF16 (as war_kv_pool_create) or WAR_KV_E4M3
  *   kv_pages      war_kv_pool_bytes(cfg, num_pages, kv_format) bytes, 16-byte aligned.
  *                 E4M3: page regions as in war_kv_pool_create but of bytes, at byte
