@@ -247,6 +247,100 @@ war_status war_attend_update(war_attend* a, int32_t B, int32_t n_max, const int3
 war_status war_attend_run(war_attend* a, int32_t layer, const void* q, int64_t q_stride, void* o,
                           int64_t o_stride, void* stream);
 
+/* ---- The other operators of a decoder layer, for decoders whose layers are the
+ * caller's (with war_attend_* between them), their weights in 4 bits: a step of few rows
+ * is bound by the bytes of its weights (Background, "Rollout Bottlenecks"). ----
+ *
+ * A matrix of microscaled numbers: 32 neighbouring columns of a row are a block with the
+ * scale 2^e, kept as the byte e + 127; a code c stands for c * 2^e.  Writing, e is the
+ * smallest integer with max |x| <= top * 2^e, at least -117 (top: 448 for e4m3, 6 for
+ * e2m1), and c is x / 2^e rounded to nearest even; a block with a number that is not
+ * finite gets the byte 255, and all of it reads as NaN.  Reading, any scale byte will do.
+ *   format        WAR_MX_E4M3: a byte a code (OCP e4m3); WAR_MX_E2M1: 4 bits (sign, two
+ *                 exponent bits, one mantissa bit), the even column in the low ones
+ *   rows, cols    rows in [0, 2^20], cols a multiple of 32 in [32, 65536], rows * cols
+ *                 <= 2^34
+ *   codes         device; rows at code_stride bytes, a multiple of 16; 16-byte aligned
+ *   scales        device; rows at scale_stride bytes, a multiple of 4 (bytes up to the
+ *                 next multiple of 4 may be read, and do not count); 4-byte aligned */
+#define WAR_MX_E4M3 2
+#define WAR_MX_E2M1 3
+#define WAR_BF16 0
+#define WAR_F32 1
+typedef struct war_mx {
+  int32_t format, rows, cols;
+  void* codes;
+  int64_t code_stride;
+  uint8_t* scales;
+  int64_t scale_stride;
+} war_mx;
+
+/* The residual's addition and the norm behind it: h += x, then y = h / sqrt(mean(h^2) +
+ * eps) * gain, rounded once to y's type.  Sums are fp32 (h, where it is bf16, is rounded as
+ * it is stored, not for y).
+ *   x        device bf16 [rows][cols] at x_stride, or NULL: h stays as it is
+ *   h        device [rows][cols] at h_stride, h_type WAR_BF16 or WAR_F32
+ *   gain     device bf16 [cols]
+ *   mx       y in codes (a HOST struct of rows by cols), or NULL and
+ *   y        device bf16 [rows][cols] at y_stride (y may be x)
+ * Strides in elements, multiples of 8; 16-byte aligned; sizes as of a war_mx. */
+war_status war_residual_norm(int32_t rows, int32_t cols, const void* x, int64_t x_stride, void* h, int64_t h_stride,
+                             int32_t h_type, const void* gain, float eps, const war_mx* mx, void* y, int64_t y_stride,
+                             void* stream);
+
+/* A matrix x into codes (mx, a HOST struct; its rows and cols are x's); with a gate g,
+ * x * g / (1 + exp(-g)): what a SwiGLU's gate and up projections leave for the one down.
+ * x and gate (NULL: none): device, type WAR_BF16 or WAR_F32, strides as above. */
+war_status war_quantize(const war_mx* mx, const void* x, int64_t x_stride, const void* gate, int64_t gate_stride,
+                        int32_t type, void* stream);
+/* The numbers that codes stand for (exact in either type while they are in its range). */
+war_status war_dequantize(const war_mx* mx, void* y, int64_t y_stride, int32_t type, void* stream);
+
+/* y = x w^T + bias with w [N, K] in WAR_MX_E2M1: an object owns w laid out for its kernels
+ * (in all 17 bits for 32 numbers' 4 bytes, padded to 256 rows and 512 columns).
+ *   w      HOST struct; N rows (at least 1), K cols; codes need no alignment here
+ *   bias   device bf16 [N], or NULL
+ * Synchronises the stream: the caller's arrays are not read afterwards. */
+typedef struct war_linear war_linear;
+war_status war_linear_create(const war_mx* w, const void* bias, void* stream, war_linear** out);
+void war_linear_destroy(war_linear* l);
+/* One product.  Any number of them may run at once (no workspace); nothing is allocated.
+ *   x   HOST struct, [rows][K] in either format
+ *   y   device [rows][N] at y_stride elements, at least N; y_type WAR_BF16 or WAR_F32
+ * Products and sums are fp32 in the matrix units.  They add e4m3 activations' products in
+ * groups of eight neighbours, where what lies more than 13 binary places below the
+ * group's largest product is cut off; e2m1 products are exact.  A row's result does not
+ * depend on the other rows' numbers. */
+war_status war_linear_run(const war_linear* l, const war_mx* x, void* y, int64_t y_stride, int32_t y_type, void* stream);
+
+/* Rotary positions of several axes (HOST struct; copied by the call).  Pair j of a head
+ * turns by (position of its row on axis axes[j]) * freqs[j].
+ *   rotary_dim  numbers of a head that turn, the first: a multiple of 8, at most head_dim
+ *   adjacent    0: pair j is (j, j + rotary_dim / 2); 1: (2 j, 2 j + 1)
+ *   n_axes      in [1, 4]
+ *   axes        HOST [rotary_dim / 2], each in [0, n_axes); NULL: all axis 0
+ *   freqs       HOST [rotary_dim / 2], finite, |f| <= 6.3 (a turn) */
+typedef struct war_rope {
+  int32_t rotary_dim, adjacent, n_axes;
+  const uint8_t* axes;
+  const double* freqs;
+} war_rope;
+
+/* The queries and keys of many sequences' new tokens turned, keys and values into their
+ * pages: war_kv_write with the rotation before it.
+ *   seq_ids, pos0, n_max, n_lens   as in war_kv_write
+ *   positions  device int32 [n_axes][B * n_max]: row b * n_max + i on each axis; NULL: the
+ *              token's place in the cache, pos0[b] + i, on every axis
+ *   q, q_out   device bf16 rows of n_q_heads * head_dim; q_out may be q (same stride)
+ *   k, v       device bf16 rows of n_kv_heads * head_dim, not written
+ * Strides in elements, multiples of 8; 16-byte aligned.  Turned numbers are rounded to
+ * bf16.  Rows beyond n_lens, and requests that are flagged as in war_kv_write, are left
+ * out: their q_out stays as it was. */
+war_status war_rope_write(war_kv_pool* p, int32_t layer, const war_rope* rope, int32_t B, const int32_t* seq_ids,
+                          const int32_t* pos0, int32_t n_max, const int32_t* n_lens, const int32_t* positions,
+                          const void* q, int64_t q_stride, void* q_out, int64_t q_out_stride, const void* k,
+                          int64_t k_stride, const void* v, int64_t v_stride, void* stream);
+
 /* Append a new turn to cached trajectories (System Design, "Overview of WAR";
  * Background, "Rollout Bottlenecks").
  *   seq_ids     device int32 [n]

@@ -10,6 +10,7 @@ Modules
   decoder   the GQA decoder forward over a block of new tokens against a
             request's cached keys/values (dense, per request, row by row).
   e4m3      keys and values cached in 8 bits: scales, rounding, tokens that are not finite.
+  mx        microscaled numbers in 8 and 4 bits, and the operators of a layer over them.
   accept    greedy argmax (ties -> lowest id) and longest-matching-prefix
             acceptance of draft tokens.
   pages     the paged-KV bookkeeping model: free stack, refcounts, block tables,

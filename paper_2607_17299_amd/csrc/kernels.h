@@ -298,3 +298,71 @@ void launch_argmax_accept(int n_req, const int32_t* ntok, int row_stride, int n_
 void launch_kv_compact(const KvGeom& kv, int n_layers, int B, const StepMeta& meta, const int32_t* table,
                        int max_pages, const int32_t* accept_lens, const int32_t* accept_path, int k_max,
                        hipStream_t st);
+
+// microscaled rows (mx_rows.hip); a matrix's codes and scale bytes at their strides
+struct MxRef {
+  uint8_t* codes;
+  uint8_t* scales;
+  int64_t code_stride, scale_stride;
+};
+struct NormArgs {
+  int rows, cols;
+  const bf16_t* x;  // nullable
+  void* h;          // bf16 or fp32
+  const bf16_t* gain;
+  bf16_t* y;        // bf16 output
+  MxRef mx;         // or codes
+  int64_t x_stride, h_stride, y_stride;
+  float eps;
+};
+struct QuantArgs {
+  int rows, cols;
+  const void *x, *gate;  // gate nullable
+  int64_t x_stride, gate_stride;
+  MxRef mx;
+};
+struct DequantArgs {
+  int rows, cols;
+  MxRef mx;
+  void* y;
+  int64_t y_stride;
+};
+// out, fmt: the format (mx.h); out -1: bf16
+void launch_residual_norm_mx(const NormArgs& a, bool h_f32, int out, hipStream_t st);
+void launch_quantize(const QuantArgs& a, bool f32, int fmt, hipStream_t st);
+void launch_dequantize(const DequantArgs& a, bool f32, int fmt, hipStream_t st);
+
+// products with e2m1 weights (mx_gemm.hip)
+struct MxGemmArgs {
+  int M, N, K;
+  MxRef x;             // [M][K]
+  const uint8_t* w;    // packed codes and scales (mx_packed_bytes)
+  const uint32_t* ws;
+  const bf16_t* bias;  // [N padded], zero where there is none
+  void* y;
+  int64_t y_stride;
+  int vec;             // rows of y may be written four columns at a time
+};
+// N in tiles of 16 rows, K in groups of 512: what a packed matrix is padded to (with
+// zero codes)
+inline int mx_tiles(int N) { return (N + 255) / 256 * 16; }
+inline int mx_groups(int K) { return (K + 511) / 512; }
+inline int64_t mx_code_bytes(int N, int K) { return (int64_t)mx_tiles(N) * mx_groups(K) * 4096; }
+inline int64_t mx_scale_words(int N, int K) { return (int64_t)mx_tiles(N) * mx_groups(K) * 64; }
+void launch_mx_pack(const MxRef& w, int N, int K, uint8_t* codes, uint32_t* scales, hipStream_t st);
+void launch_mx_gemm(const MxGemmArgs& a, int fmt, bool f32, hipStream_t st);
+
+// rotated queries, and rotated keys with values into the pages (rope.hip)
+struct RopeArgs {
+  PoolDev p;
+  KvGeom g;
+  int layer, B, n_max, pages, n_q_heads;
+  const int32_t *seq, *pos0, *n, *positions;  // n, positions nullable
+  const bf16_t *q, *k, *v;
+  bf16_t* qo;
+  int64_t q_stride, qo_stride, k_stride, v_stride;
+  int rotary, adjacent;
+  uint8_t axis[64];
+  double turns[64];  // of a full turn, for a position
+};
+void launch_rope_write(const RopeArgs& a, hipStream_t st);

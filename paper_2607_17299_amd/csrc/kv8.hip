@@ -13,28 +13,9 @@
 #include <type_traits>
 
 #include "e4m3.h"
-#include "kernels.h"
+#include "kv_page.h"
 
 namespace {
-
-constexpr int kPage = 16;
-
-// Element (bf16) or byte (e4m3) of a page's keys and values.
-template <bool Q8, int HD>
-struct PageOrder {
-  static constexpr int kElem = Q8 ? 1 : 2;            // bytes a number
-  static constexpr int kBytes = kPage * HD * kElem;   // of the keys; as many of the values
-  static constexpr int kPieces = kBytes / 16;
-  __device__ static int key(int s, int d) { return Q8 ? key_elem8(s, d, HD) : key_elem(s, d, HD) * 2; }
-  __device__ static int val(int s, int d) { return Q8 ? val_elem8(s, d) : (d * kPage + s) * 2; }
-  // slot of 16-byte piece c of the keys (in 64-byte rows), first of the eight slots of
-  // piece c of the values
-  __device__ static int key_slot(int c) {
-    const int row = c >> 2, s8 = row & 7, t = row >> 3 >= HD * kElem / 64;
-    return ((s8 >> 2) << 3) | (t << 2) | (s8 & 3);
-  }
-  __device__ static int val_slot(int c) { return (Q8 ? c >> 4 : c) & 1 ? 8 : 0; }
-};
 
 struct KvMoveArgs {
   PoolDev p;
@@ -43,28 +24,12 @@ struct KvMoveArgs {
   KvMove m;
 };
 
-// This workgroup's page: false where it has none.  A request that its pages cannot
-// hold is flagged and left out as a whole.
-struct Span {
-  int b, page, lo, hi, t0;  // slots [lo, hi) are tokens t0 + 0 ..
-};
-__device__ bool span_of(const KvMoveArgs& a, Span& s) {
-  s.b = blockIdx.x / a.pages;
-  const int j = blockIdx.x % a.pages;
+// This workgroup's page: false where it has none.
+__device__ bool span_of(const KvMoveArgs& a, PageSpan& s) {
+  const int b = blockIdx.x / a.pages, j = blockIdx.x % a.pages;
   const KvMove& m = a.m;
-  const int n = m.n ? m.n[s.b] : m.n_max, seq = m.seq ? m.seq[s.b] : m.seq0, pos = m.pos ? m.pos[s.b] : m.pos0;
-  if (seq < 0 || seq >= a.p.max_seqs || pos < 0 || n < 0 || n > m.n_max ||
-      (int64_t)pos + n > (int64_t)a.p.held[seq] * kPage) {
-    if (j == 0 && blockIdx.y == 0 && threadIdx.x == 0) atomicOr(&a.p.scalars[1], ERR_BAD_TOKEN);
-    return false;
-  }
-  const int first = pos / kPage + j, base = first * kPage;
-  s.lo = max(pos - base, 0);
-  s.hi = min(pos + n - base, kPage);
-  s.t0 = base + s.lo - pos;
-  if (s.lo >= s.hi) return false;
-  s.page = a.p.table[(int64_t)seq * a.p.max_pages + first];
-  return true;
+  return page_span(a.p, b, j, m.seq ? m.seq[b] : m.seq0, m.pos ? m.pos[b] : m.pos0, m.n ? m.n[b] : m.n_max, m.n_max,
+                   j == 0 && blockIdx.y == 0 && threadIdx.x == 0, s);
 }
 
 // R numbers (8, or 4 at head_dim 64) of a row, which may begin at any element (an import's
@@ -84,7 +49,7 @@ __global__ void __launch_bounds__(256) k_kv_write(KvMoveArgs a) {
   constexpr int R = HD / 16;  // dims a thread
   __shared__ __attribute__((aligned(16))) unsigned char s_pg[2 * O::kBytes];
   __shared__ unsigned char s_sc[32];
-  Span s;
+  PageSpan s;
   if (!span_of(a, s)) return;
   const int kvh = blockIdx.y, slot = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * R;
   if (slot >= s.lo && slot < s.hi) {
@@ -137,37 +102,7 @@ __global__ void __launch_bounds__(256) k_kv_write(KvMoveArgs a) {
     }
   }
   __syncthreads();
-  const int64_t at = a.g.page_elems(a.m.layer, s.page, kvh, 0) * O::kElem;
-  unsigned char* pg = (Q8 ? a.g.q8 : reinterpret_cast<unsigned char*>(a.g.kv)) + at;
-  for (int c = threadIdx.x; c < O::kPieces; c += 256) {
-    const int sl = O::key_slot(c);
-    if (sl >= s.lo && sl < s.hi)
-      *reinterpret_cast<uint4*>(pg + c * 16) = *reinterpret_cast<const uint4*>(&s_pg[c * 16]);
-  }
-  for (int c = threadIdx.x; c < O::kPieces; c += 256) {
-    const int s0 = O::val_slot(c), lo = max(s.lo - s0, 0), hi = min(s.hi - s0, 8);
-    unsigned char* dst = pg + O::kBytes + c * 16;
-    const unsigned char* src = &s_pg[O::kBytes + c * 16];
-    if (lo == 0 && hi == 8) {
-      *reinterpret_cast<uint4*>(dst) = *reinterpret_cast<const uint4*>(src);
-    } else {
-      for (int i = lo; i < hi; ++i) {
-        if constexpr (Q8) {
-          dst[i] = src[i];
-          dst[8 + i] = src[8 + i];
-        } else {
-          *reinterpret_cast<bf16_t*>(dst + 2 * i) = *reinterpret_cast<const bf16_t*>(src + 2 * i);
-        }
-      }
-    }
-  }
-  if constexpr (Q8) {
-    unsigned char* sc = a.g.scale + a.g.scale_bytes(a.m.layer, s.page, kvh);
-    if (threadIdx.x < 2 * kPage) {
-      const int sl = threadIdx.x & 15, i = threadIdx.x < kPage ? key_scale8(sl) : val_scale8(sl);
-      if (sl >= s.lo && sl < s.hi) sc[i] = s_sc[i];
-    }
-  }
+  store_page<Q8, HD, 256>(a.g, a.m.layer, kvh, s, s_pg, s_sc);
 }
 
 template <bool Q8, int HD>
@@ -175,7 +110,7 @@ __global__ void __launch_bounds__(256) k_kv_read(KvMoveArgs a) {
   using O = PageOrder<Q8, HD>;
   constexpr int R = HD / 16;
   __shared__ __attribute__((aligned(16))) unsigned char s_pg[2 * O::kBytes];
-  Span s;
+  PageSpan s;
   if (!span_of(a, s)) return;
   const int kvh = blockIdx.y, slot = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * R;
   const int64_t at = a.g.page_elems(a.m.layer, s.page, kvh, 0) * O::kElem;
@@ -221,7 +156,7 @@ __global__ void __launch_bounds__(256) k_kv_read(KvMoveArgs a) {
 }  // namespace
 
 void launch_kv_move(bool write, const PoolDev& p, const KvGeom& g, const KvMove& m, hipStream_t st) {
-  const KvMoveArgs a{p, g, cdiv_i(m.n_max + kPage - 1, kPage), m};
+  const KvMoveArgs a{p, g, cdiv_i(m.n_max + kPageSlots - 1, kPageSlots), m};
   const dim3 grid(m.B * a.pages, g.n_kv_heads);
   auto go = [&](auto hd) {
     constexpr int HD = decltype(hd)::value;

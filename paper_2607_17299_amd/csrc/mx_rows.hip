@@ -1,0 +1,196 @@
+// Rows into and out of microscaled codes (mx.h): the residual's addition with the RMS
+// norm behind it, matrices as they are or behind a SwiGLU gate, and back.
+//
+// All of it is bound by memory for many rows and by a launch for few.  A lane takes
+// eight neighbouring columns (16 bytes of bf16), so a block of 32 is four lanes and its
+// maximum two exchanges within them.  Sums and statistics are fp32; a number is rounded
+// once, to its code (bf16 output: to bf16).
+#include "mx.h"
+
+namespace {
+
+// eight numbers at p
+template <bool F32>
+WAR_DEV void load8(const void* p, int64_t at, float (&x)[8]) {
+  if constexpr (F32) {
+    const float* f = static_cast<const float*>(p) + at;
+    const float4 a = *reinterpret_cast<const float4*>(f), b = *reinterpret_cast<const float4*>(f + 4);
+    x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+  } else {
+    const uint4 a = *reinterpret_cast<const uint4*>(static_cast<const bf16_t*>(p) + at);
+    x[0] = lo_f(a.x), x[1] = hi_f(a.x), x[2] = lo_f(a.y), x[3] = hi_f(a.y);
+    x[4] = lo_f(a.z), x[5] = hi_f(a.z), x[6] = lo_f(a.w), x[7] = hi_f(a.w);
+  }
+}
+template <bool F32>
+WAR_DEV void store8(void* p, int64_t at, const float (&x)[8]) {
+  if constexpr (F32) {
+    float* f = static_cast<float*>(p) + at;
+    *reinterpret_cast<float4*>(f) = make_float4(x[0], x[1], x[2], x[3]);
+    *reinterpret_cast<float4*>(f + 4) = make_float4(x[4], x[5], x[6], x[7]);
+  } else {
+    *reinterpret_cast<uint4*>(static_cast<bf16_t*>(p) + at) =
+        make_uint4(pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7]));
+  }
+}
+template <int FMT>
+WAR_DEV uint8_t* codes_at(const MxRef& m, int64_t r, int c8) {
+  return m.codes + r * m.code_stride + (FMT == kMxE4M3 ? c8 * 8 : c8 * 4);
+}
+
+// h += x, y = h rsqrt(mean h^2 + eps) gain.  T threads a row (a wave's: four rows a
+// workgroup), NV runs of eight columns each, kept in registers between the two passes.
+template <int T, int NV, bool HF32, int OUT>
+__global__ void __launch_bounds__(T < 256 ? 256 : T) k_residual_norm_mx(NormArgs a) {
+  constexpr int RPW = T < 256 ? 256 / T : 1;
+  __shared__ float red[16];
+  const int t = threadIdx.x % T;
+  const int64_t r = (int64_t)blockIdx.x * RPW + threadIdx.x / T;
+  const int n8 = a.cols / 8;
+  if (T < 256 && r >= a.rows) return;
+  float h[NV][8];
+  uint4 gg[NV];
+  float ss = 0.f;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int c = t + i * T;
+    if (c < n8) {
+      gg[i] = *reinterpret_cast<const uint4*>(a.gain + c * 8);
+      load8<HF32>(a.h, r * a.h_stride + c * 8, h[i]);
+      if (a.x) {
+        float x[8];
+        load8<false>(a.x, r * a.x_stride + c * 8, x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) h[i][e] += x[e];
+        store8<HF32>(a.h, r * a.h_stride + c * 8, h[i]);
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) ss += h[i][e] * h[i][e];
+    }
+  }
+  if constexpr (T < 256) ss = wave_sum(ss);
+  else ss = block_sum(ss, red);
+  const float rs = 1.f / sqrtf(ss / (float)a.cols + a.eps);
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int c = t + i * T;
+    if (c < n8) {
+      const float g[8] = {lo_f(gg[i].x), hi_f(gg[i].x), lo_f(gg[i].y), hi_f(gg[i].y),
+                          lo_f(gg[i].z), hi_f(gg[i].z), lo_f(gg[i].w), hi_f(gg[i].w)};
+      float y[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[e] = h[i][e] * rs * g[e];
+      if constexpr (OUT < 0) store8<false>(a.y, r * a.y_stride + c * 8, y);
+      else mx_store8<OUT>(y, codes_at<OUT>(a.mx, r, c), a.mx.scales + r * a.mx.scale_stride + c / 4, c % 4 == 0);
+    }
+  }
+}
+
+// y = x, or x silu(gate), into codes: a lane a run of eight columns
+template <bool F32, bool GATE, int FMT>
+__global__ void __launch_bounds__(256) k_quantize(QuantArgs a) {
+  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int n8 = a.cols / 8;
+  if (id >= (int64_t)a.rows * n8) return;
+  const int64_t r = id / n8;
+  const int c = (int)(id % n8);
+  float y[8];
+  load8<F32>(a.x, r * a.x_stride + c * 8, y);
+  if constexpr (GATE) {
+    float g[8];
+    load8<F32>(a.gate, r * a.gate_stride + c * 8, g);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] *= g[e] / (1.f + expf(-g[e]));
+  }
+  mx_store8<FMT>(y, codes_at<FMT>(a.mx, r, c), a.mx.scales + r * a.mx.scale_stride + c / 4, c % 4 == 0);
+}
+
+// the numbers that codes stand for
+template <bool F32, int FMT>
+__global__ void __launch_bounds__(256) k_dequantize(DequantArgs a) {
+  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int n8 = a.cols / 8;
+  if (id >= (int64_t)a.rows * n8) return;
+  const int64_t r = id / n8;
+  const int c = (int)(id % n8);
+  const float s = mx_scale(a.mx.scales[r * a.mx.scale_stride + c / 4]);
+  const uint8_t* p = codes_at<FMT>(a.mx, r, c);
+  float y[8];
+  if constexpr (FMT == kMxE4M3) {
+    const uint2 w = *reinterpret_cast<const uint2*>(p);
+    y[0] = from_e4m3<0>(w.x, 1.f), y[1] = from_e4m3<1>(w.x, 1.f), y[2] = from_e4m3<2>(w.x, 1.f), y[3] = from_e4m3<3>(w.x, 1.f);
+    y[4] = from_e4m3<0>(w.y, 1.f), y[5] = from_e4m3<1>(w.y, 1.f), y[6] = from_e4m3<2>(w.y, 1.f), y[7] = from_e4m3<3>(w.y, 1.f);
+  } else {
+    const uint32_t w = *reinterpret_cast<const uint32_t*>(p);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {  // sign, two exponent bits, one mantissa bit; 0.5 is subnormal
+      const uint32_t m = (w >> (4 * e)) & 7, s4 = (w >> (4 * e + 3)) & 1;
+      const uint32_t bits = m >= 2 ? ((m >> 1) + 126) << 23 | (m & 1) << 22 : m ? 126u << 23 : 0u;
+      y[e] = __uint_as_float(bits | s4 << 31);
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) y[e] *= s;
+  store8<F32>(a.y, r * a.y_stride + c * 8, y);
+}
+
+template <bool HF32, int OUT>
+void norm_go(const NormArgs& a, hipStream_t st) {
+  const int n8 = a.cols / 8;
+  auto one = [&](auto t, auto nv) {
+    constexpr int T = decltype(t)::value, NV = decltype(nv)::value;
+    const int grid = T < 256 ? (a.rows + 256 / T - 1) / (256 / T) : a.rows;
+    k_residual_norm_mx<T, NV, HF32, OUT><<<grid, T < 256 ? 256 : T, 0, st>>>(a);
+  };
+  using std::integral_constant;
+  if (n8 <= 64) one(integral_constant<int, 64>{}, integral_constant<int, 1>{});
+  else if (n8 <= 256) one(integral_constant<int, 256>{}, integral_constant<int, 1>{});
+  else if (n8 <= 512) one(integral_constant<int, 256>{}, integral_constant<int, 2>{});
+  else if (n8 <= 1024) one(integral_constant<int, 256>{}, integral_constant<int, 4>{});
+  else if (n8 <= 2048) one(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
+  else if (n8 <= 4096) one(integral_constant<int, 1024>{}, integral_constant<int, 4>{});
+  else one(integral_constant<int, 1024>{}, integral_constant<int, 8>{});
+}
+
+}  // namespace
+
+void launch_residual_norm_mx(const NormArgs& a, bool h_f32, int out, hipStream_t st) {
+  if (h_f32) {
+    if (out < 0) norm_go<true, -1>(a, st);
+    else if (out == kMxE4M3) norm_go<true, kMxE4M3>(a, st);
+    else norm_go<true, kMxE2M1>(a, st);
+  } else {
+    if (out < 0) norm_go<false, -1>(a, st);
+    else if (out == kMxE4M3) norm_go<false, kMxE4M3>(a, st);
+    else norm_go<false, kMxE2M1>(a, st);
+  }
+}
+
+void launch_quantize(const QuantArgs& a, bool f32, int fmt, hipStream_t st) {
+  const int64_t n = (int64_t)a.rows * (a.cols / 8);
+  const int grid = (int)((n + 255) / 256);
+  auto go = [&](auto f, auto g) {
+    constexpr bool F = decltype(f)::value, G = decltype(g)::value;
+    if (fmt == kMxE4M3) k_quantize<F, G, kMxE4M3><<<grid, 256, 0, st>>>(a);
+    else k_quantize<F, G, kMxE2M1><<<grid, 256, 0, st>>>(a);
+  };
+  if (f32) {
+    if (a.gate) go(std::true_type{}, std::true_type{});
+    else go(std::true_type{}, std::false_type{});
+  } else {
+    if (a.gate) go(std::false_type{}, std::true_type{});
+    else go(std::false_type{}, std::false_type{});
+  }
+}
+
+void launch_dequantize(const DequantArgs& a, bool f32, int fmt, hipStream_t st) {
+  const int64_t n = (int64_t)a.rows * (a.cols / 8);
+  const int grid = (int)((n + 255) / 256);
+  if (f32) {
+    if (fmt == kMxE4M3) k_dequantize<true, kMxE4M3><<<grid, 256, 0, st>>>(a);
+    else k_dequantize<true, kMxE2M1><<<grid, 256, 0, st>>>(a);
+  } else {
+    if (fmt == kMxE4M3) k_dequantize<false, kMxE4M3><<<grid, 256, 0, st>>>(a);
+    else k_dequantize<false, kMxE2M1><<<grid, 256, 0, st>>>(a);
+  }
+}

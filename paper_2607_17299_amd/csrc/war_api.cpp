@@ -12,6 +12,7 @@
 #include <vector>
 
 #include "../../include/war.h"
+#include "api.h"
 #include "kernels.h"
 
 namespace {
@@ -658,6 +659,9 @@ war_status check_ids(const war_kv_pool* p, int n, const int32_t* ids) {
 }
 
 }  // namespace
+
+war_status api_fail(war_status code, const char* msg) { return fail(code, msg); }
+PoolView pool_view(const war_kv_pool* p) { return {p->dev, p->geom, p->cfg}; }
 
 // ===================================================================== C ABI
 extern "C" {

@@ -30,6 +30,8 @@ EXPORTS = ["war_weight_count", "war_model_create", "war_model_destroy", "war_kv_
            "war_kv_commit", "war_pool_state", "war_kv_pool_bytes", "war_kv_pool_create_format", "war_kv_write",
            "war_kv_read", "war_constrain_workspace", "war_constrain_logits", "war_counts_begin", "war_counts_add",
            "war_verify_step_constrained", "war_attend_create", "war_attend_destroy", "war_attend_update", "war_attend_run",
+           "war_residual_norm", "war_quantize", "war_dequantize", "war_linear_create", "war_linear_destroy",
+           "war_linear_run", "war_rope_write",
            "war_last_error", "war_debug_mfma16", "war_debug_workspace", "war_debug_sample",
            "war_debug_gemm", "war_debug_gemm_plan", "war_debug_pool_waits", "war_profile", "war_profile_read"]
 
@@ -51,6 +53,16 @@ class _Constraints(C.Structure):
     _fields_ = [("n_seqs", C.c_int32), ("counts", C.c_void_p), ("repetition", C.c_void_p), ("frequency", C.c_void_p),
                 ("presence", C.c_void_p), ("n_bias", C.c_int32), ("bias_ids", C.c_void_p), ("bias_values", C.c_void_p),
                 ("n_masks", C.c_int32), ("masks", C.c_void_p), ("mask_index", C.c_void_p)]
+
+
+class _Mx(C.Structure):
+    _fields_ = [("format", C.c_int32), ("rows", C.c_int32), ("cols", C.c_int32), ("codes", C.c_void_p),
+                ("code_stride", C.c_int64), ("scales", C.c_void_p), ("scale_stride", C.c_int64)]
+
+
+class _Rope(C.Structure):
+    _fields_ = [("rotary_dim", C.c_int32), ("adjacent", C.c_int32), ("n_axes", C.c_int32), ("axes", C.c_void_p),
+                ("freqs", C.c_void_p)]
 
 
 def load_library(path: str = LIB_PATH) -> C.CDLL:
@@ -84,6 +96,15 @@ def load_library(path: str = LIB_PATH) -> C.CDLL:
         "war_attend_destroy": (None, [vp]),
         "war_attend_update": (i32, [vp, i32, i32, vp, vp, vp, vp, vp]),
         "war_attend_run": (i32, [vp, i32, vp, C.c_int64, vp, C.c_int64, vp]),
+        "war_residual_norm": (i32, [i32, i32, vp, C.c_int64, vp, C.c_int64, i32, vp, C.c_float, C.POINTER(_Mx), vp,
+                                    C.c_int64, vp]),
+        "war_quantize": (i32, [C.POINTER(_Mx), vp, C.c_int64, vp, C.c_int64, i32, vp]),
+        "war_dequantize": (i32, [C.POINTER(_Mx), vp, C.c_int64, i32, vp]),
+        "war_linear_create": (i32, [C.POINTER(_Mx), vp, vp, C.POINTER(vp)]),
+        "war_linear_destroy": (None, [vp]),
+        "war_linear_run": (i32, [vp, C.POINTER(_Mx), vp, C.c_int64, i32, vp]),
+        "war_rope_write": (i32, [vp, i32, C.POINTER(_Rope), i32, vp, vp, i32, vp, vp, vp, C.c_int64, vp, C.c_int64, vp,
+                                 C.c_int64, vp, C.c_int64, vp]),
         "war_constrain_workspace": (C.c_int64, [i32, i32]),
         "war_constrain_logits": (i32, [C.POINTER(_Constraints), i32, i32, vp, vp, vp, vp, vp, i32, vp, C.c_int64, vp,
                                        C.c_int64, vp, vp, vp]),
@@ -455,6 +476,168 @@ def attend(plan: AttendPlan, layer: int, q: torch.Tensor, out: torch.Tensor, str
     qs, os_ = _rows_of("q", q, dev, B, n, H, D), _rows_of("out", out, dev, B, n, H, D)
     _call(lib().war_attend_run, dev, stream, plan.handle, layer, q.data_ptr(), qs, out.data_ptr(), os_)
     return out
+
+
+MX_FORMATS = {"e4m3": 2, "e2m1": 3}
+_TYPES = {torch.bfloat16: 0, torch.float32: 1}
+
+
+def _matrix(name: str, t: torch.Tensor, device, rows: int, cols: int, types=_TYPES) -> int:
+    """The row stride of a [rows, cols] matrix of one of these types."""
+    if not (t.dtype in types and t.device == device and t.shape == (rows, cols) and (cols == 1 or t.stride(1) == 1)):
+        raise ValueError(f"{name} must be [{rows}, {cols}] of {' or '.join(str(x) for x in types)} on {device}, columns "
+                         "one after the other")
+    return t.stride(0) if rows > 1 else (cols + 7) // 8 * 8
+
+
+class Mx:
+    """A matrix of microscaled numbers (war.h): codes uint8 [rows, cols] ("e4m3") or
+    [rows, cols / 2] ("e2m1": two a byte, the even column in the low bits) and scales
+    uint8 [rows, cols / 32], 2^(byte - 127) for 32 columns; rows of scales at a multiple
+    of 4 bytes.  Both stay the caller's."""
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, format: str):
+        if format not in MX_FORMATS:
+            raise ValueError(f"format must be one of {sorted(MX_FORMATS)}")
+        _require(codes.dim() == 2 and codes.dtype == torch.uint8 and scales.dtype == torch.uint8, "codes and scales must be uint8 matrices")
+        rows, cols = codes.shape[0], codes.shape[1] * (1 if format == "e4m3" else 2)
+        _require(cols >= 32 and cols % 32 == 0, "a row must hold whole blocks of 32")
+        cs = _matrix("codes", codes, codes.device, rows, codes.shape[1], (torch.uint8,))
+        ss = _matrix("scales", scales, codes.device, rows, cols // 32, (torch.uint8,))
+        self.codes, self.scales, self.format, self.device, self.shape = codes, scales, format, codes.device, (rows, cols)
+        self._c = _Mx(MX_FORMATS[format], rows, cols, codes.data_ptr(), -(-cs // 16) * 16 if rows < 2 else cs, scales.data_ptr(), ss)
+        self._ref = C.byref(self._c)
+
+    @staticmethod
+    def empty(rows: int, cols: int, format: str, device="cuda") -> "Mx":
+        """Memory for rows x cols numbers."""
+        if format not in MX_FORMATS:
+            raise ValueError(f"format must be one of {sorted(MX_FORMATS)}")
+        codes = torch.empty((rows, cols if format == "e4m3" else cols // 2), dtype=torch.uint8, device=device)
+        scales = torch.empty((rows, -(-cols // 128) * 4), dtype=torch.uint8, device=device)
+        return Mx(codes, scales[:, : cols // 32], format)
+
+    def __getitem__(self, rows: slice) -> "Mx":
+        """Some of the rows, in the same memory."""
+        return Mx(self.codes[rows], self.scales[rows], self.format)
+
+
+def residual_norm(x: Optional[torch.Tensor], h: torch.Tensor, gain: torch.Tensor, eps: float, out, stream=None):
+    """h += x (None: h stays), then out = h / sqrt(mean(h^2) + eps) * gain: into an Mx, or a
+    bf16 matrix.  h fp32 or bf16 [rows, cols], x and gain bf16."""
+    dev, (rows, cols) = h.device, h.shape
+    hs = _matrix("h", h, dev, rows, cols)
+    xs = 0 if x is None else _matrix("x", x, dev, rows, cols, (torch.bfloat16,))
+    _checked(dev, torch.bfloat16, gain=gain)
+    _require(gain.numel() == cols, "gain must hold an entry a column")
+    if isinstance(out, Mx):
+        _require(out.shape == (rows, cols) and out.device == dev, f"out must hold [{rows}, {cols}] on {dev}")
+        mx, y, ys = out._ref, None, 0
+    else:
+        mx, y, ys = None, out.data_ptr(), _matrix("out", out, dev, rows, cols, (torch.bfloat16,))
+    _call(lib().war_residual_norm, dev, stream, rows, cols, _addr(x), xs, h.data_ptr(), hs, _TYPES[h.dtype], gain.data_ptr(),
+          eps, mx, y, ys)
+    return out
+
+
+def quantize(x: torch.Tensor, out: Mx, gate: Optional[torch.Tensor] = None, stream=None) -> Mx:
+    """x (bf16 or fp32 [rows, cols]), or x * silu(gate), into codes."""
+    dev, (rows, cols) = out.device, out.shape
+    xs = _matrix("x", x, dev, rows, cols)
+    gs = 0 if gate is None else _matrix("gate", gate, dev, rows, cols, (x.dtype,))
+    _call(lib().war_quantize, dev, stream, out._ref, x.data_ptr(), xs, _addr(gate), gs, _TYPES[x.dtype])
+    return out
+
+
+def dequantize(mx: Mx, out: torch.Tensor, stream=None) -> torch.Tensor:
+    """The numbers that codes stand for, into bf16 or fp32 [rows, cols]."""
+    s = _matrix("out", out, mx.device, *mx.shape)
+    _call(lib().war_dequantize, mx.device, stream, mx._ref, out.data_ptr(), s, _TYPES[out.dtype])
+    return out
+
+
+class Linear:
+    """Weights [N, K] in 4 bits for y = x w^T + bias: an Mx in "e2m1", or a bf16 or fp32
+    matrix that is quantised here; bias bf16 [N].  Laid out in memory of its own, so the
+    arguments may be dropped afterwards."""
+
+    def __init__(self, weight, bias: Optional[torch.Tensor] = None, stream=None):
+        dev = weight.device
+        if not isinstance(weight, Mx):
+            _require(weight.dim() == 2, "weight must be a matrix")
+            make = lambda: quantize(weight, Mx.empty(*weight.shape, "e2m1", dev), stream=stream)
+            if stream is None:
+                weight = make()
+            else:  # that stream's own memory
+                with torch.cuda.stream(stream):
+                    weight = make()
+        self.device, (self.out_features, self.in_features) = dev, weight.shape
+        _checked(dev, torch.bfloat16, bias=bias)
+        _require(bias is None or bias.numel() == self.out_features, "bias must hold an entry a row of the weights")
+        h = C.c_void_p()
+        create = lambda mx, b, st: lib().war_linear_create(mx, b, st, C.byref(h))
+        _call(create, dev, stream, weight._ref, _addr(bias))
+        self.handle = h
+
+    def close(self):
+        if getattr(self, "handle", None):
+            lib().war_linear_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def linear(weights: Linear, x: Mx, out: torch.Tensor, stream=None) -> torch.Tensor:
+    """out = x w^T + bias: x [rows, K] in codes, out bf16 or fp32 [rows, N]."""
+    _require(bool(weights.handle), "the weights are closed")
+    dev, N = weights.device, weights.out_features
+    _require(x.device == dev and x.shape[1] == weights.in_features, f"x must have {weights.in_features} columns on {dev}")
+    s = _matrix("out", out, dev, x.shape[0], N)
+    _call(lib().war_linear_run, dev, stream, weights.handle, x._ref, out.data_ptr(), s, _TYPES[out.dtype])
+    return out
+
+
+class Rope:
+    """Rotary positions: pair j of a head's first rotary_dim numbers (default all) turns by
+    its row's position on axis axes[j] (default one axis) times base^(-2 j / rotary_dim),
+    or freqs[j].  Pair j is (j, j + rotary_dim / 2); adjacent: (2 j, 2 j + 1)."""
+
+    def __init__(self, head_dim: int, rotary_dim: Optional[int] = None, base: float = 10000.0,
+                 axes: Optional[Sequence[int]] = None, adjacent: bool = False, freqs: Optional[Sequence[float]] = None):
+        R = head_dim if rotary_dim is None else rotary_dim
+        _require(head_dim in (64, 128) and 8 <= R <= head_dim and R % 8 == 0, "rotary_dim must be a multiple of 8 in [8, head_dim]")
+        axes = [0] * (R // 2) if axes is None else [int(a) for a in axes]
+        freqs = [float(base) ** (-2.0 * j / R) for j in range(R // 2)] if freqs is None else [float(f) for f in freqs]
+        _require(len(axes) == R // 2 and len(freqs) == R // 2, "axes and freqs must hold an entry a pair")
+        _require(all(0 <= a < 4 for a in axes), "at most four axes")
+        self.head_dim, self.n_axes = head_dim, max(axes) + 1
+        self._axes, self._freqs = (C.c_uint8 * len(axes))(*axes), (C.c_double * len(freqs))(*freqs)
+        self._c = _Rope(R, int(adjacent), self.n_axes, C.addressof(self._axes), C.addressof(self._freqs))
+        self._ref = C.byref(self._c)
+
+
+def rope_write(pool: Pool, layer: int, rope: Rope, seq_ids: torch.Tensor, pos0: torch.Tensor, q: torch.Tensor,
+               k: torch.Tensor, v: torch.Tensor, q_out: torch.Tensor, n_lens: Optional[torch.Tensor] = None,
+               positions: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Tokens pos0[b] + i: queries bf16 [B, n, Hq, D] turned into q_out (may be q), keys
+    bf16 [B, n, Hkv, D] turned and written into their pages with the values.  positions
+    int32 [n_axes, B, n]: where each row is on each axis (default: its place in the cache
+    on all of them)."""
+    B, n, dev, c = seq_ids.numel(), k.shape[1], pool.kv.device, pool.cfg
+    _checked(dev, torch.int32, seq_ids=seq_ids, pos0=pos0, n_lens=n_lens, positions=positions)
+    _require(bool(pool.handle), "the pool is closed")
+    _require(rope.head_dim == c.head_dim, "rope is made for another head_dim")
+    _require(pos0.numel() == B and (n_lens is None or n_lens.numel() == B), "pos0 and n_lens must hold one entry a request")
+    _require(positions is None or positions.shape == (rope.n_axes, B, n), f"positions must be [{rope.n_axes}, {B}, {n}]")
+    qs, os_ = _rows_of("q", q, dev, B, n, c.n_q_heads, c.head_dim), _rows_of("q_out", q_out, dev, B, n, c.n_q_heads, c.head_dim)
+    ks, vs = _rows_of("k", k, dev, B, n, c.n_kv_heads, c.head_dim), _rows_of("v", v, dev, B, n, c.n_kv_heads, c.head_dim)
+    _call(lib().war_rope_write, dev, stream, pool.handle, layer, rope._ref, B, seq_ids.data_ptr(), pos0.data_ptr(), n,
+          _addr(n_lens), _addr(positions), q.data_ptr(), qs, q_out.data_ptr(), os_, k.data_ptr(), ks, v.data_ptr(), vs)
+    return q_out
 
 
 class Constraints:
