@@ -14,6 +14,7 @@
 // their scale bytes.  Padded with zero codes to 256 rows and 512 columns.
 #include <type_traits>
 
+#include "lds_load.h"
 #include "mx.h"
 
 namespace {
@@ -53,28 +54,46 @@ WAR_DEV f32x4 mx_mfma(i32x8 w, i32x8 x, f32x4 c, uint32_t sw, uint32_t sx) {
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, c, 4, XF == kMxE4M3 ? 0 : 4, J, (int)sw, 0, (int)sx);
 }
 
-// Four results y[m][n .. n + 3]
+// a descriptor, or one that holds nothing (loads give zeros)
+WAR_DEV i32x4 sized(i32x4 r, bool on) {
+  r[2] = on ? r[2] : 0;
+  return r;
+}
+
+// e4m3 codes of 2 and more (bit 6 of the code), and the others: products of either part
+// with e2m1 numbers span so few places that the instruction adds them without a cut.
+WAR_DEV void split_codes(const i32x8& x, i32x8& hi, i32x8& lo) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t c = (uint32_t)x[i], b = (c >> 6) & 0x01010101u, mask = (b << 8) - b;
+    hi[i] = (int)(c & mask);
+    lo[i] = (int)(c & ~mask);
+  }
+}
+
+// Four results y[m][n .. n + 3], all of them in y and in one piece
+template <bool F32>
+WAR_DEV void store_whole(const MxGemmArgs& a, int m, int n, f32x4 v) {
+  const uint2 b = *reinterpret_cast<const uint2*>(a.bias + n);
+  v[0] += lo_f(b.x), v[1] += hi_f(b.x), v[2] += lo_f(b.y), v[3] += hi_f(b.y);
+  const int64_t at = (int64_t)m * a.y_stride + n;
+  if constexpr (F32) *reinterpret_cast<f32x4*>(static_cast<float*>(a.y) + at) = v;
+  else *reinterpret_cast<uint2*>(static_cast<bf16_t*>(a.y) + at) = make_uint2(pack2(v[0], v[1]), pack2(v[2], v[3]));
+}
+// The same where some may lie outside, or rows begin anywhere
 template <bool F32>
 WAR_DEV void store_y(const MxGemmArgs& a, int m, int n, f32x4 v) {
   if (m >= a.M || n >= a.N) return;
-  const uint2 bb = *reinterpret_cast<const uint2*>(a.bias + n);
-  v[0] += lo_f(bb.x), v[1] += hi_f(bb.x), v[2] += lo_f(bb.y), v[3] += hi_f(bb.y);
+  if (a.vec && n + 4 <= a.N) return store_whole<F32>(a, m, n, v);
+  const uint2 b = *reinterpret_cast<const uint2*>(a.bias + n);  // padded
+  v[0] += lo_f(b.x), v[1] += hi_f(b.x), v[2] += lo_f(b.y), v[3] += hi_f(b.y);
   const int64_t at = (int64_t)m * a.y_stride + n;
-  if constexpr (F32) {
-    float* y = static_cast<float*>(a.y) + at;
-    if (a.vec && n + 4 <= a.N) *reinterpret_cast<f32x4*>(y) = v;
-    else
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (n + i < a.N) y[i] = v[i];
-  } else {
-    bf16_t* y = static_cast<bf16_t*>(a.y) + at;
-    if (a.vec && n + 4 <= a.N) *reinterpret_cast<uint2*>(y) = make_uint2(pack2(v[0], v[1]), pack2(v[2], v[3]));
-    else
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (n + i < a.N) y[i] = f2bf(v[i]);
-  }
+  for (int i = 0; i < 4; ++i)
+    if (n + i < a.N) {
+      if constexpr (F32) static_cast<float*>(a.y)[at + i] = v[i];
+      else static_cast<bf16_t*>(a.y)[at + i] = f2bf(v[i]);
+    }
 }
 
 // Few rows: the weights' way from memory bounds it.  A workgroup takes 16 NT columns by
@@ -82,6 +101,7 @@ WAR_DEV void store_y(const MxGemmArgs& a, int m, int n, f32x4 v) {
 // from memory to registers, and their sums meet in LDS in the waves' order.
 template <int MT, int NT, int WAVES, int XF, bool F32>
 __global__ void __launch_bounds__(WAVES * 64) k_mx_skinny(MxGemmArgs a) {
+  constexpr bool EXACT = XF == kMxE4M3 && F32;
   constexpr int XB = XF == kMxE4M3 ? 128 : 64;  // bytes of a row's k-step
   __shared__ f32x4 s_sum[WAVES][MT * NT][64];
   const int lane = threadIdx.x & 63, ln = lane & 15, lg = lane >> 4;
@@ -151,11 +171,18 @@ __global__ void __launch_bounds__(WAVES * 64) k_mx_skinny(MxGemmArgs a) {
           const uint4 hi = x[J][m][1];
           xv[4] = (int)hi.x, xv[5] = (int)hi.y, xv[6] = (int)hi.z, xv[7] = (int)hi.w;
         }
+        i32x8 xl = xv;
+        if constexpr (EXACT) {
+          const i32x8 whole = xv;
+          split_codes(whole, xv, xl);
+        }
         const uint32_t s = sx[m][J] >> (8 * lg);
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
           const uint4 c = w[J][n];
-          acc[m][n] = mx_mfma<XF, J>(i32x8{(int)c.x, (int)c.y, (int)c.z, (int)c.w, 0, 0, 0, 0}, xv, acc[m][n], sw[n], s);
+          const i32x8 wv = {(int)c.x, (int)c.y, (int)c.z, (int)c.w, 0, 0, 0, 0};
+          acc[m][n] = mx_mfma<XF, J>(wv, xv, acc[m][n], sw[n], s);
+          if constexpr (EXACT) acc[m][n] = mx_mfma<XF, J>(wv, xl, acc[m][n], sw[n], s);
         }
       }
     };
@@ -173,6 +200,236 @@ __global__ void __launch_bounds__(WAVES * 64) k_mx_skinny(MxGemmArgs a) {
     f32x4 v = s_sum[0][t][lane];
     for (int w = 1; w < WAVES; ++w) v += s_sum[w][t][lane];
     store_y<F32>(a, m0 + (t / NT) * 16 + ln, (nt0 + t % NT) * 16 + lg * 4, v);
+  }
+}
+
+// Many rows: the matrix cores bound it.  A workgroup computes a BM x BN tile from LDS; 8
+// waves as WM x WN.  A step is 128 bytes of each of x's rows: KF fragments of 128 columns
+// (e4m3: one, e2m1: two).  Every operand byte comes straight from memory to LDS, ST
+// stages of one step each: x's rows with their eight 16-byte chunks permuted so that
+// fragment reads fall on different banks, the weights' fragments as they are stored, a
+// word of scale bytes for each row and fragment; the weights' scale words come for four
+// fragments at once, into one of two buffers of their own.
+template <int BM, int BN, int WM, int WN, int ST, int XF, bool F32>
+__global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) k_mx_tile(MxGemmArgs a) {
+  static_assert(WM * WN == 8 && BM % 64 == 0 && BN % 128 == 0 && BM + BN <= 512, "8 waves, whole loads");
+  constexpr bool E8 = XF == kMxE4M3, EXACT = E8 && F32;
+  constexpr int KF = E8 ? 1 : 2, KS = 128 * KF;
+  constexpr int MT = BM / WM / 16, NT = BN / WN / 16;
+  constexpr int A_INS = BM / 64, W_INS = BN * KF / 128, INS = A_INS + W_INS + KF;  // loads of a wave and step
+  constexpr int A_B = BM * 128, W_B = BN * 64 * KF, XS_B = 2048 * KF, STAGE = A_B + W_B + XS_B, WS_B = BN * 16;
+  constexpr int GS = 4 / KF;                            // steps that a word of the weights' scales serves
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[ST * STAGE + 2 * WS_B];
+  const int tid = threadIdx.x, lane = tid & 63, ln = lane & 15, lg = lane >> 4;
+  const int wi = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wi % WM, wn = wi / WM;
+  const int mblocks = (a.M + BM - 1) / BM, NB = (a.N + BN - 1) / BN;
+  // Workgroups are dealt to the 8 XCDs round-robin by linear id: the m-blocks of one
+  // weight block get ids 8 apart, so all but the first find W in that XCD's L2; a ragged
+  // tail of fewer than 8 n-blocks falls back to consecutive ids.
+  const int full = (NB / 8) * 8 * mblocks;
+  int nb, mb;
+  if ((int)blockIdx.x < full) {
+    const int r = blockIdx.x % (8 * mblocks);
+    nb = (blockIdx.x / (8 * mblocks)) * 8 + (r & 7);
+    mb = r >> 3;
+  } else {
+    const int r = blockIdx.x - full;
+    nb = (NB / 8) * 8 + r / mblocks;
+    mb = r % mblocks;
+  }
+  const int m0 = mb * BM, rows = min(BM, a.M - m0);
+  const int groups = (a.K + 511) / 512, nsteps = (a.K + KS - 1) / KS;
+  const int kbytes = E8 ? a.K : a.K / 2, tile_b = groups * 4096;
+  const i32x4 xres = make_rsrc(a.x.codes + (int64_t)m0 * a.x.code_stride, (int64_t)(rows - 1) * a.x.code_stride + kbytes);
+  const i32x4 sres = make_rsrc(a.x.scales + (int64_t)m0 * a.x.scale_stride,
+                               (int64_t)(rows - 1) * a.x.scale_stride + ((a.K / 32 + 3) & ~3));
+  const i32x4 wres = make_rsrc(a.w + (int64_t)nb * (BN / 16) * tile_b, (int64_t)(BN / 16) * tile_b);
+  const i32x4 wsres = make_rsrc(a.ws + (int64_t)nb * (BN / 16) * groups * 64, (int64_t)(BN / 16) * groups * 256);
+  const int xstride = (int)a.x.code_stride, sstride = (int)a.x.scale_stride;
+
+  // x: load i of wave wi brings rows (i * 8 + wi) * 8 .. + 7, lane l the 16-byte slot
+  // l % 8 of row l / 8.  Slot c of row r holds chunk c ^ ((r / 2) % 8).  Rows past the
+  // last and chunks past K are past the descriptor: zero codes.
+  const int ar = wi * 8 + (lane >> 3), ac = ((lane & 7) ^ ((ar >> 1) & 7)) * 16;
+  constexpr int PAST = 0x7fff0000;                      // past every descriptor
+  const int xv = ar * xstride + ac;
+  const int wv = (wi / KF) * tile_b + (wi % KF) * 1024 + lane * 16;  // load i: 8 / KF tiles further
+  const int sv = wi * 64 + lane < BM ? (wi * 64 + lane) * sstride : PAST;  // a row's scales (the other waves': zeros)
+  // load i of k-step s into stage q; steps past the last bring zeros, so that every wave
+  // has the same loads in flight in every step
+  auto load1 = [&](int q, int s, int i) __attribute__((always_inline)) {
+    const uint32_t to = lds_addr(smem) + q * STAGE;
+    const bool on = s < nsteps;
+    if (i < KF) {
+      const int f = s * KF + i;
+      load_lds4(to + A_B + W_B + i * 2048 + wi * 256, sv + f * 4, sized(sres, f * 128 < a.K));
+    } else if (i < KF + A_INS) {
+      const int o = s * 128 + ac < kbytes ? xv + s * 128 + (i - KF) * 64 * xstride : PAST;
+      load_lds16<false>(to + (i - KF) * 8192 + wi * 1024, o, sized(xres, on));
+    } else {
+      const int j = i - KF - A_INS;
+      load_lds16<false>(to + A_B + j * 8192 + wi * 1024, wv + j * (8 / KF) * tile_b + s * KF * 1024, sized(wres, on));
+    }
+  };
+  // the weights' scale words of group g: the last waves bring four tiles each
+  auto load_ws = [&](int g) __attribute__((always_inline)) {
+    const int i = wi - (8 - BN / 64);
+    if (i >= 0 && g < groups)
+      load_lds16<false>(lds_addr(smem) + ST * STAGE + (g & 1) * WS_B + i * 1024, ((i * 4 + (lane >> 4)) * groups + g) * 256 + (lane & 15) * 16, wsres);
+  };
+
+  const int woff = wn * NT * KF * 1024 + lane * 16;
+  const int r0 = wm * (BM / WM) + ln;                   // (r0 + 16 mt) / 2 % 8 is the same for every mt
+  int aoff[2];
+#pragma unroll
+  for (int j = 0; j < 2; ++j) aoff[j] = r0 * 128 + (((j * 4 + lg) ^ ((r0 >> 1) & 7)) * 16);
+
+  f32x4 acc[MT][NT];
+#pragma unroll
+  for (int m = 0; m < MT; ++m)
+#pragma unroll
+    for (int n = 0; n < NT; ++n) acc[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+  // own loads of the next stage arrived (`left` later ones may be in flight) and own LDS
+  // reads done, then everyone's
+  auto sync = [&](auto left) __attribute__((always_inline)) {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(decltype(left)::value) : "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  // A step is KF MT slots, one x fragment (and NT products) each, read LOOK slots ahead.
+  // Before the last LOOK slots the next stage must be complete (sync); every read of this
+  // stage is then done, and step s + ST is requested into it, a few loads a slot, on into
+  // the next step's first slots.
+  constexpr int SLOTS = KF * MT, RING = SLOTS % 4 == 0 ? 4 : SLOTS % 3 == 0 ? 3 : 2, LOOK = SLOTS == 4 ? 2 : RING - 1;
+  constexpr int LPS = (INS + SLOTS - 1) / SLOTS;
+  static_assert(SLOTS % RING == 0 && RING > LOOK && SLOTS > LOOK, "a ring of fragments");
+  constexpr int HEAD = LPS * LOOK < INS ? LPS * LOOK : INS;
+  uint4 ra[RING][E8 ? 2 : 1], rb[2][NT];
+  uint32_t rs[RING], wsc[2][NT];                        // scale bytes
+  auto read_x = [&](const unsigned char* st, int i) __attribute__((always_inline)) {
+    const int m = i % MT, h = i / MT;
+    const unsigned char* p = st + m * 2048;
+    ra[i % RING][0] = *reinterpret_cast<const uint4*>(p + aoff[E8 ? 0 : h]);
+    if constexpr (E8) ra[i % RING][1] = *reinterpret_cast<const uint4*>(p + aoff[1]);
+    rs[i % RING] = st[A_B + W_B + (h * 512 + r0 + m * 16) * 4 + lg];
+  };
+  auto read_w = [&](const unsigned char* st, int to, int h, int f, int n) __attribute__((always_inline)) {  // f = s KF + h
+    rb[to][n] = *reinterpret_cast<const uint4*>(st + A_B + woff + (n * KF + h) * 1024);
+    wsc[to][n] = smem[ST * STAGE + f / 4 % 2 * WS_B + (wn * NT + n) * 256 + lane * 4 + f % 4];
+  };
+  // U: which of the unrolled steps (its stage, its fragments' buffer)
+  auto step = [&](int s, auto tag) __attribute__((always_inline)) {
+    constexpr int U = decltype(tag)::value, C = U % ST, N = (U + 1) % ST, Pv = (U + ST - 1) % ST;
+    const unsigned char *SC = smem + C * STAGE, *SN = smem + N * STAGE;
+    if (s % GS == 0) load_ws(s / GS + 1);
+#pragma unroll
+    for (int i = 0; i < SLOTS; ++i) {
+      if (i == SLOTS - LOOK) {
+        // stages s + 2 .. s + ST - 1 may still be in flight
+        sync(std::integral_constant<int, (ST - 2) * INS>{});
+      }
+      if (i < SLOTS - LOOK) read_x(SC, i + LOOK);
+      else read_x(SN, i + LOOK - SLOTS);
+      if (KF == 2 && i < MT) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+          if (n * MT / NT == i) read_w(SC, 1, 1, s * 2 + 1, n);
+      }
+      if (i >= SLOTS - LOOK) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+          if (n * LOOK / NT == i - (SLOTS - LOOK)) read_w(SN, KF == 2 ? 0 : (U + 1) % 2, 0, (s + 1) * KF, n);
+#pragma unroll
+        for (int q = 0; q < LPS; ++q)
+          if ((i - (SLOTS - LOOK)) * LPS + q < INS) load1(C, s + ST, (i - (SLOTS - LOOK)) * LPS + q);
+      } else if (HEAD + i * LPS < INS) {
+#pragma unroll
+        for (int q = 0; q < LPS; ++q)
+          if (HEAD + i * LPS + q < INS) load1(Pv, s + ST - 1, HEAD + i * LPS + q);
+      }
+      // the block of this lane's scale lies past K: zero codes, and any byte but NaN's
+      const uint32_t sx = (s * KF + i / MT) * 128 + lg * 32 < a.K ? rs[i % RING] : 127u;
+      const uint4 x0 = ra[i % RING][0];
+      i32x8 xf = {(int)x0.x, (int)x0.y, (int)x0.z, (int)x0.w, 0, 0, 0, 0}, xl = xf;
+      if constexpr (E8) {
+        const uint4 x1 = ra[i % RING][1];
+        xf[4] = (int)x1.x, xf[5] = (int)x1.y, xf[6] = (int)x1.z, xf[7] = (int)x1.w;
+        if constexpr (EXACT) {
+          const i32x8 whole = xf;
+          split_codes(whole, xf, xl);
+        }
+      }
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        const uint4 w0 = rb[KF == 2 ? i / MT : U % 2][n];
+        const i32x8 wf = {(int)w0.x, (int)w0.y, (int)w0.z, (int)w0.w, 0, 0, 0, 0};
+        acc[i % MT][n] = mx_mfma<XF, 0>(wf, xf, acc[i % MT][n], wsc[KF == 2 ? i / MT : U % 2][n], sx);
+      }
+      if constexpr (EXACT) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          const uint4 w0 = rb[U % 2][n];
+          const i32x8 wf = {(int)w0.x, (int)w0.y, (int)w0.z, (int)w0.w, 0, 0, 0, 0};
+          acc[i % MT][n] = mx_mfma<XF, 0>(wf, xl, acc[i % MT][n], wsc[U % 2][n], sx);
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+
+  load_ws(0);
+#pragma unroll
+  for (int q = 0; q < ST; ++q) {
+    // (of the last stage only what a step leaves to the one before it: step 0 brings the rest)
+#pragma unroll
+    for (int i = 0; i < (q == ST - 1 ? HEAD : INS); ++i) load1(q, q, i);
+  }
+  sync(std::integral_constant<int, (ST - 2) * INS + HEAD>{});
+#pragma unroll
+  for (int n = 0; n < NT; ++n) read_w(smem, 0, 0, 0, n);
+#pragma unroll
+  for (int i = 0; i < LOOK; ++i) read_x(smem, i);
+  __builtin_amdgcn_sched_barrier(0);
+  // (the reads past the last step are of no use, and in bounds)
+  for (int s = 0; s < nsteps;) {
+    step(s++, std::integral_constant<int, 0>{});
+    if (s < nsteps) step(s++, std::integral_constant<int, 1>{});
+    if constexpr (ST == 3) {
+      if (s < nsteps) step(s++, std::integral_constant<int, 2>{});
+      if constexpr (KF == 1) {
+        if (s < nsteps) step(s++, std::integral_constant<int, 3>{});
+        if (s < nsteps) step(s++, std::integral_constant<int, 4>{});
+        if (s < nsteps) step(s++, std::integral_constant<int, 5>{});
+      }
+    }
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // no load into LDS outlives the workgroup
+  const int n0 = nb * BN + wn * NT * 16 + lg * 4;
+  if (a.vec && n0 - lg * 4 + NT * 16 <= a.N) {
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+      if (m0 + r0 + m * 16 < a.M) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) store_whole<F32>(a, m0 + r0 + m * 16, n0 + n * 16, acc[m][n]);
+      }
+  } else {
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int n = 0; n < NT; ++n) store_y<F32>(a, m0 + r0 + m * 16, n0 + n * 16, acc[m][n]);
+  }
+}
+
+template <int BM, int BN, int WM, int WN, int ST8, int ST4>
+void tile(const MxGemmArgs& a, int fmt, bool f32, hipStream_t st) {
+  const int grid = cdiv_i(a.N, BN) * cdiv_i(a.M, BM);
+  if (fmt == kMxE4M3) {
+    if (f32) k_mx_tile<BM, BN, WM, WN, ST8, kMxE4M3, true><<<grid, 512, 0, st>>>(a);
+    else k_mx_tile<BM, BN, WM, WN, ST8, kMxE4M3, false><<<grid, 512, 0, st>>>(a);
+  } else {
+    if (f32) k_mx_tile<BM, BN, WM, WN, ST4, kMxE2M1, true><<<grid, 512, 0, st>>>(a);
+    else k_mx_tile<BM, BN, WM, WN, ST4, kMxE2M1, false><<<grid, 512, 0, st>>>(a);
   }
 }
 
@@ -195,6 +452,42 @@ void launch_mx_pack(const MxRef& w, int N, int K, uint8_t* codes, uint32_t* scal
 }
 
 void launch_mx_gemm(const MxGemmArgs& a, int fmt, bool f32, hipStream_t st) {
+#ifdef MX_TUNE
+  static const char* v = getenv("MXV");
+  if (v) {
+    const int c = atoi(v);
+    switch (c) {
+      case 1: return skinny<1, 1, 8>(a, fmt, f32, st);
+      case 2: return skinny<1, 2, 8>(a, fmt, f32, st);
+      case 3: return skinny<2, 1, 8>(a, fmt, f32, st);
+      case 4: return skinny<2, 2, 8>(a, fmt, f32, st);
+      case 5: return skinny<4, 1, 8>(a, fmt, f32, st);
+      case 6: return skinny<4, 2, 8>(a, fmt, f32, st);
+      case 7: return skinny<4, 4, 4>(a, fmt, f32, st);
+      case 8: return skinny<5, 2, 8>(a, fmt, f32, st);
+      case 9: return skinny<5, 4, 4>(a, fmt, f32, st);
+      case 10: return skinny<1, 4, 8>(a, fmt, f32, st);
+      case 11: return skinny<4, 2, 4>(a, fmt, f32, st);
+      case 12: return skinny<1, 1, 16>(a, fmt, f32, st);
+      case 13: return skinny<5, 6, 4>(a, fmt, f32, st);
+      case 20: return tile<64, 128, 1, 8, 2, 2>(a, fmt, f32, st);
+      case 21: return tile<64, 128, 2, 4, 3, 3>(a, fmt, f32, st);
+      case 22: return tile<128, 128, 2, 4, 2, 2>(a, fmt, f32, st);
+      case 23: return tile<128, 128, 2, 4, 3, 3>(a, fmt, f32, st);
+      case 24: return tile<128, 256, 2, 4, 2, 2>(a, fmt, f32, st);
+      case 25: return tile<128, 256, 2, 4, 3, 2>(a, fmt, f32, st);
+      case 26: return tile<256, 128, 4, 2, 2, 2>(a, fmt, f32, st);
+      case 27: return tile<256, 128, 4, 2, 3, 3>(a, fmt, f32, st);
+      case 28: return tile<256, 256, 2, 4, 2, 2>(a, fmt, f32, st);
+      case 29: return tile<256, 256, 2, 4, 3, 2>(a, fmt, f32, st);
+      case 30: return tile<192, 256, 2, 4, 2, 2>(a, fmt, f32, st);
+      case 31: return tile<192, 128, 2, 4, 2, 2>(a, fmt, f32, st);
+      case 32: return tile<256, 256, 4, 2, 2, 2>(a, fmt, f32, st);
+    }
+  }
+#endif
   if (a.M <= 16) skinny<1, 1, 8>(a, fmt, f32, st);
-  else skinny<2, 2, 8>(a, fmt, f32, st);
+  else if (a.M <= 64 || a.x.code_stride > 1 << 22 || a.x.scale_stride > 1 << 22) skinny<2, 2, 8>(a, fmt, f32, st);
+  else if (a.M <= 128) tile<128, 128, 2, 4, 2, 2>(a, fmt, f32, st);
+  else tile<256, 256, 2, 4, 2, 2>(a, fmt, f32, st);
 }
