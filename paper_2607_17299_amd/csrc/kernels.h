@@ -341,14 +341,13 @@ struct MxGemmArgs {
   const bf16_t* bias;  // [N padded], zero where there is none
   void* y;
   int64_t y_stride;
-  int vec;             // rows of y may be written four columns at a time
 };
-// N in tiles of 16 rows, K in groups of 512: what a packed matrix is padded to (with
+// N in tiles of 32 rows, K in groups of 512: what a packed matrix is padded to (with
 // zero codes)
-inline int mx_tiles(int N) { return (N + 255) / 256 * 16; }
+inline int mx_tiles(int N) { return (N + 255) / 256 * 8; }
 inline int mx_groups(int K) { return (K + 511) / 512; }
-inline int64_t mx_code_bytes(int N, int K) { return (int64_t)mx_tiles(N) * mx_groups(K) * 4096; }
-inline int64_t mx_scale_words(int N, int K) { return (int64_t)mx_tiles(N) * mx_groups(K) * 64; }
+inline int64_t mx_code_bytes(int N, int K) { return (int64_t)mx_tiles(N) * mx_groups(K) * 8192; }
+inline int64_t mx_scale_words(int N, int K) { return (int64_t)mx_tiles(N) * mx_groups(K) * 128; }
 void launch_mx_pack(const MxRef& w, int N, int K, uint8_t* codes, uint32_t* scales, hipStream_t st);
 void launch_mx_gemm(const MxGemmArgs& a, int fmt, bool f32, hipStream_t st);
 

@@ -133,7 +133,7 @@ war_status war_linear_create(const war_mx* w, const void* bias, void* stream, wa
   hipStream_t st = static_cast<hipStream_t>(stream);
   war_linear* l = new (std::nothrow) war_linear{w->rows, w->cols, nullptr};
   if (!l) return api_fail(WAR_ERR_HIP, "out of host memory");
-  const int64_t n_bias = (int64_t)mx_tiles(l->N) * 16;
+  const int64_t n_bias = (int64_t)mx_tiles(l->N) * 32;
   hipError_t e = hipMalloc(reinterpret_cast<void**>(&l->mem),
                            mx_code_bytes(l->N, l->K) + 4 * mx_scale_words(l->N, l->K) + 2 * n_bias);
   if (e != hipSuccess) {
@@ -181,7 +181,6 @@ war_status war_linear_run(const war_linear* l, const war_mx* x, void* y, int64_t
   a.bias = l->bias();
   a.y = y;
   a.y_stride = y_stride;
-  a.vec = y_stride % 4 == 0 && aligned(y, 4 * size);
   launch_mx_gemm(a, fmt(*x), y_type == WAR_F32, static_cast<hipStream_t>(stream));
   HIPCHK(hipGetLastError());
   return WAR_OK;

@@ -1,17 +1,20 @@
 // y = x w^T of microscaled numbers (mx.h): weights in e2m1, activations in e4m3 or e2m1,
-// fp32 sums in the scaled matrix instructions (v_mfma_scale_f32_16x16x128_f8f6f4).
+// fp32 sums in the scaled matrix instructions
+// (v_mfma_scale_f32_32x32x64_f8f6f4 for many rows, 16x16x128 for few).
 //
-// The weights are the instruction's first operand, so a lane's four results are four
-// neighbouring columns of one row of y.  Lane l holds, of row l % 16, the 32 e2m1 numbers
-// k = 32 (l / 16) .., or the 32 e4m3 numbers 16 (l / 16) .. + 15 and 64 + 16 (l / 16) ..
-// + 15; the scale of row l % 16 and block l / 16 is a byte of lane l's in both.  A block's
-// scale byte 255 makes NaN.  The instruction sums e4m3 products in groups of eight
-// neighbours in which what lies more than 13 binary places below the largest is cut off;
-// the numbers themselves carry four.  (e2m1 products span fewer places: exact.)
+// The weights are the instruction's first operand, so four neighbouring results of a lane
+// are neighbouring columns of one row of y.  A lane holds 32 numbers of a row: lane group
+// g (64 or 128 columns in two or four groups) the e2m1 numbers k = 32 g .., or the e4m3
+// numbers k = 16 g .. + 15 and as many from half the columns on; the scale of a row's block
+// b is a byte of lane group b's in both.  A block's scale byte 255 makes NaN.  The
+// instruction sums e4m3 products in groups of eight neighbours in which what lies more
+// than 13 binary places below the largest is cut off; the numbers themselves carry four.
+// (e2m1 products span fewer places: exact.)  Where y is fp32 the codes go in two parts,
+// which makes e4m3 products exact too, for twice the instructions.
 //
-// Packed weights: 1 KB fragments of 16 rows by 128 columns, 16 bytes a lane as above, the
-// fragments of a row tile one after the other; and a word a lane for four of them with
-// their scale bytes.  Padded with zero codes to 256 rows and 512 columns.
+// Packed weights: 1 KB fragments of 32 rows by 64 columns, 16 bytes a lane of the 32x32x64
+// instruction, the fragments of a row tile one after the other; and for four of them a
+// word a lane with their scale bytes.  Padded with zero codes to 256 rows and 512 columns.
 #include <type_traits>
 
 #include "lds_load.h"
@@ -19,39 +22,46 @@
 
 namespace {
 
-// grid (tile, group of 512 columns), 256 threads: fragment threadIdx / 64
-__global__ void __launch_bounds__(256) k_mx_pack(MxRef w, int N, int K, int groups, uint8_t* codes, uint32_t* scales) {
+// grid (tile of 32 rows, group of 512 columns), 512 threads: fragment threadIdx / 64
+__global__ void __launch_bounds__(512) k_mx_pack(MxRef w, int N, int K, int groups, uint8_t* codes, uint32_t* scales) {
   const int tile = blockIdx.x, grp = blockIdx.y, l = threadIdx.x & 63, j = threadIdx.x >> 6;
-  const int row = tile * 16 + (l & 15), k = grp * 512 + j * 128 + (l >> 4) * 32;
-  uint4 c = make_uint4(0, 0, 0, 0);
+  const int row = tile * 32 + (l & 31), k = grp * 512 + j * 64 + (l >> 5) * 32;
+  uint32_t c[4] = {0, 0, 0, 0};
   if (row < N && k < K) {
     const uint8_t* p = w.codes + (int64_t)row * w.code_stride + k / 2;  // (a row may begin at any byte)
-    uint32_t b[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      b[i] = 0;
-      for (int q = 0; q < 4; ++q) b[i] |= (uint32_t)p[i * 4 + q] << (8 * q);
-    }
-    c = make_uint4(b[0], b[1], b[2], b[3]);
+    for (int i = 0; i < 16; ++i) c[i / 4] |= (uint32_t)p[i] << (8 * (i % 4));
   }
-  *reinterpret_cast<uint4*>(codes + ((int64_t)(tile * (int64_t)groups + grp) * 4 + j) * 1024 + l * 16) = c;
-  if (j == 0) {
+  const int64_t at = (int64_t)tile * groups + grp;
+  *reinterpret_cast<uint4*>(codes + (at * 8 + j) * 1024 + l * 16) = make_uint4(c[0], c[1], c[2], c[3]);
+  if (j < 2) {
     uint32_t s = 0;
     for (int i = 0; i < 4; ++i) {
-      const int kk = grp * 512 + i * 128 + (l >> 4) * 32;
-      const uint32_t byte = row < N && kk < K ? w.scales[(int64_t)row * w.scale_stride + kk / 32] : 127u;
-      s |= byte << (8 * i);
+      const int kk = grp * 512 + (j * 4 + i) * 64 + (l >> 5) * 32;
+      s |= (row < N && kk < K ? w.scales[(int64_t)row * w.scale_stride + kk / 32] : 127u) << (8 * i);
     }
-    scales[(tile * (int64_t)groups + grp) * 64 + l] = s;
+    scales[(at * 2 + j) * 64 + l] = s;
   }
 }
 
-typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(4), may_alias));
+// (vector types of memory that may begin at any word, or any bf16)
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(4), may_alias));
+typedef uint32_t u32x2_half __attribute__((ext_vector_type(2), aligned(2), may_alias));
+typedef uint32_t u32x4_half __attribute__((ext_vector_type(4), aligned(2), may_alias));
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4), may_alias));
 
-// One product of fragments; J: which byte of the weights' scale word
+constexpr int GM = 8;  // row blocks of a band (k_mx_tile)
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+// One product of fragments; J: which byte of the weights' scale word, I: of x's
 template <int XF, int J>
 WAR_DEV f32x4 mx_mfma(i32x8 w, i32x8 x, f32x4 c, uint32_t sw, uint32_t sx) {
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, c, 4, XF == kMxE4M3 ? 0 : 4, J, (int)sw, 0, (int)sx);
+}
+template <int XF, int I>
+WAR_DEV f32x16 mx_mfma32(i32x8 w, i32x8 x, f32x16 c, uint32_t sw, uint32_t sx) {
+  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w, x, c, 4, XF == kMxE4M3 ? 0 : 4, 0, (int)sw, I, (int)sx);
 }
 
 // a descriptor, or one that holds nothing (loads give zeros)
@@ -71,20 +81,49 @@ WAR_DEV void split_codes(const i32x8& x, i32x8& hi, i32x8& lo) {
   }
 }
 
-// Four results y[m][n .. n + 3], all of them in y and in one piece
+// Four results y[m][n .. n + 3], all of them in y (one store, which the hardware takes at
+// any address)
 template <bool F32>
 WAR_DEV void store_whole(const MxGemmArgs& a, int m, int n, f32x4 v) {
   const uint2 b = *reinterpret_cast<const uint2*>(a.bias + n);
   v[0] += lo_f(b.x), v[1] += hi_f(b.x), v[2] += lo_f(b.y), v[3] += hi_f(b.y);
   const int64_t at = (int64_t)m * a.y_stride + n;
-  if constexpr (F32) *reinterpret_cast<f32x4*>(static_cast<float*>(a.y) + at) = v;
-  else *reinterpret_cast<uint2*>(static_cast<bf16_t*>(a.y) + at) = make_uint2(pack2(v[0], v[1]), pack2(v[2], v[3]));
+  if constexpr (F32) *reinterpret_cast<f32x4_any*>(static_cast<float*>(a.y) + at) = v;
+  else *reinterpret_cast<u32x2_half*>(static_cast<bf16_t*>(a.y) + at) = u32x2_half{pack2(v[0], v[1]), pack2(v[2], v[3])};
 }
-// The same where some may lie outside, or rows begin anywhere
+// A 32 x 32 tile's results of a lane: row m, columns n + 8 q + 4 half + 0 .. 3.  bf16: the
+// lanes of a row swap halves of two q, so that each writes eight neighbours.
+template <bool F32>
+WAR_DEV void store_tile(const MxGemmArgs& a, int m, int n, int half, const f32x16& v) {
+  uint32_t w[4][2];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const uint2 b = *reinterpret_cast<const uint2*>(a.bias + n + 8 * q + 4 * half);
+    const f32x4 y = {v[4 * q] + lo_f(b.x), v[4 * q + 1] + hi_f(b.x), v[4 * q + 2] + lo_f(b.y), v[4 * q + 3] + hi_f(b.y)};
+    if constexpr (F32) {
+      if (m < a.M) *reinterpret_cast<f32x4_any*>(static_cast<float*>(a.y) + (int64_t)m * a.y_stride + n + 8 * q + 4 * half) = y;
+    } else {
+      w[q][0] = pack2(y[0], y[1]);
+      w[q][1] = pack2(y[2], y[3]);
+    }
+  }
+  if constexpr (!F32) {
+#pragma unroll
+    for (int q = 0; q < 4; q += 2) {
+      uint4 o;
+      const auto s0 = __builtin_amdgcn_permlane32_swap(w[q][0], w[q + 1][0], false, false);
+      const auto s1 = __builtin_amdgcn_permlane32_swap(w[q][1], w[q + 1][1], false, false);
+      o.x = s0[0], o.z = s0[1], o.y = s1[0], o.w = s1[1];
+      bf16_t* y = static_cast<bf16_t*>(a.y) + (int64_t)m * a.y_stride + n + 8 * (q + half);
+      if (m < a.M) *reinterpret_cast<u32x4_half*>(y) = u32x4_half{o.x, o.y, o.z, o.w};
+    }
+  }
+}
+// The same where some may lie outside
 template <bool F32>
 WAR_DEV void store_y(const MxGemmArgs& a, int m, int n, f32x4 v) {
   if (m >= a.M || n >= a.N) return;
-  if (a.vec && n + 4 <= a.N) return store_whole<F32>(a, m, n, v);
+  if (n + 4 <= a.N) return store_whole<F32>(a, m, n, v);
   const uint2 b = *reinterpret_cast<const uint2*>(a.bias + n);  // padded
   v[0] += lo_f(b.x), v[1] += hi_f(b.x), v[2] += lo_f(b.y), v[3] += hi_f(b.y);
   const int64_t at = (int64_t)m * a.y_stride + n;
@@ -97,17 +136,19 @@ WAR_DEV void store_y(const MxGemmArgs& a, int m, int n, f32x4 v) {
 }
 
 // Few rows: the weights' way from memory bounds it.  A workgroup takes 16 NT columns by
-// 16 MT rows; its waves share the groups of 512 k between them, every fragment straight
-// from memory to registers, and their sums meet in LDS in the waves' order.
-template <int MT, int NT, int WAVES, int XF, bool F32>
-__global__ void __launch_bounds__(WAVES * 64) k_mx_skinny(MxGemmArgs a) {
-  constexpr bool EXACT = XF == kMxE4M3 && F32;
-  constexpr int XB = XF == kMxE4M3 ? 128 : 64;  // bytes of a row's k-step
+// 16 MT rows; its waves share the runs of 256 k between them, every fragment straight from
+// memory to registers, RING - 1 runs ahead of the products, and their sums meet in LDS in
+// the waves' order.
+template <int MT, int NT, int WAVES, int RING, int XF, bool F32>
+__global__ void __launch_bounds__(WAVES * 64) __attribute__((amdgpu_waves_per_eu(WAVES / 4, WAVES / 4 > 2 ? 4 : 2)))
+k_mx_skinny(MxGemmArgs a) {
+  constexpr bool E8 = XF == kMxE4M3, EXACT = E8 && F32;
+  constexpr int XB = E8 ? 128 : 64;             // bytes of a row's 128 columns
   __shared__ f32x4 s_sum[WAVES][MT * NT][64];
   const int lane = threadIdx.x & 63, ln = lane & 15, lg = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int nt0 = blockIdx.x * NT, m0 = blockIdx.y * 16 * MT;
-  const int groups = (a.K + 511) / 512;
+  const int groups = (a.K + 511) / 512, runs = (a.K + 255) / 256;
   f32x4 acc[MT][NT];
 #pragma unroll
   for (int m = 0; m < MT; ++m)
@@ -117,79 +158,128 @@ __global__ void __launch_bounds__(WAVES * 64) k_mx_skinny(MxGemmArgs a) {
 #pragma unroll
   for (int m = 0; m < MT; ++m) {  // rows past the last read the last one, and are not written
     const int64_t r = min(m0 + m * 16 + ln, a.M - 1);
-    xc[m] = a.x.codes + r * a.x.code_stride;
+    xc[m] = a.x.codes + r * a.x.code_stride + lg * 16;
     xs[m] = a.x.scales + r * a.x.scale_stride;
   }
-  for (int g = wave; g < groups; g += WAVES) {
-    const int k0 = g * 512;
-    const bool whole = k0 + 512 <= a.K;
-    uint32_t sw[NT];
-    uint4 w[4][NT];
+  const uint8_t* wc[NT];
+  const uint32_t* wsp[NT];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {  // half of a tile's rows, of two of its fragments each
+    const int64_t t = (int64_t)((nt0 + n) >> 1) * groups;
+    const int li = ((nt0 + n) & 1) * 16 + ln + (lg & 1) * 32;
+    wc[n] = a.w + (t * 8 + (lg >> 1)) * 1024 + li * 16;
+    wsp[n] = a.ws + t * 128 + li;
+  }
+  uint4 x[RING][2][MT][E8 ? 2 : 1], w[RING][2][NT];
+  uint32_t sx[RING][2][MT], sw[RING][NT];
+  // the fragments of run r into slot q
+  auto load = [&](auto tag, int r) __attribute__((always_inline)) {
+    constexpr int Q = decltype(tag)::value;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      const int64_t f = (int64_t)(nt0 + n) * groups + g;
-      sw[n] = a.ws[f * 64 + lane];
+      sw[Q][n] = wsp[n][r * 64];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) w[j][n] = *reinterpret_cast<const uint4*>(a.w + (f * 4 + j) * 1024 + lane * 16);
+      for (int j = 0; j < 2; ++j) w[Q][j][n] = *reinterpret_cast<const uint4*>(wc[n] + (int64_t)(r * 2 + j) * 2048);
     }
-    uint32_t sx[MT][4];
-    uint4 x[4][MT][XF == kMxE4M3 ? 2 : 1];
-    if (whole) {
+    const int k0 = r * 256;
+    if (k0 + 256 <= a.K) {
 #pragma unroll
       for (int m = 0; m < MT; ++m) {
-        const u32x4_any s = *reinterpret_cast<const u32x4_any*>(xs[m] + g * 16);
+        const u32x2_any s = *reinterpret_cast<const u32x2_any*>(xs[m] + r * 8);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          sx[m][j] = s[j];
-          const uint8_t* p = xc[m] + (int64_t)(g * 4 + j) * XB + lg * 16;
-          x[j][m][0] = *reinterpret_cast<const uint4*>(p);
-          if constexpr (XF == kMxE4M3) x[j][m][1] = *reinterpret_cast<const uint4*>(p + 64);
+        for (int j = 0; j < 2; ++j) {
+          sx[Q][j][m] = s[j];
+          const uint8_t* p = xc[m] + (int64_t)(r * 2 + j) * XB;
+          x[Q][j][m][0] = *reinterpret_cast<const uint4*>(p);
+          if constexpr (E8) x[Q][j][m][1] = *reinterpret_cast<const uint4*>(p + 64);
         }
       }
     } else {
-      // 16-byte pieces hold numbers of one block: zero codes where it lies past K
+      // 16-byte pieces hold numbers of one block: zero codes (and any scale but NaN's)
+      // where it lies past K
+      const uint4 zero = make_uint4(0, 0, 0, 0);
 #pragma unroll
       for (int m = 0; m < MT; ++m)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < 2; ++j) {
           const int kj = k0 + j * 128;
-          sx[m][j] = kj < a.K ? *reinterpret_cast<const uint32_t*>(xs[m] + kj / 32) : 0x7f7f7f7fu;
-          if (kj + lg * 32 >= a.K) sx[m][j] = 0x7f7f7f7fu;
-          const uint4 zero = make_uint4(0, 0, 0, 0);
-          const uint8_t* p = xc[m] + (int64_t)(g * 4 + j) * XB + lg * 16;
-          x[j][m][0] = kj + (XF == kMxE4M3 ? lg * 16 : lg * 32) < a.K ? *reinterpret_cast<const uint4*>(p) : zero;
-          if constexpr (XF == kMxE4M3) x[j][m][1] = kj + 64 + lg * 16 < a.K ? *reinterpret_cast<const uint4*>(p + 64) : zero;
+          sx[Q][j][m] = kj + lg * 32 < a.K ? *reinterpret_cast<const uint32_t*>(xs[m] + kj / 32) : 0x7f7f7f7fu;
+          const uint8_t* p = xc[m] + (int64_t)(r * 2 + j) * XB;
+          x[Q][j][m][0] = kj + (E8 ? lg * 16 : lg * 32) < a.K ? *reinterpret_cast<const uint4*>(p) : zero;
+          if constexpr (E8) x[Q][j][m][1] = kj + 64 + lg * 16 < a.K ? *reinterpret_cast<const uint4*>(p + 64) : zero;
         }
     }
-    auto step = [&](auto tag) __attribute__((always_inline)) {
-      constexpr int J = decltype(tag)::value;
+  };
+  auto products = [&](auto tag) __attribute__((always_inline)) {
+    constexpr int Q = decltype(tag)::value;
+    auto step = [&](auto tj) __attribute__((always_inline)) {
+      constexpr int J = decltype(tj)::value;
 #pragma unroll
       for (int m = 0; m < MT; ++m) {
-        const uint4 lo = x[J][m][0];
-        i32x8 xv = {(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, 0, 0, 0, 0};
-        if constexpr (XF == kMxE4M3) {
-          const uint4 hi = x[J][m][1];
+        const uint4 lo = x[Q][J][m][0];
+        i32x8 xv = {(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, 0, 0, 0, 0}, xl = xv;
+        if constexpr (E8) {
+          const uint4 hi = x[Q][J][m][1];
           xv[4] = (int)hi.x, xv[5] = (int)hi.y, xv[6] = (int)hi.z, xv[7] = (int)hi.w;
+          if constexpr (EXACT) {
+            const i32x8 all = xv;
+            split_codes(all, xv, xl);
+          }
         }
-        i32x8 xl = xv;
-        if constexpr (EXACT) {
-          const i32x8 whole = xv;
-          split_codes(whole, xv, xl);
-        }
-        const uint32_t s = sx[m][J] >> (8 * lg);
+        const uint32_t s = sx[Q][J][m] >> (8 * lg);
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-          const uint4 c = w[J][n];
+          const uint4 c = w[Q][J][n];
           const i32x8 wv = {(int)c.x, (int)c.y, (int)c.z, (int)c.w, 0, 0, 0, 0};
-          acc[m][n] = mx_mfma<XF, J>(wv, xv, acc[m][n], sw[n], s);
-          if constexpr (EXACT) acc[m][n] = mx_mfma<XF, J>(wv, xl, acc[m][n], sw[n], s);
+          const uint32_t t = sw[Q][n] >> (8 * (lg >> 1));
+          acc[m][n] = mx_mfma<XF, 2 * J>(wv, xv, acc[m][n], t, s);
+          if constexpr (EXACT) acc[m][n] = mx_mfma<XF, 2 * J>(wv, xl, acc[m][n], t, s);
         }
       }
     };
     step(std::integral_constant<int, 0>{});
     step(std::integral_constant<int, 1>{});
-    step(std::integral_constant<int, 2>{});
-    step(std::integral_constant<int, 3>{});
+  };
+  using std::integral_constant;
+  // (every load of the loop is unconditional, so that what may stay in flight behind a
+  // wait is known)
+  int r = wave;
+  if (r < runs) {
+    load(integral_constant<int, 0>{}, r);
+    if constexpr (RING == 2) {
+      for (;;) {
+        if (r + WAVES >= runs) {
+          products(integral_constant<int, 0>{});
+          break;
+        }
+        load(integral_constant<int, 1>{}, r += WAVES);
+        products(integral_constant<int, 0>{});
+        if (r + WAVES >= runs) {
+          products(integral_constant<int, 1>{});
+          break;
+        }
+        load(integral_constant<int, 0>{}, r += WAVES);
+        products(integral_constant<int, 1>{});
+      }
+    } else if (r + WAVES >= runs) {
+      products(integral_constant<int, 0>{});
+    } else {
+      load(integral_constant<int, 1>{}, r += WAVES);
+      auto turn = [&](auto t0, auto t1, auto t2) __attribute__((always_inline)) {
+        if (r + WAVES >= runs) {
+          products(t0);
+          products(t1);
+          return false;
+        }
+        load(t2, r += WAVES);
+        products(t0);
+        return true;
+      };
+      while (turn(integral_constant<int, 0>{}, integral_constant<int, 1>{}, integral_constant<int, 2>{}) &&
+             turn(integral_constant<int, 1>{}, integral_constant<int, 2>{}, integral_constant<int, 0>{}) &&
+             turn(integral_constant<int, 2>{}, integral_constant<int, 0>{}, integral_constant<int, 1>{})) {
+      }
+    }
   }
 #pragma unroll
   for (int m = 0; m < MT; ++m)
@@ -198,98 +288,98 @@ __global__ void __launch_bounds__(WAVES * 64) k_mx_skinny(MxGemmArgs a) {
   __syncthreads();
   for (int t = wave; t < MT * NT; t += WAVES) {
     f32x4 v = s_sum[0][t][lane];
-    for (int w = 1; w < WAVES; ++w) v += s_sum[w][t][lane];
+#pragma unroll
+    for (int q = 1; q < WAVES; ++q) v += s_sum[q][t][lane];
     store_y<F32>(a, m0 + (t / NT) * 16 + ln, (nt0 + t % NT) * 16 + lg * 4, v);
   }
 }
 
-// Many rows: the matrix cores bound it.  A workgroup computes a BM x BN tile from LDS; 8
-// waves as WM x WN.  A step is 128 bytes of each of x's rows: KF fragments of 128 columns
-// (e4m3: one, e2m1: two).  Every operand byte comes straight from memory to LDS, ST
-// stages of one step each: x's rows with their eight 16-byte chunks permuted so that
-// fragment reads fall on different banks, the weights' fragments as they are stored, a
-// word of scale bytes for each row and fragment; the weights' scale words come for four
-// fragments at once, into one of two buffers of their own.
-template <int BM, int BN, int WM, int WN, int ST, int XF, bool F32>
-__global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) k_mx_tile(MxGemmArgs a) {
-  static_assert(WM * WN == 8 && BM % 64 == 0 && BN % 128 == 0 && BM + BN <= 512, "8 waves, whole loads");
+// Many rows: the matrix cores bound it.  A workgroup computes a BM x BN tile from LDS, its
+// waves as WM x WN.  A step is 128 columns, two fragments' width.  Every operand byte
+// comes straight from memory to LDS, ST stages of one step each: x's rows with their
+// 16-byte chunks permuted so that fragment reads fall on different banks, the weights'
+// fragments as they are stored, a word of scale bytes for each row; the weights' scale
+// words come for two steps at once, into WSR buffers of their own.
+template <int BM, int BN, int WM, int WN, int WPE, int ST, int XF, bool F32>
+__global__ void __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(WPE, WPE))) k_mx_tile(MxGemmArgs a) {
   constexpr bool E8 = XF == kMxE4M3, EXACT = E8 && F32;
-  constexpr int KF = E8 ? 1 : 2, KS = 128 * KF;
-  constexpr int MT = BM / WM / 16, NT = BN / WN / 16;
-  constexpr int A_INS = BM / 64, W_INS = BN * KF / 128, INS = A_INS + W_INS + KF;  // loads of a wave and step
-  constexpr int A_B = BM * 128, W_B = BN * 64 * KF, XS_B = 2048 * KF, STAGE = A_B + W_B + XS_B, WS_B = BN * 16;
-  constexpr int GS = 4 / KF;                            // steps that a word of the weights' scales serves
-  __shared__ __attribute__((aligned(1024))) unsigned char smem[ST * STAGE + 2 * WS_B];
-  const int tid = threadIdx.x, lane = tid & 63, ln = lane & 15, lg = lane >> 4;
+  constexpr int NW = WM * WN, MT = BM / WM / 32, NT = BN / WN / 32;
+  static_assert(BM % (WM * 32) == 0 && BN % (WN * 32) == 0 && BN % (16 * NW) == 0 && BM <= NW * 64 && BN <= NW * 128 && ST <= 4,
+                "whole fragments and loads");
+  constexpr int RB = E8 ? 128 : 64, RPL = 1024 / RB;    // bytes of a row's step, rows of a 1 KB load
+  constexpr int A_INS = (BM / RPL + NW - 1) / NW, W_INS = BN / 16 / NW, INS = 1 + A_INS + W_INS;  // loads of a wave and step
+  constexpr int A_B = A_INS * NW * 1024, W_B = BN * 64, XS_B = NW * 256, STAGE = A_B + W_B + XS_B, WS_B = BN * 8;
+  // requested 2 LEAD steps ahead: with ST stages up to (ST - 2) INS loads may stay in flight behind them
+  constexpr int LEAD = ST > 3 ? 2 : 1, WSR = 2 * LEAD;
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[ST * STAGE + WSR * WS_B];
+  const int tid = threadIdx.x, lane = tid & 63, ln = lane & 31, lg = lane >> 5;
   const int wi = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wi % WM, wn = wi / WM;
   const int mblocks = (a.M + BM - 1) / BM, NB = (a.N + BN - 1) / BN;
-  // Workgroups are dealt to the 8 XCDs round-robin by linear id: the m-blocks of one
-  // weight block get ids 8 apart, so all but the first find W in that XCD's L2; a ragged
-  // tail of fewer than 8 n-blocks falls back to consecutive ids.
-  const int full = (NB / 8) * 8 * mblocks;
-  int nb, mb;
-  if ((int)blockIdx.x < full) {
-    const int r = blockIdx.x % (8 * mblocks);
-    nb = (blockIdx.x / (8 * mblocks)) * 8 + (r & 7);
-    mb = r >> 3;
-  } else {
-    const int r = blockIdx.x - full;
-    nb = (NB / 8) * 8 + r / mblocks;
-    mb = r % mblocks;
-  }
+  // Workgroups are dealt to the 8 XCDs round-robin by linear id: each XCD takes an eighth of
+  // the tiles, in bands of GM row blocks with the rows running fastest, so that its 32 CUs
+  // work on about GM by 32 / GM blocks at a time and its L2 serves both operands.
+  const int T = mblocks * NB, xcd = blockIdx.x & 7;
+  const int t = xcd * (T >> 3) + min(xcd, T & 7) + (int)(blockIdx.x >> 3);
+  const int band = t / (GM * NB), bm = min(mblocks - band * GM, GM), tr = t - band * GM * NB;
+  const int mb = band * GM + tr % bm, nb = tr / bm;
   const int m0 = mb * BM, rows = min(BM, a.M - m0);
-  const int groups = (a.K + 511) / 512, nsteps = (a.K + KS - 1) / KS;
-  const int kbytes = E8 ? a.K : a.K / 2, tile_b = groups * 4096;
+  const int groups = (a.K + 511) / 512, nsteps = (a.K + 127) / 128;
+  const int kbytes = E8 ? a.K : a.K / 2, tile_b = groups * 8192;
   const i32x4 xres = make_rsrc(a.x.codes + (int64_t)m0 * a.x.code_stride, (int64_t)(rows - 1) * a.x.code_stride + kbytes);
   const i32x4 sres = make_rsrc(a.x.scales + (int64_t)m0 * a.x.scale_stride,
                                (int64_t)(rows - 1) * a.x.scale_stride + ((a.K / 32 + 3) & ~3));
-  const i32x4 wres = make_rsrc(a.w + (int64_t)nb * (BN / 16) * tile_b, (int64_t)(BN / 16) * tile_b);
-  const i32x4 wsres = make_rsrc(a.ws + (int64_t)nb * (BN / 16) * groups * 64, (int64_t)(BN / 16) * groups * 256);
+  const i32x4 wres = make_rsrc(a.w + (int64_t)nb * (BN / 32) * tile_b, (int64_t)(BN / 32) * tile_b);
+  const i32x4 wsres = make_rsrc(a.ws + (int64_t)nb * (BN / 32) * groups * 128, (int64_t)(BN / 32) * groups * 512);
   const int xstride = (int)a.x.code_stride, sstride = (int)a.x.scale_stride;
 
-  // x: load i of wave wi brings rows (i * 8 + wi) * 8 .. + 7, lane l the 16-byte slot
-  // l % 8 of row l / 8.  Slot c of row r holds chunk c ^ ((r / 2) % 8).  Rows past the
-  // last and chunks past K are past the descriptor: zero codes.
-  const int ar = wi * 8 + (lane >> 3), ac = ((lane & 7) ^ ((ar >> 1) & 7)) * 16;
+  // x: load i of wave wi brings rows (i * NW + wi) * RPL .., a lane one 16-byte slot; slot
+  // c of row r holds chunk c ^ swap(r).  Rows past the last and chunks past K are past the
+  // descriptor: zero codes.
   constexpr int PAST = 0x7fff0000;                      // past every descriptor
+  auto swap = [](int r) { return E8 ? (r >> 1) & 7 : (r >> 2) & 3; };
+  const int ar = wi * RPL + lane / (RB / 16), ac = ((lane % (RB / 16)) ^ swap(ar)) * 16;
   const int xv = ar * xstride + ac;
-  const int wv = (wi / KF) * tile_b + (wi % KF) * 1024 + lane * 16;  // load i: 8 / KF tiles further
+  // weights: load i brings fragment (i * NW + wi) % 2 of tile (i * NW + wi) / 2
+  const int wv = (wi / 2) * tile_b + (wi % 2) * 1024 + lane * 16;
   const int sv = wi * 64 + lane < BM ? (wi * 64 + lane) * sstride : PAST;  // a row's scales (the other waves': zeros)
-  // load i of k-step s into stage q; steps past the last bring zeros, so that every wave
+  // load i of step s into stage q; steps past the last bring zeros, so that every wave
   // has the same loads in flight in every step
   auto load1 = [&](int q, int s, int i) __attribute__((always_inline)) {
     const uint32_t to = lds_addr(smem) + q * STAGE;
     const bool on = s < nsteps;
-    if (i < KF) {
-      const int f = s * KF + i;
-      load_lds4(to + A_B + W_B + i * 2048 + wi * 256, sv + f * 4, sized(sres, f * 128 < a.K));
-    } else if (i < KF + A_INS) {
-      const int o = s * 128 + ac < kbytes ? xv + s * 128 + (i - KF) * 64 * xstride : PAST;
-      load_lds16<false>(to + (i - KF) * 8192 + wi * 1024, o, sized(xres, on));
+    if (i == 0) {
+      load_lds4(to + A_B + W_B + wi * 256, sv + s * 4, sized(sres, on));
+    } else if (i <= A_INS) {
+      const int o = s * RB + ac < kbytes ? xv + s * RB + (i - 1) * NW * RPL * xstride : PAST;
+      load_lds16<false>(to + ((i - 1) * NW + wi) * 1024, o, sized(xres, on));
     } else {
-      const int j = i - KF - A_INS;
-      load_lds16<false>(to + A_B + j * 8192 + wi * 1024, wv + j * (8 / KF) * tile_b + s * KF * 1024, sized(wres, on));
+      const int j = i - 1 - A_INS;
+      load_lds16<false>(to + A_B + (j * NW + wi) * 1024, wv + j * (NW / 2) * tile_b + s * 2048, sized(wres, on));
     }
   };
-  // the weights' scale words of group g: the last waves bring four tiles each
-  auto load_ws = [&](int g) __attribute__((always_inline)) {
-    const int i = wi - (8 - BN / 64);
-    if (i >= 0 && g < groups)
-      load_lds16<false>(lds_addr(smem) + ST * STAGE + (g & 1) * WS_B + i * 1024, ((i * 4 + (lane >> 4)) * groups + g) * 256 + (lane & 15) * 16, wsres);
+  // the weights' scale words of steps 2 q and 2 q + 1: the last waves bring four tiles each
+  auto load_ws = [&](int q) __attribute__((always_inline)) {
+    const int i = wi - (NW - BN / 128);
+    if (i >= 0 && q < groups * 2)
+      load_lds16<false>(lds_addr(smem) + ST * STAGE + q % WSR * WS_B + i * 1024,
+                        ((i * 4 + (lane >> 4)) * groups * 2 + q) * 256 + (lane & 15) * 16, wsres);
   };
 
-  const int woff = wn * NT * KF * 1024 + lane * 16;
-  const int r0 = wm * (BM / WM) + ln;                   // (r0 + 16 mt) / 2 % 8 is the same for every mt
-  int aoff[2];
+  const int woff = A_B + wn * NT * 2048 + lane * 16;
+  const int r0 = wm * (BM / WM) + ln;                   // swap(r0 + 32 mt) is the same for every mt
+  // chunks of fragment u: e2m1 2 u + lg; e4m3 4 u + lg and 4 u + 2 + lg
+  int aoff[E8 ? 4 : 2];
 #pragma unroll
-  for (int j = 0; j < 2; ++j) aoff[j] = r0 * 128 + (((j * 4 + lg) ^ ((r0 >> 1) & 7)) * 16);
+  for (int c = 0; c < (E8 ? 4 : 2); ++c) aoff[c] = r0 * RB + (((2 * c + lg) ^ swap(r0)) * 16);
 
-  f32x4 acc[MT][NT];
+  f32x16 acc[MT][NT];
 #pragma unroll
   for (int m = 0; m < MT; ++m)
 #pragma unroll
-    for (int n = 0; n < NT; ++n) acc[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[m][n][e] = 0.f;
   // own loads of the next stage arrived (`left` later ones may be in flight) and own LDS
   // reads done, then everyone's
   auto sync = [&](auto left) __attribute__((always_inline)) {
@@ -297,59 +387,57 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(decltype(left)::value) : "memory");
     __builtin_amdgcn_sched_barrier(0);
   };
-  // A step is KF MT slots, one x fragment (and NT products) each, read LOOK slots ahead.
-  // Before the last LOOK slots the next stage must be complete (sync); every read of this
-  // stage is then done, and step s + ST is requested into it, a few loads a slot, on into
-  // the next step's first slots.
-  constexpr int SLOTS = KF * MT, RING = SLOTS % 4 == 0 ? 4 : SLOTS % 3 == 0 ? 3 : 2, LOOK = SLOTS == 4 ? 2 : RING - 1;
+  // A step is 2 MT slots, one x fragment (and NT products) each, read LOOK slots ahead; the
+  // weights of its second half are read in the first, the next step's in the last LOOK
+  // slots.  Before these the next stage must be complete (sync); every read of this stage
+  // is then done, and step s + ST is requested into it, a few loads a slot, on into the
+  // next step's first slots.
+  constexpr int SLOTS = 2 * MT, RING = SLOTS % 4 == 0 ? 4 : SLOTS % 3 == 0 ? 3 : 2, LOOK = SLOTS == 4 ? 2 : RING - 1;
   constexpr int LPS = (INS + SLOTS - 1) / SLOTS;
-  static_assert(SLOTS % RING == 0 && RING > LOOK && SLOTS > LOOK, "a ring of fragments");
+  static_assert(SLOTS % RING == 0 && RING > LOOK && LOOK <= MT, "a ring of fragments");
   constexpr int HEAD = LPS * LOOK < INS ? LPS * LOOK : INS;
   uint4 ra[RING][E8 ? 2 : 1], rb[2][NT];
-  uint32_t rs[RING], wsc[2][NT];                        // scale bytes
+  uint32_t rs[MT], wsc[2][NT];                          // scales: a row's word, a fragment's byte
   auto read_x = [&](const unsigned char* st, int i) __attribute__((always_inline)) {
-    const int m = i % MT, h = i / MT;
-    const unsigned char* p = st + m * 2048;
-    ra[i % RING][0] = *reinterpret_cast<const uint4*>(p + aoff[E8 ? 0 : h]);
-    if constexpr (E8) ra[i % RING][1] = *reinterpret_cast<const uint4*>(p + aoff[1]);
-    rs[i % RING] = st[A_B + W_B + (h * 512 + r0 + m * 16) * 4 + lg];
+    const int m = i % MT, u = i / MT;
+    ra[i % RING][0] = *reinterpret_cast<const uint4*>(st + m * 32 * RB + aoff[E8 ? 2 * u : u]);
+    if constexpr (E8) ra[i % RING][1] = *reinterpret_cast<const uint4*>(st + m * 32 * RB + aoff[2 * u + 1]);
+    if (u == 0) rs[m] = *reinterpret_cast<const uint32_t*>(st + A_B + W_B + (r0 + m * 32) * 4) >> (8 * lg);
   };
-  auto read_w = [&](const unsigned char* st, int to, int h, int f, int n) __attribute__((always_inline)) {  // f = s KF + h
-    rb[to][n] = *reinterpret_cast<const uint4*>(st + A_B + woff + (n * KF + h) * 1024);
-    wsc[to][n] = smem[ST * STAGE + f / 4 % 2 * WS_B + (wn * NT + n) * 256 + lane * 4 + f % 4];
+  auto read_w = [&](const unsigned char* st, int s, int u, int n) __attribute__((always_inline)) {
+    rb[u][n] = *reinterpret_cast<const uint4*>(st + woff + (2 * n + u) * 1024);
+    wsc[u][n] = smem[ST * STAGE + s / 2 % WSR * WS_B + (wn * NT + n) * 256 + lane * 4 + s % 2 * 2 + u];
   };
-  // U: which of the unrolled steps (its stage, its fragments' buffer)
+  // C: the step's stage
   auto step = [&](int s, auto tag) __attribute__((always_inline)) {
-    constexpr int U = decltype(tag)::value, C = U % ST, N = (U + 1) % ST, Pv = (U + ST - 1) % ST;
+    constexpr int C = decltype(tag)::value, N = (C + 1) % ST, Pv = (C + ST - 1) % ST;
     const unsigned char *SC = smem + C * STAGE, *SN = smem + N * STAGE;
-    if (s % GS == 0) load_ws(s / GS + 1);
+    if (s % 2 == 0) load_ws(s / 2 + LEAD);
 #pragma unroll
     for (int i = 0; i < SLOTS; ++i) {
-      if (i == SLOTS - LOOK) {
-        // stages s + 2 .. s + ST - 1 may still be in flight
-        sync(std::integral_constant<int, (ST - 2) * INS>{});
-      }
+      // where the block of this lane's scale lies past K: zero codes, and any byte but NaN's
+      const uint32_t sx = s * 128 + i / MT * 64 + lg * 32 < a.K ? rs[i % MT] : 0x7f7f7f7fu;
+      // stages s + 2 .. s + ST - 1 may still be in flight
+      if (i == SLOTS - LOOK) sync(std::integral_constant<int, (ST - 2) * INS>{});
       if (i < SLOTS - LOOK) read_x(SC, i + LOOK);
       else read_x(SN, i + LOOK - SLOTS);
-      if (KF == 2 && i < MT) {
+      if (i < MT) {
 #pragma unroll
         for (int n = 0; n < NT; ++n)
-          if (n * MT / NT == i) read_w(SC, 1, 1, s * 2 + 1, n);
+          if (n * MT / NT == i) read_w(SC, s, 1, n);
       }
       if (i >= SLOTS - LOOK) {
 #pragma unroll
         for (int n = 0; n < NT; ++n)
-          if (n * LOOK / NT == i - (SLOTS - LOOK)) read_w(SN, KF == 2 ? 0 : (U + 1) % 2, 0, (s + 1) * KF, n);
+          if (n * LOOK / NT == i - (SLOTS - LOOK)) read_w(SN, s + 1, 0, n);
 #pragma unroll
         for (int q = 0; q < LPS; ++q)
           if ((i - (SLOTS - LOOK)) * LPS + q < INS) load1(C, s + ST, (i - (SLOTS - LOOK)) * LPS + q);
-      } else if (HEAD + i * LPS < INS) {
+      } else {
 #pragma unroll
         for (int q = 0; q < LPS; ++q)
           if (HEAD + i * LPS + q < INS) load1(Pv, s + ST - 1, HEAD + i * LPS + q);
       }
-      // the block of this lane's scale lies past K: zero codes, and any byte but NaN's
-      const uint32_t sx = (s * KF + i / MT) * 128 + lg * 32 < a.K ? rs[i % RING] : 127u;
       const uint4 x0 = ra[i % RING][0];
       i32x8 xf = {(int)x0.x, (int)x0.y, (int)x0.z, (int)x0.w, 0, 0, 0, 0}, xl = xf;
       if constexpr (E8) {
@@ -361,24 +449,21 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))
         }
       }
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        const uint4 w0 = rb[KF == 2 ? i / MT : U % 2][n];
-        const i32x8 wf = {(int)w0.x, (int)w0.y, (int)w0.z, (int)w0.w, 0, 0, 0, 0};
-        acc[i % MT][n] = mx_mfma<XF, 0>(wf, xf, acc[i % MT][n], wsc[KF == 2 ? i / MT : U % 2][n], sx);
-      }
-      if constexpr (EXACT) {
+      for (int e = 0; e < (EXACT ? 2 : 1); ++e)
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-          const uint4 w0 = rb[U % 2][n];
+          const uint4 w0 = rb[i / MT][n];
           const i32x8 wf = {(int)w0.x, (int)w0.y, (int)w0.z, (int)w0.w, 0, 0, 0, 0};
-          acc[i % MT][n] = mx_mfma<XF, 0>(wf, xl, acc[i % MT][n], wsc[U % 2][n], sx);
+          f32x16& c = acc[i % MT][n];
+          if (i < MT) c = mx_mfma32<XF, 0>(wf, e ? xl : xf, c, wsc[0][n], sx);
+          else c = mx_mfma32<XF, 2>(wf, e ? xl : xf, c, wsc[1][n], sx);
         }
-      }
       __builtin_amdgcn_sched_barrier(0);
     }
   };
 
-  load_ws(0);
+#pragma unroll
+  for (int q = 0; q < LEAD; ++q) load_ws(q);
 #pragma unroll
   for (int q = 0; q < ST; ++q) {
     // (of the last stage only what a step leaves to the one before it: step 0 brings the rest)
@@ -387,7 +472,7 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))
   }
   sync(std::integral_constant<int, (ST - 2) * INS + HEAD>{});
 #pragma unroll
-  for (int n = 0; n < NT; ++n) read_w(smem, 0, 0, 0, n);
+  for (int n = 0; n < NT; ++n) read_w(smem, 0, 0, n);
 #pragma unroll
   for (int i = 0; i < LOOK; ++i) read_x(smem, i);
   __builtin_amdgcn_sched_barrier(0);
@@ -395,60 +480,61 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))
   for (int s = 0; s < nsteps;) {
     step(s++, std::integral_constant<int, 0>{});
     if (s < nsteps) step(s++, std::integral_constant<int, 1>{});
-    if constexpr (ST == 3) {
+    if constexpr (ST > 2)
       if (s < nsteps) step(s++, std::integral_constant<int, 2>{});
-      if constexpr (KF == 1) {
-        if (s < nsteps) step(s++, std::integral_constant<int, 3>{});
-        if (s < nsteps) step(s++, std::integral_constant<int, 4>{});
-        if (s < nsteps) step(s++, std::integral_constant<int, 5>{});
-      }
-    }
+    if constexpr (ST > 3)
+      if (s < nsteps) step(s++, std::integral_constant<int, 3>{});
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // no load into LDS outlives the workgroup
-  const int n0 = nb * BN + wn * NT * 16 + lg * 4;
-  if (a.vec && n0 - lg * 4 + NT * 16 <= a.N) {
+  // a lane's sixteen results of a tile: row ln, columns 8 q + 4 lg + 0 .. 3
+  const int n0 = nb * BN + wn * NT * 32;
+  const bool whole = n0 + NT * 32 <= a.N;
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
-      if (m0 + r0 + m * 16 < a.M) {
+  for (int m = 0; m < MT; ++m) {
+    const int row = m0 + r0 + m * 32;
+    if (whole) {
 #pragma unroll
-        for (int n = 0; n < NT; ++n) store_whole<F32>(a, m0 + r0 + m * 16, n0 + n * 16, acc[m][n]);
-      }
-  } else {
+      for (int n = 0; n < NT; ++n) store_tile<F32>(a, row, n0 + n * 32, lg, acc[m][n]);
+    } else {
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
+      for (int n = 0; n < NT; ++n)
 #pragma unroll
-      for (int n = 0; n < NT; ++n) store_y<F32>(a, m0 + r0 + m * 16, n0 + n * 16, acc[m][n]);
+        for (int q = 0; q < 4; ++q)
+          store_y<F32>(a, row, n0 + n * 32 + q * 8 + lg * 4,
+                       f32x4{acc[m][n][4 * q], acc[m][n][4 * q + 1], acc[m][n][4 * q + 2], acc[m][n][4 * q + 3]});
+    }
   }
 }
 
-template <int BM, int BN, int WM, int WN, int ST8, int ST4>
+template <int BM, int BN, int WM, int WN, int ST8, int ST4, int WPE = 2>
 void tile(const MxGemmArgs& a, int fmt, bool f32, hipStream_t st) {
   const int grid = cdiv_i(a.N, BN) * cdiv_i(a.M, BM);
+  constexpr int T = WM * WN * 64;
   if (fmt == kMxE4M3) {
-    if (f32) k_mx_tile<BM, BN, WM, WN, ST8, kMxE4M3, true><<<grid, 512, 0, st>>>(a);
-    else k_mx_tile<BM, BN, WM, WN, ST8, kMxE4M3, false><<<grid, 512, 0, st>>>(a);
+    if (f32) k_mx_tile<BM, BN, WM, WN, WPE, ST8, kMxE4M3, true><<<grid, T, 0, st>>>(a);
+    else k_mx_tile<BM, BN, WM, WN, WPE, ST8, kMxE4M3, false><<<grid, T, 0, st>>>(a);
   } else {
-    if (f32) k_mx_tile<BM, BN, WM, WN, ST4, kMxE2M1, true><<<grid, 512, 0, st>>>(a);
-    else k_mx_tile<BM, BN, WM, WN, ST4, kMxE2M1, false><<<grid, 512, 0, st>>>(a);
+    if (f32) k_mx_tile<BM, BN, WM, WN, WPE, ST4, kMxE2M1, true><<<grid, T, 0, st>>>(a);
+    else k_mx_tile<BM, BN, WM, WN, WPE, ST4, kMxE2M1, false><<<grid, T, 0, st>>>(a);
   }
 }
 
-template <int MT, int NT, int WAVES>
+template <int MT, int NT, int WAVES, int RING>
 void skinny(const MxGemmArgs& a, int fmt, bool f32, hipStream_t st) {
   const dim3 grid((a.N + 16 * NT - 1) / (16 * NT), (a.M + 16 * MT - 1) / (16 * MT));
   if (fmt == kMxE4M3) {
-    if (f32) k_mx_skinny<MT, NT, WAVES, kMxE4M3, true><<<grid, WAVES * 64, 0, st>>>(a);
-    else k_mx_skinny<MT, NT, WAVES, kMxE4M3, false><<<grid, WAVES * 64, 0, st>>>(a);
+    if (f32) k_mx_skinny<MT, NT, WAVES, RING, kMxE4M3, true><<<grid, WAVES * 64, 0, st>>>(a);
+    else k_mx_skinny<MT, NT, WAVES, RING, kMxE4M3, false><<<grid, WAVES * 64, 0, st>>>(a);
   } else {
-    if (f32) k_mx_skinny<MT, NT, WAVES, kMxE2M1, true><<<grid, WAVES * 64, 0, st>>>(a);
-    else k_mx_skinny<MT, NT, WAVES, kMxE2M1, false><<<grid, WAVES * 64, 0, st>>>(a);
+    if (f32) k_mx_skinny<MT, NT, WAVES, RING, kMxE2M1, true><<<grid, WAVES * 64, 0, st>>>(a);
+    else k_mx_skinny<MT, NT, WAVES, RING, kMxE2M1, false><<<grid, WAVES * 64, 0, st>>>(a);
   }
 }
 
 }  // namespace
 
 void launch_mx_pack(const MxRef& w, int N, int K, uint8_t* codes, uint32_t* scales, hipStream_t st) {
-  k_mx_pack<<<dim3(mx_tiles(N), mx_groups(K)), 256, 0, st>>>(w, N, K, mx_groups(K), codes, scales);
+  k_mx_pack<<<dim3(mx_tiles(N), mx_groups(K)), 512, 0, st>>>(w, N, K, mx_groups(K), codes, scales);
 }
 
 void launch_mx_gemm(const MxGemmArgs& a, int fmt, bool f32, hipStream_t st) {
@@ -457,37 +543,44 @@ void launch_mx_gemm(const MxGemmArgs& a, int fmt, bool f32, hipStream_t st) {
   if (v) {
     const int c = atoi(v);
     switch (c) {
-      case 1: return skinny<1, 1, 8>(a, fmt, f32, st);
-      case 2: return skinny<1, 2, 8>(a, fmt, f32, st);
-      case 3: return skinny<2, 1, 8>(a, fmt, f32, st);
-      case 4: return skinny<2, 2, 8>(a, fmt, f32, st);
-      case 5: return skinny<4, 1, 8>(a, fmt, f32, st);
-      case 6: return skinny<4, 2, 8>(a, fmt, f32, st);
-      case 7: return skinny<4, 4, 4>(a, fmt, f32, st);
-      case 8: return skinny<5, 2, 8>(a, fmt, f32, st);
-      case 9: return skinny<5, 4, 4>(a, fmt, f32, st);
-      case 10: return skinny<1, 4, 8>(a, fmt, f32, st);
-      case 11: return skinny<4, 2, 4>(a, fmt, f32, st);
-      case 12: return skinny<1, 1, 16>(a, fmt, f32, st);
-      case 13: return skinny<5, 6, 4>(a, fmt, f32, st);
-      case 20: return tile<64, 128, 1, 8, 2, 2>(a, fmt, f32, st);
-      case 21: return tile<64, 128, 2, 4, 3, 3>(a, fmt, f32, st);
-      case 22: return tile<128, 128, 2, 4, 2, 2>(a, fmt, f32, st);
-      case 23: return tile<128, 128, 2, 4, 3, 3>(a, fmt, f32, st);
-      case 24: return tile<128, 256, 2, 4, 2, 2>(a, fmt, f32, st);
-      case 25: return tile<128, 256, 2, 4, 3, 2>(a, fmt, f32, st);
-      case 26: return tile<256, 128, 4, 2, 2, 2>(a, fmt, f32, st);
-      case 27: return tile<256, 128, 4, 2, 3, 3>(a, fmt, f32, st);
+      case 1: return skinny<1, 1, 8, 3>(a, fmt, f32, st);
+      case 2: return skinny<1, 2, 8, 3>(a, fmt, f32, st);
+      case 3: return skinny<2, 1, 8, 3>(a, fmt, f32, st);
+      case 4: return skinny<2, 2, 8, 3>(a, fmt, f32, st);
+      case 5: return skinny<4, 1, 8, 2>(a, fmt, f32, st);
+      case 6: return skinny<4, 2, 8, 2>(a, fmt, f32, st);
+      case 7: return skinny<4, 4, 4, 3>(a, fmt, f32, st);
+      case 8: return skinny<1, 4, 8, 3>(a, fmt, f32, st);
+      case 9: return skinny<5, 4, 4, 3>(a, fmt, f32, st);
+      case 10: return skinny<5, 6, 4, 2>(a, fmt, f32, st);
+      case 11: return skinny<2, 4, 8, 2>(a, fmt, f32, st);
+      case 12: return skinny<1, 1, 16, 2>(a, fmt, f32, st);
+      case 13: return skinny<2, 4, 4, 3>(a, fmt, f32, st);
+      case 14: return skinny<3, 2, 8, 2>(a, fmt, f32, st);
+      case 15: return skinny<2, 2, 8, 2>(a, fmt, f32, st);
+      case 16: return skinny<4, 2, 4, 3>(a, fmt, f32, st);
+      case 17: return skinny<2, 2, 4, 3>(a, fmt, f32, st);
+      case 22: return tile<128, 128, 2, 4, 4, 4>(a, fmt, f32, st);
+      case 23: return tile<128, 128, 2, 2, 2, 3>(a, fmt, f32, st);
+      case 25: return tile<128, 256, 2, 4, 4, 4>(a, fmt, f32, st);
+      case 26: return tile<128, 256, 1, 4, 2, 3>(a, fmt, f32, st);
+      case 27: return tile<256, 128, 4, 2, 3, 4>(a, fmt, f32, st);
       case 28: return tile<256, 256, 2, 4, 2, 2>(a, fmt, f32, st);
-      case 29: return tile<256, 256, 2, 4, 3, 2>(a, fmt, f32, st);
-      case 30: return tile<192, 256, 2, 4, 2, 2>(a, fmt, f32, st);
-      case 31: return tile<192, 128, 2, 4, 2, 2>(a, fmt, f32, st);
-      case 32: return tile<256, 256, 4, 2, 2, 2>(a, fmt, f32, st);
+      case 29: return tile<256, 256, 2, 4, 3, 4>(a, fmt, f32, st);
+      case 30: return tile<192, 256, 2, 4, 3, 4>(a, fmt, f32, st);
+      case 31: return tile<192, 128, 2, 4, 4, 4>(a, fmt, f32, st);
+      case 32: return tile<256, 256, 2, 2, 3, 4, 1>(a, fmt, f32, st);
+      case 33: return tile<256, 256, 2, 4, 3, 3>(a, fmt, f32, st);
+      case 34: return tile<96, 128, 1, 4, 4, 4>(a, fmt, f32, st);
+      case 35: return tile<64, 128, 2, 4, 4, 4>(a, fmt, f32, st);
+      case 36: return tile<96, 256, 1, 8, 4, 4>(a, fmt, f32, st);
+      case 37: return tile<64, 256, 1, 8, 4, 4>(a, fmt, f32, st);
+      case 38: return tile<96, 128, 1, 4, 2, 2>(a, fmt, f32, st);
     }
   }
 #endif
-  if (a.M <= 16) skinny<1, 1, 8>(a, fmt, f32, st);
-  else if (a.M <= 64 || a.x.code_stride > 1 << 22 || a.x.scale_stride > 1 << 22) skinny<2, 2, 8>(a, fmt, f32, st);
-  else if (a.M <= 128) tile<128, 128, 2, 4, 2, 2>(a, fmt, f32, st);
-  else tile<256, 256, 2, 4, 2, 2>(a, fmt, f32, st);
+  if (a.M <= 16) skinny<1, 1, 8, 3>(a, fmt, f32, st);
+  else if (a.M <= 64 || a.x.code_stride > 1 << 22 || a.x.scale_stride > 1 << 22) skinny<2, 2, 8, 3>(a, fmt, f32, st);
+  else if (a.M <= 128) tile<128, 128, 2, 4, 4, 4>(a, fmt, f32, st);
+  else tile<256, 256, 2, 4, 3, 4>(a, fmt, f32, st);
 }
