@@ -297,7 +297,7 @@ war_status war_quantize(const war_mx* mx, const void* x, int64_t x_stride, const
 war_status war_dequantize(const war_mx* mx, void* y, int64_t y_stride, int32_t type, void* stream);
 
 /* y = x w^T + bias with w [N, K] in WAR_MX_E2M1: an object owns w laid out for its kernels
- * (in all 17 bits for 32 numbers' 4 bytes, padded to 256 rows and 512 columns).
+ * (17 bytes for 32 numbers, padded to 256 rows and 512 columns).
  *   w      HOST struct; N rows (at least 1), K cols; codes need no alignment here
  *   bias   device bf16 [N], or NULL
  * Synchronises the stream: the caller's arrays are not read afterwards. */
@@ -305,11 +305,11 @@ typedef struct war_linear war_linear;
 war_status war_linear_create(const war_mx* w, const void* bias, void* stream, war_linear** out);
 void war_linear_destroy(war_linear* l);
 /* One product.  Any number of them may run at once (no workspace); nothing is allocated.
- *   x   HOST struct, [rows][K] in either format
+ *   x   HOST struct, [rows][K] in either format; strides at most 2^22
  *   y   device [rows][N] at y_stride elements, at least N; y_type WAR_BF16 or WAR_F32
- * Products and sums are fp32 in the matrix units.  They add e4m3 activations' products in
- * groups of eight neighbours, where what lies more than 13 binary places below the
- * group's largest product is cut off; e2m1 products are exact.  A row's result does not
+ * Sums are fp32 in the matrix units, over products that are exact, but for a bf16 y of e4m3
+ * activations: these are added in groups of eight neighbours, where what lies more than 13
+ * binary places below the group's largest product is cut off.  A row's result does not
  * depend on the other rows' numbers. */
 war_status war_linear_run(const war_linear* l, const war_mx* x, void* y, int64_t y_stride, int32_t y_type, void* stream);
 

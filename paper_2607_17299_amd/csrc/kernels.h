@@ -341,6 +341,7 @@ struct MxGemmArgs {
   const bf16_t* bias;  // [N padded], zero where there is none
   void* y;
   int64_t y_stride;
+  int scale16;         // x's scale words may be read four at a time
 };
 // N in tiles of 32 rows, K in groups of 512: what a packed matrix is padded to (with
 // zero codes)

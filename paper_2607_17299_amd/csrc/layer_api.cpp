@@ -171,6 +171,7 @@ war_status war_linear_run(const war_linear* l, const war_mx* x, void* y, int64_t
   const int size = y_type == WAR_F32 ? 4 : 2;
   CHECK(y && aligned(y, size), "y is null or not aligned to its type");
   CHECK(y_stride >= l->N, "y_stride must hold a row");
+  CHECK(x->code_stride <= 1 << 22 && x->scale_stride <= 1 << 22, "strides of x beyond 2^22");  // (32-bit offsets in a tile)
   MxGemmArgs a{};
   a.M = x->rows;
   a.N = l->N;
@@ -181,6 +182,7 @@ war_status war_linear_run(const war_linear* l, const war_mx* x, void* y, int64_t
   a.bias = l->bias();
   a.y = y;
   a.y_stride = y_stride;
+  a.scale16 = x->cols % 512 == 0 && x->scale_stride % 16 == 0 && aligned(x->scales, 16);
   launch_mx_gemm(a, fmt(*x), y_type == WAR_F32, static_cast<hipStream_t>(stream));
   HIPCHK(hipGetLastError());
   return WAR_OK;

@@ -75,9 +75,10 @@ WAR_DEV i32x4 sized(i32x4 r, bool on) {
 WAR_DEV void split_codes(const i32x8& x, i32x8& hi, i32x8& lo) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const uint32_t c = (uint32_t)x[i], b = (c >> 6) & 0x01010101u, mask = (b << 8) - b;
+    // bit 6 of each byte, spread over it: v_perm's selectors 8 .. 11 are signs of halves
+    const uint32_t c = (uint32_t)x[i], mask = __builtin_amdgcn_perm(c << 1, c << 9, 0x0b090a08u);
     hi[i] = (int)(c & mask);
-    lo[i] = (int)(c & ~mask);
+    lo[i] = (int)(c ^ (c & mask));
   }
 }
 
@@ -298,20 +299,20 @@ k_mx_skinny(MxGemmArgs a) {
 // waves as WM x WN.  A step is 128 columns, two fragments' width.  Every operand byte
 // comes straight from memory to LDS, ST stages of one step each: x's rows with their
 // 16-byte chunks permuted so that fragment reads fall on different banks, the weights'
-// fragments as they are stored, a word of scale bytes for each row; the weights' scale
-// words come for two steps at once, into WSR buffers of their own.
-template <int BM, int BN, int WM, int WN, int WPE, int ST, int XF, bool F32>
-__global__ void __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(WPE, WPE))) k_mx_tile(MxGemmArgs a) {
+// fragments as they are stored.  The scale words come for several steps at once.
+template <int BM, int BN, int WM, int WN, int ST, int XF, bool F32>
+__global__ void __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) k_mx_tile(MxGemmArgs a) {
   constexpr bool E8 = XF == kMxE4M3, EXACT = E8 && F32;
   constexpr int NW = WM * WN, MT = BM / WM / 32, NT = BN / WN / 32;
   static_assert(BM % (WM * 32) == 0 && BN % (WN * 32) == 0 && BN % (16 * NW) == 0 && BM <= NW * 64 && BN <= NW * 128 && ST <= 4,
                 "whole fragments and loads");
   constexpr int RB = E8 ? 128 : 64, RPL = 1024 / RB;    // bytes of a row's step, rows of a 1 KB load
-  constexpr int A_INS = (BM / RPL + NW - 1) / NW, W_INS = BN / 16 / NW, INS = 1 + A_INS + W_INS;  // loads of a wave and step
-  constexpr int A_B = A_INS * NW * 1024, W_B = BN * 64, XS_B = NW * 256, STAGE = A_B + W_B + XS_B, WS_B = BN * 8;
-  // requested 2 LEAD steps ahead: with ST stages up to (ST - 2) INS loads may stay in flight behind them
-  constexpr int LEAD = ST > 3 ? 2 : 1, WSR = 2 * LEAD;
-  __shared__ __attribute__((aligned(1024))) unsigned char smem[ST * STAGE + WSR * WS_B];
+  constexpr int A_INS = (BM / RPL + NW - 1) / NW, W_INS = BN / 16 / NW, INS = A_INS + W_INS;  // loads of a wave and step
+  constexpr int A_B = A_INS * NW * 1024, W_B = BN * 64, STAGE = A_B + W_B;
+  // scales of four steps, requested four steps ahead, into one of two buffers: 16 bytes a
+  // row of x, and a row of a weights' tile and block
+  constexpr int XS_B = (BM + 63) / 64 * 1024, WS_B = BN * 16, XS = ST * STAGE, WS = XS + 2 * XS_B;
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[WS + 2 * WS_B];
   const int tid = threadIdx.x, lane = tid & 63, ln = lane & 31, lg = lane >> 5;
   const int wi = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wi % WM, wn = wi / WM;
@@ -324,11 +325,12 @@ __global__ void __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_
   const int band = t / (GM * NB), bm = min(mblocks - band * GM, GM), tr = t - band * GM * NB;
   const int mb = band * GM + tr % bm, nb = tr / bm;
   const int m0 = mb * BM, rows = min(BM, a.M - m0);
-  const int groups = (a.K + 511) / 512, nsteps = (a.K + 127) / 128;
-  const int kbytes = E8 ? a.K : a.K / 2, tile_b = groups * 8192;
+  const int K = a.K;
+  const unsigned nsteps = (K + 127) / 128, kbytes = E8 ? K : K / 2;
+  const int groups = (a.K + 511) / 512, tile_b = groups * 8192;
   const i32x4 xres = make_rsrc(a.x.codes + (int64_t)m0 * a.x.code_stride, (int64_t)(rows - 1) * a.x.code_stride + kbytes);
   const i32x4 sres = make_rsrc(a.x.scales + (int64_t)m0 * a.x.scale_stride,
-                               (int64_t)(rows - 1) * a.x.scale_stride + ((a.K / 32 + 3) & ~3));
+                               (int64_t)(rows - 1) * a.x.scale_stride + ((K / 32 + 3) & ~3));
   const i32x4 wres = make_rsrc(a.w + (int64_t)nb * (BN / 32) * tile_b, (int64_t)(BN / 32) * tile_b);
   const i32x4 wsres = make_rsrc(a.ws + (int64_t)nb * (BN / 32) * groups * 128, (int64_t)(BN / 32) * groups * 512);
   const int xstride = (int)a.x.code_stride, sstride = (int)a.x.scale_stride;
@@ -336,34 +338,45 @@ __global__ void __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_
   // x: load i of wave wi brings rows (i * NW + wi) * RPL .., a lane one 16-byte slot; slot
   // c of row r holds chunk c ^ swap(r).  Rows past the last and chunks past K are past the
   // descriptor: zero codes.
-  constexpr int PAST = 0x7fff0000;                      // past every descriptor
+  constexpr unsigned PAST = 0x7fff0000;                 // past every descriptor (and twice that, too)
   auto swap = [](int r) { return E8 ? (r >> 1) & 7 : (r >> 2) & 3; };
-  const int ar = wi * RPL + lane / (RB / 16), ac = ((lane % (RB / 16)) ^ swap(ar)) * 16;
-  const int xv = ar * xstride + ac;
+  const int ar = wi * RPL + lane / (RB / 16);
+  const unsigned ac = ((lane % (RB / 16)) ^ swap(ar)) * 16;
+  const unsigned xv = ar * xstride + ac;
   // weights: load i brings fragment (i * NW + wi) % 2 of tile (i * NW + wi) / 2
-  const int wv = (wi / 2) * tile_b + (wi % 2) * 1024 + lane * 16;
-  const int sv = wi * 64 + lane < BM ? (wi * 64 + lane) * sstride : PAST;  // a row's scales (the other waves': zeros)
+  const unsigned wv = (wi / 2) * tile_b + (wi % 2) * 1024 + lane * 16;
   // load i of step s into stage q; steps past the last bring zeros, so that every wave
   // has the same loads in flight in every step
-  auto load1 = [&](int q, int s, int i) __attribute__((always_inline)) {
+  auto load1 = [&](int q, unsigned s, int i) __attribute__((always_inline)) {
     const uint32_t to = lds_addr(smem) + q * STAGE;
-    const bool on = s < nsteps;
-    if (i == 0) {
-      load_lds4(to + A_B + W_B + wi * 256, sv + s * 4, sized(sres, on));
-    } else if (i <= A_INS) {
-      const int o = s * RB + ac < kbytes ? xv + s * RB + (i - 1) * NW * RPL * xstride : PAST;
-      load_lds16<false>(to + ((i - 1) * NW + wi) * 1024, o, sized(xres, on));
+    if (i < A_INS) {
+      const unsigned o = xv + i * NW * RPL * xstride + (s < nsteps ? s * RB : PAST);
+      load_lds16<false>(to + (i * NW + wi) * 1024, (int)(s * RB + ac < kbytes ? o : PAST), xres);
     } else {
-      const int j = i - 1 - A_INS;
-      load_lds16<false>(to + A_B + (j * NW + wi) * 1024, wv + j * (NW / 2) * tile_b + s * 2048, sized(wres, on));
+      const int j = i - A_INS;
+      load_lds16<false>(to + A_B + (j * NW + wi) * 1024, (int)(wv + j * (NW / 2) * tile_b + (s < nsteps ? s * 2048 : PAST)), wres);
     }
   };
-  // the weights' scale words of steps 2 q and 2 q + 1: the last waves bring four tiles each
-  auto load_ws = [&](int q) __attribute__((always_inline)) {
-    const int i = wi - (NW - BN / 128);
-    if (i >= 0 && q < groups * 2)
-      load_lds16<false>(lds_addr(smem) + ST * STAGE + q % WSR * WS_B + i * 1024,
-                        ((i * 4 + (lane >> 4)) * groups * 2 + q) * 256 + (lane & 15) * 16, wsres);
+  // the scale words of steps 4 g .. 4 g + 3: x's by the first waves, 64 rows each (of a row
+  // in one load where rows lie and end at multiples of four words), the weights' by the
+  // last, four tiles' halves each
+  const int xsi = wi * 64 + lane, wsi = wi - (NW - BN / 64);
+  auto load_scales = [&](unsigned g) __attribute__((always_inline)) {
+    if (g * 4 >= nsteps) return;
+    if (wi < XS_B / 1024) {
+      if (a.scale16) {
+        load_lds16<false>(lds_addr(smem) + XS + (g & 1) * XS_B + wi * 1024, (int)(xsi * sstride + g * 16), sres);
+      } else {
+        const uint8_t* p = a.x.scales + (int64_t)(m0 + min(xsi, rows - 1)) * a.x.scale_stride + g * 16;
+        uint32_t v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = (int)(g * 4 + e) * 128 < K ? *reinterpret_cast<const uint32_t*>(p + e * 4) : 0u;
+        *reinterpret_cast<uint4*>(smem + XS + (g & 1) * XS_B + xsi * 16) = make_uint4(v[0], v[1], v[2], v[3]);
+      }
+    }
+    if (wsi >= 0)  // (a tile's 512 bytes: 32 lanes)
+      load_lds16<false>(lds_addr(smem) + WS + (g & 1) * WS_B + wsi * 1024,
+                        (int)((wsi * 2 + (lane >> 5)) * groups * 512 + g * 512 + (lane & 31) * 16), wsres);
   };
 
   const int woff = A_B + wn * NT * 2048 + lane * 16;
@@ -393,43 +406,52 @@ __global__ void __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_
   // is then done, and step s + ST is requested into it, a few loads a slot, on into the
   // next step's first slots.
   constexpr int SLOTS = 2 * MT, RING = SLOTS % 4 == 0 ? 4 : SLOTS % 3 == 0 ? 3 : 2, LOOK = SLOTS == 4 ? 2 : RING - 1;
-  constexpr int LPS = (INS + SLOTS - 1) / SLOTS;
+  constexpr int LPS = (INS + SLOTS - 1) / SLOTS, HEAD = LPS * LOOK < INS ? LPS * LOOK : INS;
   static_assert(SLOTS % RING == 0 && RING > LOOK && LOOK <= MT, "a ring of fragments");
-  constexpr int HEAD = LPS * LOOK < INS ? LPS * LOOK : INS;
   uint4 ra[RING][E8 ? 2 : 1], rb[2][NT];
   uint32_t rs[MT], wsc[2][NT];                          // scales: a row's word, a fragment's byte
-  auto read_x = [&](const unsigned char* st, int i) __attribute__((always_inline)) {
+  // q: the step's stage, which is its place among its four steps where there are four stages
+  auto of_four = [](unsigned s, int q) { return ST == 4 ? (unsigned)q : s & 3; };
+  const int xsl = XS + r0 * 16, wsl = WS + wn * NT * 512 + lane * 4;
+  auto read_x = [&](int q, unsigned s, int i) __attribute__((always_inline)) {
+    const unsigned char* st = smem + q * STAGE;
     const int m = i % MT, u = i / MT;
     ra[i % RING][0] = *reinterpret_cast<const uint4*>(st + m * 32 * RB + aoff[E8 ? 2 * u : u]);
     if constexpr (E8) ra[i % RING][1] = *reinterpret_cast<const uint4*>(st + m * 32 * RB + aoff[2 * u + 1]);
-    if (u == 0) rs[m] = *reinterpret_cast<const uint32_t*>(st + A_B + W_B + (r0 + m * 32) * 4) >> (8 * lg);
+    if (u == 0) rs[m] = *reinterpret_cast<const uint32_t*>(smem + xsl + (s >> 2 & 1) * XS_B + of_four(s, q) * 4 + m * 512);
   };
-  auto read_w = [&](const unsigned char* st, int s, int u, int n) __attribute__((always_inline)) {
-    rb[u][n] = *reinterpret_cast<const uint4*>(st + woff + (2 * n + u) * 1024);
-    wsc[u][n] = smem[ST * STAGE + s / 2 % WSR * WS_B + (wn * NT + n) * 256 + lane * 4 + s % 2 * 2 + u];
+  auto read_w = [&](int q, unsigned s, int u, int n) __attribute__((always_inline)) {
+    const unsigned f = of_four(s, q);
+    rb[u][n] = *reinterpret_cast<const uint4*>(smem + q * STAGE + woff + (2 * n + u) * 1024);
+    wsc[u][n] = smem[wsl + (s >> 2 & 1) * WS_B + f / 2 * 256 + f % 2 * 2 + n * 512 + u];
   };
+  // The bytes of a row's word that are this lane's blocks, 0 and 2 of it behind the shift;
+  // where a block lies past K: zero codes, and any byte but NaN's.
+  uint32_t keep = 0xffffffffu, fill = 0;
   // C: the step's stage
-  auto step = [&](int s, auto tag) __attribute__((always_inline)) {
+  auto step = [&](unsigned s, auto tag) __attribute__((always_inline)) {
     constexpr int C = decltype(tag)::value, N = (C + 1) % ST, Pv = (C + ST - 1) % ST;
-    const unsigned char *SC = smem + C * STAGE, *SN = smem + N * STAGE;
-    if (s % 2 == 0) load_ws(s / 2 + LEAD);
+    if (of_four(s, C) == 0) load_scales((s >> 2) + 1);
+    if (s + 1 == nsteps) {
+      keep = ((int)(s * 128 + lg * 32) < K ? 0xffu : 0u) | ((int)(s * 128 + 64 + lg * 32) < K ? 0xff0000u : 0u);
+      fill = ~keep & 0x7f7f7f7fu;
+    }
 #pragma unroll
     for (int i = 0; i < SLOTS; ++i) {
-      // where the block of this lane's scale lies past K: zero codes, and any byte but NaN's
-      const uint32_t sx = s * 128 + i / MT * 64 + lg * 32 < a.K ? rs[i % MT] : 0x7f7f7f7fu;
+      const uint32_t sx = ((rs[i % MT] >> (8 * lg)) & keep) | fill;
       // stages s + 2 .. s + ST - 1 may still be in flight
       if (i == SLOTS - LOOK) sync(std::integral_constant<int, (ST - 2) * INS>{});
-      if (i < SLOTS - LOOK) read_x(SC, i + LOOK);
-      else read_x(SN, i + LOOK - SLOTS);
+      if (i < SLOTS - LOOK) read_x(C, s, i + LOOK);
+      else read_x(N, s + 1, i + LOOK - SLOTS);
       if (i < MT) {
 #pragma unroll
         for (int n = 0; n < NT; ++n)
-          if (n * MT / NT == i) read_w(SC, s, 1, n);
+          if (n * MT / NT == i) read_w(C, s, 1, n);
       }
       if (i >= SLOTS - LOOK) {
 #pragma unroll
         for (int n = 0; n < NT; ++n)
-          if (n * LOOK / NT == i - (SLOTS - LOOK)) read_w(SN, s + 1, 0, n);
+          if (n * LOOK / NT == i - (SLOTS - LOOK)) read_w(N, s + 1, 0, n);
 #pragma unroll
         for (int q = 0; q < LPS; ++q)
           if ((i - (SLOTS - LOOK)) * LPS + q < INS) load1(C, s + ST, (i - (SLOTS - LOOK)) * LPS + q);
@@ -462,8 +484,7 @@ __global__ void __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_
     }
   };
 
-#pragma unroll
-  for (int q = 0; q < LEAD; ++q) load_ws(q);
+  load_scales(0);
 #pragma unroll
   for (int q = 0; q < ST; ++q) {
     // (of the last stage only what a step leaves to the one before it: step 0 brings the rest)
@@ -472,12 +493,12 @@ __global__ void __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_
   }
   sync(std::integral_constant<int, (ST - 2) * INS + HEAD>{});
 #pragma unroll
-  for (int n = 0; n < NT; ++n) read_w(smem, 0, 0, n);
+  for (int n = 0; n < NT; ++n) read_w(0, 0, 0, n);
 #pragma unroll
-  for (int i = 0; i < LOOK; ++i) read_x(smem, i);
+  for (int i = 0; i < LOOK; ++i) read_x(0, 0, i);
   __builtin_amdgcn_sched_barrier(0);
   // (the reads past the last step are of no use, and in bounds)
-  for (int s = 0; s < nsteps;) {
+  for (unsigned s = 0; s < nsteps;) {
     step(s++, std::integral_constant<int, 0>{});
     if (s < nsteps) step(s++, std::integral_constant<int, 1>{});
     if constexpr (ST > 2)
@@ -506,16 +527,16 @@ __global__ void __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_
   }
 }
 
-template <int BM, int BN, int WM, int WN, int ST8, int ST4, int WPE = 2>
+template <int BM, int BN, int WM, int WN, int ST8, int ST4>
 void tile(const MxGemmArgs& a, int fmt, bool f32, hipStream_t st) {
   const int grid = cdiv_i(a.N, BN) * cdiv_i(a.M, BM);
   constexpr int T = WM * WN * 64;
   if (fmt == kMxE4M3) {
-    if (f32) k_mx_tile<BM, BN, WM, WN, WPE, ST8, kMxE4M3, true><<<grid, T, 0, st>>>(a);
-    else k_mx_tile<BM, BN, WM, WN, WPE, ST8, kMxE4M3, false><<<grid, T, 0, st>>>(a);
+    if (f32) k_mx_tile<BM, BN, WM, WN, ST8, kMxE4M3, true><<<grid, T, 0, st>>>(a);
+    else k_mx_tile<BM, BN, WM, WN, ST8, kMxE4M3, false><<<grid, T, 0, st>>>(a);
   } else {
-    if (f32) k_mx_tile<BM, BN, WM, WN, WPE, ST4, kMxE2M1, true><<<grid, T, 0, st>>>(a);
-    else k_mx_tile<BM, BN, WM, WN, WPE, ST4, kMxE2M1, false><<<grid, T, 0, st>>>(a);
+    if (f32) k_mx_tile<BM, BN, WM, WN, ST4, kMxE2M1, true><<<grid, T, 0, st>>>(a);
+    else k_mx_tile<BM, BN, WM, WN, ST4, kMxE2M1, false><<<grid, T, 0, st>>>(a);
   }
 }
 
@@ -523,12 +544,56 @@ template <int MT, int NT, int WAVES, int RING>
 void skinny(const MxGemmArgs& a, int fmt, bool f32, hipStream_t st) {
   const dim3 grid((a.N + 16 * NT - 1) / (16 * NT), (a.M + 16 * MT - 1) / (16 * MT));
   if (fmt == kMxE4M3) {
-    if (f32) k_mx_skinny<MT, NT, WAVES, RING, kMxE4M3, true><<<grid, WAVES * 64, 0, st>>>(a);
+    if (f32) k_mx_skinny<MT, NT, WAVES, NT < 4 ? RING : 2, kMxE4M3, true><<<grid, WAVES * 64, 0, st>>>(a);
     else k_mx_skinny<MT, NT, WAVES, RING, kMxE4M3, false><<<grid, WAVES * 64, 0, st>>>(a);
   } else {
     if (f32) k_mx_skinny<MT, NT, WAVES, RING, kMxE2M1, true><<<grid, WAVES * 64, 0, st>>>(a);
     else k_mx_skinny<MT, NT, WAVES, RING, kMxE2M1, false><<<grid, WAVES * 64, 0, st>>>(a);
   }
+}
+
+// What a kernel takes by estimate (us): `start`, then the rounds of its workgroups over the
+// 256 CUs, `step` for a step of one workgroup a CU (few rows: for 2048 columns), `full`
+// where the CUs hold all they can, `more` for a round behind the first; at least the
+// weights' bytes at 4.6 TB/s.
+struct Cost {
+  float start, step, full, more;
+};
+struct Shape {
+  int bm, bn, occ;  // rows and columns of a workgroup, workgroups a CU
+};
+constexpr int kShapes = 9, kSkinny = 3;
+constexpr Shape kShape[kShapes] = {{16, 16, 2}, {16, 32, 1}, {16, 64, 1}, {32, 128, 2}, {64, 128, 2}, {128, 128, 1}, {96, 256, 2},
+                                   {128, 256, 1}, {256, 256, 1}};
+// x in e4m3 for a bf16 y, for an fp32 y, in e2m1; fitted to the times of 368 sizes, 1 to
+// 4096 rows by 512 to 151936 columns by 256 to 12288 (each: weights of several products in turn).
+// The choice takes 3% more than the best of all shapes on average over them, 58% at most
+// (one row of 14336 by 7168).
+constexpr Cost kCost[3][9] = {
+    {{1.48f, 0.83f, 1.52f, 0.12f}, {2.27f, 0.41f, 1.65f, 0.18f}, {3.29f, 0.01f, 0.30f, 4.51f}, {3.06f, 0.20f, 0.17f, 0.56f}, {3.40f, 0.24f, 0.27f, 0.41f}, {3.70f, 0.32f, 0.46f, 1.63f}, {3.57f, 0.65f, 0.55f, 1.51f}, {4.64f, 0.53f, 0.72f, 3.41f}, {5.99f, 1.01f, 0.88f, 8.00f}},
+    {{3.09f, 0.21f, 0.97f, 2.33f}, {3.44f, 0.01f, 0.30f, 3.54f}, {1.02f, 3.74f, 2.99f, 6.34f}, {3.99f, 0.34f, 0.29f, 0.27f}, {4.34f, 0.52f, 0.47f, 0.59f}, {1.00f, 0.96f, 0.45f, 3.10f}, {1.00f, 1.25f, 1.02f, 1.89f}, {1.00f, 1.33f, 1.37f, 5.73f}, {1.00f, 2.39f, 1.72f, 8.00f}},
+    {{1.61f, 0.64f, 1.09f, 0.41f}, {2.34f, 0.01f, 1.29f, 0.16f}, {2.83f, 0.15f, 0.48f, 3.45f}, {3.06f, 0.18f, 0.16f, 0.59f}, {3.29f, 0.23f, 0.23f, 0.38f}, {3.63f, 0.28f, 0.38f, 1.65f}, {4.69f, 0.39f, 0.46f, 3.00f}, {4.76f, 0.39f, 0.59f, 2.09f}, {6.38f, 0.65f, 0.37f, 8.00f}}};
+
+int choose(const MxGemmArgs& a, int fmt, bool f32) {
+  const Cost* cost = kCost[fmt == kMxE2M1 ? 2 : f32 ? 1 : 0];
+  const float floor = (float)a.N * (float)a.K * (17.f / 32.f / 4.6e6f);
+  int best = kShapes - 1;
+  float least = 1e30f;
+  for (int c = a.M <= 64 ? 0 : kSkinny; c < kShapes; ++c) {
+    const Shape& s = kShape[c];
+    const int64_t wgs = (int64_t)cdiv_i(a.M, s.bm) * cdiv_i(a.N, s.bn);
+    if (wgs * 512 >= (int64_t)1 << 32) continue;  // a launch's work items
+    const int steps = c < kSkinny ? cdiv_i(a.K, 2048) : cdiv_i(a.K, 128);
+    const float rounds = (float)((wgs + 255) / 256), few = (float)((wgs + 256 * s.occ - 1) / (256 * s.occ));
+    float t = cost[c].step * steps * few;
+    if (wgs > 256) t = fmaxf(t, cost[c].full * steps * rounds);
+    t = cost[c].start + fmaxf(t, floor) + cost[c].more * (rounds - 1.f);
+    if (t < least) {
+      least = t;
+      best = c;
+    }
+  }
+  return best;
 }
 
 }  // namespace
@@ -538,49 +603,15 @@ void launch_mx_pack(const MxRef& w, int N, int K, uint8_t* codes, uint32_t* scal
 }
 
 void launch_mx_gemm(const MxGemmArgs& a, int fmt, bool f32, hipStream_t st) {
-#ifdef MX_TUNE
-  static const char* v = getenv("MXV");
-  if (v) {
-    const int c = atoi(v);
-    switch (c) {
-      case 1: return skinny<1, 1, 8, 3>(a, fmt, f32, st);
-      case 2: return skinny<1, 2, 8, 3>(a, fmt, f32, st);
-      case 3: return skinny<2, 1, 8, 3>(a, fmt, f32, st);
-      case 4: return skinny<2, 2, 8, 3>(a, fmt, f32, st);
-      case 5: return skinny<4, 1, 8, 2>(a, fmt, f32, st);
-      case 6: return skinny<4, 2, 8, 2>(a, fmt, f32, st);
-      case 7: return skinny<4, 4, 4, 3>(a, fmt, f32, st);
-      case 8: return skinny<1, 4, 8, 3>(a, fmt, f32, st);
-      case 9: return skinny<5, 4, 4, 3>(a, fmt, f32, st);
-      case 10: return skinny<5, 6, 4, 2>(a, fmt, f32, st);
-      case 11: return skinny<2, 4, 8, 2>(a, fmt, f32, st);
-      case 12: return skinny<1, 1, 16, 2>(a, fmt, f32, st);
-      case 13: return skinny<2, 4, 4, 3>(a, fmt, f32, st);
-      case 14: return skinny<3, 2, 8, 2>(a, fmt, f32, st);
-      case 15: return skinny<2, 2, 8, 2>(a, fmt, f32, st);
-      case 16: return skinny<4, 2, 4, 3>(a, fmt, f32, st);
-      case 17: return skinny<2, 2, 4, 3>(a, fmt, f32, st);
-      case 22: return tile<128, 128, 2, 4, 4, 4>(a, fmt, f32, st);
-      case 23: return tile<128, 128, 2, 2, 2, 3>(a, fmt, f32, st);
-      case 25: return tile<128, 256, 2, 4, 4, 4>(a, fmt, f32, st);
-      case 26: return tile<128, 256, 1, 4, 2, 3>(a, fmt, f32, st);
-      case 27: return tile<256, 128, 4, 2, 3, 4>(a, fmt, f32, st);
-      case 28: return tile<256, 256, 2, 4, 2, 2>(a, fmt, f32, st);
-      case 29: return tile<256, 256, 2, 4, 3, 4>(a, fmt, f32, st);
-      case 30: return tile<192, 256, 2, 4, 3, 4>(a, fmt, f32, st);
-      case 31: return tile<192, 128, 2, 4, 4, 4>(a, fmt, f32, st);
-      case 32: return tile<256, 256, 2, 2, 3, 4, 1>(a, fmt, f32, st);
-      case 33: return tile<256, 256, 2, 4, 3, 3>(a, fmt, f32, st);
-      case 34: return tile<96, 128, 1, 4, 4, 4>(a, fmt, f32, st);
-      case 35: return tile<64, 128, 2, 4, 4, 4>(a, fmt, f32, st);
-      case 36: return tile<96, 256, 1, 8, 4, 4>(a, fmt, f32, st);
-      case 37: return tile<64, 256, 1, 8, 4, 4>(a, fmt, f32, st);
-      case 38: return tile<96, 128, 1, 4, 2, 2>(a, fmt, f32, st);
-    }
+  switch (choose(a, fmt, f32)) {
+    case 0: skinny<1, 1, 8, 3>(a, fmt, f32, st); break;
+    case 1: skinny<1, 2, 8, 3>(a, fmt, f32, st); break;
+    case 2: skinny<1, 4, 8, 3>(a, fmt, f32, st); break;
+    case 3: tile<32, 128, 1, 4, 4, 4>(a, fmt, f32, st); break;
+    case 4: tile<64, 128, 1, 4, 4, 4>(a, fmt, f32, st); break;
+    case 5: tile<128, 128, 2, 4, 4, 4>(a, fmt, f32, st); break;
+    case 6: tile<96, 256, 1, 4, 2, 3>(a, fmt, f32, st); break;
+    case 7: tile<128, 256, 2, 4, 4, 4>(a, fmt, f32, st); break;
+    default: tile<256, 256, 2, 4, 3, 3>(a, fmt, f32, st); break;
   }
-#endif
-  if (a.M <= 16) skinny<1, 1, 8, 3>(a, fmt, f32, st);
-  else if (a.M <= 64 || a.x.code_stride > 1 << 22 || a.x.scale_stride > 1 << 22) skinny<2, 2, 8, 3>(a, fmt, f32, st);
-  else if (a.M <= 128) tile<128, 128, 2, 4, 4, 4>(a, fmt, f32, st);
-  else tile<256, 256, 2, 4, 3, 4>(a, fmt, f32, st);
 }
