@@ -356,7 +356,7 @@ void launch_mx_gemm(const MxGemmArgs& a, int fmt, bool f32, hipStream_t st);
 struct RopeArgs {
   PoolDev p;
   KvGeom g;
-  int layer, B, n_max, pages, n_q_heads;
+  int layer, B, n_max, pages, group;  // group: query heads of a kv-head, at most 8
   const int32_t *seq, *pos0, *n, *positions;  // n, positions nullable
   const bf16_t *q, *k, *v;
   bf16_t* qo;

@@ -224,7 +224,7 @@ war_status war_rope_write(war_kv_pool* p, int32_t layer, const war_rope* rope, i
   a.B = B;
   a.n_max = n_max;
   a.pages = (n_max + 15 + 15) / 16;
-  a.n_q_heads = pv.cfg.n_q_heads;
+  a.group = pv.cfg.n_q_heads / pv.cfg.n_kv_heads;
   a.seq = seq_ids;
   a.pos0 = pos0;
   a.n = n_lens;

@@ -35,26 +35,29 @@ WAR_DEV float quad_max(float v) {
   return fmaxf(v, __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), 0x4e, 0xf, 0xf, true)));
 }
 // Eight numbers of a block whose others are in the three neighbouring lanes (lanes
-// 4 i .. 4 i + 3): their codes to `codes`, the scale byte by the block's first lane.
-// NaNs leave fmaxf's result alone and a finite maximum never is infinite, so whether all
-// are finite is carried in the maximum: infinity where one is not.
+// 4 i .. 4 i + 3): their codes to `codes`, the scale byte by the block's first lane.  A
+// number that is not finite makes x * 0 NaN, which carries it into the maximum as infinity.
 template <int FMT>
 WAR_DEV void mx_store8(const float (&x)[8], uint8_t* codes, uint8_t* scale, bool first) {
-  float top = 0.f;
+  float top = 0.f, odd = 0.f;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(x[i]) < INFINITY ? fabsf(x[i]) : INFINITY);
-  top = quad_max(top);
+  for (int i = 0; i < 8; ++i) {
+    top = fmaxf(top, fabsf(x[i]));
+    odd = fmaf(x[i], 0.f, odd);
+  }
+  top = quad_max(odd == 0.f ? top : INFINITY);
   const bool bad = top == INFINITY;
   const int e = mx_exp<FMT>(bad ? 0.f : top);
   const float f = exp2_int(-e);
   float y[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) y[i] = bad ? 0.f : x[i] * f;
+  for (int i = 0; i < 8; ++i) y[i] = x[i] * f;
   if constexpr (FMT == kMxE4M3) {
-    uint2 c = make_uint2(to_e4m3x4(y[0], y[1], y[2], y[3]), to_e4m3x4(y[4], y[5], y[6], y[7]));
-    *reinterpret_cast<uint2*>(codes) = c;
+    const uint2 c = make_uint2(to_e4m3x4(y[0], y[1], y[2], y[3]), to_e4m3x4(y[4], y[5], y[6], y[7]));
+    *reinterpret_cast<uint2*>(codes) = bad ? make_uint2(0, 0) : c;
   } else {
-    *reinterpret_cast<uint32_t*>(codes) = to_e2m1x8(y);
+    const uint32_t c = to_e2m1x8(y);
+    *reinterpret_cast<uint32_t*>(codes) = bad ? 0 : c;
   }
   if (first) *scale = bad ? kNanScale : (uint8_t)(e + 127);
 }

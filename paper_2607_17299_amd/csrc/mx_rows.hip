@@ -9,6 +9,8 @@
 
 namespace {
 
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
+
 // eight numbers at p
 template <bool F32>
 WAR_DEV void load8(const void* p, int64_t at, float (&x)[8]) {
@@ -86,12 +88,23 @@ __global__ void __launch_bounds__(T < 256 ? 256 : T) k_residual_norm_mx(NormArgs
   }
 }
 
+// g / (1 + exp(-g)) to a few units of 2^-23: exp as a power of two, whose exponent's
+// rounding is made up for to first order, and a reciprocal of the hardware's.  (The
+// library's exp and division made the gate's kernel bound by arithmetic.)
+WAR_DEV float silu(float g) {
+  constexpr float kLog2e = 1.44269502f, kRest = 1.92596303e-8f, kLn2 = 0.693147182f;
+  const float t = g * -kLog2e;
+  const float d = fmaf(g, -kLog2e, -t) - g * kRest;
+  float e = __builtin_amdgcn_exp2f(t);
+  e = t < 127.f ? fmaf(e, d * kLn2, e) : e;  // (an infinite e is left alone)
+  return g * __builtin_amdgcn_rcpf(1.f + e);
+}
+
 // y = x, or x silu(gate), into codes: a lane a run of eight columns
 template <bool F32, bool GATE, int FMT>
 __global__ void __launch_bounds__(256) k_quantize(QuantArgs a) {
-  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int n8 = a.cols / 8;
-  if (id >= (int64_t)a.rows * n8) return;
+  const uint32_t id = blockIdx.x * 256 + threadIdx.x, n8 = a.cols / 8;  // (at most 2^31 runs)
+  if (id >= (uint32_t)a.rows * n8) return;
   const int64_t r = id / n8;
   const int c = (int)(id % n8);
   float y[8];
@@ -100,7 +113,7 @@ __global__ void __launch_bounds__(256) k_quantize(QuantArgs a) {
     float g[8];
     load8<F32>(a.gate, r * a.gate_stride + c * 8, g);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) y[e] *= g[e] / (1.f + expf(-g[e]));
+    for (int e = 0; e < 8; ++e) y[e] *= silu(g[e]);
   }
   mx_store8<FMT>(y, codes_at<FMT>(a.mx, r, c), a.mx.scales + r * a.mx.scale_stride + c / 4, c % 4 == 0);
 }
@@ -108,9 +121,8 @@ __global__ void __launch_bounds__(256) k_quantize(QuantArgs a) {
 // the numbers that codes stand for
 template <bool F32, int FMT>
 __global__ void __launch_bounds__(256) k_dequantize(DequantArgs a) {
-  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int n8 = a.cols / 8;
-  if (id >= (int64_t)a.rows * n8) return;
+  const uint32_t id = blockIdx.x * 256 + threadIdx.x, n8 = a.cols / 8;  // (at most 2^31 runs)
+  if (id >= (uint32_t)a.rows * n8) return;
   const int64_t r = id / n8;
   const int c = (int)(id % n8);
   const float s = mx_scale(a.mx.scales[r * a.mx.scale_stride + c / 4]);
@@ -122,12 +134,9 @@ __global__ void __launch_bounds__(256) k_dequantize(DequantArgs a) {
     y[4] = from_e4m3<0>(w.y, 1.f), y[5] = from_e4m3<1>(w.y, 1.f), y[6] = from_e4m3<2>(w.y, 1.f), y[7] = from_e4m3<3>(w.y, 1.f);
   } else {
     const uint32_t w = *reinterpret_cast<const uint32_t*>(p);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {  // sign, two exponent bits, one mantissa bit; 0.5 is subnormal
-      const uint32_t m = (w >> (4 * e)) & 7, s4 = (w >> (4 * e + 3)) & 1;
-      const uint32_t bits = m >= 2 ? ((m >> 1) + 126) << 23 | (m & 1) << 22 : m ? 126u << 23 : 0u;
-      y[e] = __uint_as_float(bits | s4 << 31);
-    }
+    const f32x2_t v0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.f, 0), v1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.f, 1);
+    const f32x2_t v2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.f, 2), v3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.f, 3);
+    y[0] = v0[0], y[1] = v0[1], y[2] = v1[0], y[3] = v1[1], y[4] = v2[0], y[5] = v2[1], y[6] = v3[0], y[7] = v3[1];
   }
 #pragma unroll
   for (int e = 0; e < 8; ++e) y[e] *= s;

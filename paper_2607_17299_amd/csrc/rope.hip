@@ -5,8 +5,8 @@
 // taken in double in units of a full turn, so that dropping whole turns is exact and
 // positions near 2^31 keep the angle to 2^-24 of a turn; sine and cosine are fp32.
 // Memory bounds it for many rows and a launch's latency for few: a workgroup takes a
-// page of one kv-head, or the same tokens' query heads, eight numbers a lane; a lane's
-// four angles are taken once for all its heads.
+// page of one kv-head with the same tokens' query heads of its group, eight numbers of a
+// head a lane; a lane's four angles are taken once for all of them, behind the loads.
 #include <type_traits>
 
 #include "e4m3.h"
@@ -14,7 +14,7 @@
 
 namespace {
 
-constexpr int kQHeads = 8;  // query heads a workgroup takes, one after the other
+constexpr int kMostGroup = 8;  // query heads of a kv-head
 
 // A lane's eight dims of a head: four at d1 and four at d2.  Turning, they are pairs
 // 4 u + e: (d1 + e, d2 + e), or neighbours of d1 .. and then of d2 ...
@@ -30,14 +30,11 @@ WAR_DEV Dims dims_of(const RopeArgs& a, int u) {
 }
 WAR_DEV void unpack4(uint2 w, float (&x)[4]) { x[0] = lo_f(w.x), x[1] = hi_f(w.x), x[2] = lo_f(w.y), x[3] = hi_f(w.y); }
 
-// cos and sin of the lane's four pairs for row `row`
-WAR_DEV void angles(const RopeArgs& a, int u, int64_t row, int pos, float (&c)[4], float (&s)[4]) {
-  const int64_t rows = (int64_t)a.B * a.n_max;
+// cos and sin of the lane's four pairs, whose positions are p
+WAR_DEV void angles(const double (&turns)[4], const int (&p)[4], float (&c)[4], float (&s)[4]) {
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    const int j = 4 * u + e;
-    const double p = a.positions ? (double)a.positions[a.axis[j] * rows + row] : (double)pos;
-    const double t = p * a.turns[j];
+    const double t = (double)p[e] * turns[e];
     sincospif(2.f * (float)(t - rint(t)), &s[e], &c[e]);
   }
 }
@@ -63,44 +60,59 @@ WAR_DEV void turn8(const RopeArgs& a, bool turn, const float (&c)[4], const floa
   w2 = make_uint2(pack2(o2[0], o2[1]), pack2(o2[2], o2[3]));
 }
 
-template <bool Q8, int HD>
+template <bool Q8, int HD, int G>
 __global__ void __launch_bounds__(2 * HD) k_rope_write(RopeArgs a) {
   using O = PageOrder<Q8, HD>;
   constexpr int L = HD / 8;  // lanes a token
   __shared__ __attribute__((aligned(16))) unsigned char s_pg[2 * O::kBytes];
   __shared__ unsigned char s_sc[32];
-  const int b = blockIdx.x / a.pages, jp = blockIdx.x % a.pages;
-  const int pos0 = a.pos0[b];
-  PageSpan sp;
-  if (!page_span(a.p, b, jp, a.seq[b], pos0, a.n ? a.n[b] : a.n_max, a.n_max, jp == 0 && blockIdx.y == 0 && threadIdx.x == 0, sp))
-    return;
+  const int b = blockIdx.x / a.pages, jp = blockIdx.x % a.pages, kvh = blockIdx.y;
   const int slot = threadIdx.x / L, u = threadIdx.x % L;
-  const bool live = slot >= sp.lo && slot < sp.hi;
-  const int i = sp.t0 + slot - sp.lo;  // token of the request
-  const int64_t row = (int64_t)b * a.n_max + i;
   const Dims d = dims_of(a, u);
-  float c[4], s[4];
-  if (live && d.turn) angles(a, u, row, pos0 + i, c, s);
-  const int kvh = blockIdx.y;
-  if (kvh >= a.g.n_kv_heads) {
-    if (!live) return;
-    const int h0 = (kvh - a.g.n_kv_heads) * kQHeads, h1 = min(h0 + kQHeads, a.n_q_heads);
-#pragma unroll 4
-    for (int h = h0; h < h1; ++h) {
-      const bf16_t* q = a.q + row * a.q_stride + h * HD;
-      bf16_t* o = a.qo + row * a.qo_stride + h * HD;
-      uint2 w1 = *reinterpret_cast<const uint2*>(q + d.d1), w2 = *reinterpret_cast<const uint2*>(q + d.d2);
-      turn8(a, d.turn, c, s, w1, w2);
-      *reinterpret_cast<uint2*>(o + d.d1) = w1;
-      *reinterpret_cast<uint2*>(o + d.d2) = w2;
-    }
-    return;
-  }
+  const int pos0 = a.pos0[b], seq = a.seq[b], n = a.n ? a.n[b] : a.n_max;
+  double turns[4];
+  int axis[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) turns[e] = a.turns[4 * u + e], axis[e] = a.axis[4 * u + e];
+  // a token's numbers are read before its request is known to fit its pages (the rows are
+  // there in any case), so that one memory round trip follows the request's numbers
+  const int i = jp * kPageSlots + slot - (pos0 & (kPageSlots - 1));  // token of the request
+  const bool live = pos0 >= 0 && i >= 0 && i < min(n, a.n_max);
+  const int64_t row = (int64_t)b * a.n_max + i;
+  uint2 k1 = {}, k2 = {}, q1[G], q2[G];
+  uint4 vw = {};
+  int p[4] = {};
   if (live) {
     const bf16_t* k = a.k + row * a.k_stride + kvh * HD;
-    uint2 w1 = *reinterpret_cast<const uint2*>(k + d.d1), w2 = *reinterpret_cast<const uint2*>(k + d.d2);
-    const uint4 vw = *reinterpret_cast<const uint4*>(a.v + row * a.v_stride + kvh * HD + 8 * u);
-    turn8(a, d.turn, c, s, w1, w2);
+    k1 = *reinterpret_cast<const uint2*>(k + d.d1);
+    k2 = *reinterpret_cast<const uint2*>(k + d.d2);
+    vw = *reinterpret_cast<const uint4*>(a.v + row * a.v_stride + kvh * HD + 8 * u);
+    const bf16_t* q = a.q + row * a.q_stride + kvh * a.group * HD;
+#pragma unroll
+    for (int h = 0; h < G; ++h)
+      if (h < a.group) {
+        q1[h] = *reinterpret_cast<const uint2*>(q + h * HD + d.d1);
+        q2[h] = *reinterpret_cast<const uint2*>(q + h * HD + d.d2);
+      }
+    const int64_t rows = (int64_t)a.B * a.n_max;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) p[e] = a.positions ? a.positions[axis[e] * rows + row] : pos0 + i;
+  }
+  PageSpan sp;
+  if (!page_span(a.p, b, jp, seq, pos0, n, a.n_max, jp == 0 && kvh == 0 && threadIdx.x == 0, sp)) return;
+  if (live) {
+    float c[4], s[4];
+    if (d.turn) angles(turns, p, c, s);
+    bf16_t* o = a.qo + row * a.qo_stride + kvh * a.group * HD;
+#pragma unroll
+    for (int h = 0; h < G; ++h)
+      if (h < a.group) {
+        turn8(a, d.turn, c, s, q1[h], q2[h]);
+        *reinterpret_cast<uint2*>(o + h * HD + d.d1) = q1[h];
+        *reinterpret_cast<uint2*>(o + h * HD + d.d2) = q2[h];
+      }
+    turn8(a, d.turn, c, s, k1, k2);
+    const uint2 w1 = k1, w2 = k2;
     const uint32_t vv[4] = {vw.x, vw.y, vw.z, vw.w};
     if constexpr (Q8) {
       float x1[4], x2[4], v[8];
@@ -158,12 +170,18 @@ __global__ void __launch_bounds__(2 * HD) k_rope_write(RopeArgs a) {
 }  // namespace
 
 void launch_rope_write(const RopeArgs& a, hipStream_t st) {
-  const dim3 grid(a.B * a.pages, a.g.n_kv_heads + cdiv_i(a.n_q_heads, kQHeads));
+  const dim3 grid(a.B * a.pages, a.g.n_kv_heads);
+  auto go = [&](auto hd, auto g) {
+    constexpr int HD = decltype(hd)::value, G = decltype(g)::value;
+    if (a.g.q8) k_rope_write<true, HD, G><<<grid, 2 * HD, 0, st>>>(a);
+    else k_rope_write<false, HD, G><<<grid, 2 * HD, 0, st>>>(a);
+  };
+  using std::integral_constant;
   if (a.g.head_dim == 128) {
-    if (a.g.q8) k_rope_write<true, 128><<<grid, 256, 0, st>>>(a);
-    else k_rope_write<false, 128><<<grid, 256, 0, st>>>(a);
+    if (a.group <= 4) go(integral_constant<int, 128>{}, integral_constant<int, 4>{});
+    else go(integral_constant<int, 128>{}, integral_constant<int, kMostGroup>{});
   } else {
-    if (a.g.q8) k_rope_write<true, 64><<<grid, 128, 0, st>>>(a);
-    else k_rope_write<false, 64><<<grid, 128, 0, st>>>(a);
+    if (a.group <= 4) go(integral_constant<int, 64>{}, integral_constant<int, 4>{});
+    else go(integral_constant<int, 64>{}, integral_constant<int, kMostGroup>{});
   }
 }
