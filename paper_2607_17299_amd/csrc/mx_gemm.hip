@@ -50,7 +50,7 @@ typedef uint32_t u32x2_half __attribute__((ext_vector_type(2), aligned(2), may_a
 typedef uint32_t u32x4_half __attribute__((ext_vector_type(4), aligned(2), may_alias));
 typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4), may_alias));
 
-constexpr int GM = 8;  // row blocks of a band (k_mx_tile)
+constexpr int GM = 4;  // row blocks of a band (k_mx_tile)
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
@@ -92,17 +92,18 @@ WAR_DEV void store_whole(const MxGemmArgs& a, int m, int n, f32x4 v) {
   if constexpr (F32) *reinterpret_cast<f32x4_any*>(static_cast<float*>(a.y) + at) = v;
   else *reinterpret_cast<u32x2_half*>(static_cast<bf16_t*>(a.y) + at) = u32x2_half{pack2(v[0], v[1]), pack2(v[2], v[3])};
 }
-// A 32 x 32 tile's results of a lane: row m, columns n + 8 q + 4 half + 0 .. 3.  bf16: the
-// lanes of a row swap halves of two q, so that each writes eight neighbours.
+// A 32 x 32 tile's results of a lane with the bias of their columns (from n on), into its
+// row in LDS: columns 8 q + 4 half + 0 .. 3.  bf16: the lanes of a row swap halves of two
+// q, so that each writes eight neighbours.
 template <bool F32>
-WAR_DEV void store_tile(const MxGemmArgs& a, int m, int n, int half, const f32x16& v) {
+WAR_DEV void tile_row(const bf16_t* bias, int half, const f32x16& v, unsigned char* row) {
   uint32_t w[4][2];
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
-    const uint2 b = *reinterpret_cast<const uint2*>(a.bias + n + 8 * q + 4 * half);
+    const uint2 b = *reinterpret_cast<const uint2*>(bias + 8 * q + 4 * half);
     const f32x4 y = {v[4 * q] + lo_f(b.x), v[4 * q + 1] + hi_f(b.x), v[4 * q + 2] + lo_f(b.y), v[4 * q + 3] + hi_f(b.y)};
     if constexpr (F32) {
-      if (m < a.M) *reinterpret_cast<f32x4_any*>(static_cast<float*>(a.y) + (int64_t)m * a.y_stride + n + 8 * q + 4 * half) = y;
+      *reinterpret_cast<f32x4*>(row + (8 * q + 4 * half) * 4) = y;
     } else {
       w[q][0] = pack2(y[0], y[1]);
       w[q][1] = pack2(y[2], y[3]);
@@ -111,12 +112,9 @@ WAR_DEV void store_tile(const MxGemmArgs& a, int m, int n, int half, const f32x1
   if constexpr (!F32) {
 #pragma unroll
     for (int q = 0; q < 4; q += 2) {
-      uint4 o;
       const auto s0 = __builtin_amdgcn_permlane32_swap(w[q][0], w[q + 1][0], false, false);
       const auto s1 = __builtin_amdgcn_permlane32_swap(w[q][1], w[q + 1][1], false, false);
-      o.x = s0[0], o.z = s0[1], o.y = s1[0], o.w = s1[1];
-      bf16_t* y = static_cast<bf16_t*>(a.y) + (int64_t)m * a.y_stride + n + 8 * (q + half);
-      if (m < a.M) *reinterpret_cast<u32x4_half*>(y) = u32x4_half{o.x, o.y, o.z, o.w};
+      *reinterpret_cast<uint4*>(row + 8 * (q + half) * 2) = make_uint4(s0[0], s1[0], s0[1], s1[1]);
     }
   }
 }
@@ -506,23 +504,36 @@ __global__ void __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_
     if constexpr (ST > 3)
       if (s < nsteps) step(s++, std::integral_constant<int, 3>{});
   }
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // no load into LDS outlives the workgroup
-  // a lane's sixteen results of a tile: row ln, columns 8 q + 4 lg + 0 .. 3
-  const int n0 = nb * BN + wn * NT * 32;
-  const bool whole = n0 + NT * 32 <= a.N;
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // no load into LDS is in flight
+  __syncthreads();
+  // The results go out by whole rows of the wave's columns, through LDS: as the matrix unit
+  // leaves them (32 rows a store, 32 bytes each) every line of y is touched four times,
+  // which took as long as a fifth of 32 steps.
+  constexpr int SZ = F32 ? 4 : 2, ROW = NT * 32 * SZ, CPR = ROW / 16, RPI = 64 / CPR, PITCH = ROW + 16;
+  static_assert(NW * 32 * PITCH <= WS + 2 * WS_B, "a wave's rows fit");
+  unsigned char* buf = smem + wi * 32 * PITCH;
+  const int n0 = nb * BN + wn * NT * 32, col = n0 + lane % CPR * (16 / SZ);
 #pragma unroll
   for (int m = 0; m < MT; ++m) {
-    const int row = m0 + r0 + m * 32;
-    if (whole) {
 #pragma unroll
-      for (int n = 0; n < NT; ++n) store_tile<F32>(a, row, n0 + n * 32, lg, acc[m][n]);
-    } else {
+    for (int n = 0; n < NT; ++n) tile_row<F32>(a.bias + n0 + n * 32, lg, acc[m][n], buf + ln * PITCH + n * 32 * SZ);
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
+    for (int i = 0; i < 32 / RPI; ++i) {
+      const int r = i * RPI + lane / CPR, row = m0 + wm * (BM / WM) + m * 32 + r;
+      const uint4 v = *reinterpret_cast<const uint4*>(buf + r * PITCH + lane % CPR * 16);
+      if (row >= a.M) continue;
+      unsigned char* y = static_cast<unsigned char*>(a.y) + ((int64_t)row * a.y_stride + col) * SZ;
+      if (col + 16 / SZ <= a.N) {
+        *reinterpret_cast<u32x4_half*>(y) = u32x4_half{v.x, v.y, v.z, v.w};
+      } else {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-          store_y<F32>(a, row, n0 + n * 32 + q * 8 + lg * 4,
-                       f32x4{acc[m][n][4 * q], acc[m][n][4 * q + 1], acc[m][n][4 * q + 2], acc[m][n][4 * q + 3]});
+        for (int e = 0; e < 16 / SZ; ++e)
+          if (col + e < a.N) {
+            if constexpr (F32) *reinterpret_cast<uint32_t*>(y + e * 4) = w[e];
+            else *reinterpret_cast<bf16_t*>(y + e * 2) = (bf16_t)(w[e / 2] >> (16 * (e & 1)));
+          }
+      }
     }
   }
 }
