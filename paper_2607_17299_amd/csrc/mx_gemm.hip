@@ -564,26 +564,32 @@ void skinny(const MxGemmArgs& a, int fmt, bool f32, hipStream_t st) {
 }
 
 // What a kernel takes by estimate (us): `start`, then the rounds of its workgroups over the
-// 256 CUs, `step` for a step of one workgroup a CU (few rows: for 2048 columns), `full`
+// 256 CUs, `step` for a step of one workgroup a CU (few rows: of 2048 columns), `full`
 // where the CUs hold all they can, `more` for a round behind the first; at least the
-// weights' bytes at 4.6 TB/s.
+// weights' bytes at 4.6 TB/s (few rows: `more` times as long).
 struct Cost {
   float start, step, full, more;
 };
 struct Shape {
   int bm, bn, occ;  // rows and columns of a workgroup, workgroups a CU
 };
-constexpr int kShapes = 9, kSkinny = 3;
-constexpr Shape kShape[kShapes] = {{16, 16, 2}, {16, 32, 1}, {16, 64, 1}, {32, 128, 2}, {64, 128, 2}, {128, 128, 1}, {96, 256, 2},
-                                   {128, 256, 1}, {256, 256, 1}};
-// x in e4m3 for a bf16 y, for an fp32 y, in e2m1; fitted to the times of 368 sizes, 1 to
-// 4096 rows by 512 to 151936 columns by 256 to 12288 (each: weights of several products in turn).
-// The choice takes 3% more than the best of all shapes on average over them, 58% at most
-// (one row of 14336 by 7168).
-constexpr Cost kCost[3][9] = {
-    {{1.48f, 0.83f, 1.52f, 0.12f}, {2.27f, 0.41f, 1.65f, 0.18f}, {3.29f, 0.01f, 0.30f, 4.51f}, {3.06f, 0.20f, 0.17f, 0.56f}, {3.40f, 0.24f, 0.27f, 0.41f}, {3.70f, 0.32f, 0.46f, 1.63f}, {3.57f, 0.65f, 0.55f, 1.51f}, {4.64f, 0.53f, 0.72f, 3.41f}, {5.99f, 1.01f, 0.88f, 8.00f}},
-    {{3.09f, 0.21f, 0.97f, 2.33f}, {3.44f, 0.01f, 0.30f, 3.54f}, {1.02f, 3.74f, 2.99f, 6.34f}, {3.99f, 0.34f, 0.29f, 0.27f}, {4.34f, 0.52f, 0.47f, 0.59f}, {1.00f, 0.96f, 0.45f, 3.10f}, {1.00f, 1.25f, 1.02f, 1.89f}, {1.00f, 1.33f, 1.37f, 5.73f}, {1.00f, 2.39f, 1.72f, 8.00f}},
-    {{1.61f, 0.64f, 1.09f, 0.41f}, {2.34f, 0.01f, 1.29f, 0.16f}, {2.83f, 0.15f, 0.48f, 3.45f}, {3.06f, 0.18f, 0.16f, 0.59f}, {3.29f, 0.23f, 0.23f, 0.38f}, {3.63f, 0.28f, 0.38f, 1.65f}, {4.69f, 0.39f, 0.46f, 3.00f}, {4.76f, 0.39f, 0.59f, 2.09f}, {6.38f, 0.65f, 0.37f, 8.00f}}};
+constexpr int kShapes = 10, kSkinny = 3;
+constexpr Shape kShape[kShapes] = {{16, 16, 2}, {16, 32, 1}, {16, 64, 1}, {32, 128, 2}, {64, 128, 2}, {128, 128, 1},
+                                   {96, 256, 2}, {128, 256, 1}, {192, 256, 1}, {256, 256, 1}};
+// x in e4m3 for a bf16 y, for an fp32 y, in e2m1; fitted to the times of 570 products of 1 to
+// 4096 rows, 128 to 151936 columns and K of 256 to 12288, the weights of several in turn.
+// Over these the choice takes 1.4% more than the best of these shapes and three others on
+// average, and 60% at most (one row of 14336 by 7168: 18.7 us for 11.7).
+constexpr Cost kCost[3][kShapes] = {
+    {{1.28f, 1.16f, 1.50f, 1.66f}, {1.66f, 1.10f, 1.66f, 1.39f}, {1.80f, 1.36f, 1.88f, 1.74f}, {2.76f, 0.19f, 0.17f, 0.63f},
+     {3.05f, 0.24f, 0.24f, 0.75f}, {3.56f, 0.32f, 0.43f, 1.98f}, {3.55f, 0.64f, 0.54f, 1.20f},
+     {4.04f, 0.53f, 0.48f, 4.75f}, {4.77f, 0.77f, 0.94f, 2.83f}, {5.51f, 0.98f, 1.21f, 3.83f}},
+    {{2.50f, 0.47f, 1.72f, 1.39f}, {2.94f, 0.30f, 1.85f, 1.23f}, {3.65f, 0.23f, 2.40f, 1.08f}, {3.23f, 0.37f, 0.28f, 0.65f},
+     {3.58f, 0.55f, 0.47f, 0.66f}, {3.38f, 0.89f, 0.60f, 2.88f}, {5.92f, 1.05f, 0.97f, 0.55f},
+     {6.18f, 1.12f, 1.31f, 2.19f}, {6.65f, 1.69f, 1.34f, 3.96f}, {7.62f, 2.14f, 1.09f, 5.14f}},
+    {{1.57f, 0.82f, 1.20f, 1.35f}, {1.77f, 0.81f, 1.35f, 1.14f}, {1.91f, 1.10f, 1.65f, 1.44f}, {2.77f, 0.18f, 0.15f, 0.68f},
+     {2.98f, 0.22f, 0.21f, 0.65f}, {3.51f, 0.27f, 0.34f, 2.03f}, {4.49f, 0.38f, 0.44f, 2.59f},
+     {4.59f, 0.35f, 0.55f, 2.02f}, {5.01f, 0.50f, 0.50f, 4.75f}, {5.93f, 0.60f, 0.40f, 6.55f}}};
 
 int choose(const MxGemmArgs& a, int fmt, bool f32) {
   const Cost* cost = kCost[fmt == kMxE2M1 ? 2 : f32 ? 1 : 0];
@@ -598,7 +604,7 @@ int choose(const MxGemmArgs& a, int fmt, bool f32) {
     const float rounds = (float)((wgs + 255) / 256), few = (float)((wgs + 256 * s.occ - 1) / (256 * s.occ));
     float t = cost[c].step * steps * few;
     if (wgs > 256) t = fmaxf(t, cost[c].full * steps * rounds);
-    t = cost[c].start + fmaxf(t, floor) + cost[c].more * (rounds - 1.f);
+    t = cost[c].start + (c < kSkinny ? fmaxf(t, floor * cost[c].more) : fmaxf(t, floor) + cost[c].more * (rounds - 1.f));
     if (t < least) {
       least = t;
       best = c;
@@ -623,6 +629,7 @@ void launch_mx_gemm(const MxGemmArgs& a, int fmt, bool f32, hipStream_t st) {
     case 5: tile<128, 128, 2, 4, 4, 4>(a, fmt, f32, st); break;
     case 6: tile<96, 256, 1, 4, 2, 3>(a, fmt, f32, st); break;
     case 7: tile<128, 256, 2, 4, 4, 4>(a, fmt, f32, st); break;
-    default: tile<256, 256, 2, 4, 3, 3>(a, fmt, f32, st); break;
+    case 8: tile<192, 256, 2, 4, 3, 4>(a, fmt, f32, st); break;
+    default: tile<256, 256, 2, 4, 3, 4>(a, fmt, f32, st); break;
   }
 }
