@@ -134,6 +134,16 @@ WAR_DEV void store_y(const MxGemmArgs& a, int m, int n, f32x4 v) {
     }
 }
 
+// Of what lanes ln (of 16) hold of rows ln % 8 (a) and 8 + ln % 8 (b), pieces g and, from
+// ln = 8 on, g + 4: both pieces of row ln.
+WAR_DEV void halves(uint4 a, uint4 b, uint4& lo, uint4& hi) {
+  // row_ror:8 (0x128); bank masks: lanes 8 .. 15, lanes 0 .. 7
+  auto low = [](uint32_t p, uint32_t q) { return (uint32_t)__builtin_amdgcn_update_dpp((int)p, (int)q, 0x128, 0xf, 0xc, false); };
+  auto high = [](uint32_t p, uint32_t q) { return (uint32_t)__builtin_amdgcn_update_dpp((int)q, (int)p, 0x128, 0xf, 0x3, false); };
+  lo = make_uint4(low(a.x, b.x), low(a.y, b.y), low(a.z, b.z), low(a.w, b.w));
+  hi = make_uint4(high(a.x, b.x), high(a.y, b.y), high(a.z, b.z), high(a.w, b.w));
+}
+
 // Few rows: the weights' way from memory bounds it.  A workgroup takes 16 NT columns by
 // 16 MT rows; its waves share the runs of 256 k between them, every fragment straight from
 // memory to registers, RING - 1 runs ahead of the products, and their sums meet in LDS in
@@ -142,7 +152,6 @@ template <int MT, int NT, int WAVES, int RING, int XF, bool F32>
 __global__ void __launch_bounds__(WAVES * 64) __attribute__((amdgpu_waves_per_eu(WAVES / 4, WAVES / 4 > 2 ? 4 : 2)))
 k_mx_skinny(MxGemmArgs a) {
   constexpr bool E8 = XF == kMxE4M3, EXACT = E8 && F32;
-  constexpr int XB = E8 ? 128 : 64;             // bytes of a row's 128 columns
   __shared__ f32x4 s_sum[WAVES][MT * NT][64];
   const int lane = threadIdx.x & 63, ln = lane & 15, lg = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -153,12 +162,17 @@ k_mx_skinny(MxGemmArgs a) {
   for (int m = 0; m < MT; ++m)
 #pragma unroll
     for (int n = 0; n < NT; ++n) acc[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const uint8_t *xc[MT], *xs[MT];
+  // x is read by whole lines: one load eight rows by 128 bytes, a lane piece pc of row ln % 8
+  // (or 8 + ln % 8); lanes ln and ln ^ 8 then swap halves (see `halves`).  Rows past the
+  // last read the last one, and are not written.
+  const int pc = lg + (ln >> 3) * 4;
+  const uint8_t *xc[MT][2], *xs[MT];
 #pragma unroll
-  for (int m = 0; m < MT; ++m) {  // rows past the last read the last one, and are not written
-    const int64_t r = min(m0 + m * 16 + ln, a.M - 1);
-    xc[m] = a.x.codes + r * a.x.code_stride + lg * 16;
-    xs[m] = a.x.scales + r * a.x.scale_stride;
+  for (int m = 0; m < MT; ++m) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      xc[m][h] = a.x.codes + (int64_t)min(m0 + m * 16 + h * 8 + (ln & 7), a.M - 1) * a.x.code_stride + pc * 16;
+    xs[m] = a.x.scales + (int64_t)min(m0 + m * 16 + ln, a.M - 1) * a.x.scale_stride;
   }
   const uint8_t* wc[NT];
   const uint32_t* wsp[NT];
@@ -169,7 +183,7 @@ k_mx_skinny(MxGemmArgs a) {
     wc[n] = a.w + (t * 8 + (lg >> 1)) * 1024 + li * 16;
     wsp[n] = a.ws + t * 128 + li;
   }
-  uint4 x[RING][2][MT][E8 ? 2 : 1], w[RING][2][NT];
+  uint4 x[RING][E8 ? 2 : 1][MT][2], w[RING][2][NT];  // x: of a line (e2m1: two steps), rows 0 .. 7 and 8 .. 15
   uint32_t sx[RING][2][MT], sw[RING][NT];
   // the fragments of run r into slot q
   auto load = [&](auto tag, int r) __attribute__((always_inline)) {
@@ -188,9 +202,10 @@ k_mx_skinny(MxGemmArgs a) {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           sx[Q][j][m] = s[j];
-          const uint8_t* p = xc[m] + (int64_t)(r * 2 + j) * XB;
-          x[Q][j][m][0] = *reinterpret_cast<const uint4*>(p);
-          if constexpr (E8) x[Q][j][m][1] = *reinterpret_cast<const uint4*>(p + 64);
+          if (j == 0 || E8) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) x[Q][j][m][h] = *reinterpret_cast<const uint4*>(xc[m][h] + (int64_t)(E8 ? r * 2 + j : r) * 128);
+          }
         }
       }
     } else {
@@ -203,9 +218,12 @@ k_mx_skinny(MxGemmArgs a) {
         for (int j = 0; j < 2; ++j) {
           const int kj = k0 + j * 128;
           sx[Q][j][m] = kj + lg * 32 < a.K ? *reinterpret_cast<const uint32_t*>(xs[m] + kj / 32) : 0x7f7f7f7fu;
-          const uint8_t* p = xc[m] + (int64_t)(r * 2 + j) * XB;
-          x[Q][j][m][0] = kj + (E8 ? lg * 16 : lg * 32) < a.K ? *reinterpret_cast<const uint4*>(p) : zero;
-          if constexpr (E8) x[Q][j][m][1] = kj + 64 + lg * 16 < a.K ? *reinterpret_cast<const uint4*>(p + 64) : zero;
+          if (j == 0 || E8) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+              x[Q][j][m][h] = (E8 ? kj + pc * 16 : k0 + pc * 32) < a.K
+                                  ? *reinterpret_cast<const uint4*>(xc[m][h] + (int64_t)(E8 ? r * 2 + j : r) * 128) : zero;
+          }
         }
     }
   };
@@ -215,10 +233,11 @@ k_mx_skinny(MxGemmArgs a) {
       constexpr int J = decltype(tj)::value;
 #pragma unroll
       for (int m = 0; m < MT; ++m) {
-        const uint4 lo = x[Q][J][m][0];
+        uint4 lo, hi;  // pieces lg and lg + 4 of row ln
+        halves(x[Q][E8 ? J : 0][m][0], x[Q][E8 ? J : 0][m][1], lo, hi);
+        if (!E8 && J == 1) lo = hi;
         i32x8 xv = {(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, 0, 0, 0, 0}, xl = xv;
         if constexpr (E8) {
-          const uint4 hi = x[Q][J][m][1];
           xv[4] = (int)hi.x, xv[5] = (int)hi.y, xv[6] = (int)hi.z, xv[7] = (int)hi.w;
           if constexpr (EXACT) {
             const i32x8 all = xv;
