@@ -76,6 +76,12 @@ war_status war_debug_pool_waits(war_kv_pool* p, int64_t* waits);
 war_status war_profile(war_model* m, int32_t enable);
 war_status war_profile_read(war_model* m, char* out, int32_t out_len);
 
+/* war_linear_run through a chosen shape of workgroups, 0 .. 9, and the shape that it
+ * chooses for a product (mx_gemm.hip). */
+war_status war_debug_linear(const war_linear* l, const war_mx* x, void* y, int64_t y_stride, int32_t y_type,
+                            int32_t shape, void* stream);
+int32_t war_debug_linear_shape(int32_t M, int32_t N, int32_t K, int32_t x_format, int32_t y_type);
+
 #ifdef __cplusplus
 }
 #endif

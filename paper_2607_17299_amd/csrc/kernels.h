@@ -350,7 +350,11 @@ inline int mx_groups(int K) { return (K + 511) / 512; }
 inline int64_t mx_code_bytes(int N, int K) { return (int64_t)mx_tiles(N) * mx_groups(K) * 8192; }
 inline int64_t mx_scale_words(int N, int K) { return (int64_t)mx_tiles(N) * mx_groups(K) * 128; }
 void launch_mx_pack(const MxRef& w, int N, int K, uint8_t* codes, uint32_t* scales, hipStream_t st);
-void launch_mx_gemm(const MxGemmArgs& a, int fmt, bool f32, hipStream_t st);
+// shape: of the workgroups, kMxShapes of them (-1: the one that plan_mx_gemm chooses);
+// false where the product has too many for one launch
+constexpr int kMxShapes = 10;
+int plan_mx_gemm(int M, int N, int K, int fmt, bool f32);
+bool launch_mx_gemm(const MxGemmArgs& a, int fmt, bool f32, int shape, hipStream_t st);
 
 // rotated queries, and rotated keys with values into the pages (rope.hip)
 struct RopeArgs {

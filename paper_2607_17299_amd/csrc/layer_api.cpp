@@ -5,6 +5,7 @@
 #include <cmath>
 #include <new>
 
+#include "../../include/war_debug.h"
 #include "api.h"
 #include "mx.h"
 
@@ -162,7 +163,8 @@ void war_linear_destroy(war_linear* l) {
   delete l;
 }
 
-war_status war_linear_run(const war_linear* l, const war_mx* x, void* y, int64_t y_stride, int32_t y_type, void* stream) {
+static war_status run_linear(const war_linear* l, const war_mx* x, void* y, int64_t y_stride, int32_t y_type, int shape,
+                             void* stream) {
   CHECK(l, "null linear");
   WARCHK(check_mx(x));
   CHECK(x->cols == l->K, "x has another number of columns than the weights");
@@ -183,9 +185,24 @@ war_status war_linear_run(const war_linear* l, const war_mx* x, void* y, int64_t
   a.y = y;
   a.y_stride = y_stride;
   a.scale16 = x->cols % 512 == 0 && x->scale_stride % 16 == 0 && aligned(x->scales, 16);
-  launch_mx_gemm(a, fmt(*x), y_type == WAR_F32, static_cast<hipStream_t>(stream));
+  if (!launch_mx_gemm(a, fmt(*x), y_type == WAR_F32, shape, static_cast<hipStream_t>(stream)))
+    return api_fail(WAR_ERR_UNSUPPORTED, "more workgroups than a launch holds");
   HIPCHK(hipGetLastError());
   return WAR_OK;
+}
+
+war_status war_linear_run(const war_linear* l, const war_mx* x, void* y, int64_t y_stride, int32_t y_type, void* stream) {
+  return run_linear(l, x, y, y_stride, y_type, -1, stream);
+}
+
+war_status war_debug_linear(const war_linear* l, const war_mx* x, void* y, int64_t y_stride, int32_t y_type, int32_t shape,
+                            void* stream) {
+  CHECK(shape >= 0 && shape < kMxShapes, "shape out of range");
+  return run_linear(l, x, y, y_stride, y_type, shape, stream);
+}
+
+int32_t war_debug_linear_shape(int32_t M, int32_t N, int32_t K, int32_t x_format, int32_t y_type) {
+  return plan_mx_gemm(M, N, K, x_format - WAR_MX_E4M3, y_type == WAR_F32);
 }
 
 war_status war_rope_write(war_kv_pool* p, int32_t layer, const war_rope* rope, int32_t B, const int32_t* seq_ids,

@@ -592,7 +592,7 @@ struct Cost {
 struct Shape {
   int bm, bn, occ;  // rows and columns of a workgroup, workgroups a CU
 };
-constexpr int kShapes = 10, kSkinny = 3;
+constexpr int kShapes = kMxShapes, kSkinny = 3;
 constexpr Shape kShape[kShapes] = {{16, 16, 2}, {16, 32, 1}, {16, 64, 1}, {32, 128, 2}, {64, 128, 2}, {128, 128, 1},
                                    {96, 256, 2}, {128, 256, 1}, {192, 256, 1}, {256, 256, 1}};
 // x in e4m3 for a bf16 y, for an fp32 y, in e2m1; fitted to the times of 570 products of 1 to
@@ -610,6 +610,10 @@ constexpr Cost kCost[3][kShapes] = {
      {2.98f, 0.22f, 0.21f, 0.65f}, {3.51f, 0.27f, 0.34f, 2.03f}, {4.49f, 0.38f, 0.44f, 2.59f},
      {4.59f, 0.35f, 0.55f, 2.02f}, {5.01f, 0.50f, 0.50f, 4.75f}, {5.93f, 0.60f, 0.40f, 6.55f}}};
 
+bool fits_launch(const MxGemmArgs& a, int c) {  // its work items below 2^32
+  return (int64_t)cdiv_i(a.M, kShape[c].bm) * cdiv_i(a.N, kShape[c].bn) * 512 < (int64_t)1 << 32;
+}
+
 int choose(const MxGemmArgs& a, int fmt, bool f32) {
   const Cost* cost = kCost[fmt == kMxE2M1 ? 2 : f32 ? 1 : 0];
   const float floor = (float)a.N * (float)a.K * (17.f / 32.f / 4.6e6f);
@@ -618,7 +622,7 @@ int choose(const MxGemmArgs& a, int fmt, bool f32) {
   for (int c = a.M <= 64 ? 0 : kSkinny; c < kShapes; ++c) {
     const Shape& s = kShape[c];
     const int64_t wgs = (int64_t)cdiv_i(a.M, s.bm) * cdiv_i(a.N, s.bn);
-    if (wgs * 512 >= (int64_t)1 << 32) continue;  // a launch's work items
+    if (!fits_launch(a, c)) continue;
     const int steps = c < kSkinny ? cdiv_i(a.K, 2048) : cdiv_i(a.K, 128);
     const float rounds = (float)((wgs + 255) / 256), few = (float)((wgs + 256 * s.occ - 1) / (256 * s.occ));
     float t = cost[c].step * steps * few;
@@ -638,8 +642,18 @@ void launch_mx_pack(const MxRef& w, int N, int K, uint8_t* codes, uint32_t* scal
   k_mx_pack<<<dim3(mx_tiles(N), mx_groups(K)), 512, 0, st>>>(w, N, K, mx_groups(K), codes, scales);
 }
 
-void launch_mx_gemm(const MxGemmArgs& a, int fmt, bool f32, hipStream_t st) {
-  switch (choose(a, fmt, f32)) {
+int plan_mx_gemm(int M, int N, int K, int fmt, bool f32) {
+  MxGemmArgs a{};
+  a.M = M;
+  a.N = N;
+  a.K = K;
+  return choose(a, fmt, f32);
+}
+
+bool launch_mx_gemm(const MxGemmArgs& a, int fmt, bool f32, int shape, hipStream_t st) {
+  if (shape < 0) shape = choose(a, fmt, f32);
+  if (shape >= kShapes || !fits_launch(a, shape) || (shape < kSkinny && a.M > 65535 * 16)) return false;
+  switch (shape) {
     case 0: skinny<1, 1, 8, 3>(a, fmt, f32, st); break;
     case 1: skinny<1, 2, 8, 3>(a, fmt, f32, st); break;
     case 2: skinny<1, 4, 8, 3>(a, fmt, f32, st); break;
@@ -651,4 +665,5 @@ void launch_mx_gemm(const MxGemmArgs& a, int fmt, bool f32, hipStream_t st) {
     case 8: tile<192, 256, 2, 4, 3, 4>(a, fmt, f32, st); break;
     default: tile<256, 256, 2, 4, 3, 4>(a, fmt, f32, st); break;
   }
+  return true;
 }

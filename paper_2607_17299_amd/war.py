@@ -33,7 +33,8 @@ EXPORTS = ["war_weight_count", "war_model_create", "war_model_destroy", "war_kv_
            "war_residual_norm", "war_quantize", "war_dequantize", "war_linear_create", "war_linear_destroy",
            "war_linear_run", "war_rope_write",
            "war_last_error", "war_debug_mfma16", "war_debug_workspace", "war_debug_sample",
-           "war_debug_gemm", "war_debug_gemm_plan", "war_debug_pool_waits", "war_profile", "war_profile_read"]
+           "war_debug_gemm", "war_debug_gemm_plan", "war_debug_pool_waits", "war_profile", "war_profile_read", "war_debug_linear",
+           "war_debug_linear_shape"]
 
 
 class WarError(RuntimeError):
@@ -119,6 +120,8 @@ def load_library(path: str = LIB_PATH) -> C.CDLL:
         "war_debug_gemm": (i32, [vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp]),
         "war_debug_gemm_plan": (i32, [i32, i32, i32, i32, C.c_int64, pi32, pi32, pi32]),
         "war_debug_pool_waits": (i32, [vp, C.POINTER(C.c_int64)]),
+        "war_debug_linear": (i32, [vp, C.POINTER(_Mx), vp, C.c_int64, i32, i32, vp]),
+        "war_debug_linear_shape": (i32, [i32, i32, i32, i32, i32]),
         "war_profile": (i32, [vp, i32]),
         "war_profile_read": (i32, [vp, C.c_char_p, i32]),
     }
@@ -808,6 +811,13 @@ def debug_sample(logits: torch.Tensor, ntok: torch.Tensor, drafts: torch.Tensor,
     _check(lib().war_debug_sample(_ptr(logits), V, B, k_max, _ptr(ntok), _ptr(drafts), _ptr(uniforms),
                                   float(temperature), int(top_k), _ptr(accept_lens), _ptr(next_tokens),
                                   _stream(stream)))
+
+
+def debug_linear(weights: Linear, x: Mx, out: torch.Tensor, shape: int, stream=None) -> torch.Tensor:
+    """linear() through a chosen shape of workgroups (war_debug.h)."""
+    s = _matrix("out", out, weights.device, x.shape[0], weights.out_features)
+    _call(lib().war_debug_linear, weights.device, stream, weights.handle, x._ref, out.data_ptr(), s, _TYPES[out.dtype], shape)
+    return out
 
 
 def debug_gemm_plan(M: int, N: int, K: int, epi: int, cap_elems: int = 64 << 20) -> tuple:

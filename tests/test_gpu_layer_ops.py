@@ -279,6 +279,28 @@ def test_products_that_fp32_holds_are_exact(M, N, K, fmt, y_type):
     assert torch.equal(even[:, :N], y) and bool((even[:, N:] == 9).all())
 
 
+@pytest.mark.parametrize("y_type", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("shape", range(10))
+def test_every_shape_of_workgroups(shape, fmt, y_type):
+    """Each shape on rows, columns and blocks that fill no tile, one step and many, scales
+    that are read one at a time and four, whatever shape such a product would get."""
+    war = _war()
+    rng = np.random.default_rng(shape)
+    for M, N, K, pad in ((1, 1, 32, 16), (33, 129, 64, 16), (97, 260, 160, 0), (130, 65, 512, 48), (17, 300, 544, 16), (258, 513, 1024, 16),
+                         (100, 40, 2080, 16), (40, 257, 3584, 0)):
+        (x, xn), (w, wn) = coded(rng, M, K, fmt, True, pad=pad), coded(rng, N, K, "e2m1", True)
+        x.whole[1][M:] = 255
+        bias = torch.tensor(rng.integers(-64, 65, N) / 4).bfloat16().to(DEV)
+        lin = war.Linear(w, bias)
+        want = torch.tensor(xn @ wn.T + as64(bias)).float().to(y_type)
+        for gap in (3, -N % 8):
+            y = padded(M + 1, N, gap, y_type, 9.0)
+            war.debug_linear(lin, x, y[:M], shape)
+            torch.testing.assert_close(y[:M].cpu(), want, rtol=0, atol=0)
+            assert bool((y._base[:, N:] == 9).all()) and bool((y._base[M] == 9).all())
+
+
 @pytest.mark.parametrize("fmt", FMTS)
 @pytest.mark.parametrize("M,N,K", [(3, 40, 4096), (65, 96, 2080), (200, 384, 1536), (520, 140, 768)])
 def test_products_of_activations(M, N, K, fmt):

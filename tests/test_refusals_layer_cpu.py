@@ -64,6 +64,19 @@ def test_linear_refuses():
     lib.war_linear_destroy(None)
 
 
+def test_shapes_are_chosen_for_every_size():
+    lib = war.lib()
+    for fmt in (2, 3):
+        for yt in (0, 1):
+            for M in (1, 16, 17, 64, 65, 100, 1000, 65536, 1 << 20):
+                for N in (1, 100, 5003, 151936, 1 << 20):
+                    for K in (32, 544, 4096, 65536):
+                        s = lib.war_debug_linear_shape(M, N, K, fmt, yt)
+                        assert 0 <= s < 10 and (s >= 3 or M <= 64)
+    assert lib.war_debug_linear(None, C.byref(mx()), A, 64, 0, 10, None) == INVALID
+    assert lib.war_debug_linear(None, C.byref(mx()), A, 64, 0, -1, None) == INVALID
+
+
 def test_rope_write_refuses():
     lib = war.lib()
     r = war.Rope(64)
