@@ -276,8 +276,8 @@ typedef struct war_mx {
 } war_mx;
 
 /* The residual's addition and the norm behind it: h += x, then y = h / sqrt(mean(h^2) +
- * eps) * gain, rounded once to y's type.  Sums are fp32 (h, where it is bf16, is rounded as
- * it is stored, not for y).
+ * eps) * gain, rounded once to y's type.  h^2 and its sum are fp32 (h, where it is bf16, is
+ * rounded as it is stored, not for y).
  *   x        device bf16 [rows][cols] at x_stride, or NULL: h stays as it is
  *   h        device [rows][cols] at h_stride, h_type WAR_BF16 or WAR_F32
  *   gain     device bf16 [cols]
@@ -331,7 +331,8 @@ typedef struct war_rope {
  *   seq_ids, pos0, n_max, n_lens   as in war_kv_write
  *   positions  device int32 [n_axes][B * n_max]: row b * n_max + i on each axis; NULL: the
  *              token's place in the cache, pos0[b] + i, on every axis
- *   q, q_out   device bf16 rows of n_q_heads * head_dim; q_out may be q (same stride)
+ *   q, q_out   device bf16 rows of n_q_heads * head_dim; q_out may be q (same stride),
+ *              and overlaps nothing else
  *   k, v       device bf16 rows of n_kv_heads * head_dim, not written
  * Strides in elements, multiples of 8; 16-byte aligned.  Turned numbers are rounded to
  * bf16.  Rows beyond n_lens, and requests that are flagged as in war_kv_write, are left

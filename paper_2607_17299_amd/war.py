@@ -387,6 +387,8 @@ def _checked(device, dtype, **arrays) -> None:
 def _call(fn, device, stream, *args) -> None:
     """fn(*args, stream) with `device` current; its current stream by default (read raw:
     a Stream object is made in 2 us, a third of a small call)."""
+    if device.index is None:
+        raise ValueError(f"tensors must be on the GPU, not on {device}")
     raw = torch._C._cuda_getCurrentRawStream(device.index) if stream is None else stream.cuda_stream
     if torch._C._cuda_getDevice() == device.index:
         status = fn(*args, raw)
@@ -643,7 +645,8 @@ def rope_write(pool: Pool, layer: int, rope: Rope, seq_ids: torch.Tensor, pos0: 
     _require(bool(pool.handle), "the pool is closed")
     _require(rope.head_dim == c.head_dim, "rope is made for another head_dim")
     _require(pos0.numel() == B and (n_lens is None or n_lens.numel() == B), "pos0 and n_lens must hold one entry a request")
-    _require(positions is None or positions.shape == (rope.n_axes, B, n), f"positions must be [{rope.n_axes}, {B}, {n}]")
+    _require(positions is None or (positions.shape[0] >= rope.n_axes and positions.shape[1:] == (B, n)),
+             f"positions must be [{rope.n_axes}, {B}, {n}]")
     Hq, Hkv, D = c.n_q_heads, c.n_kv_heads, c.head_dim
     qs, os_ = _rows_of("q", q, dev, B, n, Hq, D), _rows_of("q_out", q_out, dev, B, n, Hq, D)
     ks, vs = _rows_of("k", k, dev, B, n, Hkv, D), _rows_of("v", v, dev, B, n, Hkv, D)

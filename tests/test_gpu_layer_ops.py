@@ -471,7 +471,7 @@ def test_rope_in_place_by_default_positions_and_one_row_at_a_time():
     a, b, c = (pool_of(heads, [p + n for p in ctx], "e4m3") for _ in range(3))
     out = torch.empty((B, n, 8, 128), dtype=torch.bfloat16, device=DEV)
     war.rope_write(a, 0, rope, t32([0, 1, 2]), t32(ctx), x[:, :, :8], x[:, :, 8:10], x[:, :, 10:], out)
-    pos = t32([[[p + i for i in range(n)] for p in ctx]])
+    pos = t32([[[p + i for i in range(n)] for p in ctx]] + [[[-1] * n] * B])      # an axis that no pair follows
     y = x.clone()
     war.rope_write(b, 0, rope, t32([0, 1, 2]), t32(ctx), y[:, :, :8], y[:, :, 8:10], y[:, :, 10:], y[:, :, :8], positions=pos)
     assert torch.equal(y[:, :, :8], out) and torch.equal(y[:, :, 8:], x[:, :, 8:])
@@ -499,7 +499,7 @@ def test_rope_flags_what_kv_write_flags():
     bad = torch.zeros((5, 2), dtype=torch.bool)
     bad[2, 1] = True
     assert torch.equal(k[3].isnan().all(-1).cpu(), bad) and torch.equal(v[3].isnan().all(-1).cpu(), bad)
-    for wrong in (dict(rope=war.Rope(128)), dict(positions=t32(np.zeros((2, 4, 5)))), dict(out=out[:3])):
+    for wrong in (dict(rope=war.Rope(128)), dict(positions=t32(np.zeros((1, 3, 5)))), dict(out=out[:3])):
         with pytest.raises(ValueError):
             war.rope_write(pool, 0, wrong.get("rope", rope), t32([0, 1, 2, 3]), t32([0] * 4), x[:, :, :4], x[:, :, 4:6], x[:, :, 6:],
                            wrong.get("out", out), positions=wrong.get("positions"))

@@ -104,6 +104,10 @@ def test_matrices_are_checked():
                  (x, h, g[:32], 1e-6, m), (x, h, g, 1e-6, e), (x, h, g, 1e-6, h)):
         with pytest.raises(ValueError):
             war.residual_norm(*args)
+    with pytest.raises(ValueError, match="GPU"):
+        war.residual_norm(x, h, g, 1e-6, m)
+    with pytest.raises(ValueError, match="GPU"):
+        war.dequantize(m, x)
     with pytest.raises(ValueError):
         war.quantize(x, m, gate=h)
     with pytest.raises(ValueError):
