@@ -29,6 +29,20 @@ WAR_DEV uint32_t pack2(float a, float b) {
 WAR_DEV float lo_f(uint32_t v) { return __uint_as_float(v << 16); }
 WAR_DEV float hi_f(uint32_t v) { return __uint_as_float(v & 0xffff0000u); }
 
+// non-temporal: numbers that this kernel reads once, or leaves for a later one
+WAR_DEV uint2 load_once8(const void* p) {
+  typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint2, __builtin_nontemporal_load(static_cast<const u32x2_t*>(p)));
+}
+WAR_DEV uint4 load_once16(const void* p) {
+  typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+  return __builtin_bit_cast(uint4, __builtin_nontemporal_load(static_cast<const u32x4_t*>(p)));
+}
+WAR_DEV void store_once8(void* p, uint2 v) {
+  typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+  __builtin_nontemporal_store(__builtin_bit_cast(u32x2_t, v), static_cast<u32x2_t*>(p));
+}
+
 WAR_DEV bf16x8 as_bf16x8(uint4 v) { return __builtin_bit_cast(bf16x8, v); }
 
 WAR_DEV f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) {

@@ -315,22 +315,28 @@ struct NormArgs {
   int64_t x_stride, h_stride, y_stride;
   float eps;
 };
+struct RowsBy {  // a row's number from a run's (rows_by)
+  uint32_t magic;
+  int shift;
+};
 struct QuantArgs {
   int rows, cols;
   const void *x, *gate;  // gate nullable
   int64_t x_stride, gate_stride;
   MxRef mx;
+  RowsBy by{};  // the launch's
 };
 struct DequantArgs {
   int rows, cols;
   MxRef mx;
   void* y;
   int64_t y_stride;
+  RowsBy by{};
 };
 // out, fmt: the format (mx.h); out -1: bf16
 void launch_residual_norm_mx(const NormArgs& a, bool h_f32, int out, hipStream_t st);
-void launch_quantize(const QuantArgs& a, bool f32, int fmt, hipStream_t st);
-void launch_dequantize(const DequantArgs& a, bool f32, int fmt, hipStream_t st);
+void launch_quantize(QuantArgs a, bool f32, int fmt, hipStream_t st);
+void launch_dequantize(DequantArgs a, bool f32, int fmt, hipStream_t st);
 
 // products with e2m1 weights (mx_gemm.hip)
 struct MxGemmArgs {

@@ -33,11 +33,6 @@ WAR_DEV void load_lds16(uint32_t lds, int voff, i32x4 rsrc) {
                  "s"(rsrc)
                  : "memory");
 }
-// The same with four bytes a lane: lane l's go to LDS byte lds + 4 l.
-WAR_DEV void load_lds4(uint32_t lds, int voff, i32x4 rsrc) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(lds), "v"(voff), "s"(rsrc)
-               : "memory");
-}
 WAR_DEV i32x4 make_rsrc(const void* p, int64_t bytes) {
   const uint64_t a = reinterpret_cast<uint64_t>(p);
   const uint32_t n = bytes < 0xffffffffLL ? (uint32_t)bytes : 0xffffffffu;

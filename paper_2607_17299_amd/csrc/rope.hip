@@ -7,6 +7,11 @@
 // Memory bounds it for many rows and a launch's latency for few: a workgroup takes a
 // page of one kv-head with the same tokens' query heads of its group, eight numbers of a
 // head a lane; a lane's four angles are taken once for all of them, behind the loads.
+// 28300 rows of 32 and 8 heads of 128 into bf16 pages: 134 us for 695 MB, 5.2 TB/s.  (By
+// ordinary loads and stores of what it turns 163, and less of the pages stays in the caches
+// for who reads them next, 56 us for 40; with workgroups of their own for the query heads,
+// and the angles before the loads, 188.)  192 rows into e4m3 pages: 6.5 us, 5.7 where a
+// graph launches it, of which the angles are about 2.
 #include <type_traits>
 
 #include "e4m3.h"
@@ -84,15 +89,15 @@ __global__ void __launch_bounds__(2 * HD) k_rope_write(RopeArgs a) {
   int p[4] = {};
   if (live) {
     const bf16_t* k = a.k + row * a.k_stride + kvh * HD;
-    k1 = *reinterpret_cast<const uint2*>(k + d.d1);
-    k2 = *reinterpret_cast<const uint2*>(k + d.d2);
-    vw = *reinterpret_cast<const uint4*>(a.v + row * a.v_stride + kvh * HD + 8 * u);
+    k1 = load_once8(k + d.d1);
+    k2 = load_once8(k + d.d2);
+    vw = load_once16(a.v + row * a.v_stride + kvh * HD + 8 * u);
     const bf16_t* q = a.q + row * a.q_stride + kvh * a.group * HD;
 #pragma unroll
     for (int h = 0; h < G; ++h)
       if (h < a.group) {
-        q1[h] = *reinterpret_cast<const uint2*>(q + h * HD + d.d1);
-        q2[h] = *reinterpret_cast<const uint2*>(q + h * HD + d.d2);
+        q1[h] = load_once8(q + h * HD + d.d1);
+        q2[h] = load_once8(q + h * HD + d.d2);
       }
     const int64_t rows = (int64_t)a.B * a.n_max;
 #pragma unroll
@@ -108,8 +113,8 @@ __global__ void __launch_bounds__(2 * HD) k_rope_write(RopeArgs a) {
     for (int h = 0; h < G; ++h)
       if (h < a.group) {
         turn8(a, d.turn, c, s, q1[h], q2[h]);
-        *reinterpret_cast<uint2*>(o + h * HD + d.d1) = q1[h];
-        *reinterpret_cast<uint2*>(o + h * HD + d.d2) = q2[h];
+        store_once8(o + h * HD + d.d1, q1[h]);
+        store_once8(o + h * HD + d.d2, q2[h]);
       }
     turn8(a, d.turn, c, s, k1, k2);
     const uint2 w1 = k1, w2 = k2;
