@@ -36,12 +36,20 @@ WAR_DEV Dims dims_of(const RopeArgs& a, int u) {
 WAR_DEV void unpack4(uint2 w, float (&x)[4]) { x[0] = lo_f(w.x), x[1] = hi_f(w.x), x[2] = lo_f(w.y), x[3] = hi_f(w.y); }
 
 // cos and sin of the lane's four pairs, whose positions are p
-WAR_DEV void angles(const double (&turns)[4], const int (&p)[4], float (&c)[4], float (&s)[4]) {
+WAR_DEV void angles(const double (&turns)[4], const int (&p)[4], double (&c)[4], double (&s)[4]) {
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     const double t = (double)p[e] * turns[e];
-    sincospif(2.f * (float)(t - rint(t)), &s[e], &c[e]);
+    sincospi(2. * (t - rint(t)), &s[e], &c[e]);
   }
+}
+// d as a float that rounds to the bf16 that d rounds to: cut towards an odd last bit
+WAR_DEV float sticky(double d) {
+  const float f = (float)d;
+  const double rest = d - (double)f;
+  const uint32_t u = __float_as_uint(f);
+  if (rest == 0. || (u & 1)) return f;  // (u odd: no tie of a bf16's)
+  return __uint_as_float((rest < 0.) == (bool)(u >> 31) ? u + 1 : u - 1);
 }
 // the two runs turned and rounded to bf16
 WAR_DEV void turn8(const RopeArgs& a, bool turn, const float (&c)[4], const float (&s)[4], uint2& w1, uint2& w2) {
@@ -60,6 +68,28 @@ WAR_DEV void turn8(const RopeArgs& a, bool turn, const float (&c)[4], const floa
       o1[e] = x[e] * c[e] - y[e] * s[e];
       o2[e] = y[e] * c[e] + x[e] * s[e];
     }
+  }
+  w1 = make_uint2(pack2(o1[0], o1[1]), pack2(o1[2], o1[3]));
+  w2 = make_uint2(pack2(o2[0], o2[1]), pack2(o2[2], o2[3]));
+}
+
+// The same in double, for keys: they are rounded again, to their code, and a bf16 on the
+// wrong side of a tie (in fp32 one of 10^5) may be the next code.
+WAR_DEV void turn8(const RopeArgs& a, bool turn, const double (&c)[4], const double (&s)[4], uint2& w1, uint2& w2) {
+  if (!turn) return;
+  float x[4], y[4], o1[4], o2[4];
+  unpack4(w1, x);
+  unpack4(w2, y);
+  auto pair = [](float x, float y, double c, double s, float& p, float& q) {
+    p = sticky((double)x * c - (double)y * s);
+    q = sticky((double)y * c + (double)x * s);
+  };
+  if (a.adjacent) {
+    pair(x[0], x[1], c[0], s[0], o1[0], o1[1]), pair(x[2], x[3], c[1], s[1], o1[2], o1[3]);
+    pair(y[0], y[1], c[2], s[2], o2[0], o2[1]), pair(y[2], y[3], c[3], s[3], o2[2], o2[3]);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) pair(x[e], y[e], c[e], s[e], o1[e], o2[e]);
   }
   w1 = make_uint2(pack2(o1[0], o1[1]), pack2(o1[2], o1[3]));
   w2 = make_uint2(pack2(o2[0], o2[1]), pack2(o2[2], o2[3]));
@@ -107,7 +137,11 @@ __global__ void __launch_bounds__(2 * HD) k_rope_write(RopeArgs a) {
   if (!page_span(a.p, b, jp, seq, pos0, n, a.n_max, jp == 0 && kvh == 0 && threadIdx.x == 0, sp)) return;
   if (live) {
     float c[4], s[4];
-    if (d.turn) angles(turns, p, c, s);
+    double c64[4] = {}, s64[4] = {};
+    if (d.turn) angles(turns, p, c64, s64);
+    turn8(a, d.turn, c64, s64, k1, k2);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) c[e] = (float)c64[e], s[e] = (float)s64[e];
     bf16_t* o = a.qo + row * a.qo_stride + kvh * a.group * HD;
 #pragma unroll
     for (int h = 0; h < G; ++h)
@@ -116,7 +150,6 @@ __global__ void __launch_bounds__(2 * HD) k_rope_write(RopeArgs a) {
         store_once8(o + h * HD + d.d1, q1[h]);
         store_once8(o + h * HD + d.d2, q2[h]);
       }
-    turn8(a, d.turn, c, s, k1, k2);
     const uint2 w1 = k1, w2 = k2;
     const uint32_t vv[4] = {vw.x, vw.y, vw.z, vw.w};
     if constexpr (Q8) {

@@ -301,6 +301,26 @@ def test_every_shape_of_workgroups(shape, fmt, y_type):
             assert bool((y._base[:, N:] == 9).all()) and bool((y._base[M] == 9).all())
 
 
+@pytest.mark.parametrize("y_type", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("bm,bn,shape", [(128, 128, 5), (96, 256, 6), (128, 256, 7), (192, 256, 8), (256, 256, 9)])
+def test_more_tiles_than_compute_units(bm, bn, shape, fmt, y_type):
+    """Several bands of tiles on every XCD, the last ones not whole, of one step of the
+    columns and of several."""
+    war = _war()
+    rng = np.random.default_rng(shape)
+    M, N = 24 * bm + 17, 22 * bn + 9
+    for K, gap in ((96, 7), (672, 1)):
+        (x, xn), (w, wn) = coded(rng, M, K, fmt, True), coded(rng, N, K, "e2m1", True)
+        bias = torch.tensor(rng.integers(-64, 65, N) / 4).bfloat16().to(DEV)
+        lin = war.Linear(w, bias)
+        y = padded(M + 1, N, gap, y_type, 9.0)
+        war.debug_linear(lin, x, y[:M], shape)
+        want = torch.tensor(xn @ wn.T + as64(bias)).float().to(y_type)
+        assert torch.equal(y[:M].cpu(), want)
+        assert bool((y._base[:, N:] == 9).all()) and bool((y._base[M] == 9).all())
+
+
 @pytest.mark.parametrize("fmt", FMTS)
 @pytest.mark.parametrize("M,N,K", [(3, 40, 4096), (65, 96, 2080), (200, 384, 1536), (520, 140, 768)])
 def test_products_of_activations(M, N, K, fmt):
