@@ -111,8 +111,9 @@ WAR_DEV uint32_t row_of(uint32_t id, RowsBy by) { return __umulhi(id, by.magic) 
 // whose largest they find by two swaps.  Memory bounds it once the arithmetic is short
 // (the row by a product in place of a division, silu's seven instructions) and what it
 // reads does not push what others need out of the caches.  16384 x 12288 of bf16 with a
-// gate into e2m1: 912 MB in 155 us, 5.9 TB/s; by ordinary loads 193, and a lane with
-// sixteen columns, whose loads leave out every other 16 bytes, 178.
+// gate into e2m1: 912 MB in 155 us, 5.9 TB/s; by ordinary loads 193 (4096 rows just written,
+// which the last cache holds: 30.8 by ordinary ones, 31.9 so), and a lane with sixteen
+// columns, whose loads leave out every other 16 bytes, 178.
 template <bool F32, bool GATE, int FMT>
 __global__ void __launch_bounds__(256) k_quantize(QuantArgs a) {
   const uint32_t id = blockIdx.x * 256 + threadIdx.x, n8 = a.cols / 8;  // (at most 2^31 runs)
@@ -140,8 +141,8 @@ WAR_DEV void from_e2m1x8(uint32_t w, float* y) {
   y[0] = v0[0], y[1] = v0[1], y[2] = v1[0], y[3] = v1[1], y[4] = v2[0], y[5] = v2[1], y[6] = v3[0], y[7] = v3[1];
 }
 
-// the numbers that codes stand for, sixteen a lane.  16384 x 12288 of e2m1 into bf16: 92 us for 510 MB, 5.5
-// TB/s (the numbers put together from the codes' bits: 135).
+// the numbers that codes stand for, sixteen a lane.  16384 x 12288 of e2m1 into bf16: 85 us
+// for 510 MB, 6.0 TB/s (eight a lane 92, the numbers put together from the codes' bits 135).
 template <bool F32, int FMT>
 __global__ void __launch_bounds__(256) k_dequantize(DequantArgs a) {
   const uint32_t id = blockIdx.x * 256 + threadIdx.x, n16 = a.cols / 16;

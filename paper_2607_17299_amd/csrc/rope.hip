@@ -2,16 +2,18 @@
 // turned and go into the cache's pages with their values (bf16 or e4m3, kv_page.h).
 //
 // Pair j of a head turns by position a(j) of its row times a frequency.  The product is
-// taken in double in units of a full turn, so that dropping whole turns is exact and
-// positions near 2^31 keep the angle to 2^-24 of a turn; sine and cosine are fp32.
+// taken in double in units of a full turn, so that dropping whole turns is exact at any
+// position; sine and cosine are double, too, and so are the keys' turns, as these are
+// rounded twice (bf16, then a code).  Queries turn in fp32.
 // Memory bounds it for many rows and a launch's latency for few: a workgroup takes a
 // page of one kv-head with the same tokens' query heads of its group, eight numbers of a
 // head a lane; a lane's four angles are taken once for all of them, behind the loads.
-// 28300 rows of 32 and 8 heads of 128 into bf16 pages: 134 us for 695 MB, 5.2 TB/s.  (By
-// ordinary loads and stores of what it turns 163, and less of the pages stays in the caches
-// for who reads them next, 56 us for 40; with workgroups of their own for the query heads,
-// and the angles before the loads, 188.)  192 rows into e4m3 pages: 6.5 us, 5.7 where a
-// graph launches it, of which the angles are about 2.
+// 28300 rows of 32 and 8 heads of 128 into bf16 pages: 148 us for 695 MB, 4.7 TB/s; 134
+// with sine, cosine and keys in fp32, of whose codes one in some 10^5 was another.  (By
+// ordinary loads and stores of what it turns 163 for these 134, and less of the pages stays
+// in the caches for who reads them next, 56 us for 40; with workgroups of their own for
+// the query heads, and the angles before the loads, 188.)  192 rows into e4m3 pages: 7.6
+// us, of which the angles are about 3.
 #include <type_traits>
 
 #include "e4m3.h"
@@ -48,7 +50,7 @@ WAR_DEV float sticky(double d) {
   const float f = (float)d;
   const double rest = d - (double)f;
   const uint32_t u = __float_as_uint(f);
-  if (rest == 0. || (u & 1)) return f;  // (u odd: no tie of a bf16's)
+  if (!(rest < 0. || rest > 0.) || (u & 1)) return f;  // exact, not finite, or no tie of a bf16's
   return __uint_as_float((rest < 0.) == (bool)(u >> 31) ? u + 1 : u - 1);
 }
 // the two runs turned and rounded to bf16

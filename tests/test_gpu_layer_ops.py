@@ -432,6 +432,44 @@ def pool_of(heads, tokens, fmt, layers=1):
 AXES = {"one": lambda n: [0] * n, "blocks": lambda n: [0 if j < n // 4 else 1 + (j % 2) for j in range(n)], "turns": lambda n: [j % 4 for j in range(n)]}
 
 
+@pytest.mark.parametrize("adjacent", [False, True])
+def test_rope_of_numbers_that_are_not_finite(adjacent):
+    """Infinities, NaN and turns past bf16's range are what the formula makes of them, and no
+    other number's business."""
+    war = _war()
+    rng = np.random.default_rng(3)
+    D, R, top = 64, 64, 3.3895313892515355e38
+    x = rng.standard_normal((1, 4, 4, D))
+    a, b = ([0, 2, 4, 6], [1, 3, 5, 7]) if adjacent else ([0, 1, 2, 3], [32, 33, 34, 35])
+    for h in (0, 2):                                    # a query's head and a key's
+        x[0, 0, h, a[0]], x[0, 1, h, b[1]], x[0, 2, h, a[2]] = np.inf, -np.inf, np.nan
+        x[0, 3, h, a[3]] = x[0, 3, h, b[3]] = top
+    x = torch.tensor(x).bfloat16().to(DEV)
+    pool = pool_of((2, 1, D), [9], "bf16")
+    out = torch.empty((1, 4, 2, D), dtype=torch.bfloat16, device=DEV)
+    war.rope_write(pool, 0, war.Rope(D, R, adjacent=adjacent), t32([0]), t32([5]), x[:, :, :2], x[:, :, 2:3], x[:, :, 3:4], out)
+    k, v = (torch.empty((1, 4, 1, D), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    war.kv_read(pool, 0, t32([0]), t32([5]), k, v)
+    j = np.arange(R // 2)
+    angle = np.arange(5, 9)[:, None, None] * 10000.0 ** (-2 * j / R)
+    pairs = (slice(0, R, 2), slice(1, R, 2)) if adjacent else (slice(0, R // 2), slice(R // 2, R))
+    z = as64(x[0])
+    with np.errstate(invalid="ignore", over="ignore"):
+        want = z.copy()
+        want[..., pairs[0]] = z[..., pairs[0]] * np.cos(angle) - z[..., pairs[1]] * np.sin(angle)
+        want[..., pairs[1]] = z[..., pairs[1]] * np.cos(angle) + z[..., pairs[0]] * np.sin(angle)
+    want[np.abs(want) >= 3.4e38] *= np.inf              # (bf16's largest and half a step: 3.396e38)
+    size = np.zeros_like(z)
+    size[..., pairs[0]] = size[..., pairs[1]] = np.abs(z[..., pairs[0]]) + np.abs(z[..., pairs[1]])
+    for got, lo in ((as64(out[0]), 0), (as64(k[0]), 2)):
+        ref = want[:, lo:lo + got.shape[1]]
+        assert (np.isnan(got) == np.isnan(ref)).all() and (np.isinf(got) == np.isinf(ref)).all()
+        assert (np.sign(got) == np.sign(ref))[np.isinf(ref)].all()
+        f = np.isfinite(ref)
+        assert (np.abs(got[f] - ref[f]) <= 2.0 ** -8 * np.abs(ref[f]) + 2.0 ** -20 * size[:, lo:lo + got.shape[1]][f]).all()
+    torch.testing.assert_close(v, x[:, :, 3:4], rtol=0, atol=0)
+
+
 @pytest.mark.parametrize("axes", list(AXES))
 @pytest.mark.parametrize("rotary,adjacent", [(1.0, False), (0.5, True), (0.5, False), (1.0, True), (24, False)])
 @pytest.mark.parametrize("heads", [(4, 2, 64), (32, 8, 128), (9, 3, 128)])
