@@ -322,15 +322,17 @@ k_mx_skinny(MxGemmArgs a) {
 // fragments as they are stored.  The scale words come for several steps at once.
 //
 // 256 x 256 by 8 waves: 128 sums a lane, and an LDS byte read once for 128 of a fragment's
-// products, which takes 40% of the cycles.  8192 x 24576 x 4096: e2m1 440 to 470 us (3.6
-// PFLOP/s; the instruction alone reaches 8.9), e4m3 590 to 610 us (2.8 of 4.95).  Over the
-// whole kernel the matrix pipes are busy 52% and 76% of the cycles, at 1.8 GHz, to which
-// power holds the clock; in the loop 63% and 86%, the rest being a tile's first loads and
-// its results, about 11 us each.  Slower on this size: two workgroups of 128 x 256 a CU,
-// which overlap these (582 us); one that goes on to its next tile and requests the first
-// stages before it stores the results, as these stages then wait for the stores (458 us
-// become 492, in e4m3 586 become 636); bands of 8 and 16 row blocks (508, 511); stores
-// past the caches (956).  Six stages are no faster than four.
+// products, which takes 40% of the cycles.  8192 x 24576 x 4096: e2m1 440 to 480 us (3.6
+// PFLOP/s; the instruction alone reaches 8.9), e4m3 590 to 640 us (2.7 of 4.95).  Over the
+// whole kernel the matrix pipes are busy 52% and 76% of the cycles, in the loop 63% and
+// 86%, at 1.8 GHz, to which power holds the clock: on codes of zeros the same instructions
+// take 395 and 470 us, and without the loop's loads 3% less than with them.  The rest is a
+// tile's first loads and its results, about 11 us each.  Not faster on this size: two
+// workgroups of 128 x 256 a CU, which overlap these (582 us); one that goes on to its next
+// tile and requests the first stages before it stores the results, which these then wait
+// for (458 us become 492); stages requested a step later, for a barrier that waits for no
+// LDS read (488, 489); bands of 8 and 16 row blocks (508, 511); stores past the caches
+// (956); six stages.
 template <int BM, int BN, int WM, int WN, int ST, int XF, bool F32>
 __global__ void __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) k_mx_tile(MxGemmArgs a) {
   constexpr bool E8 = XF == kMxE4M3, EXACT = E8 && F32;
