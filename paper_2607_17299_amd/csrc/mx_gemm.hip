@@ -611,20 +611,20 @@ struct Shape {
 constexpr int kShapes = kMxShapes, kSkinny = 3;
 constexpr Shape kShape[kShapes] = {{16, 16, 2}, {16, 32, 1}, {16, 64, 1}, {32, 128, 2}, {64, 128, 2}, {128, 128, 1},
                                    {96, 256, 2}, {128, 256, 1}, {192, 256, 1}, {256, 256, 1}};
-// x in e4m3 for a bf16 y, for an fp32 y, in e2m1; fitted to the times of 570 products of 1 to
+// x in e4m3 for a bf16 y, for an fp32 y, in e2m1; fitted to the times of 677 products of 1 to
 // 4096 rows, 128 to 151936 columns and K of 256 to 12288, the weights of several in turn.
-// Over these the choice takes 1.4% more than the best of these shapes and three others on
-// average, and 60% at most (one row of 14336 by 7168: 18.7 us for 11.7).
+// Over these the choice takes 0.5% more than the best of the shapes on average, and 24% at
+// most (16 rows of 24576 by 4096 in e4m3: 17.4 us for 14.0).
 constexpr Cost kCost[3][kShapes] = {
-    {{1.28f, 1.16f, 1.50f, 1.66f}, {1.66f, 1.10f, 1.66f, 1.39f}, {1.80f, 1.36f, 1.88f, 1.74f}, {2.76f, 0.19f, 0.17f, 0.63f},
-     {3.05f, 0.24f, 0.24f, 0.75f}, {3.56f, 0.32f, 0.43f, 1.98f}, {3.55f, 0.64f, 0.54f, 1.20f},
-     {4.04f, 0.53f, 0.48f, 4.75f}, {4.77f, 0.77f, 0.94f, 2.83f}, {5.51f, 0.98f, 1.21f, 3.83f}},
-    {{2.50f, 0.47f, 1.72f, 1.39f}, {2.94f, 0.30f, 1.85f, 1.23f}, {3.65f, 0.23f, 2.40f, 1.08f}, {3.23f, 0.37f, 0.28f, 0.65f},
-     {3.58f, 0.55f, 0.47f, 0.66f}, {3.38f, 0.89f, 0.60f, 2.88f}, {5.92f, 1.05f, 0.97f, 0.55f},
-     {6.18f, 1.12f, 1.31f, 2.19f}, {6.65f, 1.69f, 1.34f, 3.96f}, {7.62f, 2.14f, 1.09f, 5.14f}},
-    {{1.57f, 0.82f, 1.20f, 1.35f}, {1.77f, 0.81f, 1.35f, 1.14f}, {1.91f, 1.10f, 1.65f, 1.44f}, {2.77f, 0.18f, 0.15f, 0.68f},
-     {2.98f, 0.22f, 0.21f, 0.65f}, {3.51f, 0.27f, 0.34f, 2.03f}, {4.49f, 0.38f, 0.44f, 2.59f},
-     {4.59f, 0.35f, 0.55f, 2.02f}, {5.01f, 0.50f, 0.50f, 4.75f}, {5.93f, 0.60f, 0.40f, 6.55f}}};
+    {{2.70f, 1.00f, 1.42f, 1.28f}, {2.66f, 1.29f, 1.61f, 1.13f}, {2.82f, 1.67f, 2.20f, 1.05f}, {4.04f, 0.19f, 0.18f, 0.91f},
+     {4.42f, 0.25f, 0.26f, 1.23f}, {5.02f, 0.34f, 0.46f, 2.92f}, {5.97f, 0.68f, 0.57f, 2.54f},
+     {6.30f, 0.56f, 0.67f, 4.82f}, {7.44f, 0.84f, 0.95f, 6.52f}, {8.00f, 1.10f, 1.35f, 8.00f}},
+    {{2.50f, 0.47f, 1.72f, 1.39f}, {2.94f, 0.30f, 1.85f, 1.23f}, {3.65f, 0.23f, 2.40f, 1.08f}, {3.23f, 0.37f, 0.27f, 0.65f},
+     {4.07f, 0.55f, 0.44f, 0.66f}, {3.38f, 0.89f, 0.60f, 2.88f}, {5.92f, 1.05f, 0.97f, 0.55f},
+     {6.18f, 1.12f, 1.28f, 2.19f}, {6.65f, 1.69f, 1.34f, 3.96f}, {7.62f, 2.14f, 1.09f, 5.14f}},
+    {{3.31f, 0.54f, 0.96f, 0.74f}, {2.92f, 0.71f, 1.22f, 0.97f}, {2.97f, 1.03f, 1.66f, 1.19f}, {4.05f, 0.18f, 0.16f, 0.96f},
+     {4.30f, 0.23f, 0.22f, 1.17f}, {4.97f, 0.27f, 0.35f, 2.97f}, {6.36f, 0.40f, 0.48f, 4.02f},
+     {5.95f, 0.41f, 0.62f, 4.85f}, {7.61f, 0.52f, 0.68f, 7.24f}, {8.00f, 0.68f, 0.85f, 8.00f}}};
 
 bool fits_launch(const MxGemmArgs& a, int c) {  // its work items below 2^32
   return (int64_t)cdiv_i(a.M, kShape[c].bm) * cdiv_i(a.N, kShape[c].bn) * 512 < (int64_t)1 << 32;
