@@ -282,7 +282,7 @@ typedef struct war_mx {
  *   h        device [rows][cols] at h_stride, h_type WAR_BF16 or WAR_F32
  *   gain     device bf16 [cols]
  *   mx       y in codes (a HOST struct of rows by cols), or NULL and
- *   y        device bf16 [rows][cols] at y_stride (y may be x)
+ *   y        device bf16 [rows][cols] at y_stride (y may be x, at the same stride)
  * Strides in elements, multiples of 8; 16-byte aligned; sizes as of a war_mx. */
 war_status war_residual_norm(int32_t rows, int32_t cols, const void* x, int64_t x_stride, void* h, int64_t h_stride,
                              int32_t h_type, const void* gain, float eps, const war_mx* mx, void* y, int64_t y_stride,

@@ -82,6 +82,7 @@ war_status war_residual_norm(int32_t rows, int32_t cols, const void* x, int64_t 
   if (x) WARCHK(check_rows(x, x_stride, cols));
   WARCHK(check_rows(h, h_stride, cols));
   if (y) WARCHK(check_rows(y, y_stride, cols));
+  CHECK(!x || x != y || x_stride == y_stride, "in place, the strides must be the same");
   CHECK(gain && aligned(gain, 16), "gain must be 16-byte aligned");
   NormArgs a{};
   a.rows = rows;

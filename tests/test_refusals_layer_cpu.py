@@ -114,3 +114,12 @@ def test_matrices_are_checked():
         war.quantize(x.t(), m)
     with pytest.raises(ValueError):
         war.dequantize(m, x[:2])
+
+
+def test_residual_norm_in_place_wants_one_stride():
+    """A row of y at another stride than x's would land on rows of x that other workgroups
+    have yet to read."""
+    lib = war.lib()
+    for xs, ys in ((72, 64), (64, 72)):
+        assert lib.war_residual_norm(3, 64, A, xs, 2 * A, 64, 1, A, 1e-6, None, A, ys, None) == INVALID
+        assert b"in place" in lib.war_last_error()
