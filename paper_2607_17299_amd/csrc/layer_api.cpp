@@ -73,7 +73,7 @@ war_status war_residual_norm(int32_t rows, int32_t cols, const void* x, int64_t 
   WARCHK(check_size(rows, cols));
   CHECK(is_type(h_type), "h_type must be WAR_BF16 or WAR_F32");
   CHECK(eps >= 0.f && std::isfinite(eps), "eps must be finite and not negative");
-  CHECK((mx != nullptr) != (y != nullptr), "one of mx and y is wanted");
+  CHECK((mx != nullptr) != (y != nullptr) || (rows == 0 && !mx), "one of mx and y is wanted");  // (no rows have no address)
   if (mx) {
     WARCHK(check_mx(mx));
     CHECK(mx->rows == rows && mx->cols == cols, "mx has another size");

@@ -782,3 +782,21 @@ def test_matrices_past_4_gb():
     war.linear(wide, a, big[:, :131072])
     num = war.dequantize(a, torch.empty((9000, 32), device=DEV))
     assert torch.equal(big[:, 0], num.sum(1)) and torch.equal(big[:, 131071], num.sum(1)) and torch.equal(big[8999, :131072].min(), big[8999, 0])
+
+
+def test_no_rows():
+    """Empty batches are no work for any of the operators."""
+    war = _war()
+    bf = lambda *shape: torch.empty(shape, dtype=torch.bfloat16, device=DEV)
+    gain, m = torch.ones(64, device=DEV).bfloat16(), war.Mx.empty(0, 64, "e4m3", DEV)
+    for h in (bf(0, 64), torch.empty((0, 64), device=DEV)):
+        for x in (None, bf(0, 64)):
+            for out in (bf(0, 64), m, war.Mx.empty(0, 64, "e2m1", DEV)):
+                war.residual_norm(x, h, gain, 1e-6, out)
+    war.quantize(bf(0, 64), m, gate=bf(0, 64))
+    war.dequantize(m, bf(0, 64))
+    war.linear(war.Linear(torch.ones((24, 64), device=DEV)), m, bf(0, 24))
+    pool = pool_of((4, 2, 64), [16], "bf16")
+    war.rope_write(pool, 0, war.Rope(64), t32([0]), t32([3]), bf(1, 0, 4, 64), bf(1, 0, 2, 64), bf(1, 0, 2, 64), bf(1, 0, 4, 64))
+    torch.cuda.synchronize()
+    assert pool.state()["status"] == 0

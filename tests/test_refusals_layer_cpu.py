@@ -123,3 +123,11 @@ def test_residual_norm_in_place_wants_one_stride():
     for xs, ys in ((72, 64), (64, 72)):
         assert lib.war_residual_norm(3, 64, A, xs, 2 * A, 64, 1, A, 1e-6, None, A, ys, None) == INVALID
         assert b"in place" in lib.war_last_error()
+
+
+def test_residual_norm_of_no_rows():
+    """An empty tensor has no address: no rows are no work, whichever output they go to."""
+    lib = war.lib()
+    norm = lambda m, y, rows=0: lib.war_residual_norm(rows, 64, None, 64, None, 64, 1, A, 1e-6, m, y, 64, None)
+    assert norm(None, None) == 0 and norm(None, A) == 0 and norm(C.byref(mx(rows=0)), None) == 0
+    assert norm(C.byref(mx(rows=0)), A) == INVALID and norm(None, None, 1) == INVALID
