@@ -532,6 +532,7 @@ class Mx:
 
     def __getitem__(self, rows: slice) -> "Mx":
         """Some of the rows, in the same memory."""
+        _require(isinstance(rows, slice), "rows must be a slice: other indices would copy")
         return Mx(self.codes[rows], self.scales[rows], self.format)
 
 

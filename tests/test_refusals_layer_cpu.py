@@ -131,3 +131,14 @@ def test_residual_norm_of_no_rows():
     norm = lambda m, y, rows=0: lib.war_residual_norm(rows, 64, None, 64, None, 64, 1, A, 1e-6, m, y, 64, None)
     assert norm(None, None) == 0 and norm(None, A) == 0 and norm(C.byref(mx(rows=0)), None) == 0
     assert norm(C.byref(mx(rows=0)), A) == INVALID and norm(None, None, 1) == INVALID
+
+
+def test_rows_of_a_matrix_share_its_memory():
+    m = war.Mx.empty(6, 64, "e2m1", "cpu")
+    for rows in (slice(1, 4), slice(None, None, 2), slice(6, 6)):
+        part = m[rows]
+        assert part.codes.untyped_storage().data_ptr() == m.codes.untyped_storage().data_ptr()
+        assert part.shape == (len(range(6)[rows]), 64)
+    for rows in (torch.tensor([0, 2]), [0, 2], torch.ones(6, dtype=torch.bool), 3, (slice(0, 2), slice(0, 16))):
+        with pytest.raises(ValueError):                          # (copies, which a call would write to in vain)
+            m[rows]
