@@ -1,0 +1,80 @@
+"""Products whose codes lie past 32-bit offsets, every row of them, in every shape of
+workgroups."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import mx as omx
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+
+
+def _war():
+    from paper_2607_17299_amd import war
+    return war
+
+
+def held(codes, scales, fmt):
+    """An Mx of codes (one a number) and scale bytes."""
+    m = _war().Mx.empty(*codes.shape, fmt, DEV)
+    m.codes.copy_(torch.tensor(codes if fmt == "e4m3" else omx.pack_e2m1(codes), dtype=torch.uint8))
+    m.scales.copy_(torch.tensor(scales, dtype=torch.uint8))
+    return m
+
+
+def rows_of_seven(rows, cols, fmt):
+    """(Mx, its seven different rows' numbers, which of them each row is): a row 2^15 or 2^16
+    further, 2^31 or 2^32 bytes on, is another one."""
+    k = (torch.arange(cols, device=DEV) // (cols // 16))[None]
+    c = (torch.arange(7, device=DEV)[:, None] + k) % 7
+    codes = (0x38 + c if fmt == "e4m3" else (1 + c) * 17).to(torch.uint8)
+    which = torch.arange(rows, device=DEV) * 5 % 7
+    scales = torch.full((rows, cols // (32 if fmt == "e4m3" else 16)), 127, dtype=torch.uint8, device=DEV)
+    m = _war().Mx(codes[which], scales, fmt)
+    c = codes.cpu().numpy()
+    c = c.astype(np.int64) if fmt == "e4m3" else omx.unpack_e2m1(c)
+    return m, omx.numbers(c, np.full((7, c.shape[1] // 32), 127), fmt), which.cpu()
+
+
+@pytest.mark.parametrize("fmt,rows", [("e4m3", 70000), ("e2m1", 140000)])
+def test_activations_past_4_gb(fmt, rows):
+    """Every row of codes of 4.6 GB, in every shape.  Products are multiples of 2^-4 and their
+    magnitudes add up to less than 2^20 (e2m1: 2^-2 and 2^22): fp32 holds all sums."""
+    war = _war()
+    K, N = 65536, 24
+    x, num, which = rows_of_seven(rows, K if fmt == "e4m3" else K // 2, fmt)
+    assert x.codes.numel() > 2 ** 32
+    rng = np.random.default_rng(0)
+    wc = rng.integers(0, 16, (N, K))
+    wn = omx.numbers(wc, np.full((N, K // 32), 127), "e2m1")
+    assert (np.abs(num) @ np.abs(wn).T).max() * (16 if fmt == "e4m3" else 4) < 2 ** 24
+    lin = war.Linear(held(wc, np.full((N, K // 32), 127), "e2m1"))
+    want = torch.tensor(num @ wn.T).float()
+    assert len(set(want[:, 0].tolist())) == 7
+    for shape in range(10):
+        for t in (torch.float32, torch.bfloat16):
+            y = war.debug_linear(lin, x, torch.full((rows, N), 9.0, dtype=t, device=DEV), shape)
+            assert torch.equal(y.cpu(), want.to(t)[which]), (shape, t)
+    y = war.linear(lin, x, torch.full((rows, N), 9.0, device=DEV))
+    assert torch.equal(y.cpu(), want[which])
+
+
+def test_weights_past_4_gb():
+    """Every row of weights of 4.6 GB in codes; multiples of 2^-5 below 2^19."""
+    war = _war()
+    rows, K, M = 140000, 65536, 9
+    w, num, which = rows_of_seven(rows, K // 2, "e2m1")
+    lin = war.Linear(w)
+    del w
+    rng = np.random.default_rng(1)
+    xc = rng.integers(0x30, 0x48, (M, K)) + 128 * rng.integers(0, 2, (M, K))
+    xn = omx.numbers(xc, np.full((M, K // 32), 127), "e4m3")
+    assert (np.abs(xn) @ np.abs(num).T).max() * 32 < 2 ** 24
+    x = held(xc, np.full((M, K // 32), 127), "e4m3")
+    want = torch.tensor(xn @ num.T).float()
+    assert len(set(want[0].tolist())) == 7
+    for shape in range(10):
+        y = war.debug_linear(lin, x, torch.full((M, rows), 9.0, device=DEV), shape)
+        assert torch.equal(y.cpu(), want[:, which]), shape
+    assert torch.equal(war.linear(lin, x, y.zero_()).cpu(), want[:, which])
