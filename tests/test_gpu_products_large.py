@@ -1,5 +1,5 @@
 """Products whose codes lie past 32-bit offsets, every row of them, in every shape of
-workgroups."""
+workgroups; the largest matrices into codes and back."""
 import numpy as np
 import pytest
 import torch
@@ -78,3 +78,24 @@ def test_weights_past_4_gb():
         y = war.debug_linear(lin, x, torch.full((M, rows), 9.0, device=DEV), shape)
         assert torch.equal(y.cpu(), want[:, which]), shape
     assert torch.equal(war.linear(lin, x, y.zero_()).cpu(), want[:, which])
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "e2m1"])
+def test_the_largest_matrix_into_codes_and_back(fmt):
+    """2^20 rows of 511 blocks, 2^34 numbers less a 512th: every row against one of seven."""
+    war = _war()
+    rows, cols = 1 << 20, 32 * 511
+    g = torch.Generator(device=DEV).manual_seed(7)
+    some = torch.randn((7, cols), device=DEV, generator=g).bfloat16()
+    which = torch.arange(rows, device=DEV) * 5 % 7
+    x = some[which]
+    m, seven = war.Mx.empty(rows, cols, fmt, DEV), war.Mx.empty(7, cols, fmt, DEV)
+    war.quantize(x, m)
+    war.quantize(some, seven)
+    y = war.dequantize(seven, torch.empty_like(some))
+    step = 1 << 17
+    for i in range(0, rows, step):
+        w = which[i: i + step]
+        assert torch.equal(m.codes[i: i + step], seven.codes[w]) and torch.equal(m.scales[i: i + step], seven.scales[w])
+    war.dequantize(m, x)
+    assert all(torch.equal(x[i: i + step], y[which[i: i + step]]) for i in range(0, rows, step))
