@@ -326,7 +326,7 @@ k_mx_skinny(MxGemmArgs a) {
 // fragments as they are stored.  The scale words come for several steps at once.
 //
 // 256 x 256 by 8 waves: 128 sums a lane, and an LDS byte read once for 128 of a fragment's
-// products, which takes 40% of the cycles.  8192 x 24576 x 4096: e2m1 440 to 480 us (3.6
+// products, which takes 40% of the cycles.  8192 x 24576 x 4096: e2m1 435 to 480 us (3.6
 // PFLOP/s; the instruction alone reaches 8.9), e4m3 590 to 640 us (2.7 of 4.95).  Over the
 // whole kernel the matrix pipes are busy 52% and 76% of the cycles, in the loop 63% and
 // 86%, at 1.8 GHz, to which power holds the clock: on codes of zeros the same instructions
@@ -616,7 +616,7 @@ constexpr int kShapes = kMxShapes, kSkinny = 3;
 constexpr Shape kShape[kShapes] = {{16, 16, 2}, {16, 32, 1}, {16, 64, 1}, {32, 128, 2}, {64, 128, 2}, {128, 128, 1},
                                    {96, 256, 2}, {128, 256, 1}, {192, 256, 1}, {256, 256, 1}};
 // x in e4m3 for a bf16 y, for an fp32 y, in e2m1; fitted to the times of 677 products of 1 to
-// 4096 rows, 128 to 151936 columns and K of 256 to 12288, the weights of several in turn.
+// 4096 rows, 128 to 151936 columns and K of 256 to 12288, the weights of up to eight in turn.
 // Over these the choice takes 0.5% more than the best of the shapes on average, and 24% at
 // most (16 rows of 24576 by 4096 in e4m3: 17.4 us for 14.0).
 constexpr Cost kCost[3][kShapes] = {

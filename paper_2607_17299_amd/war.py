@@ -606,7 +606,8 @@ class Linear:
 
 
 def linear(weights: Linear, x: Mx, out: torch.Tensor, stream=None) -> torch.Tensor:
-    """out = x w^T + bias: x [rows, K] in codes, out bf16 or fp32 [rows, N]."""
+    """out = x w^T + bias: x [rows, K] in codes, out bf16 or fp32 [rows, N] (sums of e4m3 rows
+    are cut on their way to bf16, as war.h says; fp32 has all of them)."""
     _require(bool(weights.handle), "the weights are closed")
     dev, N = weights.device, weights.out_features
     _require(x.device == dev and x.shape[1] == weights.in_features, f"x must have {weights.in_features} columns on {dev}")
