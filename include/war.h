@@ -290,6 +290,7 @@ war_status war_residual_norm(int32_t rows, int32_t cols, const void* x, int64_t 
 
 /* A matrix x into codes (mx, a HOST struct; its rows and cols are x's); with a gate g,
  * x * g / (1 + exp(-g)): what a SwiGLU's gate and up projections leave for the one down.
+ * (Zero where exp(-g) is past fp32, g below -88.7.)
  * x and gate (NULL: none): device, type WAR_BF16 or WAR_F32, strides as above. */
 war_status war_quantize(const war_mx* mx, const void* x, int64_t x_stride, const void* gate, int64_t gate_stride,
                         int32_t type, void* stream);

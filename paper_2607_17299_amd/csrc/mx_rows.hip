@@ -95,13 +95,14 @@ __global__ void __launch_bounds__(T < 256 ? 256 : T) k_residual_norm_mx(NormArgs
 }
 
 // g / (1 + exp(-g)) to a few units of 2^-23: exp as a power of two, whose exponent's
-// rounding is made up for to first order, and a reciprocal of the hardware's.  (Arithmetic
-// bounds the gate's kernel, with the library's exp and division by far.)
+// rounding is made up for to first order, and a reciprocal of the hardware's, of a quarter:
+// 1 + exp(-g) reaches 2^128, and what is below 2^-126 comes out of the reciprocal as zero.
+// (Arithmetic bounds the gate's kernel, with the library's exp and division by far.)
 WAR_DEV float silu(float g) {
   constexpr float kLog2e = 1.44269502f, kLn2 = 0.693147182f;
   const float c = __builtin_amdgcn_fmed3f(g, -100.f, 128.f);  // past these: an infinite power, none
   const float t = c * -kLog2e, rest = fmaf(t, -kLn2, -c);      // exp(-c) = 2^t (1 + rest)
-  return g * __builtin_amdgcn_rcpf(fmaf(__builtin_amdgcn_exp2f(t), 1.f + rest, 1.f));
+  return 0.25f * g * __builtin_amdgcn_rcpf(fmaf(__builtin_amdgcn_exp2f(t), fmaf(rest, 0.25f, 0.25f), 0.25f));
 }
 
 // row of run id < 2^31 of a matrix with `by` (rows_by) runs a row

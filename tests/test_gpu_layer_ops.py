@@ -800,3 +800,17 @@ def test_no_rows():
     war.rope_write(pool, 0, war.Rope(64), t32([0]), t32([3]), bf(1, 0, 4, 64), bf(1, 0, 2, 64), bf(1, 0, 2, 64), bf(1, 0, 4, 64))
     torch.cuda.synchronize()
     assert pool.state()["status"] == 0
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+def test_gates_whose_exp_is_close_to_the_largest_number(fmt):
+    """Down to a gate of -88.7, where exp(-g) is 2^127.97, the result is not zero: its
+    reciprocal is below the smallest normal number, its product with x need not be."""
+    war = _war()
+    near = torch.cat([torch.linspace(-88.7, -86.0, 32 * 20), torch.linspace(-87.4, -87.3, 32 * 4)]).view(-1, 32)
+    for g in (near, (torch.arange(32 * 6) // 32 * 0.5 - 88.5).view(-1, 32).bfloat16()):
+        for x in (1.0, -1e30, 3e38, 2.0 ** 40):
+            x = torch.full_like(g, x).to(DEV)
+            m = mx_of(len(g), 32, fmt)
+            war.quantize(x, m, gate=g.to(DEV))
+            check_codes(m, omx.gated(as64(x), as64(g)), 2.0 ** -20)
